@@ -383,6 +383,182 @@ int32_t logbq_linear_kernel(int32_t bits, int64_t m, int64_t k, int64_t n, const
 int32_t logbq_dequantize8(const uint8_t* codes_dev, int64_t n, int64_t k, const float* codebook,
                           float* w_dev, void* stream);
 
+/*
+ * ---- A serving step around the linears: paged 4-bit key/value cache, attention over it, and the
+ * log probabilities of the step's tokens. The paper leaves the cache in 16 bits and names its
+ * quantization as future work; the format here is this library's.
+ *
+ * Cache format. One layer's cache holds `pages` pages of `page` tokens each, for `heads` key/value
+ * heads of `dim` channels. A token sits in slot = page id * page + offset. A row (one token's keys
+ * or values of one head) is dim codes of 4 bits and one bfloat16 scale. A code is a nibble
+ * sign<<3 | magnitude, as the weight codes are; it stands for
+ *   +-(0, 0.5, 1, 1.5, 2, 3, 4, 6)[magnitude] * scale,
+ * the values that gfx950 converts from 4 bits in one instruction.
+ *   scale     = the smallest bfloat16 s with 6 s >= max |x| over the row's finite elements
+ *               (0 for a row without a finite nonzero element; its codes are 0);
+ *   magnitude = number of thresholds t in (0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5) with |x| >= t s;
+ *   NaN has magnitude 0, +-Inf the largest with its sign; the sign bit is set only for a nonzero
+ *   magnitude.
+ * Buffers (device, 16-byte aligned, owned by the caller):
+ *   k_codes   [pages][heads][page][dim/2]            low nibble = even channel
+ *   v_codes   [pages][heads][page/8][16][8][dim/32]  8 tokens interleaved: 16 groups of dim/16
+ *                                                    channels, each with its 8 tokens in turn
+ *   k_scales, v_scales  [pages][heads][page]         bfloat16
+ * dim is 64, 128 or 256; page a power of two, 16 to 1024; 1 <= heads <= 1024.
+ * Device-held indices (slots, page ids, lengths, starts) are checked in the kernels: no value of
+ * theirs makes a call read or write outside the buffers.
+ */
+typedef enum logbq_dtype {
+  LOGBQ_DTYPE_F32 = 0,
+  LOGBQ_DTYPE_F16 = 1,
+  LOGBQ_DTYPE_BF16 = 2
+} logbq_dtype;
+
+typedef struct logbq_kv4 {
+  uint8_t* k_codes;
+  uint8_t* v_codes;
+  uint16_t* k_scales;
+  uint16_t* v_scales;
+  int64_t pages;
+  int32_t heads;
+  int32_t page;
+  int32_t dim;
+  int32_t reserved;
+} logbq_kv4;
+
+/*
+ * logbq_batch_tables -- block tables, slot map and starts of a step from its requests' lengths,
+ * in one launch.
+ *   cached_dev : device, [requests] int32, tokens that each request has in the cache.
+ *   new_dev    : device, [requests] int32, tokens that it adds in this step. Negative lengths
+ *                count as 0.
+ *   requests   : 0 .. 4096.
+ *   free_dev   : device, [free_count] int32 ids of free pages, taken from the front, request by
+ *                request.
+ *   table_dev  : device, [requests][width] int32, in/out. Request r has its ceil(cached / page)
+ *                first entries; entries up to ceil((cached + new) / page) are written.
+ *   page       : tokens in a page, a power of two, 16 .. 1024.
+ *   tokens     : entries of slots_dev and positions_dev (at least the sum of new; tokens past the
+ *                sum get slot -1 and position 0).
+ *   slots_dev     : device, [tokens] int64, written: slot of each new token, request by request.
+ *   positions_dev : device, [tokens] int32, written: its position in its request.
+ *   q_starts_dev  : device, [requests + 1] int32, written: first token of each request (at most
+ *                   `tokens`).
+ *   seq_lens_dev  : device, [requests] int32, written: cached + new.
+ *   info_dev      : device, [4] int32, written: sum of new, pages taken from the free list,
+ *                   largest cached + new, and a sum of 1 (free pages were short), 2 (a request
+ *                   needs more than `width` pages) and 4 (`tokens` is less than the sum of new).
+ * A token without a page has slot -1, and a missing page's entry is -1. Lengths, positions and
+ * sums saturate at 2^31 - 1.
+ * A second call on the same input lengths gives the same results.
+ * Errors: INVALID_ARG (null pointer, negative size), UNSUPPORTED (page, requests > 4096, width or
+ * free_count or tokens above 2^31 - 1), HIP.
+ */
+int32_t logbq_batch_tables(const int32_t* cached_dev, const int32_t* new_dev, int64_t requests,
+                           const int32_t* free_dev, int64_t free_count, int32_t* table_dev,
+                           int64_t width, int32_t page, int64_t tokens, int64_t* slots_dev,
+                           int32_t* positions_dev, int32_t* q_starts_dev, int32_t* seq_lens_dev,
+                           int32_t* info_dev, void* stream);
+
+/*
+ * logbq_kv4_append -- keys and values of `tokens` tokens, quantized into their slots.
+ *   k_dev, v_dev : device, row t of head h at element t * stride + h * dim; 16-byte aligned, and
+ *                  so is every row (stride in elements, at least heads * dim).
+ *   dtype        : logbq_dtype of both.
+ *   cache        : host, the buffers; codes and scales of the slots are written.
+ *   slots_dev    : device, [tokens] int64. A token whose slot is negative or past the cache is
+ *                  left out. Two tokens with one slot: either may be kept.
+ * Errors: INVALID_ARG, UNSUPPORTED (dim, page, dtype, alignment, stride), HIP.
+ */
+int32_t logbq_kv4_append(const void* k_dev, int64_t k_stride, const void* v_dev, int64_t v_stride,
+                         int32_t dtype, int64_t tokens, const logbq_kv4* cache,
+                         const int64_t* slots_dev, void* stream);
+
+/*
+ * logbq_kv4_read -- the values that the cache holds in given slots, e.g. to export a prefix.
+ *   slots_dev    : device, [tokens] int64; a slot that is negative or past the cache gives zeros.
+ *   k_dev, v_dev : device, [tokens][heads][dim], written; 16-byte aligned.
+ *   dtype        : logbq_dtype of both. Exact in float32, and in float16 within its range;
+ *                  rounded to nearest in bfloat16.
+ * Errors: INVALID_ARG, UNSUPPORTED, HIP.
+ */
+int32_t logbq_kv4_read(const logbq_kv4* cache, const int64_t* slots_dev, int64_t tokens,
+                       void* k_dev, void* v_dev, int32_t dtype, void* stream);
+
+/* Bytes of workspace with which logbq_kv4_attention runs any call. */
+#define LOGBQ_KV4_WORKSPACE_BYTES 268435456
+
+/*
+ * logbq_kv4_attention -- softmax attention of a step's queries over the 4-bit cache, for requests
+ * of one token (decode), a few (speculative decode), a chunk or a whole prompt, in one call.
+ *   q_dev      : device, query head h of token t at element t * q_stride + h * dim; 16-byte
+ *                aligned, and so is every row.
+ *   q_dtype    : logbq_dtype.
+ *   tokens     : rows of q.
+ *   q_heads    : a multiple of cache->heads, at most 16 times it; query head h reads key/value
+ *                head h / (q_heads / heads).
+ *   table_dev  : device, [requests][width] int32 page ids; a negative entry, or one past the
+ *                cache, hides its page.
+ *   seq_lens_dev : device, [requests] int32, cached tokens with this step's, which are already
+ *                appended.
+ *   q_starts_dev : device, [requests + 1] int32, first token of each request.
+ *   max_new    : upper bound of a request's tokens (host). Tokens past it may be left out.
+ *   scale      : factor on the products q . k.
+ *   window     : a token sees itself and the window - 1 positions before it; 0: all.
+ *   out_dev    : device, [tokens][q_heads][dim], written for the tokens that belong to a request.
+ *   out_dtype  : logbq_dtype.
+ *   lse_dev    : device, [tokens][q_heads] float32, or NULL: log of the sum of exp(scale q . k).
+ *   work_dev   : device, work_bytes bytes, 16-byte aligned, overwritten; LOGBQ_KV4_WORKSPACE_BYTES
+ *                are enough for any call.
+ * Token i of n new ones of a request of length s has position p = s - n + i and sees positions
+ * max(0, p - window + 1) .. p (0 .. p without a window). A token that sees nothing has output 0
+ * and lse -inf. Products of q are taken in float16 (float32 queries as a sum of two float16
+ * values), all sums and the softmax in float32, its weights rounded to float16 for the product
+ * with the values.
+ * Errors: INVALID_ARG, UNSUPPORTED (dim, page, heads, dtypes, alignment, sizes, a workspace that
+ * is too small), HIP.
+ */
+int32_t logbq_kv4_attention(const void* q_dev, int64_t q_stride, int32_t q_dtype, int64_t tokens,
+                            int32_t q_heads, const logbq_kv4* cache, const int32_t* table_dev,
+                            int64_t requests, int64_t width, const int32_t* seq_lens_dev,
+                            const int32_t* q_starts_dev, int64_t max_new, float scale,
+                            int32_t window, void* out_dev, int32_t out_dtype, float* lse_dev,
+                            void* work_dev, int64_t work_bytes, void* stream);
+
+/* Bytes of workspace that logbq_token_logprobs needs, whatever the call. */
+#define LOGBQ_LOGPROBS_WORKSPACE_BYTES 4194304
+/* Most alternatives that it returns. */
+#define LOGBQ_LOGPROBS_MAX_TOP 32
+
+/*
+ * logbq_token_logprobs -- log probabilities of given tokens, entropy and top alternatives of
+ * `tokens` rows of logits.
+ *   logits_dev : device, row t at element t * stride, vocab elements; aligned to its type.
+ *   dtype      : logbq_dtype.
+ *   targets_dev : device, [tokens] int64; a target outside 0 .. vocab - 1 asks for nothing and
+ *                 gives log probability 0.
+ *   top        : 0 .. LOGBQ_LOGPROBS_MAX_TOP, at most vocab.
+ *   logprob_dev, entropy_dev : device, [tokens] float32, written: x[target] - L and
+ *                 L - sum_j exp(x_j - L) x_j with L = log sum_j exp(x_j), in nats.
+ *   top_index_dev, top_logprob_dev : device, [tokens][top] int32 / float32, written: the largest
+ *                 logits in descending order (equal ones by index) and their x - L. May be NULL
+ *                 if top is 0.
+ *   work_dev   : device, LOGBQ_LOGPROBS_WORKSPACE_BYTES bytes, 16-byte aligned. Zero before the
+ *                first call; each call leaves it so. Calls that overlap need one each.
+ * A logit of -inf (a forbidden token) has probability 0 and adds nothing to the entropy; it is
+ * returned among the top ones only when fewer than `top` others are left, with log probability
+ * -inf. Rows with a NaN, a +inf or nothing but -inf have log probabilities and entropy NaN; NaN
+ * ranks above every number.
+ * Sums are float32.
+ * Errors: INVALID_ARG (null pointer, negative size, top > vocab), UNSUPPORTED (dtype, alignment,
+ * vocab >= 2^31, top, stride, a workspace that is too small), HIP.
+ */
+int32_t logbq_token_logprobs(const void* logits_dev, int32_t dtype, int64_t tokens, int64_t vocab,
+                             int64_t stride, const int64_t* targets_dev, int32_t top,
+                             float* logprob_dev, float* entropy_dev, int32_t* top_index_dev,
+                             float* top_logprob_dev, void* work_dev, int64_t work_bytes,
+                             void* stream);
+
 #ifdef __cplusplus
 }
 #endif

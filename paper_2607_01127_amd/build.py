@@ -1,4 +1,5 @@
-"""Build liblogbq.so in-tree: the host fit with g++, the gfx950 kernels with hipcc. Also builds
+"""Build liblogbq.so in-tree: the host fit with g++, the gfx950 kernels with hipcc (the linears and
+the quantizer in logbq_kernels.hip, the serving operators in serving_kernels.hip). Also builds
 libhbmread.so, the streaming-read kernel bench.py measures the HBM read ceiling with.
 
 The host fit is compiled without -ffast-math and with -ffp-contract=off so that its float64
@@ -37,14 +38,18 @@ def _run(cmd, verbose):
     subprocess.run(cmd, check=True)
 
 
+KERNEL_SOURCES = ("logbq_kernels", "serving_kernels")
+
+
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     fit_o = os.path.join(BUILD, "fit.o")
-    ker_o = os.path.join(BUILD, "logbq_kernels.o")
+    ker_o = [os.path.join(BUILD, name + ".o") for name in KERNEL_SOURCES]
     _run(["g++", *HOST_FLAGS, "-c", os.path.join(CSRC, "fit.cpp"), "-o", fit_o], verbose)
-    _run([HIPCC, *HIP_FLAGS, "-c", os.path.join(CSRC, "logbq_kernels.hip"), "-o", ker_o], verbose)
+    for name, obj in zip(KERNEL_SOURCES, ker_o):
+        _run([HIPCC, *HIP_FLAGS, "-c", os.path.join(CSRC, name + ".hip"), "-o", obj], verbose)
     tmp = LIB + ".tmp"
-    _run([HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, fit_o, ker_o], verbose)
+    _run([HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, fit_o, *ker_o], verbose)
     os.replace(tmp, LIB)
     tmp = READ_LIB + ".tmp"
     _run([HIPCC, *HIP_FLAGS, "-shared", "-o", tmp, os.path.join(CSRC, "hbm_read.hip")], verbose)
@@ -68,13 +73,14 @@ def build_sanitized(sanitize: str, verbose: bool = False) -> str:
     san = [f"-fsanitize={sanitize}", "-fno-sanitize-recover=all", "-fno-omit-frame-pointer",
            "-g", "-shared-libsan"]
     fit_o = os.path.join(out_dir, "fit.o")
-    ker_o = os.path.join(out_dir, "logbq_kernels.o")
+    ker_o = [os.path.join(out_dir, name + ".o") for name in KERNEL_SOURCES]
     host_flags = [f for f in HOST_FLAGS if f != "-O2"] + ["-O1"]
     _run([CLANG, *host_flags, *san, "-c", os.path.join(CSRC, "fit.cpp"), "-o", fit_o], verbose)
-    _run([HIPCC, *HIP_FLAGS, *[a for f in san for a in ("-Xarch_host", f)], "-c",
-          os.path.join(CSRC, "logbq_kernels.hip"), "-o", ker_o], verbose)
+    for name, obj in zip(KERNEL_SOURCES, ker_o):
+        _run([HIPCC, *HIP_FLAGS, *[a for f in san for a in ("-Xarch_host", f)], "-c",
+              os.path.join(CSRC, name + ".hip"), "-o", obj], verbose)
     lib = os.path.join(out_dir, "liblogbq.so")
-    _run([HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", *san, "-o", lib, fit_o, ker_o],
+    _run([HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", *san, "-o", lib, fit_o, *ker_o],
          verbose)
     return lib
 

@@ -1,7 +1,8 @@
 """Python binding of liblogbq (ctypes): argument marshalling only.
 
 Every step of the computation runs in the library: ``fit`` in its host code, ``encode``,
-``linear`` and ``dequantize`` in its gfx950 kernels. PyTorch provides device memory and the
+``linear``, ``dequantize`` and a serving step's operators (``batch_tables``, ``kv4_append``,
+``kv4_read``, ``kv4_attention``, ``token_logprobs``) in its gfx950 kernels. PyTorch provides device memory and the
 current stream; nothing here computes on the data. If the library is not built, every call
 raises ``LogbqUnavailable``: there is no fallback path.
 """
@@ -10,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import os
 from ctypes import POINTER, c_double, c_float, c_int32, c_int64, c_uint8, c_uint16, c_void_p
+from typing import NamedTuple
 
 import numpy as np
 
@@ -61,6 +63,13 @@ class Uniform(ctypes.Structure):
         return np.ctypeslib.as_array(self.thresholds).copy()
 
 
+class Kv4Struct(ctypes.Structure):
+    """Mirror of ``logbq_kv4`` (include/logbq.h)."""
+    _fields_ = [("k_codes", c_void_p), ("v_codes", c_void_p), ("k_scales", c_void_p),
+                ("v_scales", c_void_p), ("pages", c_int64), ("heads", c_int32), ("page", c_int32),
+                ("dim", c_int32), ("reserved", c_int32)]
+
+
 _lib = None
 
 SIGNATURES = {
@@ -93,6 +102,20 @@ SIGNATURES = {
     "logbq_fit_device": (c_int32, [c_void_p, c_int64, c_int32, c_double, c_void_p,
                                    POINTER(Params), c_void_p]),
     "logbq_fit_exact": (c_int32, [POINTER(c_float), c_int64, c_int32, c_double, POINTER(Params)]),
+    "logbq_batch_tables": (c_int32, [c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_void_p,
+                                     c_int64, c_int32, c_int64, c_void_p, c_void_p, c_void_p,
+                                     c_void_p, c_void_p, c_void_p]),
+    "logbq_kv4_append": (c_int32, [c_void_p, c_int64, c_void_p, c_int64, c_int32, c_int64,
+                                   POINTER(Kv4Struct), c_void_p, c_void_p]),
+    "logbq_kv4_read": (c_int32, [POINTER(Kv4Struct), c_void_p, c_int64, c_void_p, c_void_p, c_int32,
+                                 c_void_p]),
+    "logbq_kv4_attention": (c_int32, [c_void_p, c_int64, c_int32, c_int64, c_int32,
+                                      POINTER(Kv4Struct), c_void_p, c_int64, c_int64, c_void_p,
+                                      c_void_p, c_int64, c_float, c_int32, c_void_p, c_int32,
+                                      c_void_p, c_void_p, c_int64, c_void_p]),
+    "logbq_token_logprobs": (c_int32, [c_void_p, c_int32, c_int64, c_int64, c_int64, c_void_p,
+                                       c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                       c_int64, c_void_p]),
 }
 
 FIT_WORKSPACE_BYTES = 110600
@@ -380,3 +403,218 @@ def gptq(w, u, params, out_codes=None, workspace=None, stream=None):
                             c_void_p(workspace.data_ptr()), c_void_p(out_codes.data_ptr()),
                             _stream(stream)), "logbq_gptq")
     return out_codes
+
+
+# ------------------------------------------------------------------ a serving step's operators
+
+KV4_WORKSPACE_BYTES = 1 << 28
+LOGPROBS_WORKSPACE_BYTES = 1 << 22
+LOGPROBS_MAX_TOP = 32
+
+
+class Kv4Cache(NamedTuple):
+    """The buffers of one layer's 4-bit key/value cache (``logbq_kv4`` in include/logbq.h); any
+    4-tuple of such tensors serves as well."""
+    k_codes: object       # uint8 [pages][heads][page][dim/2]
+    k_scales: object      # bfloat16 [pages][heads][page]
+    v_codes: object       # uint8 [pages][heads][page/8][16][8][dim/32]
+    v_scales: object      # bfloat16 [pages][heads][page]
+
+
+def kv4_cache(pages: int, heads: int, dim: int, page: int = 64, device="cuda") -> Kv4Cache:
+    """An empty (zeroed) cache of `pages` pages of `page` tokens."""
+    import torch
+    if dim not in (64, 128, 256) or page not in (16, 32, 64, 128, 256, 512, 1024):
+        raise ValueError("dim must be 64, 128 or 256; page a power of two, 16 to 1024")
+    u8 = dict(dtype=torch.uint8, device=device)
+    bf = dict(dtype=torch.bfloat16, device=device)
+    return Kv4Cache(torch.zeros((pages, heads, page, dim // 2), **u8),
+                    torch.zeros((pages, heads, page), **bf),
+                    torch.zeros((pages, heads, page // 8, 16, 8, dim // 32), **u8),
+                    torch.zeros((pages, heads, page), **bf))
+
+
+_dtype_codes = None
+
+
+def _dtype_code(dtype) -> int:
+    """logbq_dtype of a torch type."""
+    global _dtype_codes
+    if _dtype_codes is None:
+        import torch
+        _dtype_codes = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+    try:
+        return _dtype_codes[dtype]
+    except KeyError:
+        raise ValueError(f"{dtype} is none of float32, float16, bfloat16") from None
+
+
+def _device_array(x, dtype, shape, name):
+    """Raises unless x is a contiguous device tensor of a type and shape."""
+    if x.dtype != dtype or x.shape != shape or not x.is_contiguous() or not x.is_cuda:
+        raise ValueError(f"{name} must be a contiguous {tuple(shape)} {dtype} device tensor, not "
+                         f"{tuple(x.shape)} {x.dtype} on {x.device}")
+
+
+def _kv4_struct(cache) -> Kv4Struct:
+    import torch
+    kc, ks, vc, vs = cache
+    if kc.dim() != 4 or vc.dim() != 6:
+        raise ValueError("k_codes must be [pages][heads][page][dim/2], v_codes "
+                         "[pages][heads][page/8][16][8][dim/32]")
+    pages, heads, page, half = kc.shape
+    _device_array(kc, torch.uint8, kc.shape, "k_codes")
+    _device_array(vc, torch.uint8, (pages, heads, page // 8, 16, 8, half // 16), "v_codes")
+    _device_array(ks, torch.bfloat16, (pages, heads, page), "k_scales")
+    _device_array(vs, torch.bfloat16, (pages, heads, page), "v_scales")
+    return Kv4Struct(kc.data_ptr(), vc.data_ptr(), ks.data_ptr(), vs.data_ptr(), pages, heads, page,
+                     2 * half, 0)
+
+
+def _rows(x, heads, dim, name):
+    """Elements between the tokens of x [tokens][heads][dim], whose heads and channels are
+    contiguous."""
+    if x.dim() != 3 or not x.is_cuda or x.shape[2] != dim or (heads and x.shape[1] != heads):
+        raise ValueError(f"{name} must be a [tokens][{heads or 'heads'}][{dim}] device tensor")
+    stride = x.stride()
+    if stride[2] != 1 or (stride[1] != dim and x.shape[1] != 1):
+        raise ValueError(f"the heads and channels of {name} must be contiguous")
+    # One token has no distance to the next; its stride may be anything.
+    return stride[0] if x.shape[0] > 1 else x.shape[1] * dim
+
+
+def batch_tables(cached, new, free_pages, table, page: int, tokens: int, out=None, stream=None):
+    """logbq_batch_tables: slot map, positions and starts of a step, and the block table's new
+    entries, from the requests' lengths (int32 device tensors `cached` and `new`). `free_pages`
+    (int32) gives new pages from its front; `table` (int32 [requests][width]) is updated in place.
+    Returns a dict of slots (int64 [tokens]), positions (int32 [tokens]), q_starts (int32
+    [requests + 1]), seq_lens (int32 [requests]) and info (int32 [4]: new tokens, pages taken,
+    longest length, 1 pages short + 2 table too narrow + 4 `tokens` too few); `out` may hold the
+    tensors to write."""
+    import torch
+    i32 = torch.int32
+    n = cached.numel()
+    _device_array(cached, i32, (n,), "cached")
+    _device_array(new, i32, (n,), "new")
+    _device_array(free_pages, i32, (free_pages.numel(),), "free_pages")
+    if table.dim() != 2:
+        raise ValueError("table must be [requests][width]")
+    width = table.shape[1]
+    _device_array(table, i32, (n, width), "table")
+    if out is None:
+        e = dict(device=cached.device, dtype=i32)
+        out = dict(slots=torch.empty(tokens, device=cached.device, dtype=torch.int64),
+                   positions=torch.empty(tokens, **e), q_starts=torch.empty(n + 1, **e),
+                   seq_lens=torch.empty(n, **e), info=torch.empty(4, **e))
+    else:
+        _device_array(out["slots"], torch.int64, (tokens,), "slots")
+        _device_array(out["positions"], i32, (tokens,), "positions")
+        _device_array(out["q_starts"], i32, (n + 1,), "q_starts")
+        _device_array(out["seq_lens"], i32, (n,), "seq_lens")
+        _device_array(out["info"], i32, (4,), "info")
+    _check(lib().logbq_batch_tables(
+        cached.data_ptr(), new.data_ptr(), n, free_pages.data_ptr(), free_pages.numel(),
+        table.data_ptr(), width, page, tokens, out["slots"].data_ptr(), out["positions"].data_ptr(),
+        out["q_starts"].data_ptr(), out["seq_lens"].data_ptr(), out["info"].data_ptr(),
+        _stream(stream)), "logbq_batch_tables")
+    return out
+
+
+def kv4_append(k, v, cache, slots, stream=None):
+    """logbq_kv4_append: keys and values [tokens][heads][dim] (float32, float16 or bfloat16; the
+    tokens may be strided) quantized into `slots` (int64 [tokens]; negative: left out) of a
+    Kv4Cache."""
+    import torch
+    c = _kv4_struct(cache)
+    k_stride, v_stride = _rows(k, c.heads, c.dim, "k"), _rows(v, c.heads, c.dim, "v")
+    if v.dtype != k.dtype or v.shape[0] != k.shape[0]:
+        raise ValueError("k and v must have one type and number of tokens")
+    _device_array(slots, torch.int64, (k.shape[0],), "slots")
+    _check(lib().logbq_kv4_append(k.data_ptr(), k_stride, v.data_ptr(), v_stride,
+                                  _dtype_code(k.dtype), k.shape[0], ctypes.byref(c),
+                                  slots.data_ptr(), _stream(stream)), "logbq_kv4_append")
+
+
+def kv4_read(cache, slots, dtype=None, stream=None):
+    """logbq_kv4_read: (k, v), each [tokens][heads][dim] of `dtype` (float16 unless given), the
+    values that a Kv4Cache holds in `slots` (zeros for a slot outside it)."""
+    import torch
+    c = _kv4_struct(cache)
+    _device_array(slots, torch.int64, (slots.numel(),), "slots")
+    shape = (slots.numel(), c.heads, c.dim)
+    k = torch.empty(shape, dtype=dtype or torch.float16, device=slots.device)
+    v = torch.empty_like(k)
+    _check(lib().logbq_kv4_read(ctypes.byref(c), slots.data_ptr(), shape[0], k.data_ptr(),
+                                v.data_ptr(), _dtype_code(k.dtype), _stream(stream)),
+           "logbq_kv4_read")
+    return k, v
+
+
+def kv4_attention(q, cache, table, seq_lens, q_starts, max_new: int, scale=None, window: int = 0,
+                  out=None, lse=None, workspace=None, stream=None):
+    """logbq_kv4_attention: attention of q [tokens][q_heads][dim] (float32, float16 or bfloat16;
+    the tokens may be strided) over a Kv4Cache. `table` (int32 [requests][width]), `seq_lens`
+    (int32 [requests]) and `q_starts` (int32 [requests + 1]) are batch_tables' results; `max_new`
+    bounds a request's tokens. `scale` is dim ** -0.5 unless given; `window` 0 sees everything.
+    Returns `out` ([tokens][q_heads][dim], float16 unless given); `lse` (float32
+    [tokens][q_heads]), if given, receives the log sums of exponentials. `workspace`
+    (KV4_WORKSPACE_BYTES bytes serve any call) is allocated if not given."""
+    import torch
+    c = _kv4_struct(cache)
+    q_stride = _rows(q, 0, c.dim, "q")
+    tokens, q_heads = q.shape[0], q.shape[1]
+    if table.dim() != 2:
+        raise ValueError("table must be [requests][width]")
+    n, width = table.shape
+    i32 = torch.int32
+    _device_array(table, i32, (n, width), "table")
+    _device_array(seq_lens, i32, (n,), "seq_lens")
+    _device_array(q_starts, i32, (n + 1,), "q_starts")
+    if out is None:
+        out = torch.empty((tokens, q_heads, c.dim), dtype=torch.float16, device=q.device)
+    else:
+        _device_array(out, out.dtype, (tokens, q_heads, c.dim), "out")
+    if lse is not None:
+        _device_array(lse, torch.float32, (tokens, q_heads), "lse")
+    if workspace is None:
+        workspace = torch.empty(KV4_WORKSPACE_BYTES, dtype=torch.uint8, device=q.device)
+    _check(lib().logbq_kv4_attention(
+        q.data_ptr(), q_stride, _dtype_code(q.dtype), tokens, q_heads, ctypes.byref(c),
+        table.data_ptr(), n, width, seq_lens.data_ptr(), q_starts.data_ptr(), max_new,
+        c.dim ** -0.5 if scale is None else scale, window, out.data_ptr(), _dtype_code(out.dtype),
+        None if lse is None else lse.data_ptr(), workspace.data_ptr(),
+        workspace.numel() * workspace.element_size(), _stream(stream)), "logbq_kv4_attention")
+    return out
+
+
+def token_logprobs(logits, targets, top: int = 0, out=None, workspace=None, stream=None):
+    """logbq_token_logprobs: of each row of logits [tokens][vocab] (float32, float16 or bfloat16;
+    the rows may be strided) the log probability of its target (int64 [tokens]; outside the
+    vocabulary: 0), the entropy, and the `top` (up to 32) likeliest tokens. Returns a dict of
+    logprob and entropy (float32 [tokens]), top_index (int32) and top_logprob (float32, both
+    [tokens][top]); `out` may hold the tensors to write. `workspace` (LOGPROBS_WORKSPACE_BYTES
+    bytes, zeroed once by the caller, one for each stream) is allocated and zeroed if not given."""
+    import torch
+    if logits.dim() != 2 or not logits.is_cuda or (logits.stride(1) != 1 and logits.shape[1] != 1):
+        raise ValueError("logits must be a [tokens][vocab] device tensor with contiguous rows")
+    tokens, vocab = logits.shape
+    _device_array(targets, torch.int64, (tokens,), "targets")
+    if out is None:
+        f = dict(dtype=torch.float32, device=logits.device)
+        out = dict(logprob=torch.empty(tokens, **f), entropy=torch.empty(tokens, **f),
+                   top_index=torch.empty((tokens, top), dtype=torch.int32, device=logits.device),
+                   top_logprob=torch.empty((tokens, top), **f))
+    else:
+        _device_array(out["logprob"], torch.float32, (tokens,), "logprob")
+        _device_array(out["entropy"], torch.float32, (tokens,), "entropy")
+        _device_array(out["top_index"], torch.int32, (tokens, top), "top_index")
+        _device_array(out["top_logprob"], torch.float32, (tokens, top), "top_logprob")
+    if workspace is None:
+        workspace = torch.zeros(LOGPROBS_WORKSPACE_BYTES, dtype=torch.uint8, device=logits.device)
+    _check(lib().logbq_token_logprobs(
+        logits.data_ptr(), _dtype_code(logits.dtype), tokens, vocab,
+        logits.stride(0) if tokens > 1 else vocab, targets.data_ptr(), top,
+        out["logprob"].data_ptr(), out["entropy"].data_ptr(), out["top_index"].data_ptr(),
+        out["top_logprob"].data_ptr(), workspace.data_ptr(),
+        workspace.numel() * workspace.element_size(), _stream(stream)), "logbq_token_logprobs")
+    return out

@@ -1,0 +1,530 @@
+"""The serving operators on the GPU, through the public binding, against the float64 oracle:
+block tables and slot maps (exact), the 4-bit append and read-back (bit for bit), attention over
+the cache and token log probabilities (bounds derived below), at the sizes, masks, strides and
+values where they can go wrong."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import serving_oracle as S
+from paper_2607_01127_amd import logbq as L
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+def dev(x, dtype=None):
+    t = torch.from_numpy(np.ascontiguousarray(x)).to(DEV)
+    return t if dtype is None else t.to(dtype)
+
+
+def host(t):
+    return t.double().cpu().numpy() if t.is_floating_point() else t.cpu().numpy()
+
+
+# ------------------------------------------------------------------ block tables
+
+def check_tables(cached, new, free, width, page, tokens, seed=0):
+    rng = np.random.default_rng(seed)
+    n = len(cached)
+    table = rng.integers(0, 1000, (n, width)).astype(np.int32)
+    want = S.batch_tables(cached, new, free, table, page, tokens)
+    i32 = lambda v: dev(np.asarray(v, dtype=np.int32))  # noqa: E731
+    t = dev(table)
+    args = (i32(cached), i32(new), i32(free), t, page, tokens)
+    for _ in range(2):                       # the second call finds the first one's entries
+        got = L.batch_tables(*args)
+        for name in ("slots", "positions", "q_starts", "seq_lens", "info"):
+            assert np.array_equal(got[name].cpu().numpy(), want[name]), name
+        assert np.array_equal(t.cpu().numpy(), want["table"])
+
+
+@pytest.mark.parametrize("n,page", [(0, 16), (1, 16), (5, 64), (64, 32), (257, 16), (1000, 128),
+                                    (4096, 1024)])
+def test_tables_random(n, page):
+    say("tables", n, page)
+    rng = np.random.default_rng(n)
+    cached = rng.integers(-2, 6 * page, n)
+    new = np.where(rng.random(n) < 0.6, 1, rng.integers(-1, 3 * page // 2, n))
+    if n > 500:
+        new = np.minimum(new, 40)
+    pages = int((-(-np.maximum(new, 0) // page) + 1).sum())
+    total = int(np.maximum(new, 0).sum())
+    check_tables(cached, new, rng.permutation(pages + 7).astype(np.int32), 9, page, total + 3, seed=n)
+
+
+@pytest.mark.parametrize("what", ["short", "narrow", "few", "none", "exact", "big"])
+def test_tables_edges(what):
+    say("tables", what)
+    free = list(range(100, 140))
+    if what == "short":        # the free list ends inside a request
+        check_tables([0, 30, 0], [40, 40, 40], free[:5], 6, 16, 120)
+    if what == "narrow":       # requests longer than the table is wide, cached ones among them
+        check_tables([0, 80, 200, 1], [100, 5, 1, 2], free, 4, 16, 108)
+    if what == "few":          # fewer map entries than new tokens
+        check_tables([3, 3, 3], [30, 30, 30], free, 8, 16, 47)
+    if what == "none":
+        check_tables([0, 0], [0, 0], [], 0, 16, 0)
+        check_tables([7, 0, 9], [0, 0, 0], [], 2, 16, 5)
+    if what == "exact":        # lengths that end on a page
+        check_tables([16, 0, 15, 32], [16, 32, 1, 0], free, 4, 16, 49)
+    if what == "big":          # lengths whose sums pass 32 bits
+        check_tables([2**31 - 1, 2**31 - 1000, 5], [3, 900, 2], free, 3, 1024, 905)
+
+
+# ------------------------------------------------------------------ append and read
+
+def awkward_rows(rng, shape):
+    x = rng.standard_normal(shape).astype(np.float32) * np.exp(rng.uniform(-4, 4, shape[:2] + (1,)))
+    flat = x.reshape(-1, shape[-1])
+    flat[0] = 0.0
+    if len(flat) > 8:
+        flat[1, 3] = np.nan
+        flat[2, 5], flat[2, 6] = np.inf, -np.inf
+        flat[3] = np.nan
+        flat[4] = 6.0 * np.tile([1, 0.25 / 6, -0.75 / 6, 5 / 6], shape[-1] // 4)   # exact thresholds
+        flat[5] = -0.0
+        flat[6] *= 1e-30
+        flat[7, 1:] = 0.0
+    return x.astype(np.float32)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("tokens,heads,dim,page", [(1, 1, 64, 16), (3, 2, 128, 16), (37, 3, 256, 32),
+                                                   (130, 8, 128, 64), (65, 5, 64, 1024)])
+def test_append_and_read(tokens, heads, dim, page, dtype):
+    say("append", tokens, heads, dim, page, dtype)
+    rng = np.random.default_rng(tokens)
+    pages = -(-tokens // page) + 2
+    k = dev(awkward_rows(rng, (tokens, heads, dim))).to(TYPES[dtype])
+    v = dev(awkward_rows(rng, (tokens, heads, dim))).to(TYPES[dtype])
+    slots = rng.permutation(pages * page)[:tokens].astype(np.int64)
+    if tokens > 10:
+        slots[3], slots[7], slots[9] = -1, pages * page, 2**40        # left out
+    fill = [rng.integers(0, 256, t.shape) for t in L.kv4_cache(pages, heads, dim, page, device="cpu")]
+    cache = L.Kv4Cache(dev(fill[0].astype(np.uint8)), dev(fill[1].astype(np.float32), torch.bfloat16),
+                       dev(fill[2].astype(np.uint8)), dev(fill[3].astype(np.float32), torch.bfloat16))
+    want = {}
+    for name, x, codes, scales, unpack in (("k", k, 0, 1, S.unpack_keys), ("v", v, 2, 3, S.unpack_values)):
+        rows, row_scales = S.kv4_quantize(host(x))
+        c, s = unpack(fill[codes].astype(np.uint8)), fill[scales].astype(np.float64)
+        for t, slot in enumerate(slots):
+            if 0 <= slot < pages * page:
+                c[slot // page, :, slot % page] = rows[t]
+                s[slot // page, :, slot % page] = row_scales[t]
+        want[name] = (c, s)
+    L.kv4_append(k, v, cache, dev(slots))
+    # The whole cache: the slots' rows are the oracle's, the others are as they were.
+    assert np.array_equal(S.unpack_keys(cache.k_codes.cpu().numpy()), want["k"][0])
+    assert np.array_equal(S.unpack_values(cache.v_codes.cpu().numpy()), want["v"][0])
+    assert np.array_equal(host(cache.k_scales), want["k"][1])
+    assert np.array_equal(host(cache.v_scales), want["v"][1])
+    for to in ("f32", "f16", "bf16"):
+        got = L.kv4_read(cache, dev(slots), TYPES[to])
+        for g, name in zip(got, "kv"):
+            c, s = want[name]
+            rows = np.zeros((tokens, heads, dim))
+            for t, slot in enumerate(slots):
+                if 0 <= slot < pages * page:
+                    rows[t] = S.kv4_values(c[slot // page, :, slot % page], s[slot // page, :, slot % page])
+            ref = dev(rows.astype(np.float32)).to(TYPES[to])
+            assert torch.equal(g, ref), (to, name)
+
+
+def test_append_strided_rows():
+    """Keys and values as slices of one fused buffer, an odd number of tokens."""
+    say("append strided")
+    rng = np.random.default_rng(1)
+    fused = dev(rng.standard_normal((29, 2 * 4 * 128 + 64)).astype(np.float32))
+    k, v = fused[:, :512].view(29, 4, 128), fused[:, 512:1024].view(29, 4, 128)
+    assert not k.is_contiguous()
+    slots = dev(rng.permutation(64)[:29].astype(np.int64))
+    a, b = L.kv4_cache(4, 4, 128, 16), L.kv4_cache(4, 4, 128, 16)
+    L.kv4_append(k, v, a, slots)
+    L.kv4_append(k.contiguous(), v.contiguous(), b, slots)
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+# ------------------------------------------------------------------ attention
+
+def make_cache(rng, pages, heads, dim, page, spread=0.5):
+    k = rng.standard_normal((pages, heads, page, dim))
+    v = rng.standard_normal((pages, heads, page, dim)) * np.exp(
+        spread * rng.standard_normal((pages, heads, page, 1)))
+    kc, ks = S.kv4_quantize(k)
+    vc, vs = S.kv4_quantize(v)
+    bf = lambda s: dev(s.astype(np.float32), torch.bfloat16)  # noqa: E731
+    cache = L.Kv4Cache(dev(S.pack_keys(kc)), bf(ks), dev(S.pack_values(vc)), bf(vs))
+    return cache, S.kv4_values(kc, ks), S.kv4_values(vc, vs)
+
+
+def attend(rng, lens, new, heads, group, dim, page, dtype="f16", out="f16", window=0, table=None,
+           pages=None, cache=None, q_scale=1.0, scale=None, max_new=None):
+    """One call against the oracle, within the bound that the arithmetic allows.
+
+    With A = sum w |v| and R = max_j scale sum_i |q_i k_ji|: products of float16 queries and codes
+    are exact, their float32 sum has a relative error of at most (D + 4) 2^-24 of R, the scaling
+    and exp2 add 4 2^-24 (|s| + 8) <= 2^-21 (R + 2); a float32 query is held to 2^-22 of itself.
+    So a logit is off by at most d = (D + 16) 2^-23 (R + 2), a weight by a factor 1 +- 2 d, and its
+    rounding to float16 by 2^-11 more; float32 sums over at most 2^13 positions by 2^-11 A at the
+    very worst. The output's own type adds its half ulp. A is taken per channel.
+    """
+    lens, new = np.asarray(lens), np.asarray(new)
+    n = len(lens)
+    width = max(1, int(-(-lens.max(initial=1) // page)))
+    if table is None:
+        pages = pages or int((-(-lens // page)).sum()) + 2
+        order = rng.permutation(pages)
+        table = np.full((n, width), -1, dtype=np.int32)
+        at = 0
+        for r in range(n):
+            m = -(-int(lens[r]) // page)
+            table[r, :m] = order[at:at + m]
+            at += m
+    if cache is None:
+        cache = make_cache(rng, pages, heads, dim, page)
+    buffers, k, v = cache
+    tokens = int(new.sum())
+    starts = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    q = dev((q_scale * rng.standard_normal((tokens, heads * group, dim))).astype(np.float32)).to(TYPES[dtype])
+    scale = dim ** -0.5 if scale is None else scale
+    lse = torch.full((tokens, heads * group), 7.0, device=DEV)
+    res = torch.full(q.shape, float("nan"), device=DEV, dtype=TYPES[out])
+    L.kv4_attention(q, buffers, dev(table), dev(lens.astype(np.int32)), dev(starts),
+                    int(new.max(initial=0)) if max_new is None else max_new, scale=scale,
+                    window=window, out=res, lse=lse)
+    ref, ref_lse, size, reach = S.attention(host(q), k, v, table, lens, starts, page, scale, window)
+    got, got_lse = host(res), host(lse)
+    d = (dim + 16) * 2.0 ** -23 * (reach + 2)
+    half_ulp = {"f32": 0.0, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}[out]
+    bound = (2 * d[..., None] + 2.0 ** -10) * size + half_ulp * np.abs(ref) + 2.0 ** -24
+    assert not np.isnan(got).any()
+    worst = float(np.max(np.abs(got - ref) / bound, initial=0.0))
+    assert worst <= 1.0, worst
+    empty = np.isneginf(ref_lse)
+    assert np.array_equal(np.isneginf(got_lse), empty) and not got[empty].any()
+    off = np.abs(got_lse[~empty] - ref_lse[~empty]) - d[~empty] - 2.0 ** -11
+    assert float(np.max(off, initial=-1.0)) <= 0.0
+    return buffers, q, res, lse, table, lens, starts
+
+
+HEADS = [(8, 4, 128), (2, 1, 64), (1, 7, 128), (2, 16, 64), (3, 5, 256), (1, 8, 256), (2, 4, 64)]
+
+
+@pytest.mark.parametrize("heads,group,dim", HEADS)
+@pytest.mark.parametrize("page", [16, 64])
+def test_attention_decode(heads, group, dim, page):
+    """One token a request: lengths of zero and one, around tiles and pages, ragged."""
+    say("decode", heads, group, dim, page)
+    rng = np.random.default_rng(heads * dim + page)
+    lens = [1, 0, 2, 15, 16, 17, 31, 33, 63, 64, 65, 127, 128, 129, 300]
+    attend(rng, lens, [1] * len(lens), heads, group, dim, page)
+
+
+@pytest.mark.parametrize("dtype,out", [("f32", "f16"), ("f32", "f32"), ("f16", "f32"),
+                                       ("bf16", "bf16"), ("bf16", "f16"), ("f16", "bf16")])
+def test_attention_types(dtype, out):
+    say("types", dtype, out)
+    rng = np.random.default_rng(3)
+    attend(rng, [90, 33], [1, 1], 2, 4, 128, 32, dtype=dtype, out=out)
+    attend(rng, [90, 33], [40, 33], 2, 4, 128, 32, dtype=dtype, out=out)
+
+
+@pytest.mark.parametrize("new", [[2, 1, 3], [5, 5, 5], [1, 16, 4], [17, 9, 1], [0, 3, 0]])
+@pytest.mark.parametrize("heads,group,dim", [(2, 4, 128), (1, 7, 64), (1, 3, 256), (1, 16, 64)])
+def test_attention_few_tokens(new, heads, group, dim):
+    """Speculative steps, and decode beside chunks."""
+    say("few", new, heads, group, dim)
+    rng = np.random.default_rng(sum(new) + dim)
+    attend(rng, [200, 77, 130], new, heads, group, dim, 16)
+
+
+@pytest.mark.parametrize("heads,group,dim,page", [(2, 4, 128, 64), (1, 1, 64, 16), (1, 7, 128, 128),
+                                                  (2, 2, 256, 32), (1, 16, 64, 16)])
+def test_attention_prompts(heads, group, dim, page):
+    """Whole prompts and chunks behind a cached part, odd lengths."""
+    say("prompts", heads, group, dim, page)
+    rng = np.random.default_rng(dim + group)
+    attend(rng, [129, 64, 1, 200, 333], [129, 64, 1, 70, 5], heads, group, dim, page)
+
+
+@pytest.mark.parametrize("window", [1, 2, 31, 64, 100, 5000])
+def test_attention_window(window):
+    say("window", window)
+    rng = np.random.default_rng(window)
+    attend(rng, [1, 0, 40, 64, 65, 290], [1] * 6, 2, 4, 128, 16, window=window)
+    attend(rng, [150, 290], [150, 81], 2, 4, 64, 32, window=window)
+
+
+def test_attention_more_tokens_than_cached():
+    """A token before the first cached position sees nothing: zeros and -inf."""
+    say("more tokens than cached")
+    rng = np.random.default_rng(8)
+    attend(rng, [2, 0, 5], [4, 3, 5], 2, 4, 128, 16)
+    attend(rng, [20, 0], [60, 30], 2, 4, 128, 16)
+
+
+def test_attention_hidden_pages():
+    """Pages whose entries are negative or past the cache are hidden, up to all of a request's;
+    lengths past the table's width end there."""
+    say("hidden pages")
+    rng = np.random.default_rng(9)
+    cache = make_cache(rng, 8, 2, 128, 16)
+    table = np.array([[0, -1, 2, 3], [-1, -1, -1, -1], [7, 8, 2**30, 6], [-1, -1, -1, 5]], dtype=np.int32)
+    for new in ([1, 1, 1, 1], [20, 50, 49, 3]):
+        attend(rng, [50, 64, 49, 60], new, 2, 4, 128, 16, table=table, cache=cache)
+    attend(rng, [64, 200, 49, 64], [1, 1, 1, 1], 2, 4, 128, 16, table=table, cache=cache)
+    attend(rng, [64, 200, 49, 64], [30, 150, 49, 40], 2, 4, 128, 16, table=table, cache=cache, window=120)
+
+
+def test_attention_shared_pages():
+    """Requests that share a prefix read the same pages."""
+    say("shared pages")
+    rng = np.random.default_rng(10)
+    cache = make_cache(rng, 9, 2, 64, 32)
+    table = np.array([[3, 1, 4], [3, 1, 5], [3, 1, 8]], dtype=np.int32)
+    attend(rng, [96, 70, 65], [1, 1, 1], 2, 4, 64, 32, table=table, cache=cache)
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_attention_wide_values(new):
+    """Scales over many orders of magnitude, large logits, a scale of zero, one huge value row."""
+    say("wide values", new)
+    rng = np.random.default_rng(11)
+    k = rng.standard_normal((20, 2, 16, 128))
+    v = rng.standard_normal((20, 2, 16, 128)) * np.exp(rng.uniform(-14, 9, (20, 2, 16, 1)))
+    k[3], v[5], v[7, :, 3] = 0.0, 0.0, 1e8
+    kc, ks = S.kv4_quantize(k)
+    vc, vs = S.kv4_quantize(v)
+    bf = lambda s: dev(s.astype(np.float32), torch.bfloat16)  # noqa: E731
+    cache = (L.Kv4Cache(dev(S.pack_keys(kc)), bf(ks), dev(S.pack_values(vc)), bf(vs)),
+             S.kv4_values(kc, ks), S.kv4_values(vc, vs))
+    table = rng.permutation(20).reshape(1, 20).astype(np.int32)
+    for q_scale, scale in ((1.0, None), (30.0, None), (1.0, -0.2), (1.0, 0.0)):
+        attend(rng, [311], [new], 2, 4, 128, 16, table=table, cache=cache, q_scale=q_scale,
+               scale=scale, out="f32")
+    # Tiny values throughout: the weights times the values' scales are far below 2^-24.
+    small = (cache[0]._replace(v_scales=(cache[0].v_scales.float() * 2.0 ** -40).to(torch.bfloat16)),
+             cache[1], cache[2] * 2.0 ** -40)
+    buffers, q, res, lse, *_ = attend(rng, [311], [new], 2, 4, 128, 16, table=table, cache=small, out="f32")
+    big = L.kv4_attention(q, cache[0], dev(table), dev(np.array([311], np.int32)),
+                          dev(np.array([0, new], np.int32)), new,
+                          out=torch.empty_like(res))
+    # Powers of two change nothing but the exponent.
+    assert torch.allclose(res * 2.0 ** 40, big, rtol=1e-5, atol=1e-5)
+
+
+def test_attention_garbage_beyond_the_lengths():
+    """What lies past a request's length (poisoned scales) reaches no output."""
+    say("garbage")
+    rng = np.random.default_rng(12)
+    (buffers, k, v), page = make_cache(rng, 12, 2, 128, 16), 16
+    table = np.arange(12).reshape(3, 4).astype(np.int32)
+    lens = [5, 33, 64]
+    for r, n in enumerate(lens):
+        for p in range(n, 64):
+            for s in (buffers.k_scales, buffers.v_scales):
+                s[table[r, p // page], :, p % page] = [float("nan"), float("inf"), -float("inf")][p % 3]
+    attend(rng, lens, [1, 1, 1], 2, 4, 128, 16, table=table, cache=(buffers, k, v))
+    attend(rng, lens, [5, 20, 40], 2, 4, 128, 16, table=table, cache=(buffers, k, v))
+
+
+def test_attention_long_context():
+    """Few rows over a long axis: the work is split and joined. Offsets of the code bytes pass 32
+    bits (a cache of more than 4 GiB, most of it unread)."""
+    say("long")
+    rng = np.random.default_rng(13)
+    pages, heads, page, dim = 70000, 8, 128, 128
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("needs 24 GiB of device memory")
+    small, k, v = make_cache(rng, 12, heads, dim, page)
+    where = np.sort(rng.choice(pages, 12, replace=False))
+    where[-1] = pages - 1
+    big = L.kv4_cache(pages, heads, dim, page)
+    for b, s in zip(big, small):
+        b[dev(where)] = s
+    n = 8000
+    pick = rng.integers(0, 12, (2, -(-n // page)))
+    lens, starts = np.array([n, 4097]), np.array([0, 1, 2])
+    q = dev(rng.standard_normal((2, 32, dim)).astype(np.float32)).half()
+    lse = torch.empty((2, 32), device=DEV)
+    out = L.kv4_attention(q, big, dev(where[pick].astype(np.int32)), dev(lens.astype(np.int32)),
+                          dev(starts.astype(np.int32)), 1, lse=lse)
+    ref, ref_lse, size, reach = S.attention(host(q), k, v, pick, lens, starts, page, dim ** -0.5)
+    d = (dim + 16) * 2.0 ** -23 * (reach + 2)
+    bound = (2 * d[..., None] + 2.0 ** -10) * size + 2.0 ** -11 * np.abs(ref)
+    assert float(np.max(np.abs(host(out) - ref) / bound)) <= 1.0
+    assert float(np.max(np.abs(host(lse) - ref_lse) - d)) <= 2.0 ** -11
+
+
+def test_attention_strided_queries_streams_and_graph():
+    """Queries inside a fused buffer; a call on another stream; a replayed graph with new inputs;
+    results that do not change from call to call."""
+    say("strides, streams, graph")
+    rng = np.random.default_rng(14)
+    lens, new = [700, 65, 1200], [1, 1, 1]
+    buffers, q, out, lse, table, lens, starts = attend(rng, lens, new, 2, 4, 128, 64)
+    args = (dev(table), dev(np.asarray(lens, dtype=np.int32)), dev(starts), 1)
+    fused = torch.zeros((3, 8 * 128 + 256), device=DEV, dtype=torch.float16)
+    fused[:, 128:1152] = q.flatten(1)
+    strided = fused[:, 128:1152].view(3, 8, 128)
+    assert torch.equal(L.kv4_attention(strided, buffers, *args), out)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    other = L.kv4_attention(q, buffers, *args, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(other, out)
+    work = torch.empty(L.KV4_WORKSPACE_BYTES, dtype=torch.uint8, device=DEV)
+    held, res = q.clone(), torch.empty_like(out)
+    L.kv4_attention(held, buffers, *args, out=res, workspace=work)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        L.kv4_attention(held, buffers, *args, out=res, workspace=work)
+    for i in range(4):
+        fresh = torch.randn_like(q)
+        held.copy_(fresh)
+        res.fill_(9)
+        graph.replay()
+        torch.cuda.synchronize()
+        work.fill_(255 if i % 2 else 0)          # nothing is kept in the workspace
+        assert torch.equal(res, L.kv4_attention(fresh, buffers, *args)), i
+
+
+# ------------------------------------------------------------------ token log probabilities
+
+def check_logprobs(x, targets, top, workspace=None):
+    """The sums are float32: n terms in a chain of at most vocab / 256 + 64 additions, each term off
+    by 2^-22 (|x - peak| + 2) of itself, which weighs little where |x - peak| is large."""
+    got = L.token_logprobs(x, targets, top, workspace=workspace)
+    vocab = x.shape[1]
+    row = host(x)
+    lp, ent, index, best = S.token_logprobs(row, targets.cpu().numpy(), top)
+    eps = (vocab / 256 + 64) * 2.0 ** -24 + 2.0 ** -20
+    big = np.abs(np.where(np.isfinite(row), row, 0)).max(1)
+
+    def near(a, b, tol):
+        a, b, tol = np.broadcast_arrays(a, b, tol)
+        assert np.array_equal(np.isnan(a), np.isnan(b))
+        assert np.array_equal(np.isneginf(a), np.isneginf(b))
+        f = np.isfinite(b)
+        assert float(np.max((np.abs(a - b) - tol)[f], initial=-1.0)) <= 0.0
+
+    near(host(got["logprob"]), lp, eps + 2.0 ** -22 * big)
+    near(host(got["entropy"]), ent, (eps + 2.0 ** -22 * big) * (2 + np.nan_to_num(np.abs(ent))))
+    assert np.array_equal(got["top_index"].cpu().numpy(), index)
+    near(host(got["top_logprob"]), best, (eps + 2.0 ** -22 * big)[:, None])
+    return got
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("tokens,vocab,top", [(1, 1, 1), (1, 1, 0), (3, 7, 7), (2, 33, 32), (5, 64, 3),
+                                              (4, 1000, 20), (2, 4097, 5), (1, 50001, 32),
+                                              (1, 131072, 20), (37, 2049, 1), (300, 513, 4)])
+def test_logprobs_sizes(tokens, vocab, top, dtype):
+    say("logprobs", tokens, vocab, top, dtype)
+    g = torch.Generator(device=DEV).manual_seed(vocab)
+    x = (3 * torch.randn((tokens, vocab), generator=g, device=DEV)).to(TYPES[dtype])
+    check_logprobs(x, torch.randint(0, vocab, (tokens,), generator=g, device=DEV), top)
+
+
+@pytest.mark.parametrize("tokens,vocab", [(1, 9000), (40, 3001)])
+def test_logprobs_ties_and_order(tokens, vocab):
+    """Equal logits everywhere, rising and falling rows (every element a new best), many ties, -0."""
+    say("logprobs ties", tokens, vocab)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    target = torch.randint(0, vocab, (tokens,), generator=g, device=DEV)
+    rise = torch.arange(vocab, device=DEV, dtype=torch.float32).repeat(tokens, 1)
+    for x in (torch.zeros((tokens, vocab), device=DEV), rise * 0.01, rise.flip(1) * 0.01,
+              torch.randint(0, 5, (tokens, vocab), generator=g, device=DEV).float(),
+              torch.where(rise % 2 == 0, 0.0, -0.0), -rise):
+        check_logprobs(x, target, 32)
+        check_logprobs(x.half(), target, 6)
+
+
+def test_logprobs_special_values():
+    """-inf (all but one, all but few, all), +inf, NaN, targets outside, huge logits."""
+    say("logprobs special")
+    inf, nan = math.inf, math.nan
+    for vocab in (40, 5000):
+        x = torch.randn((9, vocab), device=DEV, generator=torch.Generator(device=DEV).manual_seed(1))
+        x[0, 1:] = -inf
+        x[1, 3:] = -inf
+        x[2] = -inf
+        x[3, 5] = inf
+        x[4, 7] = nan
+        x[5] = nan
+        x[6] = 1e38 * x[6].sign()
+        x[7, ::2] = -inf
+        x[8, 0], x[8, vocab - 1] = torch.finfo(torch.float32).min, 80.0
+        for targets in ([0, 0, 0, 0, 0, 0, 0, 0, 0], [5, vocab - 1, 3, 5, 7, 9, 11, 0, 0],
+                        [-1, vocab, -100, 2**40, 1, -1, -1, -1, vocab]):
+            check_logprobs(x, torch.tensor(targets, device=DEV), 6)
+
+
+def test_logprobs_strided_streams_and_graph():
+    """Rows inside wider ones at odd strides and offsets; another stream; a replayed graph; one
+    workspace from call to call, left zero."""
+    say("logprobs strides, graph")
+    work = torch.zeros(L.LOGPROBS_WORKSPACE_BYTES, dtype=torch.uint8, device=DEV)
+    for dtype in TYPES.values():
+        wide = torch.randn((6, 3003), device=DEV).to(dtype)
+        for x in (wide[:, 1:2999], wide[::2, 3:], wide[1:2, 5:2000]):
+            t = torch.randint(0, x.shape[1], (x.shape[0],), device=DEV)
+            check_logprobs(x, t, 9, workspace=work)
+    x = torch.randn((2, 70001), device=DEV)
+    t = torch.tensor([5, 70000], device=DEV)
+    ref = check_logprobs(x, t, 11, workspace=work)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = L.token_logprobs(x, t, 11)
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(ref[n], other[n]) for n in ref)
+    held, out = x.clone(), {n: torch.empty_like(r) for n, r in ref.items()}
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        L.token_logprobs(held, t, 11, out=out, workspace=work)
+    for i in range(4):
+        fresh = torch.randn_like(x)
+        held.copy_(fresh)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert not work.any()
+        want = L.token_logprobs(fresh, t, 11)
+        assert all(torch.equal(want[n], out[n]) for n in out), i
+
+
+# ------------------------------------------------------------------ together
+
+def test_step_of_appended_tokens():
+    """Tables, append and attention of two steps (a prompt, then a token each) equal attention
+    over the values that the cache stands for."""
+    say("step")
+    rng = np.random.default_rng(21)
+    page, heads, group, dim, n = 16, 2, 4, 64, 3
+    cache = L.kv4_cache(40, heads, dim, page)
+    table = torch.full((n, 8), -1, dtype=torch.int32, device=DEV)
+    free = dev(rng.permutation(40).astype(np.int32))
+    cached, new = np.zeros(n, dtype=np.int32), np.array([33, 1, 90], dtype=np.int32)
+    for step in range(2):
+        total = int(new.sum())
+        t = L.batch_tables(dev(cached), dev(new), free, table, page, total)
+        free = free[int(t["info"][1]):].contiguous()
+        k, v = (dev(rng.standard_normal((total, heads, dim)).astype(np.float32)) for _ in range(2))
+        q = dev(rng.standard_normal((total, heads * group, dim)).astype(np.float32)).half()
+        L.kv4_append(k, v, cache, t["slots"])
+        out = L.kv4_attention(q, cache, table, t["seq_lens"], t["q_starts"], int(new.max()))
+        kk = S.kv4_values(S.unpack_keys(cache.k_codes.cpu().numpy()), host(cache.k_scales))
+        vv = S.kv4_values(S.unpack_values(cache.v_codes.cpu().numpy()), host(cache.v_scales))
+        ref, _, size, _ = S.attention(host(q), kk, vv, table.cpu().numpy(), host(t["seq_lens"]),
+                                      host(t["q_starts"]), page, dim ** -0.5)
+        assert float(np.max(np.abs(host(out) - ref) / (size + 1e-9))) <= 2.0 ** -8
+        cached, new = cached + new, np.ones(n, dtype=np.int32)
