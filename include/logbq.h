@@ -498,7 +498,7 @@ int32_t logbq_kv4_read(const logbq_kv4* cache, const int64_t* slots_dev, int64_t
  *   q_heads    : a multiple of cache->heads, at most 16 times it; query head h reads key/value
  *                head h / (q_heads / heads).
  *   table_dev  : device, [requests][width] int32 page ids; a negative entry, or one past the
- *                cache, hides its page.
+ *                cache, hides its page. width * page <= 2^30.
  *   seq_lens_dev : device, [requests] int32, cached tokens with this step's, which are already
  *                appended.
  *   q_starts_dev : device, [requests + 1] int32, first token of each request.
@@ -513,8 +513,8 @@ int32_t logbq_kv4_read(const logbq_kv4* cache, const int64_t* slots_dev, int64_t
  * Token i of n new ones of a request of length s has position p = s - n + i and sees positions
  * max(0, p - window + 1) .. p (0 .. p without a window). A token that sees nothing has output 0
  * and lse -inf. Products of q are taken in float16 (float32 queries as a sum of two float16
- * values), all sums and the softmax in float32, its weights rounded to float16 for the product
- * with the values.
+ * values), all sums and the softmax in float32; its weights are rounded to 11 bits at least for the
+ * product with the values.
  * Errors: INVALID_ARG, UNSUPPORTED (dim, page, heads, dtypes, alignment, sizes, a workspace that
  * is too small), HIP.
  */

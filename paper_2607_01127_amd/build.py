@@ -1,5 +1,6 @@
 """Build liblogbq.so in-tree: the host fit with g++, the gfx950 kernels with hipcc (the linears and
-the quantizer in logbq_kernels.hip, the serving operators in serving_kernels.hip). Also builds
+the quantizer in logbq_kernels.hip, the serving operators in serving_kernels.hip
+and kv4_attention.hip). Also builds
 libhbmread.so, the streaming-read kernel bench.py measures the HBM read ceiling with.
 
 The host fit is compiled without -ffast-math and with -ffp-contract=off so that its float64
@@ -38,7 +39,7 @@ def _run(cmd, verbose):
     subprocess.run(cmd, check=True)
 
 
-KERNEL_SOURCES = ("logbq_kernels", "serving_kernels")
+KERNEL_SOURCES = ("logbq_kernels", "serving_kernels", "kv4_attention")
 
 
 def build(verbose: bool = False) -> str:

@@ -1,11 +1,10 @@
 // gfx950 kernels of a serving step around the linears, and their entry points of the C ABI: block
-// tables and slot maps, the 4-bit key/value cache's append and read-back, attention over it, and
-// token log probabilities.
+// tables and slot maps, the 4-bit key/value cache's append and read-back, and token log
+// probabilities (attention over the cache is in kv4_attention.hip).
 //
 //   k_batch_tables   prefix sums of the requests' lengths, then slots, positions and new pages.
 //   k_kv4_append     rows of keys and values -> 4-bit codes and bfloat16 scales in their slots.
 //   k_kv4_read       the values that the cache holds in given slots.
-//   k_kv4_attention  softmax(scale q K^T) V over the paged 4-bit cache.
 //   k_token_logprobs log softmax of given tokens, entropy and top alternatives.
 
 #include <hip/hip_runtime.h>
@@ -13,43 +12,10 @@
 #include <cmath>
 #include <cstdint>
 
+#include "kv4_detail.h"
 #include "logbq.h"
 
 namespace {
-
-typedef _Float16 half_t;
-typedef half_t half2v __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-
-inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-
-int32_t launch_status() {
-  return hipGetLastError() == hipSuccess ? LOGBQ_OK : LOGBQ_ERR_HIP;
-}
-
-// Bytes of one element, or 0 for a type that is none.
-int dtype_bytes(int32_t dtype) {
-  return dtype == LOGBQ_DTYPE_F32 ? 4 : dtype == LOGBQ_DTYPE_F16 || dtype == LOGBQ_DTYPE_BF16 ? 2 : 0;
-}
-
-__device__ __forceinline__ float bf16_value(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
-
-// float32 value of element i of an array of a type.
-template <int DT>
-__device__ __forceinline__ float load_element(const void* p, int64_t i) {
-  if (DT == LOGBQ_DTYPE_F32) return static_cast<const float*>(p)[i];
-  if (DT == LOGBQ_DTYPE_F16) return (float)static_cast<const half_t*>(p)[i];
-  return bf16_value(static_cast<const uint16_t*>(p)[i]);
-}
-
-// x rounded to nearest into element i of an array of a type.
-__device__ __forceinline__ void store_element(void* p, int32_t dtype, int64_t i, float x) {
-  if (dtype == LOGBQ_DTYPE_F32) static_cast<float*>(p)[i] = x;
-  else if (dtype == LOGBQ_DTYPE_F16) static_cast<half_t*>(p)[i] = (half_t)x;
-  else static_cast<__bf16*>(p)[i] = (__bf16)x;
-}
 
 // ------------------------------------------------------------------ block tables
 // Every workgroup takes the prefix sums of all requests (a request's first token, and the pages
@@ -188,35 +154,11 @@ __global__ __launch_bounds__(kTabThreads) void k_batch_tables(TabArgs a) {
 }
 
 // ------------------------------------------------------------------ the 4-bit cache
-struct Kv4 {
-  uint8_t* k_codes;
-  uint8_t* v_codes;
-  uint16_t* k_scales;
-  uint16_t* v_scales;
-  int64_t slots;          // pages * page
-  int32_t heads, page_shift;
-};
-
 // 16 lanes take a row: lane c has channels c D/16 .. (c + 1) D/16 - 1, which are one group of the
 // value layout. A wavefront takes 4 consecutive tokens of one head.
 constexpr int kRowLanes = 16;
 constexpr int kRowThreads = 256;
 constexpr int kRowTokens = 4;
-
-// Byte offset of a lane's codes of one row, and the index of the row's scale.
-template <int D, bool VALUES>
-__device__ __forceinline__ int64_t code_offset(const Kv4& c, int64_t slot, int head, int group) {
-  const int64_t page = slot >> c.page_shift;
-  const int off = (int)slot & ((1 << c.page_shift) - 1);
-  const int64_t block = (page * c.heads + head) << c.page_shift;       // rows before this page
-  if (VALUES)
-    return (block + (off & ~7)) * (D / 2) + group * (D / 4) + (off & 7) * (D / 32);
-  return (block + off) * (D / 2) + group * (D / 32);
-}
-__device__ __forceinline__ int64_t scale_index(const Kv4& c, int64_t slot, int head) {
-  const int64_t page = slot >> c.page_shift;
-  return ((page * c.heads + head) << c.page_shift) + (slot & ((1 << c.page_shift) - 1));
-}
 
 // N codes of 4 bits as N / 8 words (N = 4: the low half of one word).
 template <int N>
@@ -233,28 +175,6 @@ __device__ __forceinline__ void load_codes(const uint8_t* from, uint32_t (&w)[(N
     const u32x2 v = *reinterpret_cast<const u32x2*>(from);
     w[0] = v.x;
     w[(N + 7) / 8 - 1] = v.y;
-  }
-}
-
-template <int DT, int N>
-__device__ __forceinline__ void load_row(const void* p, int64_t i, float (&x)[N]) {
-  if (DT == LOGBQ_DTYPE_F32) {
-#pragma unroll
-    for (int j = 0; j < N; j += 4) {
-      const f32x4 v = *reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + i + j);
-      x[j] = v.x; x[j + 1] = v.y; x[j + 2] = v.z; x[j + 3] = v.w;
-    }
-    return;
-  }
-#pragma unroll
-  for (int j = 0; j < N; j += 4) {
-    const u32x2 v = *reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(p) + i + j);
-    const uint32_t w[2] = {v.x, v.y};
-#pragma unroll
-    for (int h = 0; h < 4; ++h) {
-      const uint16_t b = (uint16_t)(w[h >> 1] >> (16 * (h & 1)));
-      x[j + h] = DT == LOGBQ_DTYPE_BF16 ? bf16_value(b) : (float)__builtin_bit_cast(half_t, b);
-    }
   }
 }
 
@@ -316,14 +236,6 @@ __global__ __launch_bounds__(kRowThreads) void k_kv4_append(const void* k, int64
   append_row<D, DT, true>(v, t * v_stride + at, c, slot, head, group);
 }
 
-// float32 value of a code.
-__device__ __forceinline__ float code_value(uint32_t nibble) {
-  const uint32_t m = nibble & 7u;
-  // 2^(m >> 1) (1 + (m & 1) / 2) / 2 for m >= 2, m / 2 below.
-  const float x = m < 2u ? 0.5f * (float)m : __uint_as_float(((126u + (m >> 1)) << 23) | ((m & 1u) << 22));
-  return nibble & 8u ? -x : x;
-}
-
 template <int D, bool VALUES>
 __device__ __forceinline__ void read_row(const Kv4& c, int64_t slot, bool held, int head, int group,
                                          void* to, int64_t at, int32_t dtype) {
@@ -352,96 +264,6 @@ __global__ __launch_bounds__(kRowThreads) void k_kv4_read(Kv4 c, const int64_t* 
   const int64_t at = (t * c.heads + head) * D + group * (D / 16);
   read_row<D, false>(c, slot, held, head, group, k, at, dtype);
   read_row<D, true>(c, slot, held, head, group, v, at, dtype);
-}
-
-// ------------------------------------------------------------------ attention
-struct AttnArgs {
-  const void* q;
-  const int32_t* table;
-  const int32_t* seq_lens;
-  const int32_t* q_starts;
-  void* out;
-  float* lse;
-  Kv4 c;
-  int64_t q_stride, width, tokens;
-  float scale;
-  int32_t requests, group, window, q_dtype, out_dtype;
-};
-
-// One wavefront takes one query head of one token and goes over the positions it sees, 64 at a
-// time: lane j has the score of position j of the 64, then D / 64 channels of the output.
-template <int D>
-__global__ __launch_bounds__(64) void k_kv4_attention(AttnArgs a) {
-  __shared__ float q[D];
-  const int lane = threadIdx.x;
-  const int64_t t = blockIdx.x;
-  const int qh = blockIdx.y, head = qh / a.group;
-  int lo = 0, hi = a.requests;              // the request of token t
-  if (t < a.q_starts[0] || t >= a.q_starts[hi]) return;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (a.q_starts[mid] <= t) lo = mid; else hi = mid;
-  }
-  const int64_t span = a.width << a.c.page_shift;
-  const int64_t place = (int64_t)a.seq_lens[lo] - a.q_starts[lo + 1] + t;
-  int64_t from = a.window ? place - a.window + 1 : 0;
-  from = from > 0 ? from : 0;
-  const int64_t end = place + 1 < span ? place + 1 : span;
-  const int64_t qat = t * a.q_stride + (int64_t)qh * D;
-  for (int i = lane; i < D; i += 64) {
-    const float x = a.q_dtype == LOGBQ_DTYPE_F32 ? load_element<LOGBQ_DTYPE_F32>(a.q, qat + i)
-                    : a.q_dtype == LOGBQ_DTYPE_F16 ? load_element<LOGBQ_DTYPE_F16>(a.q, qat + i)
-                                                   : load_element<LOGBQ_DTYPE_BF16>(a.q, qat + i);
-    q[i] = x * a.scale;
-  }
-  __syncthreads();
-  float top = -INFINITY, total = 0.0f, o[D / 64] = {};
-  for (int64_t base = from; base < end; base += 64) {
-    const int64_t p = base + lane;
-    float s = -INFINITY, v_scale = 0.0f;
-    int64_t slot = -1;
-    if (p < end) {
-      const int32_t id = a.table[lo * a.width + (p >> a.c.page_shift)];
-      slot = ((int64_t)id << a.c.page_shift) + (p & ((1 << a.c.page_shift) - 1));
-      if (id < 0 || slot >= a.c.slots) slot = -1;
-    }
-    if (slot >= 0) {
-      const uint8_t* row = a.c.k_codes + code_offset<D, false>(a.c, slot, head, 0);
-      float dot = 0.0f;
-      for (int i = 0; i < D / 2; ++i) {
-        const uint32_t b = row[i];
-        dot += q[2 * i] * code_value(b & 15u) + q[2 * i + 1] * code_value(b >> 4);
-      }
-      const int64_t si = scale_index(a.c, slot, head);
-      s = dot * bf16_value(a.c.k_scales[si]);
-      v_scale = bf16_value(a.c.v_scales[si]);
-    }
-    float m = s;
-    for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
-    if (m == -INFINITY) continue;
-    m = fmaxf(m, top);
-    const float old = __expf(top - m), e = __expf(s - m);
-    float sum = e;
-    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
-    total = total * old + sum;
-    top = m;
-    for (int i = 0; i < D / 64; ++i) o[i] *= old;
-    const float weight = e * v_scale;
-    for (int j = 0; j < 64; ++j) {
-      const float w = __shfl(weight, j);
-      const int64_t at = __shfl(slot, j);
-      if (at < 0) continue;
-      for (int i = 0; i < D / 64; ++i) {
-        const int ch = lane + 64 * i, g = ch / (D / 16), n = ch % (D / 16);
-        const uint8_t b = a.c.v_codes[code_offset<D, true>(a.c, at, head, g) + n / 2];
-        o[i] += w * code_value((uint32_t)b >> (4 * (n & 1)) & 15u);
-      }
-    }
-  }
-  const int heads = gridDim.y;
-  for (int i = 0; i < D / 64; ++i)
-    store_element(a.out, a.out_dtype, (t * heads + qh) * D + lane + 64 * i, total > 0 ? o[i] / total : 0.0f);
-  if (a.lse && lane == 0) a.lse[t * heads + qh] = total > 0 ? top + logf(total) : -INFINITY;
 }
 
 // ------------------------------------------------------------------ token log probabilities
@@ -521,24 +343,6 @@ __global__ __launch_bounds__(kLpThreads) void k_token_logprobs(
 }
 
 // ------------------------------------------------------------------ host side
-// The cache as the kernels take it; LOGBQ_OK or what is wrong with it.
-int32_t kv4_of(const logbq_kv4* c, Kv4* to) {
-  if (!c || c->pages < 0 || c->heads < 1) return LOGBQ_ERR_INVALID_ARG;
-  if (c->dim != 64 && c->dim != 128 && c->dim != 256) return LOGBQ_ERR_UNSUPPORTED;
-  if (c->page < 16 || c->page > 1024 || (c->page & (c->page - 1))) return LOGBQ_ERR_UNSUPPORTED;
-  // Slots fit 31 bits, and no buffer's size passes 2^49 bytes.
-  if (c->heads > 1024 || c->pages > INT32_MAX / c->page) return LOGBQ_ERR_UNSUPPORTED;
-  if (c->pages > 0) {
-    if (!c->k_codes || !c->v_codes || !c->k_scales || !c->v_scales) return LOGBQ_ERR_INVALID_ARG;
-    if (!aligned16(c->k_codes) || !aligned16(c->v_codes) || !aligned16(c->k_scales) ||
-        !aligned16(c->v_scales))
-      return LOGBQ_ERR_UNSUPPORTED;
-  }
-  *to = {c->k_codes, c->v_codes, c->k_scales, c->v_scales, c->pages * c->page, c->heads,
-         __builtin_ctz((unsigned)c->page)};
-  return LOGBQ_OK;
-}
-
 // Workgroups for `tokens` tokens of all heads, or 0 if they are too many for one launch.
 unsigned row_grid(int64_t tokens, int32_t heads) {
   const int64_t units = (tokens + kRowTokens - 1) / kRowTokens * heads;
@@ -624,42 +428,6 @@ int32_t logbq_kv4_read(const logbq_kv4* cache, const int64_t* slots_dev, int64_t
                        slots_dev, tokens, k_dev, v_dev, dtype)
   READ(64); READ(128); READ(256);
 #undef READ
-  return launch_status();
-}
-
-int32_t logbq_kv4_attention(const void* q_dev, int64_t q_stride, int32_t q_dtype, int64_t tokens,
-                            int32_t q_heads, const logbq_kv4* cache, const int32_t* table_dev,
-                            int64_t requests, int64_t width, const int32_t* seq_lens_dev,
-                            const int32_t* q_starts_dev, int64_t max_new, float scale,
-                            int32_t window, void* out_dev, int32_t out_dtype, float* lse_dev,
-                            void* work_dev, int64_t work_bytes, void* stream) {
-  Kv4 c;
-  if (tokens < 0 || requests < 0 || width < 0 || max_new < 0 || window < 0 || q_heads < 1 ||
-      work_bytes < 0 || !std::isfinite(scale))
-    return LOGBQ_ERR_INVALID_ARG;
-  const int32_t bad = kv4_of(cache, &c);
-  if (bad != LOGBQ_OK) return bad;
-  const int bytes = dtype_bytes(q_dtype);
-  if (!bytes || !dtype_bytes(out_dtype)) return LOGBQ_ERR_UNSUPPORTED;
-  if (q_heads % c.heads || q_heads / c.heads > 16) return LOGBQ_ERR_UNSUPPORTED;
-  if (tokens >= INT32_MAX || requests >= INT32_MAX || width > INT32_MAX / cache->page)
-    return LOGBQ_ERR_UNSUPPORTED;
-  if (tokens == 0 || requests == 0 || max_new == 0) return LOGBQ_OK;
-  if (!q_dev || !out_dev || !seq_lens_dev || !q_starts_dev || !work_dev || (width > 0 && !table_dev))
-    return LOGBQ_ERR_INVALID_ARG;
-  if (!aligned16(work_dev) || work_bytes < LOGBQ_KV4_WORKSPACE_BYTES) return LOGBQ_ERR_UNSUPPORTED;
-  if (q_stride < (int64_t)q_heads * cache->dim || q_stride > INT64_MAX / 8 / tokens)
-    return LOGBQ_ERR_UNSUPPORTED;
-  if (!aligned16(q_dev) || !aligned16(out_dev) || q_stride * bytes % 16) return LOGBQ_ERR_UNSUPPORTED;
-  AttnArgs a = {q_dev, table_dev, seq_lens_dev, q_starts_dev, out_dev, lse_dev, c, q_stride, width,
-                tokens, scale, (int32_t)requests, q_heads / c.heads, window, q_dtype, out_dtype};
-  const dim3 grid((unsigned)tokens, (unsigned)q_heads);
-  if (cache->dim == 64)
-    hipLaunchKernelGGL(k_kv4_attention<64>, grid, dim3(64), 0, (hipStream_t)stream, a);
-  else if (cache->dim == 128)
-    hipLaunchKernelGGL(k_kv4_attention<128>, grid, dim3(64), 0, (hipStream_t)stream, a);
-  else
-    hipLaunchKernelGGL(k_kv4_attention<256>, grid, dim3(64), 0, (hipStream_t)stream, a);
   return launch_status();
 }
 
