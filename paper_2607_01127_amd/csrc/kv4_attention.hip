@@ -3,7 +3,8 @@
 //   k_kv4_decode   requests of one token or a few: all query heads of a key/value head at once, the
 //                  cached positions of the whole batch dealt out evenly over the workgroups.
 //   k_kv4_join     sums the parts of what more than one workgroup of k_kv4_decode had.
-//   k_kv4_prompt   requests with more tokens.
+//   k_kv4_prompt   requests with more tokens: 128 query rows a workgroup, converted keys and values in
+//                  LDS; few rows have their positions split, and k_kv4_prompt_join sums the splits.
 
 #include <hip/hip_runtime.h>
 
@@ -106,6 +107,11 @@ __device__ __forceinline__ half8v values_of(uint32_t w) {
   const half2v c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 2);
   const half2v d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 3);
   return half8v{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+}
+// Bfloat16 values of a byte of a word.
+template <int BYTE>
+__device__ __forceinline__ bf16x2 fp4_pair(uint32_t w) {
+  return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, BYTE);
 }
 // Bfloat16 values of the same byte of four words.
 template <int BYTE>
@@ -519,84 +525,450 @@ __global__ __launch_bounds__(kDecThreads) void k_kv4_join(AttnArgs a, int kRows)
   if (a.lse && ch == 0) a.lse[at] = l > 0.0f ? (top + __log2f(l)) * kLn2 : -INFINITY;
 }
 
-// One wavefront takes one query head of one token and goes over the positions it sees, 64 at a
-// time: lane j has the score of position j of the 64, then D / 64 channels of the output.
-template <int D>
-__global__ __launch_bounds__(64) void k_kv4_prompt(AttnArgs a, int min_rows) {
-  __shared__ float q[D];
-  const int lane = threadIdx.x;
-  const int64_t t = blockIdx.x;
-  const int qh = blockIdx.y, head = qh / a.group;
-  int lo = 0, hi = a.requests;              // the request of token t
-  if (t < a.q_starts[0] || t >= a.q_starts[hi]) return;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (a.q_starts[mid] <= t) lo = mid; else hi = mid;
+// ------------------------------------------------------------------ prompts
+// A workgroup takes 128 NB query rows (tokens x the query heads of one key/value head) and goes over
+// the positions they see, 64 at a time. All four wavefronts turn the 64 positions' codes into
+// float16 operands in LDS, in the order in which the MFMAs read them; each wavefront then has
+// 32 NB rows: S^T = K Q^T and O^T = V^T P^T with 32x32x16 MFMAs, where a lane's 8 weights of 16
+// positions are the second product's B operand as they are. Tiles are double buffered: the next
+// tile's codes are loaded before this one's products and converted after them, one barrier a tile.
+//
+// Converted keys carry their rows' scales (a code has at most 2 significant bits and a scale 8, so
+// the product is exact in float16) divided by a power of two that keeps the largest below 2^13; it
+// goes back into the scores' factor. The values' scales multiply the weights, which go into the
+// second product as two bfloat16 numbers, for the reason given above.
+constexpr int kPromptThreads = 256;
+constexpr int kPromptTile = 64;
+constexpr int kPromptMinRows = 17;           // fewer go through the decode kernel
+
+// Offset of a slot of a value fragment: the lanes of a converting wavefront differ in the chunk of
+// positions and the half, which the exclusive or spreads over the banks.
+__device__ __forceinline__ int value_slot(int frag, int chunk, int half, int channel) {
+  return frag * 64 + ((half * 32 + channel) ^ (chunk * 2 + half));
+}
+
+template <int D, int NB, bool QSPLIT>
+__global__ __launch_bounds__(kPromptThreads, D / 64 * NB <= 2 ? 2 : 1)
+void k_kv4_prompt(AttnArgs a, int splits) {
+  constexpr int kRows = 128 * NB, kKc = D / 16, kCb = D / 32, kItems = D == 256 ? 2 : 1;
+  __shared__ half8v kbuf[2][2 * kKc * 64];
+  __shared__ bf16x8 vbuf[2][kCb * 4 * 64];
+  __shared__ float vscale[2][kPromptTile];
+  __shared__ int64_t scan[4];
+  __shared__ int64_t found[2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int col = lane & 31, half = lane >> 5;
+
+  // ---- which request and rows: tiles in order of requests, the last first, as later ones of a
+  // prompt see more positions
+  const auto tiles_of = [&](const Request& q) -> int64_t {
+    const int64_t rows = (int64_t)q.n * a.group;
+    return rows < kPromptMinRows ? 0 : (rows + kRows - 1) / kRows;
+  };
+  const int head = blockIdx.x % a.c.heads;
+  const int64_t unit = gridDim.x / a.c.heads - 1 - blockIdx.x / a.c.heads;
+  const int per = (a.requests + kPromptThreads - 1) / kPromptThreads;
+  const int r0 = tid * per < a.requests ? tid * per : a.requests;
+  const int r1 = r0 + per < a.requests ? r0 + per : a.requests;
+  int64_t mine = 0;
+  for (int r = r0; r < r1; ++r) mine += tiles_of(request_of(a, r));
+  int64_t upto = mine;
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t x = __shfl_up(upto, d);
+    if (lane >= d) upto += x;
   }
-  if ((a.q_starts[lo + 1] - a.q_starts[lo]) * (int64_t)a.group < min_rows) return;
-  const int64_t span = (int64_t)a.width << a.c.page_shift;
-  const int64_t place = (int64_t)a.seq_lens[lo] - a.q_starts[lo + 1] + t;
-  int64_t from = a.window ? place - a.window + 1 : 0;
-  from = from > 0 ? from : 0;
-  const int64_t end = place + 1 < span ? place + 1 : span;
-  const int64_t qat = t * a.q_stride + (int64_t)qh * D;
-  for (int i = lane; i < D; i += 64) {
-    const float x = a.q_dtype == LOGBQ_DTYPE_F32 ? load_element<LOGBQ_DTYPE_F32>(a.q, qat + i)
-                    : a.q_dtype == LOGBQ_DTYPE_F16 ? load_element<LOGBQ_DTYPE_F16>(a.q, qat + i)
-                                                   : load_element<LOGBQ_DTYPE_BF16>(a.q, qat + i);
-    q[i] = x * a.scale;
+  if (lane == 63) scan[wave] = upto;
+  if (tid == 0) found[0] = -1;
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) upto += scan[w];
+  if (upto - mine <= unit && unit < upto) {
+    int64_t at = upto - mine;
+    for (int r = r0; r < r1; ++r) {
+      const int64_t n = tiles_of(request_of(a, r));
+      if (unit < at + n) {
+        found[0] = r;
+        found[1] = unit - at;
+        break;
+      }
+      at += n;
+    }
   }
   __syncthreads();
-  float top = -INFINITY, total = 0.0f, o[D / 64] = {};
-  for (int64_t base = from; base < end; base += 64) {
-    const int64_t p = base + lane;
-    float s = -INFINITY, v_scale = 0.0f;
-    int64_t slot = -1;
-    if (p < end) {
-      const int32_t id = a.table[(int64_t)lo * a.width + (p >> a.c.page_shift)];
-      slot = ((int64_t)id << a.c.page_shift) + (p & ((1 << a.c.page_shift) - 1));
-      if (id < 0 || slot >= a.c.slots) slot = -1;
-    }
-    if (slot >= 0) {
-      const uint8_t* row = a.c.k_codes + code_offset<D, false>(a.c, slot, head, 0);
-      float dot = 0.0f;
-      for (int i = 0; i < D / 2; ++i) {
-        const uint32_t b = row[i];
-        dot += q[2 * i] * code_value(b & 15u) + q[2 * i + 1] * code_value(b >> 4);
+  const int r = __builtin_amdgcn_readfirstlane((int)found[0]);
+  const int64_t part = ((unit * a.c.heads + head) * splits + blockIdx.y) * kRows;
+  if (r < 0) {
+    if (splits > 1 && tid == 0 && blockIdx.y == 0) a.desc[4 * (unit * a.c.heads + head)] = -1;
+    return;
+  }
+  const Request req = request_of(a, r);
+  const int row0 = __builtin_amdgcn_readfirstlane((int)found[1]) * kRows;
+  const int rows = req.n * a.group;
+  if (splits > 1 && tid == 0 && blockIdx.y == 0) {
+    int32_t* desc = a.desc + 4 * (unit * a.c.heads + head);
+    desc[0] = r;
+    desc[1] = row0;
+  }
+
+  // ---- positions: those that some row of the workgroup sees, this split's share of their tiles
+  const int row_end = row0 + kRows < rows ? row0 + kRows : rows;
+  const int seen_end = req.first + (row_end - 1) / a.group + 1;
+  const int kv_end = seen_end < req.end ? seen_end : req.end;
+  int64_t from = a.window ? (int64_t)req.first + row0 / a.group - a.window + 1 : 0;
+  const int kv_from = from > 0 ? (int)from & ~(kPromptTile - 1) : 0;
+  const int tiles = kv_end > kv_from ? (kv_end - kv_from + kPromptTile - 1) / kPromptTile : 0;
+  const int tile0 = (int)((int64_t)tiles * blockIdx.y / splits);
+  const int tile1 = (int)((int64_t)tiles * (blockIdx.y + 1) / splits);
+
+  // ---- queries
+  half8v qf[NB][kKc], ql[QSPLIT ? NB : 1][QSPLIT ? kKc : 1];
+  float qs[NB], ref[NB], sum[NB];
+  int32_t last[NB];
+  float16v o[NB][kCb];
+  const int wave_row = row0 + wave * 32 * NB;
+  const bool has_rows = wave_row < rows;
+  const int wave_end = wave_row + 32 * NB < rows ? wave_row + 32 * NB : rows;
+  const int place_lo = req.first + wave_row / a.group;              // of the wavefront's rows
+  const int place_hi = req.first + (wave_end - 1) / a.group;
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const int row = wave_row + nb * 32 + col;
+    const int token = row / a.group;
+    const int64_t at = (int64_t)(req.t0 + token) * a.q_stride +
+                       (int64_t)(head * a.group + row % a.group) * D + half * 8;
+    float x[kKc][8];
+    float most = 0.0f;
+#pragma unroll
+    for (int c = 0; c < kKc; ++c) {
+      if (row < rows) {
+        if (a.q_dtype == LOGBQ_DTYPE_F32) load_row<LOGBQ_DTYPE_F32>(a.q, at + 16 * c, x[c]);
+        else if (a.q_dtype == LOGBQ_DTYPE_F16) load_row<LOGBQ_DTYPE_F16>(a.q, at + 16 * c, x[c]);
+        else load_row<LOGBQ_DTYPE_BF16>(a.q, at + 16 * c, x[c]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[c][j] = 0.0f;
       }
-      const int64_t si = scale_index(a.c, slot, head);
-      s = dot * bf16_value(a.c.k_scales[si]);
-      v_scale = bf16_value(a.c.v_scales[si]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) most = fmaxf(most, __builtin_fabsf(x[c][j]));
     }
-    float m = s;
-    for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
-    if (m == -INFINITY) continue;
-    m = fmaxf(m, top);
-    const float old = __expf(top - m), e = __expf(s - m);
-    float sum = e;
-    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
-    total = total * old + sum;
-    top = m;
-    for (int i = 0; i < D / 64; ++i) o[i] *= old;
-    const float weight = e * v_scale;
-    for (int j = 0; j < 64; ++j) {
-      const float w = __shfl(weight, j);
-      const int64_t at = __shfl(slot, j);
-      if (at < 0) continue;
-      for (int i = 0; i < D / 64; ++i) {
-        const int ch = lane + 64 * i, g = ch / (D / 16), n = ch % (D / 16);
-        const uint8_t b = a.c.v_codes[code_offset<D, true>(a.c, at, head, g) + n / 2];
-        o[i] += w * code_value((uint32_t)b >> (4 * (n & 1)) & 15u);
+    most = fmaxf(most, __shfl_xor(most, 32));
+    const int e = most > 0.0f && most < INFINITY ? (int)(__float_as_uint(most) >> 23) - 127 : 0;
+    const float down = ldexpf(a.scale < 0.0f ? -1.0f : 1.0f, -e);
+    qs[nb] = __builtin_fabsf(a.scale) * kLog2e * ldexpf(1.0f, e);
+#pragma unroll
+    for (int c = 0; c < kKc; ++c)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float y = x[c][j] * down;
+        qf[nb][c][j] = (half_t)y;
+        if constexpr (QSPLIT) ql[nb][c][j] = (half_t)(y - (float)(half_t)y);
+      }
+    ref[nb] = kNone;
+    sum[nb] = 0.0f;
+    last[nb] = row < rows ? req.first + token : INT32_MAX;
+#pragma unroll
+    for (int c = 0; c < kCb; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[nb][c][i] = 0.0f;
+  }
+
+  // ---- loading and converting a tile. A thread has 32 channels of one position's keys (D = 256:
+  // twice), and 4 positions of 8 channels of values (D = 256: 16 channels); at D = 64 half of the
+  // threads have keys and the others 8 positions of 4 channels of values.
+  constexpr bool kSplitWaves = D == 64;
+  const bool has_keys = !kSplitWaves || wave < 2, has_values = !kSplitWaves || wave >= 2;
+  const int key_pos = kSplitWaves ? (wave & 1) * 32 + (lane & 31) : wave * 16 + (lane & 15);
+  const int key_item = kSplitWaves ? lane >> 5 : lane >> 4;
+  const int v_block = kSplitWaves ? lane >> 3 : (lane >> 1) & 7;            // of 8 positions
+  const int v_group = kSplitWaves ? (wave & 1) * 8 + (lane & 7)
+                                  : wave * 4 + (lane >> 5) * 2 + (lane & 1);
+  const int v_half = kSplitWaves ? 0 : (lane >> 4) & 1;
+  const int32_t* table = a.table + (int64_t)r * a.width;
+  const int page_mask = (1 << a.c.page_shift) - 1;
+  const int64_t pages = a.c.slots >> a.c.page_shift;
+  struct Ids { int32_t lane, key, value; };
+  struct Raw {
+    u32x4 k[kItems], v[kItems];
+    uint16_t ks, lane_ks, lane_vs;           // of its keys' position, and of position `lane`
+    uint64_t valid;                          // positions of the tile that can be seen
+    bool key_ok, value_ok;
+  };
+  const auto load_ids = [&](int base) {
+    Ids ids;
+    const auto id_at = [&](int p) { return p < kv_end ? table[p >> a.c.page_shift] : -1; };
+    ids.lane = id_at(base + lane);
+    ids.key = id_at(base + key_pos);
+    ids.value = id_at(base + 8 * v_block);
+    return ids;
+  };
+  const auto load_raw = [&](int base, const Ids& ids) {
+    Raw t;
+    const auto row_of = [&](int32_t id, int p) {
+      const int32_t page = id >= 0 && id < pages ? id : 0;
+      return (((int64_t)page * a.c.heads + head) << a.c.page_shift) + (p & page_mask);
+    };
+    const auto ok = [&](int32_t id) { return id >= 0 && id < pages; };
+    const int64_t lr = row_of(ids.lane, base + lane);
+    t.lane_ks = a.c.k_scales[lr];
+    t.lane_vs = a.c.v_scales[lr];
+    t.valid = __builtin_amdgcn_ballot_w64(ok(ids.lane));
+    t.key_ok = ok(ids.key);
+    t.value_ok = ok(ids.value);
+    if (has_keys) {
+      const int64_t kr = row_of(ids.key, base + key_pos);
+      t.ks = a.c.k_scales[kr];
+#pragma unroll
+      for (int i = 0; i < kItems; ++i)
+        t.k[i] = *reinterpret_cast<const u32x4*>(a.c.k_codes + kr * (D / 2) + (key_item + 4 * i) * 16);
+    }
+    if (has_values) {
+      const int64_t vr = row_of(ids.value, base + 8 * v_block);
+      const uint8_t* from = a.c.v_codes + vr * (D / 2) + v_group * (D / 4) + v_half * (D / 8);
+#pragma unroll
+      for (int i = 0; i < kItems; ++i) t.v[i] = *reinterpret_cast<const u32x4*>(from + 16 * i);
+    }
+    return t;
+  };
+  int ek = -200;                        // exponent that the keys' scales are divided by
+  const auto convert = [&](const Raw& t, int buf) {
+    // The exponent first; every wavefront sees all 64 scales, so all come to the same one.
+    const bool seen = (t.valid >> lane) & 1;
+    const int xk = seen ? (int)(t.lane_ks >> 7) - 127 : -127;
+    if (__builtin_amdgcn_ballot_w64(xk - ek > 12)) {
+      int mk = xk;
+      for (int d = 1; d < 64; d <<= 1) mk = max(mk, __shfl_xor(mk, d));
+      ek = mk - 10;
+    }
+    if (wave == 0) vscale[buf][lane] = seen ? bf16_value(t.lane_vs) : 0.0f;
+    if (has_keys) {
+      const half_t s = (half_t)(t.key_ok ? ldexpf(bf16_value(t.ks), -ek) : 0.0f);
+      const half8v s8 = {s, s, s, s, s, s, s, s};
+#pragma unroll
+      for (int i = 0; i < kItems; ++i)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const int chunk = 2 * (key_item + 4 * i) + (c >> 1), h = c & 1;
+          kbuf[buf][((key_pos >> 5) * kKc + chunk) * 64 + h * 32 + (key_pos & 31)] = values_of(t.k[i][c]) * s8;
+        }
+    }
+    if (has_values) {
+      const int chunk = v_block >> 1;
+      const auto put = [&](int channel, int h, bf16x2 x01, bf16x2 x23) {
+        bf16x2* to = reinterpret_cast<bf16x2*>(&vbuf[buf][value_slot((channel >> 5) * 4 + chunk, chunk, h, channel & 31)]) +
+                     2 * (v_block & 1);
+        *reinterpret_cast<bf16x4*>(to) = bf16x4{x01.x, x01.y, x23.x, x23.y};
+      };
+      constexpr uint32_t kLow = 0x0f0f0f0fu;
+      if constexpr (D == 64) {
+        // Word q: positions 2q and 2q + 1, 4 channels each.
+        uint32_t even[4], odd[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const uint32_t x = t.v[0][q] & kLow, y = (t.v[0][q] >> 4) & kLow;
+          even[q] = x | (x >> 12);
+          odd[q] = y | (y >> 12);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          put(4 * v_group, h, fp4_pair<0>(even[2 * h]), fp4_pair<0>(even[2 * h + 1]));
+          put(4 * v_group + 1, h, fp4_pair<0>(odd[2 * h]), fp4_pair<0>(odd[2 * h + 1]));
+          put(4 * v_group + 2, h, fp4_pair<1>(even[2 * h]), fp4_pair<1>(even[2 * h + 1]));
+          put(4 * v_group + 3, h, fp4_pair<1>(odd[2 * h]), fp4_pair<1>(odd[2 * h + 1]));
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+          // Position j's word of 8 channels.
+          uint32_t w[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            w[j] = D == 256 ? t.v[j >> 1][2 * (j & 1) + i] : t.v[0][j];
+          const uint32_t e01 = (w[0] & kLow) | ((w[1] << 4) & ~kLow), o01 = ((w[0] >> 4) & kLow) | (w[1] & ~kLow);
+          const uint32_t e23 = (w[2] & kLow) | ((w[3] << 4) & ~kLow), o23 = ((w[2] >> 4) & kLow) | (w[3] & ~kLow);
+          const int ch = v_group * (D / 16) + 8 * i;
+          put(ch, v_half, fp4_pair<0>(e01), fp4_pair<0>(e23));
+          put(ch + 1, v_half, fp4_pair<0>(o01), fp4_pair<0>(o23));
+          put(ch + 2, v_half, fp4_pair<1>(e01), fp4_pair<1>(e23));
+          put(ch + 3, v_half, fp4_pair<1>(o01), fp4_pair<1>(o23));
+          put(ch + 4, v_half, fp4_pair<2>(e01), fp4_pair<2>(e23));
+          put(ch + 5, v_half, fp4_pair<2>(o01), fp4_pair<2>(o23));
+          put(ch + 6, v_half, fp4_pair<3>(e01), fp4_pair<3>(e23));
+          put(ch + 7, v_half, fp4_pair<3>(o01), fp4_pair<3>(o23));
+        }
+      }
+    }
+  };
+
+  // ---- a tile's products and softmax
+  const auto compute = [&](int base, uint64_t valid, int ek_of, int buf) {
+    if (!has_rows || base > place_hi ||
+        (a.window && base + kPromptTile - 1 <= (int64_t)place_lo - a.window))
+      return;
+    const bool full = base + kPromptTile - 1 <= place_lo && valid == ~0ull &&
+                      (!a.window || base > (int64_t)place_hi - a.window);
+    const float up = exp2_fast((float)ek_of);
+#pragma unroll
+    for (int pb = 0; pb < 2; ++pb) {
+      float16v s[NB];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[nb][i] = 0.0f;
+#pragma unroll
+      for (int c = 0; c < kKc; ++c) {
+        const half8v kf = kbuf[buf][(pb * kKc + c) * 64 + lane];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          s[nb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[nb][c], s[nb], 0, 0, 0);
+          if constexpr (QSPLIT)
+            s[nb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, ql[nb][c], s[nb], 0, 0, 0);
+        }
+      }
+      bf16x8 hi[NB][2], lo[NB][2];
+      f32x4 vs[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        vs[i] = *reinterpret_cast<const f32x4*>(&vscale[buf][32 * pb + 8 * i + 4 * half]);
+      const uint32_t bits = (uint32_t)(valid >> (32 * pb)) >> (4 * half);
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        const float f = qs[nb] * up;
+        bool seen[16];
+        if (!full) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int at = 8 * (i >> 2) + (i & 3), pos = base + 32 * pb + 4 * half + at;
+            seen[i] = ((bits >> at) & 1u) && pos <= last[nb] &&
+                      (!a.window || last[nb] == INT32_MAX || pos > (int64_t)last[nb] - a.window);
+            s[nb][i] = seen[i] ? s[nb][i] : kNone;
+          }
+        }
+        float top = s[nb][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[nb][i]);
+        const float reach = top * f;
+        if (__builtin_amdgcn_ballot_w64(reach - ref[nb] > 8.0f)) {
+          const float most = fmaxf(reach, __shfl_xor(reach, 32));
+          const float next = most - ref[nb] > 8.0f ? most : ref[nb];
+          const float g = exp2_fast(ref[nb] - next);
+          ref[nb] = next;
+          sum[nb] *= g;
+#pragma unroll
+          for (int c = 0; c < kCb; ++c) o[nb][c] *= g;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float e = exp2_fast(__builtin_fmaf(s[nb][i], f, -ref[nb]));
+          if (!full) e = seen[i] ? e : 0.0f;
+          sum[nb] += e;
+          const float w = e * vs[i >> 2][i & 3];
+          const __bf16 h = (__bf16)w;
+          hi[nb][i >> 3][i & 7] = h;
+          lo[nb][i >> 3][i & 7] = (__bf16)(w - (float)h);
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int c = 0; c < kCb; ++c) {
+          const bf16x8 vf = vbuf[buf][value_slot(c * 4 + 2 * pb + h, 2 * pb + h, half, col)];
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) {
+            o[nb][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, lo[nb][h], o[nb][c], 0, 0, 0);
+            o[nb][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, hi[nb][h], o[nb][c], 0, 0, 0);
+          }
+        }
+    }
+  };
+
+  if (tile0 < tile1) {
+    const int stop = kv_from + tile1 * kPromptTile;
+    int base = kv_from + tile0 * kPromptTile;
+    Raw raw = load_raw(base, load_ids(base));
+    Ids ids = load_ids(base + kPromptTile);
+    convert(raw, 0);
+    uint64_t valid = raw.valid;
+    int buf = 0, ek_of = ek;
+    __syncthreads();
+    for (; base < stop; base += kPromptTile) {
+      const bool more = base + kPromptTile < stop;
+      if (more) {
+        raw = load_raw(base + kPromptTile, ids);
+        ids = load_ids(base + 2 * kPromptTile);
+      }
+      compute(base, valid, ek_of, buf);
+      if (more) {
+        convert(raw, buf ^ 1);
+        valid = raw.valid;
+        ek_of = ek;
+      }
+      buf ^= 1;
+      __syncthreads();
+    }
+  }
+
+  // ---- out: a lane has 4 consecutive channels of its row at a time
+  if (!has_rows) return;
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const int row = wave_row + nb * 32 + col;
+    const float l = sum[nb] + __shfl_xor(sum[nb], 32);
+    if (row >= rows) continue;
+    const int64_t at = (int64_t)(req.t0 + row / a.group) * (a.c.heads * a.group) +
+                       head * a.group + row % a.group;
+    const float inv = splits > 1 ? 1.0f : l > 0.0f ? 1.0f / l : 0.0f;
+#pragma unroll
+    for (int c = 0; c < kCb; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x4 v = {o[nb][c][4 * i] * inv, o[nb][c][4 * i + 1] * inv, o[nb][c][4 * i + 2] * inv,
+                         o[nb][c][4 * i + 3] * inv};
+        const int ch = 32 * c + 8 * i + 4 * half;
+        if (splits > 1) *reinterpret_cast<f32x4*>(a.part_o + (part + row - row0) * D + ch) = v;
+        else store_four(a.out, a.out_dtype, at * D + ch, v);
+      }
+    if (half == 0) {
+      if (splits > 1) {
+        a.part_rl[(part + row - row0) * 2] = ref[nb];
+        a.part_rl[(part + row - row0) * 2 + 1] = l;
+      } else if (a.lse) {
+        a.lse[at] = l > 0.0f ? (ref[nb] + __log2f(l)) * kLn2 : -INFINITY;
       }
     }
   }
-  const int heads = gridDim.y;
-  for (int i = 0; i < D / 64; ++i)
-    store_element(a.out, a.out_dtype, (t * heads + qh) * D + lane + 64 * i, total > 0 ? o[i] / total : 0.0f);
-  if (a.lse && lane == 0) a.lse[t * heads + qh] = total > 0 ? top + logf(total) : -INFINITY;
+}
+
+// Sums the splits of k_kv4_prompt: D / 4 threads a row.
+template <int D>
+__global__ __launch_bounds__(kPromptThreads) void k_kv4_prompt_join(AttnArgs a, int splits, int kRows) {
+  constexpr int kPer = kPromptThreads / (D / 4);
+  const int32_t* desc = a.desc + 4 * (int64_t)blockIdx.x;
+  if (desc[0] < 0) return;
+  const Request req = request_of(a, desc[0]);
+  const int head = blockIdx.x % a.c.heads;
+  const int sub = blockIdx.y * kPer + threadIdx.x / (D / 4), ch = threadIdx.x % (D / 4) * 4;
+  const int row = desc[1] + sub;
+  if (row >= req.n * a.group) return;
+  const int64_t first = (int64_t)blockIdx.x * splits * kRows + sub;
+  float top = kNone, l = 0.0f;
+  for (int i = 0; i < splits; ++i) top = fmaxf(top, a.part_rl[(first + (int64_t)i * kRows) * 2]);
+  f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+  for (int i = 0; i < splits; ++i) {
+    const int64_t p = first + (int64_t)i * kRows;
+    const float f = exp2_fast(a.part_rl[p * 2] - top);
+    l += a.part_rl[p * 2 + 1] * f;
+    v += *reinterpret_cast<const f32x4*>(a.part_o + p * D + ch) * f;
+  }
+  const int64_t at = (int64_t)(req.t0 + row / a.group) * (a.c.heads * a.group) +
+                     head * a.group + row % a.group;
+  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+  store_four(a.out, a.out_dtype, at * D + ch, l > 0.0f ? v * inv : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+  if (a.lse && ch == 0) a.lse[at] = l > 0.0f ? (top + __log2f(l)) * kLn2 : -INFINITY;
 }
 
 // ------------------------------------------------------------------ host side
+constexpr int kPromptBlocks = 1;      // 32-row blocks of a wavefront of the prompt kernel
+constexpr int kPromptGrid = 1024;     // workgroups that the splits of few rows aim at
 constexpr int kDecParts = 512;      // workgroups of the decode kernel: two a CU
 constexpr int64_t kDescBytes = 16 * kDecParts;
 
@@ -619,6 +991,34 @@ int32_t launch_decode(AttnArgs a, void* work, hipStream_t stream) {
   return launch_status();
 }
 
+template <int D, int NB>
+int32_t launch_prompt(AttnArgs a, void* work, hipStream_t stream) {
+  constexpr int kRows = 128 * NB;
+  // As many row tiles as the requests can have; each has at least kPromptMinRows rows.
+  const int64_t rows = (int64_t)a.tokens * a.group;
+  const int64_t short_ones = rows / kPromptMinRows < a.requests ? rows / kPromptMinRows : a.requests;
+  const int64_t tiles = (rows / kRows + short_ones) * a.c.heads;
+  if (tiles == 0) return LOGBQ_OK;
+  if (tiles > INT32_MAX) return LOGBQ_ERR_UNSUPPORTED;
+  int64_t splits = kPromptGrid / tiles;
+  splits = splits < 1 ? 1 : splits > 32 ? 32 : splits;
+  uint8_t* at = static_cast<uint8_t*>(work);
+  a.desc = reinterpret_cast<int32_t*>(at);
+  a.part_rl = reinterpret_cast<float*>(at + 16 * kPromptGrid);
+  a.part_o = a.part_rl + 2 * (int64_t)kPromptGrid * kRows;
+  static_assert(16 * kPromptGrid + (int64_t)kPromptGrid * kRows * (D + 2) * 4 <= LOGBQ_KV4_WORKSPACE_BYTES,
+                "the workspace holds every part");
+  const dim3 grid((unsigned)tiles, (unsigned)splits);
+  if (a.q_dtype == LOGBQ_DTYPE_F32)
+    hipLaunchKernelGGL((k_kv4_prompt<D, NB, true>), grid, dim3(kPromptThreads), 0, stream, a, (int)splits);
+  else
+    hipLaunchKernelGGL((k_kv4_prompt<D, NB, false>), grid, dim3(kPromptThreads), 0, stream, a, (int)splits);
+  if (splits == 1 || launch_status() != LOGBQ_OK) return launch_status();
+  hipLaunchKernelGGL(k_kv4_prompt_join<D>, dim3((unsigned)tiles, kRows / (kPromptThreads / (D / 4))),
+                     dim3(kPromptThreads), 0, stream, a, (int)splits, kRows);
+  return launch_status();
+}
+
 template <int D>
 int32_t launch_attention(const AttnArgs& a, int64_t max_new, void* work, hipStream_t stream) {
   const int64_t rows = max_new > INT32_MAX ? INT32_MAX : max_new * a.group;
@@ -628,9 +1028,7 @@ int32_t launch_attention(const AttnArgs& a, int64_t max_new, void* work, hipStre
   // A prompt among them: decode requests apart from the longer ones.
   const int32_t status = launch_decode<D, 1>(a, work, stream);
   if (status != LOGBQ_OK) return status;
-  hipLaunchKernelGGL(k_kv4_prompt<D>, dim3((unsigned)a.tokens, (unsigned)(a.c.heads * a.group)), dim3(64), 0,
-                     stream, a, 17);
-  return launch_status();
+  return launch_prompt<D, kPromptBlocks>(a, work, stream);
 }
 
 }  // namespace

@@ -14,7 +14,9 @@ typedef _Float16 half_t;
 typedef half_t half2v __attribute__((ext_vector_type(2)));
 typedef half_t half8v __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float float16v __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -45,6 +47,20 @@ __device__ __forceinline__ void store_element(void* p, int32_t dtype, int64_t i,
   if (dtype == LOGBQ_DTYPE_F32) static_cast<float*>(p)[i] = x;
   else if (dtype == LOGBQ_DTYPE_F16) static_cast<half_t*>(p)[i] = (half_t)x;
   else static_cast<__bf16*>(p)[i] = (__bf16)x;
+}
+
+// Four consecutive elements.
+__device__ __forceinline__ void store_four(void* p, int32_t dtype, int64_t i, f32x4 x) {
+  if (dtype == LOGBQ_DTYPE_F32) {
+    *reinterpret_cast<f32x4*>(static_cast<float*>(p) + i) = x;
+  } else if (dtype == LOGBQ_DTYPE_F16) {
+    typedef half_t half4v __attribute__((ext_vector_type(4)));
+    *reinterpret_cast<half4v*>(static_cast<half_t*>(p) + i) =
+        half4v{(half_t)x.x, (half_t)x.y, (half_t)x.z, (half_t)x.w};
+  } else {
+    *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(p) + i) =
+        bf16x4{(__bf16)x.x, (__bf16)x.y, (__bf16)x.z, (__bf16)x.w};
+  }
 }
 
 // float32 values of N consecutive elements (8-byte aligned).
