@@ -275,70 +275,354 @@ __device__ __forceinline__ uint32_t logit_key(float x) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// One workgroup a row: the largest logit, then the sums, then one pass for each alternative.
-constexpr int kLpThreads = 256;
+// A workgroup goes over its part of a row once, kLpVecs 16-byte vectors a thread at a time, the next
+// ones loaded before the present ones are used. Each thread keeps a maximum m, s = sum exp(x - m)
+// and t = sum exp(x - m) (x - m) of its own; they are joined at the end.
+//
+// Alternatives: `list` holds the best keys so far, in order, and `bound` what a new one has to
+// pass. Few elements do, so a thread looks at its elements one by one only if its maximum of the
+// step reaches the bound's value. Those that pass go into `cand`, and the list is made anew from
+// both by counting for each how many are larger. The first bound comes from the threads' maxima:
+// the top-th largest of a wavefront's 64 has at least `top` elements from it on. If a step has more
+// candidates than `cand` holds (logits in rising order), the list is made from those that found
+// room, which raises the bound, and the step is looked at again.
+//
+// Few rows are split into parts, one workgroup each; the last one of a row to finish joins them.
+constexpr int kLpThreads = 512;
+constexpr int kLpWaves = kLpThreads / 64;
+constexpr int kLpVecs = 4;
+constexpr int kLpCand = 1024;
+constexpr int kLpMaxParts = 512;                 // parts of all rows, where rows are split
+constexpr int kLpTop = LOGBQ_LOGPROBS_MAX_TOP;
 
-__device__ __forceinline__ uint64_t block_max(uint64_t v, uint64_t* tmp) {
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint64_t x = __shfl_xor((unsigned long long)v, d);
-    v = v > x ? v : x;
+struct LpPart {
+  float m, s, t, unused;
+  uint64_t keys[kLpTop];
+};
+static_assert(4 * kLpMaxParts + kLpMaxParts * sizeof(LpPart) <= LOGBQ_LOGPROBS_WORKSPACE_BYTES,
+              "the workspace holds every part");
+
+struct LpArgs {
+  const void* logits;
+  const int64_t* targets;
+  float* logprob;
+  float* entropy;
+  int32_t* top_index;
+  float* top_logprob;
+  uint32_t* arrived;          // [rows], zero between calls
+  LpPart* parts;              // [rows][splits], zero between calls
+  int64_t stride;
+  int32_t vocab, top, splits;
+};
+
+struct LpShared {
+  uint64_t cand[kLpCand];
+  uint64_t list[kLpTop];
+  uint64_t bound;             // key that a candidate has to pass
+  float m[kLpWaves], s[kLpWaves], t[kLpWaves];
+  uint32_t first[kLpWaves];   // wavefronts' first bounds
+  uint32_t listed, added, last;
+};
+
+__device__ __forceinline__ uint64_t element_key(float x, int32_t i) {
+  return (uint64_t)logit_key(x) << 32 | (uint32_t)~i;
+}
+// A float32 number no larger than any logit whose key passes the bound.
+__device__ __forceinline__ float bound_value(uint64_t key) {
+  const uint32_t k = (uint32_t)(key >> 32);
+  if (k > 0xff800000u) return INFINITY;          // NaN: looked for apart
+  if (k < 0x007fffffu) return -INFINITY;
+  return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
+}
+
+// Puts a thread's candidate down; false if there is no room.
+__device__ __forceinline__ bool add_candidate(LpShared& sh, uint64_t key) {
+  const uint32_t at = atomicAdd(&sh.added, 1u);
+  if (at < kLpCand) sh.cand[at] = key;
+  return at < kLpCand;
+}
+
+// The list from itself and the candidates; true if some found no room. All threads call it, after a
+// barrier that follows their last candidate.
+__device__ __forceinline__ bool merge_candidates(LpShared& sh, int top) {
+  const uint32_t added = sh.added, held = sh.listed;
+  if (added == 0) return false;          // nothing is written before the next barrier
+  const uint32_t n = added < kLpCand ? added : kLpCand;
+  uint64_t key[(kLpCand + kLpTop + kLpThreads - 1) / kLpThreads];
+  uint32_t rank[(kLpCand + kLpTop + kLpThreads - 1) / kLpThreads];
+  int own = 0;
+#pragma unroll
+  for (uint32_t j = 0; j < (kLpCand + kLpTop + kLpThreads - 1) / kLpThreads; ++j) {
+    const uint32_t i = threadIdx.x + j * kLpThreads;
+    if (i < n + held) own = j + 1;
+    key[j] = i < n ? sh.cand[i] : i < n + held ? sh.list[i - n] : 0;
+    rank[j] = 0;
+  }
+  if (own) {
+#pragma unroll 4
+    for (uint32_t i = 0; i < n; ++i) {
+      const uint64_t x = sh.cand[i];
+#pragma unroll
+      for (uint32_t j = 0; j < sizeof(key) / sizeof(key[0]); ++j) rank[j] += x > key[j] ? 1u : 0u;
+    }
+    for (uint32_t i = 0; i < held; ++i) {
+      const uint64_t x = sh.list[i];
+#pragma unroll
+      for (uint32_t j = 0; j < sizeof(key) / sizeof(key[0]); ++j) rank[j] += x > key[j] ? 1u : 0u;
+    }
   }
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6] = v;
+#pragma unroll
+  for (uint32_t j = 0; j < sizeof(key) / sizeof(key[0]); ++j)
+    if ((int)j < own && threadIdx.x + j * kLpThreads < n + held && rank[j] < (uint32_t)top) {
+      sh.list[rank[j]] = key[j];
+      if (rank[j] == (uint32_t)top - 1) sh.bound = key[j];
+    }
+  if (threadIdx.x == 0) {
+    sh.listed = n + held < (uint32_t)top ? n + held : (uint32_t)top;
+    sh.added = 0;
+  }
   __syncthreads();
-  for (int w = 0; w < kLpThreads / 64; ++w) v = v > tmp[w] ? v : tmp[w];
-  return v;
+  return added > kLpCand;
 }
-__device__ __forceinline__ float block_sum(float v, float* tmp) {
-  for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = 0.0f;
-  for (int w = 0; w < kLpThreads / 64; ++w) v += tmp[w];
-  return v;
+
+// Float32 values of a 16-byte vector's elements.
+template <int DT>
+__device__ __forceinline__ void vector_values(const u32x4& v, float* x) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (DT == LOGBQ_DTYPE_F32) {
+      x[i] = __uint_as_float(v[i]);
+    } else if (DT == LOGBQ_DTYPE_BF16) {
+      x[2 * i] = __uint_as_float(v[i] << 16);
+      x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+    } else {
+      const half2v h = __builtin_bit_cast(half2v, (uint32_t)v[i]);
+      x[2 * i] = (float)h.x;
+      x[2 * i + 1] = (float)h.y;
+    }
+  }
+}
+
+// Adds a term to a thread's sums about its maximum m. exp(-300) is 0 in float32, so the lower limit
+// only keeps 0 times -inf from being one of the terms; a NaN reaches both sums through e.
+__device__ __forceinline__ void add_term(float x, float m, float& s, float& t) {
+  const float d = x - m, e = __builtin_amdgcn_exp2f(d * 1.44269504088896340736f);
+  s += e;
+  t += e * fmaxf(d, -300.0f);
+}
+// Sums about m, about `to` >= m.
+__device__ __forceinline__ void move_sums(float& m, float& s, float& t, float to) {
+  const float d = m - to, f = __builtin_amdgcn_exp2f(d * 1.44269504088896340736f);
+  t = f * t + f * s * fmaxf(d, -300.0f);
+  s *= f;
+  m = to;
 }
 
 template <int DT>
-__global__ __launch_bounds__(kLpThreads) void k_token_logprobs(
-    const void* logits, int64_t vocab, int64_t stride, const int64_t* targets, int32_t top,
-    float* logprob, float* entropy, int32_t* top_index, float* top_logprob) {
-  __shared__ uint64_t keys[kLpThreads / 64];
-  __shared__ float sums[kLpThreads / 64];
-  const int64_t row = blockIdx.x, at = row * stride;
-  uint64_t below = ~0ull, first = 0;
-  float best[LOGBQ_LOGPROBS_MAX_TOP];
-  int32_t which[LOGBQ_LOGPROBS_MAX_TOP];
-  for (int n = 0; n < (top > 1 ? top : 1); ++n) {
-    uint64_t key = 0;
-    for (int64_t i = threadIdx.x; i < vocab; i += kLpThreads) {
-      const uint64_t k = (uint64_t)logit_key(load_element<DT>(logits, at + i)) << 32 | (uint32_t)~i;
-      if (k < below && k > key) key = k;
-    }
-    below = block_max(key, keys);
-    if (n == 0) first = below;
-    if (n < top && threadIdx.x == 0) {
-      which[n] = (int32_t)~(uint32_t)below;
-      best[n] = load_element<DT>(logits, at + which[n]);
-    }
+__global__ __launch_bounds__(kLpThreads) void k_token_logprobs(LpArgs a) {
+  constexpr int kBytes = DT == LOGBQ_DTYPE_F32 ? 4 : 2, kEach = 16 / kBytes, kElems = kLpVecs * kEach;
+  __shared__ LpShared sh;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t row = blockIdx.x / a.splits;
+  const int part = blockIdx.x % a.splits;
+  const uint8_t* base = static_cast<const uint8_t*>(a.logits) + row * a.stride * kBytes;
+  // The row as aligned vectors, with up to kEach - 1 elements before and after them.
+  const int skew = (int)((uintptr_t)base & 15u) / kBytes;
+  const int head = skew ? (kEach - skew < a.vocab ? kEach - skew : a.vocab) : 0;
+  const int vectors = (a.vocab - head) / kEach;
+  const int tail = a.vocab - head - vectors * kEach;
+  const u32x4* body = reinterpret_cast<const u32x4*>(base + head * kBytes);
+  const int v0 = (int)((int64_t)vectors * part / a.splits), v1 = (int)((int64_t)vectors * (part + 1) / a.splits);
+  if (tid == 0) {
+    sh.bound = 0;
+    sh.listed = sh.added = 0;
   }
-  const float peak = load_element<DT>(logits, at + (int32_t)~(uint32_t)first);
-  float sum = 0.0f, weighted = 0.0f;
-  for (int64_t i = threadIdx.x; i < vocab; i += kLpThreads) {
-    const float x = load_element<DT>(logits, at + i) - peak, e = __expf(x);
-    sum += e;
-    weighted += x == -INFINITY ? 0.0f : e * x;
+
+  u32x4 next[kLpVecs];
+  const auto fetch = [&](int from) {
+#pragma unroll
+    for (int j = 0; j < kLpVecs; ++j) {
+      const int v = from + j * kLpThreads + tid;
+      if (v < v1) next[j] = __builtin_nontemporal_load(body + v);
+    }
+  };
+  if (v0 < v1) fetch(v0);
+  // The elements outside the vectors: one a thread, in the first part.
+  const bool extra = part == 0 && tid < head + tail;
+  const int extra_at = tid < head ? tid : vectors * kEach + tid;
+  float m = -3.4028235e38f, s = 0.0f, t = 0.0f;
+  const float extra_x = extra ? load_element<DT>(base, extra_at) : -INFINITY;
+  if (extra) {
+    m = fmaxf(m, extra_x);
+    add_term(extra_x, m, s, t);
   }
-  sum = block_sum(sum, sums);
-  weighted = block_sum(weighted, sums);
-  if (threadIdx.x != 0) return;
-  const float l = logf(sum);
-  const int64_t target = targets[row];
-  logprob[row] = target >= 0 && target < vocab ? load_element<DT>(logits, at + target) - peak - l : 0.0f;
-  entropy[row] = l - weighted / sum;
-  for (int n = 0; n < top; ++n) {
-    top_index[row * top + n] = which[n];
-    top_logprob[row * top + n] = best[n] - peak - l;
+
+  for (int from = v0; from < v1 || (from == v0 && part == 0); from += kLpVecs * kLpThreads) {
+    float x[kElems];
+    int count = 0;                       // vectors that the thread has in this step
+#pragma unroll
+    for (int j = 0; j < kLpVecs; ++j) {
+      if (from + j * kLpThreads + tid < v1) {
+        vector_values<DT>(next[j], x + j * kEach);
+        count = j + 1;
+      } else {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) x[j * kEach + i] = -INFINITY;
+      }
+    }
+    if (from + kLpVecs * kLpThreads < v1) fetch(from + kLpVecs * kLpThreads);
+    float top = x[0];
+#pragma unroll
+    for (int i = 1; i < kElems; ++i) top = fmaxf(top, x[i]);
+    if (top > m) move_sums(m, s, t, top);
+#pragma unroll
+    for (int j = 0; j < kLpVecs; ++j)
+      if (from + j * kLpThreads < v1) {          // the same for all threads
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) add_term(x[j * kEach + i], m, s, t);
+      }
+    if (a.top == 0) continue;
+    const bool first = from == v0;
+    if (first) {
+      if (extra) top = fmaxf(top, extra_x);
+      const uint32_t key = logit_key(top);
+      uint32_t low = 0;
+      for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t at = low | 1u << bit;
+        if (__popcll(__builtin_amdgcn_ballot_w64(key >= at)) >= a.top) low = at;
+      }
+      if (lane == 0) sh.first[wave] = low;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < kLpWaves; ++w) low = max(low, sh.first[w]);
+      if (tid == 0) sh.bound = (uint64_t)low << 32;
+      __syncthreads();
+    }
+    uint64_t taken = 0;                          // a bit an element, the last one the extra
+    for (bool again = true; again;) {
+      const uint64_t bound = sh.bound;
+      if (top >= bound_value(bound) || s != s) {
+#pragma unroll
+        for (int i = 0; i < kElems; ++i) {
+          const int32_t at = head + (from + i / kEach * kLpThreads + tid) * kEach + i % kEach;
+          const uint64_t key = element_key(x[i], at);
+          if (i / kEach < count && key > bound && !(taken >> i & 1) && add_candidate(sh, key))
+            taken |= 1ull << i;
+        }
+        if (first && extra) {
+          const uint64_t key = element_key(extra_x, extra_at);
+          if (key > bound && !(taken >> 63) && add_candidate(sh, key)) taken |= 1ull << 63;
+        }
+      }
+      __syncthreads();
+      again = merge_candidates(sh, a.top);
+    }
+    __syncthreads();
+  }
+
+  // The threads' sums, joined over the wavefront and then the workgroup.
+  for (int d = 1; d < 64; d <<= 1) {
+    float m2 = __shfl_xor(m, d), s2 = __shfl_xor(s, d), t2 = __shfl_xor(t, d);
+    const float to = fmaxf(m, m2);
+    move_sums(m, s, t, to);
+    move_sums(m2, s2, t2, to);
+    s += s2;
+    t += t2;
+  }
+  if (lane == 0) {
+    sh.m[wave] = m;
+    sh.s[wave] = s;
+    sh.t[wave] = t;
+  }
+  __syncthreads();
+  m = sh.m[0], s = sh.s[0], t = sh.t[0];
+  for (int w = 1; w < kLpWaves; ++w) {
+    float m2 = sh.m[w], s2 = sh.s[w], t2 = sh.t[w];
+    const float to = fmaxf(m, m2);
+    move_sums(m, s, t, to);
+    move_sums(m2, s2, t2, to);
+    s += s2;
+    t += t2;
+  }
+
+  if (a.splits > 1) {
+    LpPart* parts = a.parts + row * a.splits;
+    if (tid == 0) {
+      parts[part].m = m;
+      parts[part].s = s;
+      parts[part].t = t;
+    }
+    if (tid < a.top) parts[part].keys[tid] = tid < (int)sh.listed ? sh.list[tid] : 0;
+    __threadfence();
+    __syncthreads();
+    if (tid == 0) sh.last = atomicAdd(a.arrived + row, 1u);
+    __syncthreads();
+    if (sh.last != (uint32_t)a.splits - 1) return;
+    __threadfence();
+    // All parts are there. Their last alternatives bound the row's; a key of 0 is none.
+    if (tid == 0) {
+      sh.listed = sh.added = 0;
+      sh.bound = 0;
+    }
+    __syncthreads();
+    if (a.top > 0) {
+      uint64_t bound = 0;
+      for (int i = lane; i < a.splits; i += 64) {
+        const uint64_t k = parts[i].keys[a.top - 1];
+        bound = k > bound ? k : bound;
+      }
+      for (int d = 1; d < 64; d <<= 1) {
+        const uint64_t k = __shfl_xor((unsigned long long)bound, d);
+        bound = k > bound ? k : bound;
+      }
+      if (tid == 0 && bound) sh.bound = bound - 1;
+      __syncthreads();
+      bool left = true;                          // this thread has candidates to put down
+      uint64_t taken = 0;
+      for (bool again = true; again;) {
+        const uint64_t b = sh.bound;
+        if (left) {
+          int n = 0;
+          left = false;
+          for (int i = tid; i < a.splits * a.top; i += kLpThreads, ++n) {
+            const uint64_t k = parts[i / a.top].keys[i % a.top];
+            if (k <= b || (taken >> n & 1)) continue;
+            if (add_candidate(sh, k)) taken |= 1ull << n;
+            else left = true;
+          }
+        }
+        __syncthreads();
+        again = merge_candidates(sh, a.top);
+      }
+    }
+    m = parts[0].m, s = parts[0].s, t = parts[0].t;
+    for (int i = 1; i < a.splits; ++i) {
+      float m2 = parts[i].m, s2 = parts[i].s, t2 = parts[i].t;
+      const float to = fmaxf(m, m2);
+      move_sums(m, s, t, to);
+      move_sums(m2, s2, t2, to);
+      s += s2;
+      t += t2;
+    }
+    // The workspace is left as it was found.
+    __syncthreads();
+    uint64_t* clear = reinterpret_cast<uint64_t*>(parts);
+    for (int i = tid; i < a.splits * (int)(sizeof(LpPart) / 8); i += kLpThreads) clear[i] = 0;
+    if (tid == 0) a.arrived[row] = 0;
+  }
+
+  // The sums are about m, which is the row's largest logit unless that is NaN or -inf.
+  const float l = __log2f(s) * 0.69314718055994530942f;
+  if (tid == 0) {
+    const int64_t target = a.targets[row];
+    a.logprob[row] = target >= 0 && target < a.vocab ? load_element<DT>(base, target) - m - l : 0.0f;
+    a.entropy[row] = l - t / s;
+  }
+  if (tid < a.top) {
+    const int32_t at = (int32_t)~(uint32_t)sh.list[tid];
+    a.top_index[row * a.top + tid] = at;
+    a.top_logprob[row * a.top + tid] = load_element<DT>(base, at) - m - l;
   }
 }
 
@@ -447,11 +731,29 @@ int32_t logbq_token_logprobs(const void* logits_dev, int32_t dtype, int64_t toke
   if (stride < vocab || stride > INT64_MAX / 8 / tokens) return LOGBQ_ERR_UNSUPPORTED;
   if ((uintptr_t)logits_dev % bytes || !aligned16(work_dev) || work_bytes < LOGBQ_LOGPROBS_WORKSPACE_BYTES)
     return LOGBQ_ERR_UNSUPPORTED;
+  LpArgs a = {};
+  a.logits = logits_dev;
+  a.targets = targets_dev;
+  a.logprob = logprob_dev;
+  a.entropy = entropy_dev;
+  a.top_index = top_index_dev;
+  a.top_logprob = top_logprob_dev;
+  a.arrived = static_cast<uint32_t*>(work_dev);
+  a.parts = reinterpret_cast<LpPart*>(static_cast<uint8_t*>(work_dev) + 4 * kLpMaxParts);
+  a.stride = stride;
+  a.vocab = (int32_t)vocab;
+  a.top = top;
+  // Few rows: parts of at least two vectors a thread.
+  const int64_t most = vocab * bytes / (16 * 2 * kLpThreads);
+  int64_t splits = kLpMaxParts / tokens;
+  splits = splits > 32 ? 32 : splits;
+  splits = splits > most ? most : splits;
+  a.splits = splits < 1 ? 1 : (int32_t)splits;
+  if (tokens * a.splits > INT32_MAX) return LOGBQ_ERR_UNSUPPORTED;
 #define LOGPROBS(DT)                                                                              \
   if (dtype == DT)                                                                                \
-    hipLaunchKernelGGL((k_token_logprobs<DT>), dim3((unsigned)tokens), dim3(kLpThreads), 0,       \
-                       (hipStream_t)stream, logits_dev, vocab, stride, targets_dev, top,          \
-                       logprob_dev, entropy_dev, top_index_dev, top_logprob_dev)
+    hipLaunchKernelGGL((k_token_logprobs<DT>), dim3((unsigned)(tokens * a.splits)),               \
+                       dim3(kLpThreads), 0, (hipStream_t)stream, a)
   LOGPROBS(LOGBQ_DTYPE_F32); LOGPROBS(LOGBQ_DTYPE_F16); LOGPROBS(LOGBQ_DTYPE_BF16);
 #undef LOGPROBS
   return launch_status();
