@@ -111,12 +111,10 @@ __device__ __forceinline__ int64_t scale_index(const Kv4& c, int64_t slot, int h
   return ((page * c.heads + head) << c.page_shift) + (slot & ((1 << c.page_shift) - 1));
 }
 
-// float32 value of a code.
-__device__ __forceinline__ float code_value(uint32_t nibble) {
-  const uint32_t m = nibble & 7u;
-  // 2^(m >> 1) (1 + (m & 1) / 2) / 2 for m >= 2, m / 2 below.
-  const float x = m < 2u ? 0.5f * (float)m : __uint_as_float(((126u + (m >> 1)) << 23) | ((m & 1u) << 22));
-  return nibble & 8u ? -x : x;
+// float32 value of a code (the low 4 bits).
+__device__ __forceinline__ float code_value(uint32_t code) {
+  const half2v pair = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(code, 1.0f, 0);
+  return (float)pair.x;
 }
 
 // The cache as the kernels take it; LOGBQ_OK or what is wrong with it.

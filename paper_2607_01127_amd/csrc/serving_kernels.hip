@@ -247,8 +247,11 @@ __device__ __forceinline__ void read_row(const Kv4& c, int64_t slot, bool held, 
     scale = bf16_value((VALUES ? c.v_scales : c.k_scales)[scale_index(c, slot, head)]);
   }
 #pragma unroll
-  for (int j = 0; j < N; ++j)
-    store_element(to, dtype, at + j, code_value(w[j / 8] >> (4 * (j % 8))) * scale);
+  for (int j = 0; j < N; j += 4) {
+    const uint32_t c4 = w[j / 8] >> (4 * (j % 8));
+    store_four(to, dtype, at + j, f32x4{code_value(c4), code_value(c4 >> 4), code_value(c4 >> 8),
+                                        code_value(c4 >> 12)} * scale);
+  }
 }
 
 template <int D>
@@ -348,33 +351,24 @@ __device__ __forceinline__ bool merge_candidates(LpShared& sh, int top) {
   const uint32_t added = sh.added, held = sh.listed;
   if (added == 0) return false;          // nothing is written before the next barrier
   const uint32_t n = added < kLpCand ? added : kLpCand;
-  uint64_t key[(kLpCand + kLpTop + kLpThreads - 1) / kLpThreads];
-  uint32_t rank[(kLpCand + kLpTop + kLpThreads - 1) / kLpThreads];
-  int own = 0;
+  constexpr int kSlots = (kLpCand + kLpTop + kLpThreads - 1) / kLpThreads;
+  uint64_t key[kSlots];
+  uint32_t rank[kSlots];
 #pragma unroll
-  for (uint32_t j = 0; j < (kLpCand + kLpTop + kLpThreads - 1) / kLpThreads; ++j) {
+  for (int j = 0; j < kSlots; ++j) {
     const uint32_t i = threadIdx.x + j * kLpThreads;
-    if (i < n + held) own = j + 1;
     key[j] = i < n ? sh.cand[i] : i < n + held ? sh.list[i - n] : 0;
-    rank[j] = 0;
-  }
-  if (own) {
+    rank[j] = i < n + held ? 0u : kLpTop;
+    if (i >= n + held) continue;
+#pragma unroll 8
+    for (uint32_t k = 0; k < n; ++k) rank[j] += sh.cand[k] > key[j] ? 1u : 0u;
 #pragma unroll 4
-    for (uint32_t i = 0; i < n; ++i) {
-      const uint64_t x = sh.cand[i];
-#pragma unroll
-      for (uint32_t j = 0; j < sizeof(key) / sizeof(key[0]); ++j) rank[j] += x > key[j] ? 1u : 0u;
-    }
-    for (uint32_t i = 0; i < held; ++i) {
-      const uint64_t x = sh.list[i];
-#pragma unroll
-      for (uint32_t j = 0; j < sizeof(key) / sizeof(key[0]); ++j) rank[j] += x > key[j] ? 1u : 0u;
-    }
+    for (uint32_t k = 0; k < held; ++k) rank[j] += sh.list[k] > key[j] ? 1u : 0u;
   }
   __syncthreads();
 #pragma unroll
-  for (uint32_t j = 0; j < sizeof(key) / sizeof(key[0]); ++j)
-    if ((int)j < own && threadIdx.x + j * kLpThreads < n + held && rank[j] < (uint32_t)top) {
+  for (int j = 0; j < kSlots; ++j)
+    if (rank[j] < (uint32_t)top) {
       sh.list[rank[j]] = key[j];
       if (rank[j] == (uint32_t)top - 1) sh.bound = key[j];
     }
@@ -417,6 +411,18 @@ __device__ __forceinline__ void move_sums(float& m, float& s, float& t, float to
   t = f * t + f * s * fmaxf(d, -300.0f);
   s *= f;
   m = to;
+}
+
+// The sums of a wavefront's lanes, in every lane.
+__device__ __forceinline__ void join_lanes(float& m, float& s, float& t) {
+  for (int d = 1; d < 64; d <<= 1) {
+    float m2 = __shfl_xor(m, d), s2 = __shfl_xor(s, d), t2 = __shfl_xor(t, d);
+    const float to = fmaxf(m, m2);
+    move_sums(m, s, t, to);
+    move_sums(m2, s2, t2, to);
+    s += s2;
+    t += t2;
+  }
 }
 
 template <int DT>
@@ -487,8 +493,8 @@ __global__ __launch_bounds__(kLpThreads) void k_token_logprobs(LpArgs a) {
     if (first) {
       if (extra) top = fmaxf(top, extra_x);
       const uint32_t key = logit_key(top);
-      uint32_t low = 0;
-      for (int bit = 31; bit >= 0; --bit) {
+      uint32_t low = 0;                  // to 16 bits, which lets few more elements through
+      for (int bit = 31; bit >= 16; --bit) {
         const uint32_t at = low | 1u << bit;
         if (__popcll(__builtin_amdgcn_ballot_w64(key >= at)) >= a.top) low = at;
       }
@@ -522,29 +528,17 @@ __global__ __launch_bounds__(kLpThreads) void k_token_logprobs(LpArgs a) {
   }
 
   // The threads' sums, joined over the wavefront and then the workgroup.
-  for (int d = 1; d < 64; d <<= 1) {
-    float m2 = __shfl_xor(m, d), s2 = __shfl_xor(s, d), t2 = __shfl_xor(t, d);
-    const float to = fmaxf(m, m2);
-    move_sums(m, s, t, to);
-    move_sums(m2, s2, t2, to);
-    s += s2;
-    t += t2;
-  }
+  join_lanes(m, s, t);
   if (lane == 0) {
     sh.m[wave] = m;
     sh.s[wave] = s;
     sh.t[wave] = t;
   }
   __syncthreads();
-  m = sh.m[0], s = sh.s[0], t = sh.t[0];
-  for (int w = 1; w < kLpWaves; ++w) {
-    float m2 = sh.m[w], s2 = sh.s[w], t2 = sh.t[w];
-    const float to = fmaxf(m, m2);
-    move_sums(m, s, t, to);
-    move_sums(m2, s2, t2, to);
-    s += s2;
-    t += t2;
-  }
+  m = lane < kLpWaves ? sh.m[lane] : -3.4028235e38f;
+  s = lane < kLpWaves ? sh.s[lane] : 0.0f;
+  t = lane < kLpWaves ? sh.t[lane] : 0.0f;
+  join_lanes(m, s, t);
 
   if (a.splits > 1) {
     LpPart* parts = a.parts + row * a.splits;
@@ -560,7 +554,12 @@ __global__ __launch_bounds__(kLpThreads) void k_token_logprobs(LpArgs a) {
     __syncthreads();
     if (sh.last != (uint32_t)a.splits - 1) return;
     __threadfence();
-    // All parts are there. Their last alternatives bound the row's; a key of 0 is none.
+    // All parts are there: a lane takes the sums of one (a.splits <= 64).
+    m = lane < a.splits ? parts[lane].m : -3.4028235e38f;
+    s = lane < a.splits ? parts[lane].s : 0.0f;
+    t = lane < a.splits ? parts[lane].t : 0.0f;
+    join_lanes(m, s, t);
+    // Their last alternatives bound the row's; a key of 0 is none.
     if (tid == 0) {
       sh.listed = sh.added = 0;
       sh.bound = 0;
@@ -595,15 +594,6 @@ __global__ __launch_bounds__(kLpThreads) void k_token_logprobs(LpArgs a) {
         __syncthreads();
         again = merge_candidates(sh, a.top);
       }
-    }
-    m = parts[0].m, s = parts[0].s, t = parts[0].t;
-    for (int i = 1; i < a.splits; ++i) {
-      float m2 = parts[i].m, s2 = parts[i].s, t2 = parts[i].t;
-      const float to = fmaxf(m, m2);
-      move_sums(m, s, t, to);
-      move_sums(m2, s2, t2, to);
-      s += s2;
-      t += t2;
     }
     // The workspace is left as it was found.
     __syncthreads();

@@ -151,10 +151,25 @@ def _check(status: int, where: str):
         raise LogbqError(status, where)
 
 
+_current_stream = None
+
+
+def _current_stream_getter():
+    """A function that returns the current device's current stream as a number. torch's own raw
+    getter takes 0.1 us where building a Stream object takes 2.7 us, as much as a launch."""
+    import torch
+    raw, device = (getattr(torch._C, n, None) for n in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
+    if raw is None or device is None or not torch.cuda.is_initialized():
+        return lambda: torch.cuda.current_stream().cuda_stream
+    return lambda: raw(device())
+
+
 def _stream(stream):
     if stream is None:
-        import torch
-        return c_void_p(torch.cuda.current_stream().cuda_stream)
+        global _current_stream
+        if _current_stream is None:
+            _current_stream = _current_stream_getter()
+        return c_void_p(_current_stream())
     if isinstance(stream, int):
         return c_void_p(stream)
     return c_void_p(stream.cuda_stream)
@@ -459,14 +474,19 @@ def _device_array(x, dtype, shape, name):
 def _kv4_struct(cache) -> Kv4Struct:
     import torch
     kc, ks, vc, vs = cache
-    if kc.dim() != 4 or vc.dim() != 6:
-        raise ValueError("k_codes must be [pages][heads][page][dim/2], v_codes "
-                         "[pages][heads][page/8][16][8][dim/32]")
-    pages, heads, page, half = kc.shape
-    _device_array(kc, torch.uint8, kc.shape, "k_codes")
-    _device_array(vc, torch.uint8, (pages, heads, page // 8, 16, 8, half // 16), "v_codes")
-    _device_array(ks, torch.bfloat16, (pages, heads, page), "k_scales")
-    _device_array(vs, torch.bfloat16, (pages, heads, page), "v_scales")
+    if kc.dim() != 4:
+        raise ValueError("k_codes must be [pages][heads][page][dim/2]")
+    shape = kc.shape
+    pages, heads, page, half = shape
+    values, scales = (pages, heads, page // 8, 16, 8, half // 16), shape[:3]
+    u8, bf16 = torch.uint8, torch.bfloat16
+    if not (vc.shape == values and ks.shape == vs.shape == scales and kc.is_cuda and vc.is_cuda
+            and ks.is_cuda and vs.is_cuda and kc.dtype == vc.dtype == u8 and ks.dtype == vs.dtype == bf16
+            and kc.is_contiguous() and vc.is_contiguous() and ks.is_contiguous()
+            and vs.is_contiguous()):
+        for x, dtype, s, name in ((kc, u8, shape, "k_codes"), (vc, u8, values, "v_codes"),
+                                  (ks, bf16, scales, "k_scales"), (vs, bf16, scales, "v_scales")):
+            _device_array(x, dtype, s, name)
     return Kv4Struct(kc.data_ptr(), vc.data_ptr(), ks.data_ptr(), vs.data_ptr(), pages, heads, page,
                      2 * half, 0)
 
