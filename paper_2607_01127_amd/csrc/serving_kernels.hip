@@ -279,23 +279,21 @@ __device__ __forceinline__ uint32_t logit_key(float x) {
 }
 
 // A workgroup goes over its part of a row once, kLpVecs 16-byte vectors a thread at a time, the next
-// ones loaded before the present ones are used. Each thread keeps a maximum m, s = sum exp(x - m)
-// and t = sum exp(x - m) (x - m) of its own; they are joined at the end.
+// ones loaded before the present ones are used. Each thread keeps a maximum and the sums of exp and
+// of exp times its argument about it; they are joined at the end.
 //
-// Alternatives: `list` holds the best keys so far, in order, and `bound` what a new one has to
-// pass. Few elements do, so a thread looks at its elements one by one only if its maximum of the
-// step reaches the bound's value. Those that pass go into `cand`, and the list is made anew from
-// both by counting for each how many are larger. The first bound comes from the threads' maxima:
-// the top-th largest of a wavefront's 64 has at least `top` elements from it on. If a step has more
-// candidates than `cand` holds (logits in rising order), the list is made from those that found
-// room, which raises the bound, and the step is looked at again.
+// Alternatives: each wavefront keeps a buffer of keys of its own, `bound` is what a new one has to
+// pass, and elements are looked at one by one only in steps whose maximum reaches the bound's
+// value, so wavefronts wait for each other at the end alone. The first bound is what `top` of the
+// lanes' maxima reach. When the buffer fills up its best `top` keys are put in order (each key's
+// place is the number of larger ones), and the last of them is the next bound.
 //
 // Few rows are split into parts, one workgroup each; the last one of a row to finish joins them.
-constexpr int kLpThreads = 512;
-constexpr int kLpWaves = kLpThreads / 64;
-constexpr int kLpVecs = 4;
-constexpr int kLpCand = 1024;
+constexpr int kLpVecs = 2;
+constexpr int kLpAhead = 2;                      // steps whose vectors are in flight
+constexpr int kLpKeys = 192;                     // of a wavefront's buffer: more than 64 + kLpTop
 constexpr int kLpMaxParts = 512;                 // parts of all rows, where rows are split
+constexpr int kLpManyRows = 900;                 // workgroups from which 256 threads fill the chip
 constexpr int kLpTop = LOGBQ_LOGPROBS_MAX_TOP;
 
 struct LpPart {
@@ -318,15 +316,6 @@ struct LpArgs {
   int32_t vocab, top, splits;
 };
 
-struct LpShared {
-  uint64_t cand[kLpCand];
-  uint64_t list[kLpTop];
-  uint64_t bound;             // key that a candidate has to pass
-  float m[kLpWaves], s[kLpWaves], t[kLpWaves];
-  uint32_t first[kLpWaves];   // wavefronts' first bounds
-  uint32_t listed, added, last;
-};
-
 __device__ __forceinline__ uint64_t element_key(float x, int32_t i) {
   return (uint64_t)logit_key(x) << 32 | (uint32_t)~i;
 }
@@ -338,47 +327,58 @@ __device__ __forceinline__ float bound_value(uint64_t key) {
   return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
 }
 
-// Puts a thread's candidate down; false if there is no room.
-__device__ __forceinline__ bool add_candidate(LpShared& sh, uint64_t key) {
-  const uint32_t at = atomicAdd(&sh.added, 1u);
-  if (at < kLpCand) sh.cand[at] = key;
-  return at < kLpCand;
-}
+// A thread's sums, in powers of two: s = sum 2^u, t = sum 2^u u with u = (x - m) log2 e.
+struct LpSums { float m, s, t; };
+// A wavefront's keys. All lanes call its functions together.
+struct LpKeys {
+  uint64_t* keys;             // kLpKeys of them, in LDS
+  uint64_t bound;             // the same in every lane, as is `held`
+  int held;
 
-// The list from itself and the candidates; true if some found no room. All threads call it, after a
-// barrier that follows their last candidate.
-__device__ __forceinline__ bool merge_candidates(LpShared& sh, int top) {
-  const uint32_t added = sh.added, held = sh.listed;
-  if (added == 0) return false;          // nothing is written before the next barrier
-  const uint32_t n = added < kLpCand ? added : kLpCand;
-  constexpr int kSlots = (kLpCand + kLpTop + kLpThreads - 1) / kLpThreads;
-  uint64_t key[kSlots];
-  uint32_t rank[kSlots];
+  // LDS accesses of one wavefront are in order; this keeps the compiler's in order too.
+  static __device__ __forceinline__ void settle() {
+    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+  // The best `top` keys to the front, in order.
+  __device__ __forceinline__ void order(int top) {
+    const int lane = threadIdx.x & 63;
+    constexpr int kSlots = kLpKeys / 64;
+    uint64_t key[kSlots];
+    int rank[kSlots];
+    settle();
 #pragma unroll
-  for (int j = 0; j < kSlots; ++j) {
-    const uint32_t i = threadIdx.x + j * kLpThreads;
-    key[j] = i < n ? sh.cand[i] : i < n + held ? sh.list[i - n] : 0;
-    rank[j] = i < n + held ? 0u : kLpTop;
-    if (i >= n + held) continue;
+    for (int j = 0; j < kSlots; ++j) {
+      const int i = lane + 64 * j;
+      key[j] = i < held ? keys[i] : 0;
+      rank[j] = i < held ? 0 : kLpTop;
+      if (64 * j >= held) continue;
 #pragma unroll 8
-    for (uint32_t k = 0; k < n; ++k) rank[j] += sh.cand[k] > key[j] ? 1u : 0u;
-#pragma unroll 4
-    for (uint32_t k = 0; k < held; ++k) rank[j] += sh.list[k] > key[j] ? 1u : 0u;
-  }
-  __syncthreads();
-#pragma unroll
-  for (int j = 0; j < kSlots; ++j)
-    if (rank[j] < (uint32_t)top) {
-      sh.list[rank[j]] = key[j];
-      if (rank[j] == (uint32_t)top - 1) sh.bound = key[j];
+      for (int k = 0; k < held; ++k) rank[j] += keys[k] > key[j] ? 1 : 0;
     }
-  if (threadIdx.x == 0) {
-    sh.listed = n + held < (uint32_t)top ? n + held : (uint32_t)top;
-    sh.added = 0;
+    settle();
+#pragma unroll
+    for (int j = 0; j < kSlots; ++j)
+      if (rank[j] < top) keys[rank[j]] = key[j];
+    settle();
+    held = held < top ? held : top;
+    if (held == top) {
+      const uint64_t last = keys[top - 1];
+      bound = last > bound ? last : bound;
+    }
   }
-  __syncthreads();
-  return added > kLpCand;
-}
+  // Takes the lanes' keys that pass the bound.
+  __device__ __forceinline__ void add(uint64_t key, bool has, int top) {
+    uint64_t mask = __builtin_amdgcn_ballot_w64(has && key > bound);
+    if (held + __popcll(mask) > kLpKeys) {
+      order(top);
+      mask = __builtin_amdgcn_ballot_w64(has && key > bound);
+    }
+    if (mask >> (threadIdx.x & 63) & 1)
+      keys[held + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0))] = key;
+    held += __popcll(mask);
+  }
+};
 
 // Float32 values of a 16-byte vector's elements.
 template <int DT>
@@ -398,37 +398,99 @@ __device__ __forceinline__ void vector_values(const u32x4& v, float* x) {
   }
 }
 
-// Adds a term to a thread's sums about its maximum m. exp(-300) is 0 in float32, so the lower limit
-// only keeps 0 times -inf from being one of the terms; a NaN reaches both sums through e.
-__device__ __forceinline__ void add_term(float x, float m, float& s, float& t) {
-  const float d = x - m, e = __builtin_amdgcn_exp2f(d * 1.44269504088896340736f);
-  s += e;
-  t += e * fmaxf(d, -300.0f);
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+constexpr float kLn2Low = -1.90465429e-9f;             // ln 2 - float(ln 2)
+constexpr float kLargest = 3.4028235e38f;
+// Up to here m log2 e is a float32 number, and u is one fma about it; past it the difference comes
+// first.
+constexpr float kFmaMost = 1e38f;
+
+// Adds terms whose largest is at most m. 2^-1000 is 0 in float32, so the lower limit on u only keeps
+// 0 times -inf out of t; it is taken where a logit of -inf has shown itself there. A NaN or a
+// difference of infinities reaches s.
+template <int N>
+__device__ __forceinline__ void add_terms(const float (&x)[N], LpSums& p) {
+  float s = 0.0f, t = 0.0f;
+  if (__builtin_fabsf(p.m) < kFmaMost) {
+    const float mc = p.m * kLog2e;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float u = __builtin_fmaf(x[i], kLog2e, -mc), e = __builtin_amdgcn_exp2f(u);
+      s += e;
+      t = __builtin_fmaf(e, u, t);
+    }
+    if (t != t) {
+      t = 0.0f;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float u = __builtin_fmaf(x[i], kLog2e, -mc);
+        t += __builtin_amdgcn_exp2f(u) * fmaxf(u, -1000.0f);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float u = (x[i] - p.m) * kLog2e, e = __builtin_amdgcn_exp2f(u);
+      s += e;
+      t += e * fmaxf(u, -1000.0f);
+    }
+  }
+  p.s += s;
+  p.t += t;
 }
 // Sums about m, about `to` >= m.
-__device__ __forceinline__ void move_sums(float& m, float& s, float& t, float to) {
-  const float d = m - to, f = __builtin_amdgcn_exp2f(d * 1.44269504088896340736f);
-  t = f * t + f * s * fmaxf(d, -300.0f);
-  s *= f;
-  m = to;
+__device__ __forceinline__ void move_sums(LpSums& p, float to) {
+  const float u = __builtin_fabsf(to) < kFmaMost && __builtin_fabsf(p.m) < kFmaMost
+                      ? p.m * kLog2e - to * kLog2e : (p.m - to) * kLog2e;
+  const float f = __builtin_amdgcn_exp2f(u);
+  p.t = f * (p.t + p.s * fmaxf(u, -1000.0f));
+  p.s *= f;
+  p.m = to;
 }
-
 // The sums of a wavefront's lanes, in every lane.
-__device__ __forceinline__ void join_lanes(float& m, float& s, float& t) {
+__device__ __forceinline__ void join_lanes(LpSums& p) {
+  float to = p.m;
+  for (int d = 1; d < 64; d <<= 1) to = fmaxf(to, __shfl_xor(to, d));
+  move_sums(p, to);
   for (int d = 1; d < 64; d <<= 1) {
-    float m2 = __shfl_xor(m, d), s2 = __shfl_xor(s, d), t2 = __shfl_xor(t, d);
-    const float to = fmaxf(m, m2);
-    move_sums(m, s, t, to);
-    move_sums(m2, s2, t2, to);
-    s += s2;
-    t += t2;
+    p.s += __shfl_xor(p.s, d);
+    p.t += __shfl_xor(p.t, d);
   }
 }
 
-template <int DT>
+// Accesses to what other workgroups of the launch wrote or will read: coherent over the chip's
+// L2 caches one by one, so that no cache has to be written back as a whole.
+template <typename T>
+__device__ __forceinline__ T load_shared(const T* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <typename T>
+__device__ __forceinline__ void store_shared(T* p, T x) {
+  __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// The largest 16-bit prefix (in the top bits) that at least `top` of the values reach.
+template <int N>
+__device__ __forceinline__ uint32_t reached_by(const uint32_t (&key)[N], int top) {
+  uint32_t low = 0;
+  for (int bit = 31; bit >= 16; --bit) {
+    const uint32_t at = low | 1u << bit;
+    int n = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) n += __popcll(__builtin_amdgcn_ballot_w64(key[j] >= at));
+    if (n >= top) low = at;
+  }
+  return low;
+}
+
+template <int DT, int kLpThreads>
 __global__ __launch_bounds__(kLpThreads) void k_token_logprobs(LpArgs a) {
-  constexpr int kBytes = DT == LOGBQ_DTYPE_F32 ? 4 : 2, kEach = 16 / kBytes, kElems = kLpVecs * kEach;
-  __shared__ LpShared sh;
+  constexpr int kLpWaves = kLpThreads / 64;
+  constexpr int kBytes = DT == LOGBQ_DTYPE_F32 ? 4 : 2, kEach = 16 / kBytes;
+  __shared__ uint64_t keys[kLpWaves][kLpKeys];
+  __shared__ LpSums wave_sums[kLpWaves];
+  __shared__ int wave_held[kLpWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t row = blockIdx.x / a.splits;
   const int part = blockIdx.x % a.splits;
@@ -440,179 +502,176 @@ __global__ __launch_bounds__(kLpThreads) void k_token_logprobs(LpArgs a) {
   const int tail = a.vocab - head - vectors * kEach;
   const u32x4* body = reinterpret_cast<const u32x4*>(base + head * kBytes);
   const int v0 = (int)((int64_t)vectors * part / a.splits), v1 = (int)((int64_t)vectors * (part + 1) / a.splits);
-  if (tid == 0) {
-    sh.bound = 0;
-    sh.listed = sh.added = 0;
-  }
+  __shared__ unsigned long long common;        // what some wavefront's bound lets be left out
+  if (tid == 0) common = 0;
+  __syncthreads();
+  LpKeys best = {keys[wave], 0, 0};
 
-  u32x4 next[kLpVecs];
-  const auto fetch = [&](int from) {
+  u32x4 next[kLpAhead][kLpVecs];
+  const auto fetch = [&](int from, u32x4 (&to)[kLpVecs]) {
 #pragma unroll
     for (int j = 0; j < kLpVecs; ++j) {
       const int v = from + j * kLpThreads + tid;
-      if (v < v1) next[j] = __builtin_nontemporal_load(body + v);
+      if (v < v1) to[j] = __builtin_nontemporal_load(body + v);
     }
   };
-  if (v0 < v1) fetch(v0);
+#pragma unroll
+  for (int k = 0; k < kLpAhead; ++k) fetch(v0 + k * kLpVecs * kLpThreads, next[k]);
   // The elements outside the vectors: one a thread, in the first part.
   const bool extra = part == 0 && tid < head + tail;
   const int extra_at = tid < head ? tid : vectors * kEach + tid;
-  float m = -3.4028235e38f, s = 0.0f, t = 0.0f;
+  LpSums sums = {-kLargest, 0.0f, 0.0f};
   const float extra_x = extra ? load_element<DT>(base, extra_at) : -INFINITY;
   if (extra) {
-    m = fmaxf(m, extra_x);
-    add_term(extra_x, m, s, t);
+    const float x[1] = {extra_x};
+    sums.m = fmaxf(sums.m, extra_x);
+    add_terms(x, sums);
   }
 
-  for (int from = v0; from < v1 || (from == v0 && part == 0); from += kLpVecs * kLpThreads) {
-    float x[kElems];
+  const auto step = [&](int from, u32x4 (&raw)[kLpVecs]) {
+    float x[kLpVecs][kEach];
+    float top = -INFINITY;
     int count = 0;                       // vectors that the thread has in this step
 #pragma unroll
     for (int j = 0; j < kLpVecs; ++j) {
       if (from + j * kLpThreads + tid < v1) {
-        vector_values<DT>(next[j], x + j * kEach);
+        vector_values<DT>(raw[j], x[j]);
         count = j + 1;
-      } else {
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) x[j * kEach + i] = -INFINITY;
+        for (int i = 0; i < kEach; ++i) top = fmaxf(top, x[j][i]);
       }
     }
-    if (from + kLpVecs * kLpThreads < v1) fetch(from + kLpVecs * kLpThreads);
-    float top = x[0];
-#pragma unroll
-    for (int i = 1; i < kElems; ++i) top = fmaxf(top, x[i]);
-    if (top > m) move_sums(m, s, t, top);
+    fetch(from + kLpAhead * kLpVecs * kLpThreads, raw);
+    if (top > sums.m) move_sums(sums, top);
 #pragma unroll
     for (int j = 0; j < kLpVecs; ++j)
-      if (from + j * kLpThreads < v1) {          // the same for all threads
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) add_term(x[j * kEach + i], m, s, t);
-      }
-    if (a.top == 0) continue;
+      if (j < count) add_terms(x[j], sums);
+    if (a.top == 0) return;
     const bool first = from == v0;
     if (first) {
       if (extra) top = fmaxf(top, extra_x);
-      const uint32_t key = logit_key(top);
-      uint32_t low = 0;                  // to 16 bits, which lets few more elements through
-      for (int bit = 31; bit >= 16; --bit) {
-        const uint32_t at = low | 1u << bit;
-        if (__popcll(__builtin_amdgcn_ballot_w64(key >= at)) >= a.top) low = at;
-      }
-      if (lane == 0) sh.first[wave] = low;
-      __syncthreads();
-#pragma unroll
-      for (int w = 0; w < kLpWaves; ++w) low = max(low, sh.first[w]);
-      if (tid == 0) sh.bound = (uint64_t)low << 32;
-      __syncthreads();
+      const uint32_t key[1] = {logit_key(top)};
+      best.bound = (uint64_t)reached_by(key, a.top) << 32;
+      if (lane == 0) atomicMax(&common, (unsigned long long)best.bound);
     }
-    uint64_t taken = 0;                          // a bit an element, the last one the extra
-    for (bool again = true; again;) {
-      const uint64_t bound = sh.bound;
-      if (top >= bound_value(bound) || s != s) {
+    const uint64_t others = __hip_atomic_load(&common, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    best.bound = best.bound > others ? best.bound : others;
+    const float least = bound_value(best.bound);
+    if (__builtin_amdgcn_ballot_w64(top >= least || sums.s != sums.s)) {
 #pragma unroll
-        for (int i = 0; i < kElems; ++i) {
-          const int32_t at = head + (from + i / kEach * kLpThreads + tid) * kEach + i % kEach;
-          const uint64_t key = element_key(x[i], at);
-          if (i / kEach < count && key > bound && !(taken >> i & 1) && add_candidate(sh, key))
-            taken |= 1ull << i;
-        }
-        if (first && extra) {
-          const uint64_t key = element_key(extra_x, extra_at);
-          if (key > bound && !(taken >> 63) && add_candidate(sh, key)) taken |= 1ull << 63;
+      for (int j = 0; j < kLpVecs; ++j) {
+        if (from + j * kLpThreads >= v1) continue;       // the same for all lanes
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+          const bool has = j < count && !(x[j][i] < least);          // NaN passes
+          if (!__builtin_amdgcn_ballot_w64(has)) continue;
+          best.add(element_key(x[j][i], head + (from + j * kLpThreads + tid) * kEach + i), has, a.top);
         }
       }
-      __syncthreads();
-      again = merge_candidates(sh, a.top);
+      if (first) best.add(element_key(extra_x, extra_at), extra, a.top);
+      if (best.held >= 2 * a.top) {
+        best.order(a.top);
+        // Its last key has to pass in the end, so the others may leave out what is below it.
+        if (lane == 0) atomicMax(&common, (unsigned long long)best.keys[a.top - 1] - 1);
+      }
     }
-    __syncthreads();
+  };
+  if (v0 == v1 && part == 0) step(v0, next[0]);        // a row without a whole vector
+  for (int from = v0; from < v1; from += kLpAhead * kLpVecs * kLpThreads) {
+#pragma unroll
+    for (int k = 0; k < kLpAhead; ++k)
+      if (from + k * kLpVecs * kLpThreads < v1) step(from + k * kLpVecs * kLpThreads, next[k]);
   }
 
-  // The threads' sums, joined over the wavefront and then the workgroup.
-  join_lanes(m, s, t);
+  // The sums and alternatives of the lanes, then of the wavefronts; the last is the first
+  // wavefront's work.
+  join_lanes(sums);
   if (lane == 0) {
-    sh.m[wave] = m;
-    sh.s[wave] = s;
-    sh.t[wave] = t;
+    wave_sums[wave] = sums;
+    wave_held[wave] = best.held;
   }
   __syncthreads();
-  m = lane < kLpWaves ? sh.m[lane] : -3.4028235e38f;
-  s = lane < kLpWaves ? sh.s[lane] : 0.0f;
-  t = lane < kLpWaves ? sh.t[lane] : 0.0f;
-  join_lanes(m, s, t);
+  if (wave != 0) return;
+  sums = lane < kLpWaves ? wave_sums[lane] : LpSums{-kLargest, 0.0f, 0.0f};
+  join_lanes(sums);
+  if (a.top > 0) {
+    uint32_t key[kLpWaves];
+#pragma unroll
+    for (int w = 0; w < kLpWaves; ++w) key[w] = lane < wave_held[w] ? (uint32_t)(keys[w][lane] >> 32) : 0;
+    const uint64_t bound = (uint64_t)reached_by(key, a.top) << 32;
+    best.bound = best.bound > bound ? best.bound : bound;
+    for (int w = 1; w < kLpWaves; ++w)
+      for (int at = 0; at < wave_held[w]; at += 64) {
+        const bool has = at + lane < wave_held[w];
+        best.add(has ? keys[w][at + lane] : 0, has, a.top);
+      }
+    best.order(a.top);
+  }
 
   if (a.splits > 1) {
     LpPart* parts = a.parts + row * a.splits;
-    if (tid == 0) {
-      parts[part].m = m;
-      parts[part].s = s;
-      parts[part].t = t;
+    // All stores have arrived before the part counts itself.
+    if (lane == 0) {
+      store_shared(&parts[part].m, sums.m);
+      store_shared(&parts[part].s, sums.s);
+      store_shared(&parts[part].t, sums.t);
     }
-    if (tid < a.top) parts[part].keys[tid] = tid < (int)sh.listed ? sh.list[tid] : 0;
-    __threadfence();
-    __syncthreads();
-    if (tid == 0) sh.last = atomicAdd(a.arrived + row, 1u);
-    __syncthreads();
-    if (sh.last != (uint32_t)a.splits - 1) return;
-    __threadfence();
+    if (lane < a.top) store_shared(&parts[part].keys[lane], lane < best.held ? best.keys[lane] : (uint64_t)0);
+    __builtin_amdgcn_s_waitcnt(0);
+    uint32_t before = 0;
+    if (lane == 0) before = __hip_atomic_fetch_add(a.arrived + row, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (__builtin_amdgcn_readfirstlane(before) != (uint32_t)a.splits - 1) return;
     // All parts are there: a lane takes the sums of one (a.splits <= 64).
-    m = lane < a.splits ? parts[lane].m : -3.4028235e38f;
-    s = lane < a.splits ? parts[lane].s : 0.0f;
-    t = lane < a.splits ? parts[lane].t : 0.0f;
-    join_lanes(m, s, t);
-    // Their last alternatives bound the row's; a key of 0 is none.
-    if (tid == 0) {
-      sh.listed = sh.added = 0;
-      sh.bound = 0;
-    }
-    __syncthreads();
+    sums = LpSums{-kLargest, 0.0f, 0.0f};
+    if (lane < a.splits)
+      sums = LpSums{load_shared(&parts[lane].m), load_shared(&parts[lane].s), load_shared(&parts[lane].t)};
+    join_lanes(sums);
     if (a.top > 0) {
-      uint64_t bound = 0;
-      for (int i = lane; i < a.splits; i += 64) {
-        const uint64_t k = parts[i].keys[a.top - 1];
-        bound = k > bound ? k : bound;
-      }
-      for (int d = 1; d < 64; d <<= 1) {
-        const uint64_t k = __shfl_xor((unsigned long long)bound, d);
-        bound = k > bound ? k : bound;
-      }
-      if (tid == 0 && bound) sh.bound = bound - 1;
-      __syncthreads();
-      bool left = true;                          // this thread has candidates to put down
-      uint64_t taken = 0;
-      for (bool again = true; again;) {
-        const uint64_t b = sh.bound;
-        if (left) {
-          int n = 0;
-          left = false;
-          for (int i = tid; i < a.splits * a.top; i += kLpThreads, ++n) {
-            const uint64_t k = parts[i / a.top].keys[i % a.top];
-            if (k <= b || (taken >> n & 1)) continue;
-            if (add_candidate(sh, k)) taken |= 1ull << n;
-            else left = true;
-          }
+      // The first bound: what `top` of the parts' best keys reach, as many of each part as it takes
+      // to have `top` of them (at most 64). A key of 0 is none.
+      const int each = (a.top + a.splits - 1) / a.splits;
+      uint32_t key[1] = {0};
+      if (lane < each * a.splits)
+        key[0] = (uint32_t)(load_shared(&parts[lane % a.splits].keys[lane / a.splits]) >> 32);
+      best.held = 0;
+      best.bound = (uint64_t)reached_by(key, a.top) << 32;
+      constexpr int kAtOnce = 8;                 // loads in flight
+      for (int at = 0; at < a.splits * a.top; at += 64 * kAtOnce) {
+        uint64_t k[kAtOnce];
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+          const int i = at + 64 * j + lane;
+          k[j] = i < a.splits * a.top ? load_shared(&parts[i / a.top].keys[i % a.top]) : 0;
         }
-        __syncthreads();
-        again = merge_candidates(sh, a.top);
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) best.add(k[j], k[j] != 0, a.top);
       }
+      best.order(a.top);
     }
     // The workspace is left as it was found.
-    __syncthreads();
     uint64_t* clear = reinterpret_cast<uint64_t*>(parts);
-    for (int i = tid; i < a.splits * (int)(sizeof(LpPart) / 8); i += kLpThreads) clear[i] = 0;
-    if (tid == 0) a.arrived[row] = 0;
+    for (int i = lane; i < a.splits * (int)(sizeof(LpPart) / 8); i += 64) store_shared(clear + i, (uint64_t)0);
+    if (lane == 0) store_shared(a.arrived + row, 0u);
   }
 
-  // The sums are about m, which is the row's largest logit unless that is NaN or -inf.
-  const float l = __log2f(s) * 0.69314718055994530942f;
+  // x - L for a logit x, with L = m + ln s: the sums are about m log2 e as rounded, and its product
+  // with ln 2 is taken to twice the precision.
+  const float log2_s = __log2f(sums.s);
+  const bool by_fma = __builtin_fabsf(sums.m) < kFmaMost;
+  const float mc = sums.m * kLog2e;
+  const auto log_probability = [&](float x) {
+    return by_fma ? __builtin_fmaf(-mc, kLn2, x) - __builtin_fmaf(mc, kLn2Low, kLn2 * log2_s)
+                  : x - sums.m - kLn2 * log2_s;
+  };
   if (tid == 0) {
     const int64_t target = a.targets[row];
-    a.logprob[row] = target >= 0 && target < a.vocab ? load_element<DT>(base, target) - m - l : 0.0f;
-    a.entropy[row] = l - t / s;
+    a.logprob[row] = target >= 0 && target < a.vocab ? log_probability(load_element<DT>(base, target)) : 0.0f;
+    a.entropy[row] = kLn2 * (log2_s - sums.t / sums.s);
   }
   if (tid < a.top) {
-    const int32_t at = (int32_t)~(uint32_t)sh.list[tid];
+    const int32_t at = (int32_t)~(uint32_t)best.keys[tid];
     a.top_index[row * a.top + tid] = at;
-    a.top_logprob[row * a.top + tid] = load_element<DT>(base, at) - m - l;
+    a.top_logprob[row * a.top + tid] = log_probability(load_element<DT>(base, at));
   }
 }
 
@@ -733,18 +792,20 @@ int32_t logbq_token_logprobs(const void* logits_dev, int32_t dtype, int64_t toke
   a.stride = stride;
   a.vocab = (int32_t)vocab;
   a.top = top;
-  // Few rows: parts of at least two vectors a thread.
-  const int64_t most = vocab * bytes / (16 * 2 * kLpThreads);
+  // Few rows: parts of at least 32 KiB.
+  const int64_t most = vocab * bytes / 32768;
   int64_t splits = kLpMaxParts / tokens;
   splits = splits > 32 ? 32 : splits;
   splits = splits > most ? most : splits;
   a.splits = splits < 1 ? 1 : (int32_t)splits;
   if (tokens * a.splits > INT32_MAX) return LOGBQ_ERR_UNSUPPORTED;
-#define LOGPROBS(DT)                                                                              \
-  if (dtype == DT)                                                                                \
-    hipLaunchKernelGGL((k_token_logprobs<DT>), dim3((unsigned)(tokens * a.splits)),               \
-                       dim3(kLpThreads), 0, (hipStream_t)stream, a)
-  LOGPROBS(LOGBQ_DTYPE_F32); LOGPROBS(LOGBQ_DTYPE_F16); LOGPROBS(LOGBQ_DTYPE_BF16);
+#define LOGPROBS(DT, THREADS)                                                                     \
+  if (dtype == DT && threads == THREADS)                                                          \
+    hipLaunchKernelGGL((k_token_logprobs<DT, THREADS>), dim3((unsigned)(tokens * a.splits)),      \
+                       dim3(THREADS), 0, (hipStream_t)stream, a)
+  const int threads = tokens * a.splits < kLpManyRows ? 512 : 256;
+  LOGPROBS(LOGBQ_DTYPE_F32, 256); LOGPROBS(LOGBQ_DTYPE_F16, 256); LOGPROBS(LOGBQ_DTYPE_BF16, 256);
+  LOGPROBS(LOGBQ_DTYPE_F32, 512); LOGPROBS(LOGBQ_DTYPE_F16, 512); LOGPROBS(LOGBQ_DTYPE_BF16, 512);
 #undef LOGPROBS
   return launch_status();
 }
