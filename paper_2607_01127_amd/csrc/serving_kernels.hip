@@ -283,15 +283,18 @@ __device__ __forceinline__ uint32_t logit_key(float x) {
 // of exp times its argument about it; they are joined at the end.
 //
 // Alternatives: each wavefront keeps a buffer of keys of its own, `bound` is what a new one has to
-// pass, and elements are looked at one by one only in steps whose maximum reaches the bound's
-// value, so wavefronts wait for each other at the end alone. The first bound is what `top` of the
-// lanes' maxima reach. When the buffer fills up its best `top` keys are put in order (each key's
-// place is the number of larger ones), and the last of them is the next bound.
+// pass, and elements are looked at one by one only in vectors whose maximum reaches the bound's
+// value. The bound is what `top` of the workgroup's threads' maxima reach, after the first step and
+// again after 2, 4, 8, ..., so about `top` elements pass between two of them. The wavefronts find
+// these bounds in turn and do not wait for each other after the first: maxima of some time ago
+// bound as well. A buffer that fills up keeps its best `top` keys, in order: each key's place is the
+// number of larger ones.
 //
 // Few rows are split into parts, one workgroup each; the last one of a row to finish joins them.
 constexpr int kLpVecs = 2;
 constexpr int kLpAhead = 2;                      // steps whose vectors are in flight
 constexpr int kLpKeys = 192;                     // of a wavefront's buffer: more than 64 + kLpTop
+constexpr int kLpMaxSplits = 32;                 // parts of one row
 constexpr int kLpMaxParts = 512;                 // parts of all rows, where rows are split
 constexpr int kLpManyRows = 900;                 // workgroups from which 256 threads fill the chip
 constexpr int kLpTop = LOGBQ_LOGPROBS_MAX_TOP;
@@ -502,9 +505,9 @@ __global__ __launch_bounds__(kLpThreads) void k_token_logprobs(LpArgs a) {
   const int tail = a.vocab - head - vectors * kEach;
   const u32x4* body = reinterpret_cast<const u32x4*>(base + head * kBytes);
   const int v0 = (int)((int64_t)vectors * part / a.splits), v1 = (int)((int64_t)vectors * (part + 1) / a.splits);
-  __shared__ unsigned long long common;        // what some wavefront's bound lets be left out
+  __shared__ uint32_t maxima[kLpWaves][64];    // keys of the lanes' maxima so far, or some time ago
+  __shared__ unsigned long long common;        // a bound for all wavefronts
   if (tid == 0) common = 0;
-  __syncthreads();
   LpKeys best = {keys[wave], 0, 0};
 
   u32x4 next[kLpAhead][kLpVecs];
@@ -528,39 +531,53 @@ __global__ __launch_bounds__(kLpThreads) void k_token_logprobs(LpArgs a) {
     add_terms(x, sums);
   }
 
+  int steps = 1;
   const auto step = [&](int from, u32x4 (&raw)[kLpVecs]) {
-    float x[kLpVecs][kEach];
-    float top = -INFINITY;
+    float x[kLpVecs][kEach], top[kLpVecs];
     int count = 0;                       // vectors that the thread has in this step
 #pragma unroll
     for (int j = 0; j < kLpVecs; ++j) {
+      top[j] = -INFINITY;
       if (from + j * kLpThreads + tid < v1) {
         vector_values<DT>(raw[j], x[j]);
         count = j + 1;
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) top = fmaxf(top, x[j][i]);
+        for (int i = 0; i < kEach; ++i) top[j] = fmaxf(top[j], x[j][i]);
       }
     }
     fetch(from + kLpAhead * kLpVecs * kLpThreads, raw);
-    if (top > sums.m) move_sums(sums, top);
+    float most = top[0];
+#pragma unroll
+    for (int j = 1; j < kLpVecs; ++j) most = fmaxf(most, top[j]);
+    if (most > sums.m) move_sums(sums, most);
 #pragma unroll
     for (int j = 0; j < kLpVecs; ++j)
       if (j < count) add_terms(x[j], sums);
     if (a.top == 0) return;
     const bool first = from == v0;
-    if (first) {
-      if (extra) top = fmaxf(top, extra_x);
-      const uint32_t key[1] = {logit_key(top)};
-      best.bound = (uint64_t)reached_by(key, a.top) << 32;
-      if (lane == 0) atomicMax(&common, (unsigned long long)best.bound);
+    if ((steps & (steps - 1)) == 0) {
+      // -kLargest is also the maximum of none.
+      maxima[wave][lane] = logit_key(sums.m > -kLargest ? sums.m : -INFINITY);
+      if (first) __syncthreads();
+      if ((31 - __builtin_clz(steps)) % kLpWaves == wave) {
+        uint32_t key[kLpWaves];
+#pragma unroll
+        for (int w = 0; w < kLpWaves; ++w)
+          key[w] = __hip_atomic_load(&maxima[w][lane], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        const uint64_t bound = (uint64_t)reached_by(key, a.top) << 32;
+        if (lane == 0) atomicMax(&common, (unsigned long long)bound);
+      }
+      if (first) __syncthreads();
     }
-    const uint64_t others = __hip_atomic_load(&common, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-    best.bound = best.bound > others ? best.bound : others;
+    const uint64_t bound = __hip_atomic_load(&common, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    best.bound = best.bound > bound ? best.bound : bound;
     const float least = bound_value(best.bound);
-    if (__builtin_amdgcn_ballot_w64(top >= least || sums.s != sums.s)) {
+    ++steps;
+    const bool odd = sums.s != sums.s;          // a NaN is no maximum
+    if (__builtin_amdgcn_ballot_w64(most >= least || odd)) {
 #pragma unroll
       for (int j = 0; j < kLpVecs; ++j) {
-        if (from + j * kLpThreads >= v1) continue;       // the same for all lanes
+        if (!__builtin_amdgcn_ballot_w64(j < count && (top[j] >= least || odd))) continue;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
           const bool has = j < count && !(x[j][i] < least);          // NaN passes
@@ -568,13 +585,8 @@ __global__ __launch_bounds__(kLpThreads) void k_token_logprobs(LpArgs a) {
           best.add(element_key(x[j][i], head + (from + j * kLpThreads + tid) * kEach + i), has, a.top);
         }
       }
-      if (first) best.add(element_key(extra_x, extra_at), extra, a.top);
-      if (best.held >= 2 * a.top) {
-        best.order(a.top);
-        // Its last key has to pass in the end, so the others may leave out what is below it.
-        if (lane == 0) atomicMax(&common, (unsigned long long)best.keys[a.top - 1] - 1);
-      }
     }
+    if (first && part == 0) best.add(element_key(extra_x, extra_at), extra, a.top);
   };
   if (v0 == v1 && part == 0) step(v0, next[0]);        // a row without a whole vector
   for (int from = v0; from < v1; from += kLpAhead * kLpVecs * kLpThreads) {
@@ -595,11 +607,16 @@ __global__ __launch_bounds__(kLpThreads) void k_token_logprobs(LpArgs a) {
   sums = lane < kLpWaves ? wave_sums[lane] : LpSums{-kLargest, 0.0f, 0.0f};
   join_lanes(sums);
   if (a.top > 0) {
-    uint32_t key[kLpWaves];
+    int total = 0;
 #pragma unroll
-    for (int w = 0; w < kLpWaves; ++w) key[w] = lane < wave_held[w] ? (uint32_t)(keys[w][lane] >> 32) : 0;
-    const uint64_t bound = (uint64_t)reached_by(key, a.top) << 32;
-    best.bound = best.bound > bound ? best.bound : bound;
+    for (int w = 0; w < kLpWaves; ++w) total += wave_held[w];
+    if (total > kLpKeys) {               // else all of them fit the buffer
+      uint32_t key[kLpWaves];
+#pragma unroll
+      for (int w = 0; w < kLpWaves; ++w) key[w] = lane < wave_held[w] ? (uint32_t)(keys[w][lane] >> 32) : 0;
+      const uint64_t bound = (uint64_t)reached_by(key, a.top) << 32;
+      best.bound = best.bound > bound ? best.bound : bound;
+    }
     for (int w = 1; w < kLpWaves; ++w)
       for (int at = 0; at < wave_held[w]; at += 64) {
         const bool has = at + lane < wave_held[w];
@@ -621,31 +638,29 @@ __global__ __launch_bounds__(kLpThreads) void k_token_logprobs(LpArgs a) {
     uint32_t before = 0;
     if (lane == 0) before = __hip_atomic_fetch_add(a.arrived + row, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (__builtin_amdgcn_readfirstlane(before) != (uint32_t)a.splits - 1) return;
-    // All parts are there: a lane takes the sums of one (a.splits <= 64).
+    // All parts are there: a lane takes the sums of one (a.splits <= 64), and every 64th key.
+    constexpr int kMost = kLpMaxSplits * kLpTop / 64;
+    uint64_t k[kMost], first = 0;
     sums = LpSums{-kLargest, 0.0f, 0.0f};
     if (lane < a.splits)
       sums = LpSums{load_shared(&parts[lane].m), load_shared(&parts[lane].s), load_shared(&parts[lane].t)};
+    // The first bound: what `top` of the parts' best keys reach, as many of each part as it takes
+    // to have `top` of them (at most 64). A key of 0 is none.
+    if (lane < (a.top + a.splits - 1) / a.splits * a.splits)
+      first = load_shared(&parts[lane % a.splits].keys[lane / a.splits]);
+#pragma unroll
+    for (int j = 0; j < kMost; ++j) {
+      const int i = 64 * j + lane;
+      k[j] = i < a.splits * a.top ? load_shared(&parts[i / a.top].keys[i % a.top]) : 0;
+    }
     join_lanes(sums);
     if (a.top > 0) {
-      // The first bound: what `top` of the parts' best keys reach, as many of each part as it takes
-      // to have `top` of them (at most 64). A key of 0 is none.
-      const int each = (a.top + a.splits - 1) / a.splits;
-      uint32_t key[1] = {0};
-      if (lane < each * a.splits)
-        key[0] = (uint32_t)(load_shared(&parts[lane % a.splits].keys[lane / a.splits]) >> 32);
+      const uint32_t key[1] = {(uint32_t)(first >> 32)};
       best.held = 0;
       best.bound = (uint64_t)reached_by(key, a.top) << 32;
-      constexpr int kAtOnce = 8;                 // loads in flight
-      for (int at = 0; at < a.splits * a.top; at += 64 * kAtOnce) {
-        uint64_t k[kAtOnce];
 #pragma unroll
-        for (int j = 0; j < kAtOnce; ++j) {
-          const int i = at + 64 * j + lane;
-          k[j] = i < a.splits * a.top ? load_shared(&parts[i / a.top].keys[i % a.top]) : 0;
-        }
-#pragma unroll
-        for (int j = 0; j < kAtOnce; ++j) best.add(k[j], k[j] != 0, a.top);
-      }
+      for (int j = 0; j < kMost; ++j)
+        if (64 * j < a.splits * a.top) best.add(k[j], k[j] != 0, a.top);
       best.order(a.top);
     }
     // The workspace is left as it was found.
@@ -792,10 +807,10 @@ int32_t logbq_token_logprobs(const void* logits_dev, int32_t dtype, int64_t toke
   a.stride = stride;
   a.vocab = (int32_t)vocab;
   a.top = top;
-  // Few rows: parts of at least 32 KiB.
-  const int64_t most = vocab * bytes / 32768;
+  // Few rows: parts of at least 16 KiB.
+  const int64_t most = vocab * bytes / 16384;
   int64_t splits = kLpMaxParts / tokens;
-  splits = splits > 32 ? 32 : splits;
+  splits = splits > kLpMaxSplits ? kLpMaxSplits : splits;
   splits = splits > most ? most : splits;
   a.splits = splits < 1 ? 1 : (int32_t)splits;
   if (tokens * a.splits > INT32_MAX) return LOGBQ_ERR_UNSUPPORTED;
