@@ -10,6 +10,7 @@
 
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "kv4_detail.h"
 #include "logbq.h"
@@ -143,6 +144,20 @@ __device__ __forceinline__ void pair_positions(const uint32_t (&v)[D / 16], uint
   }
 }
 
+// Float32 weights as sums of two bfloat16 numbers.
+__device__ __forceinline__ void split_weights(const float (&w)[8], bf16x8& hi, bf16x8& lo) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int j = 0; j < 8; j += 2) {
+    const bf16x2 h = __builtin_convertvector((f32x2{w[j], w[j + 1]}), bf16x2);
+    const uint32_t b = __builtin_bit_cast(uint32_t, h);
+    const bf16x2 l = __builtin_convertvector(
+        (f32x2{w[j] - __uint_as_float(b << 16), w[j + 1] - __uint_as_float(b & 0xffff0000u)}), bf16x2);
+    hi[j] = h.x; hi[j + 1] = h.y;
+    lo[j] = l.x; lo[j + 1] = l.y;
+  }
+}
+
 __device__ __forceinline__ float scale_at(const u32x4& s, int j) {
   const uint32_t w = s[j >> 1];
   return __uint_as_float(j & 1 ? w & 0xffff0000u : w << 16);
@@ -161,7 +176,7 @@ __device__ __forceinline__ float column_sum(float x) {
 template <int D, int NT, bool QSPLIT>
 __global__ __launch_bounds__(kDecThreads, (D / 64 * NT <= 2 ? 2 : 1))
 void k_kv4_decode(AttnArgs a) {
-  constexpr int kRows = 16 * NT, kChunks = D / 32, kCh = D / 16;
+  constexpr int kRows = 16 * NT, kChunks = D / 32, kCh = D / 16, kAhead = 2;
   __shared__ float merged[kDecWaves][16][D + 4];
   __shared__ float ref_s[kDecWaves][kRows], sum_s[kDecWaves][kRows];
   __shared__ int64_t scan[kDecWaves];
@@ -279,24 +294,46 @@ void k_kv4_decode(AttnArgs a) {
     // ---- the wavefront's tiles of the piece
     const int32_t* table = a.table + (int64_t)r * a.width;
     const int page_mask = (1 << a.c.page_shift) - 1;
-    const auto load_tile = [&](int32_t base, RawTile<D>& t) {
-      // Keys: lane (col, grp) has position 8 (col / 4) + col % 4 (+ 4), channels grp D/4 ..;
-      // values and scales: positions 8 grp .. 8 grp + 7.
-      int32_t kp = base + 8 * (col >> 2), vp = base + 8 * grp;
-      int32_t k_id = kp < req.end ? table[kp >> a.c.page_shift] : -1;
-      int32_t v_id = vp < req.end ? table[vp >> a.c.page_shift] : -1;
-      const int64_t pages = a.c.slots >> a.c.page_shift;
-      t.valid = v_id >= 0 && v_id < pages;
-      k_id = k_id >= 0 && k_id < pages ? k_id : 0;       // hidden: any page, masked below
-      v_id = t.valid ? v_id : 0;
-      const int64_t kb = (((int64_t)k_id * a.c.heads + head) << a.c.page_shift) + (kp & page_mask);
-      const int64_t vb = (((int64_t)v_id * a.c.heads + head) << a.c.page_shift) + (vp & page_mask);
-      const uint8_t* kr = a.c.k_codes + (kb + (col & 3)) * (D / 2) + grp * (D / 8);
+    const int64_t pages = a.c.slots >> a.c.page_shift;
+    // Keys: lane (col, grp) has position 8 (col / 4) + col % 4 (+ 4), channels grp D/4 ..;
+    // values and scales: positions 8 grp .. 8 grp + 7. A tile lies in one page, or (16 positions a
+    // page) in two.
+    const bool one_page = a.c.page_shift >= 5;
+    const int k_at = 8 * (col >> 2), v_at = 8 * grp;
+    const auto load_ids = [&](int32_t base) {
+      const int32_t kp = one_page ? base : base + k_at, vp = one_page ? base : base + v_at;
+      const int32_t v = vp < req.end ? table[vp >> a.c.page_shift] : -1;
+      const int32_t k = one_page ? v : kp < req.end ? table[kp >> a.c.page_shift] : -1;
+      return int2{k, v};
+    };
+    const auto load_tile = [&](int32_t base, int2 ids, RawTile<D>& t) {
+      const uint8_t *kr, *vr;
+      const uint16_t *ks, *vs;
+      if (one_page) {
+        const int32_t id = __builtin_amdgcn_readfirstlane(ids.y);
+        t.valid = id >= 0 && id < pages;
+        const int64_t row = (((int64_t)(t.valid ? id : 0) * a.c.heads + head) << a.c.page_shift) + (base & page_mask);
+        kr = a.c.k_codes + row * (D / 2) + ((k_at + (col & 3)) * (D / 2) + grp * (D / 8));
+        vr = a.c.v_codes + row * (D / 2) + (v_at * (D / 2) + col * (D / 4));
+        ks = a.c.k_scales + row + v_at;
+        vs = a.c.v_scales + row + v_at;
+      } else {
+        const auto row_of = [&](int32_t id, int32_t p) {       // hidden: any page, masked below
+          const int32_t page = id >= 0 && id < pages ? id : 0;
+          return (((int64_t)page * a.c.heads + head) << a.c.page_shift) + (p & page_mask);
+        };
+        t.valid = ids.y >= 0 && ids.y < pages;
+        const int64_t k_row = row_of(ids.x, base + k_at), v_row = row_of(ids.y, base + v_at);
+        kr = a.c.k_codes + (k_row + (col & 3)) * (D / 2) + grp * (D / 8);
+        vr = a.c.v_codes + v_row * (D / 2) + col * (D / 4);
+        ks = a.c.k_scales + v_row;
+        vs = a.c.v_scales + v_row;
+      }
       load_words(kr, t.k[0]);
       load_words(kr + 4 * (D / 2), t.k[1]);
-      load_words(a.c.v_codes + vb * (D / 2) + col * (D / 4), t.v);
-      t.ks = *reinterpret_cast<const u32x4*>(a.c.k_scales + vb);
-      t.vs = *reinterpret_cast<const u32x4*>(a.c.v_scales + vb);
+      load_words(vr, t.v);
+      t.ks = *reinterpret_cast<const u32x4*>(ks);
+      t.vs = *reinterpret_cast<const u32x4*>(vs);
     };
     const auto tile = [&](int32_t base, const RawTile<D>& t) {
       f32x4 s[NT][2];
@@ -328,50 +365,49 @@ void k_kv4_decode(AttnArgs a) {
         kscale[j] = scale_at(t.ks, j);
         vscale[j] = scale_at(t.vs, j);
       }
+      const auto weigh = [&](auto all_seen) {
+        constexpr bool kAll = decltype(all_seen)::value;
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        float x[8], vsc[8];
-        bool seen[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          x[j] = s[nt][j >> 2][j & 3] * kscale[j];
-          vsc[j] = vscale[j];
-          seen[j] = true;
-        }
-        if (!full) {
+        for (int nt = 0; nt < NT; ++nt) {
+          float x[8];
+          bool seen[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const int32_t pos = base + 8 * grp + j;
-            // Rows past the request's see what any position allows; they are not written.
-            seen[j] = t.valid && pos < req.end && pos <= last[nt] &&
-                      (!a.window || last[nt] == INT32_MAX || pos > (int64_t)last[nt] - a.window);
-            x[j] = seen[j] ? x[j] : kNone;
-            vsc[j] = seen[j] ? vsc[j] : 0.0f;
+            x[j] = s[nt][j >> 2][j & 3] * kscale[j];
+            if constexpr (!kAll) {
+              const int32_t pos = base + 8 * grp + j;
+              // Rows past the request's see what any position allows; they are not written.
+              seen[j] = t.valid && pos < req.end && pos <= last[nt] &&
+                        (!a.window || last[nt] == INT32_MAX || pos > (int64_t)last[nt] - a.window);
+              x[j] = seen[j] ? x[j] : kNone;
+            }
           }
-        }
-        float top = x[0];
+          float top = x[0];
 #pragma unroll
-        for (int j = 1; j < 8; ++j) top = fmaxf(top, x[j]);
-        const float reach = top * qs[nt];
-        if (__builtin_amdgcn_ballot_w64(reach - ref[nt] > 8.0f)) {
-          const float most = column_max(reach);
-          const float next = most - ref[nt] > 8.0f ? most : ref[nt];
-          const float f = exp2_fast(ref[nt] - next);
-          ref[nt] = next;
-          sum[nt] *= f;
+          for (int j = 1; j < 8; ++j) top = fmaxf(top, x[j]);
+          const float reach = top * qs[nt];
+          if (__builtin_amdgcn_ballot_w64(reach - ref[nt] > 8.0f)) {
+            const float most = column_max(reach);
+            const float next = most - ref[nt] > 8.0f ? most : ref[nt];
+            const float f = exp2_fast(ref[nt] - next);
+            ref[nt] = next;
+            sum[nt] *= f;
 #pragma unroll
-          for (int i = 0; i < kCh; ++i) o[nt][i] *= f;
-        }
+            for (int i = 0; i < kCh; ++i) o[nt][i] *= f;
+          }
+          float w[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          float e = exp2_fast(__builtin_fmaf(x[j], qs[nt], -ref[nt]));
-          if (!full) e = seen[j] ? e : 0.0f;
-          sum[nt] += e;
-          const float weight = e * vsc[j];
-          hi[nt][j] = (__bf16)weight;
-          lo[nt][j] = (__bf16)(weight - (float)hi[nt][j]);
+          for (int j = 0; j < 8; ++j) {
+            float e = exp2_fast(__builtin_fmaf(x[j], qs[nt], -ref[nt]));
+            if constexpr (!kAll) e = seen[j] ? e : 0.0f;
+            sum[nt] += e;
+            w[j] = e * (kAll || seen[j] ? vscale[j] : 0.0f);
+          }
+          split_weights(w, hi[nt], lo[nt]);
         }
-      }
+      };
+      if (full) weigh(std::true_type{});
+      else weigh(std::false_type{});
       // O^T += V^T P^T: MFMA i has channel D/16 m + i in row m.
 #pragma unroll
       for (int b = 0; b < (D == 256 ? 2 : 1); ++b) {
@@ -402,13 +438,21 @@ void k_kv4_decode(AttnArgs a) {
     {
       const int32_t stop = req.end < req.from + unit1 * kUnit ? req.end : req.from + unit1 * kUnit;
       int32_t base = req.from + unit0 * kUnit + wave * kTile;
-      RawTile<D> cur, next;
-      if (base < stop) load_tile(base, cur);
-      for (; base < stop; base += kUnit) {
-        if (base + kUnit < stop) load_tile(base + kUnit, next);
-        tile(base, cur);
-        cur = next;
-      }
+      // kAhead tiles are in flight while one is used, and the page id of the next is known.
+      RawTile<D> t[kAhead + 1];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (base + k * kUnit < stop) load_tile(base + k * kUnit, load_ids(base + k * kUnit), t[k]);
+      int2 ids = load_ids(base + kAhead * kUnit);
+      for (; base < stop; base += (kAhead + 1) * kUnit)
+#pragma unroll
+        for (int k = 0; k < kAhead + 1; ++k) {
+          const int32_t at = base + k * kUnit;
+          if (k && at >= stop) break;
+          if (at + kAhead * kUnit < stop) load_tile(at + kAhead * kUnit, ids, t[(k + kAhead) % (kAhead + 1)]);
+          ids = load_ids(at + (kAhead + 1) * kUnit);
+          tile(at, t[k]);
+        }
     }
 
     // ---- the wavefronts' sums together, and out
@@ -832,39 +876,47 @@ void k_kv4_prompt(AttnArgs a, int splits) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         const float f = qs[nb] * up;
-        bool seen[16];
-        if (!full) {
+        const auto weigh = [&](auto all_seen) {
+          constexpr bool kAll = decltype(all_seen)::value;
+          bool seen[16];
+          if constexpr (!kAll) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int at = 8 * (i >> 2) + (i & 3), pos = base + 32 * pb + 4 * half + at;
-            seen[i] = ((bits >> at) & 1u) && pos <= last[nb] &&
-                      (!a.window || last[nb] == INT32_MAX || pos > (int64_t)last[nb] - a.window);
-            s[nb][i] = seen[i] ? s[nb][i] : kNone;
+            for (int i = 0; i < 16; ++i) {
+              const int at = 8 * (i >> 2) + (i & 3), pos = base + 32 * pb + 4 * half + at;
+              seen[i] = ((bits >> at) & 1u) && pos <= last[nb] &&
+                        (!a.window || last[nb] == INT32_MAX || pos > (int64_t)last[nb] - a.window);
+              s[nb][i] = seen[i] ? s[nb][i] : kNone;
+            }
           }
-        }
-        float top = s[nb][0];
+          float top = s[nb][0];
 #pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[nb][i]);
-        const float reach = top * f;
-        if (__builtin_amdgcn_ballot_w64(reach - ref[nb] > 8.0f)) {
-          const float most = fmaxf(reach, __shfl_xor(reach, 32));
-          const float next = most - ref[nb] > 8.0f ? most : ref[nb];
-          const float g = exp2_fast(ref[nb] - next);
-          ref[nb] = next;
-          sum[nb] *= g;
+          for (int i = 1; i < 16; ++i) top = fmaxf(top, s[nb][i]);
+          const float reach = top * f;
+          if (__builtin_amdgcn_ballot_w64(reach - ref[nb] > 8.0f)) {
+            const float most = fmaxf(reach, __shfl_xor(reach, 32));
+            const float next = most - ref[nb] > 8.0f ? most : ref[nb];
+            const float g = exp2_fast(ref[nb] - next);
+            ref[nb] = next;
+            sum[nb] *= g;
 #pragma unroll
-          for (int c = 0; c < kCb; ++c) o[nb][c] *= g;
-        }
+            for (int c = 0; c < kCb; ++c) o[nb][c] *= g;
+          }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          float e = exp2_fast(__builtin_fmaf(s[nb][i], f, -ref[nb]));
-          if (!full) e = seen[i] ? e : 0.0f;
-          sum[nb] += e;
-          const float w = e * vs[i >> 2][i & 3];
-          const __bf16 h = (__bf16)w;
-          hi[nb][i >> 3][i & 7] = h;
-          lo[nb][i >> 3][i & 7] = (__bf16)(w - (float)h);
-        }
+          for (int h = 0; h < 2; ++h) {
+            float w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const int i = 8 * h + j;
+              float e = exp2_fast(__builtin_fmaf(s[nb][i], f, -ref[nb]));
+              if constexpr (!kAll) e = seen[i] ? e : 0.0f;
+              sum[nb] += e;
+              w[j] = e * vs[i >> 2][i & 3];
+            }
+            split_weights(w, hi[nb][h], lo[nb][h]);
+          }
+        };
+        if (full) weigh(std::true_type{});
+        else weigh(std::false_type{});
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h)
