@@ -498,7 +498,8 @@ int32_t logbq_kv4_read(const logbq_kv4* cache, const int64_t* slots_dev, int64_t
  *   q_heads    : a multiple of cache->heads, at most 16 times it; query head h reads key/value
  *                head h / (q_heads / heads).
  *   table_dev  : device, [requests][width] int32 page ids; a negative entry, or one past the
- *                cache, hides its page. width * page <= 2^30.
+ *                cache, hides its page. width * page <= 2^30, and
+ *                requests * heads * (width * page / 128 + 1) < 2^31.
  *   seq_lens_dev : device, [requests] int32, cached tokens with this step's, which are already
  *                appended.
  *   q_starts_dev : device, [requests + 1] int32, first token of each request.

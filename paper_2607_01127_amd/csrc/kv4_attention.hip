@@ -64,28 +64,26 @@ __device__ __forceinline__ Request request_of(const AttnArgs& a, int r) {
 }
 
 // ------------------------------------------------------------------ decode
-// A wavefront takes 32 positions at a time, on its own: scores S^T = K Q^T with 16x16x32 MFMAs (the
-// keys as the A operand, so a lane has 8 consecutive positions of one query row), weights, and
-// O^T = V^T P^T, for which the lane's 8 weights are the B operand as they are. 4-bit codes become
-// float16 by v_cvt_scalef32_pk_f16_fp4 (two values an instruction, exact); the rows' scales stay
-// out of the products: those of the keys multiply the scores, those of the values the weights.
+// A wavefront takes blocks of 32 positions: scores S^T = K Q^T with 16x16x32 MFMAs (the keys as the A
+// operand, so a lane has 8 consecutive positions of one query row), weights, and O^T = V^T P^T, for
+// which the lane's 8 weights are the B operand as they are. 4-bit codes become float16 or bfloat16 by
+// v_cvt_scalef32_pk_{f16,bf16}_fp4 (two values an instruction, exact); the rows' scales stay out of
+// the products: those of the keys multiply the scores, those of the values the weights.
 //
-// Weights are exp2(x - R) with one reference R a query row, raised to the row's largest score when
+// A key/value head rarely has 16 query rows, so a tile is CG blocks: the rows are repeated CG times
+// over the 16 columns, and lanes of column group b keep the scores of block b. One pass over the
+// scores then serves all blocks; for the second product of block b the other groups' weights are
+// masked to 0, so the columns gather CG separate sums a row, which the end adds up like those of
+// different wavefronts. A block's codes are loaded for the next tile as soon as they are used.
+//
+// Weights are exp2(x - R) with one reference R a column, raised to the column's largest score when
 // one passes it by 2^8; their sum is float32. A weight times its value's scale is split into two
 // bfloat16 numbers (16 bits, the range of float32), one MFMA each: float16 would lose the small
 // ones where the scales of a request's values span many orders of magnitude.
 constexpr int kDecThreads = 256;
 constexpr int kDecWaves = kDecThreads / 64;
-constexpr int kTile = 32;                          // positions of a wavefront's step
-constexpr int kUnit = kTile * kDecWaves;           // positions of a workgroup's step
-
-template <int D>
-struct RawTile {
-  uint32_t k[2][D / 32];       // a position's codes of D/4 channels, twice
-  uint32_t v[D / 16];          // 8 positions' codes of D/16 channels
-  u32x4 ks, vs;                // 8 positions' scales
-  int32_t valid;               // the lane's 8 positions are in a page
-};
+constexpr int kBlock = 32;                         // positions of a block
+constexpr int kUnit = kBlock * kDecWaves;          // positions that workgroups' shares are counted in
 
 template <int N>
 __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[N]) {
@@ -173,18 +171,21 @@ __device__ __forceinline__ float column_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
-template <int D, int NT, bool QSPLIT>
+template <int D, int NT, int CG, bool QSPLIT>
 __global__ __launch_bounds__(kDecThreads, (D / 64 * NT <= 2 ? 2 : 1))
 void k_kv4_decode(AttnArgs a) {
-  constexpr int kRows = 16 * NT, kChunks = D / 32, kCh = D / 16, kAhead = 2;
+  static_assert(NT == 1 || CG == 1, "columns are shared only within one tile of 16");
+  constexpr int kCols = 16 / CG;                   // columns of a group
+  constexpr int kRows = kCols * NT, kChunks = D / 32, kCh = D / 16;
   __shared__ float merged[kDecWaves][16][D + 4];
-  __shared__ float ref_s[kDecWaves][kRows], sum_s[kDecWaves][kRows];
-  __shared__ int64_t scan[kDecWaves];
-  __shared__ int64_t found[2];
+  __shared__ float ref_s[kDecWaves][16 * NT], sum_s[kDecWaves][16 * NT];
+  __shared__ int32_t scan[kDecWaves];
+  __shared__ int32_t found[2];
+  __shared__ Request found_request;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int col = lane & 15, grp = lane >> 4;
+  const int col = lane & 15, grp = lane >> 4, blk = col / kCols;
 
-  // ---- this workgroup's part of all requests' units
+  // ---- this workgroup's part of all requests' units (the host has seen that they fit 31 bits)
   const auto units_of = [&](const Request& q) -> int {
     if (q.n <= 0 || q.n * (int64_t)a.group > kRows) return 0;
     return q.end > q.from ? (q.end - q.from + kUnit - 1) / kUnit : 1;    // at least zeros to write
@@ -192,60 +193,150 @@ void k_kv4_decode(AttnArgs a) {
   const int per = (a.requests + kDecThreads - 1) / kDecThreads;
   const int r0 = tid * per < a.requests ? tid * per : a.requests;
   const int r1 = r0 + per < a.requests ? r0 + per : a.requests;
-  int64_t mine = 0;
-  for (int r = r0; r < r1; ++r) mine += (int64_t)units_of(request_of(a, r)) * a.c.heads;
-  int64_t upto = mine;
+  int mine = 0;
+  for (int r = r0; r < r1; ++r) mine += units_of(request_of(a, r)) * a.c.heads;
+  int upto = mine;
   for (int d = 1; d < 64; d <<= 1) {
-    const int64_t x = __shfl_up(upto, d);
+    const int x = __shfl_up(upto, d);
     if (lane >= d) upto += x;
   }
   if (lane == 63) scan[wave] = upto;
   __syncthreads();
-  int64_t total = 0;
+  int total = 0;
   for (int w = 0; w < kDecWaves; ++w) {
     if (w < wave) upto += scan[w];
     total += scan[w];
   }
-  const int64_t parts = total < a.parts ? total : a.parts;       // workgroups with work
-  const int64_t w = blockIdx.x;
-  int32_t* desc = a.desc + 4 * w;
-  if (w >= parts) {
-    if (tid == 0) desc[0] = 0;
-    return;
-  }
-  int64_t u = total * w / parts;
-  const int64_t u_end = total * (w + 1) / parts;
+  total = __builtin_amdgcn_readfirstlane(total);
+  const int parts = total < a.parts ? total : a.parts;       // workgroups with work
+  const int w = blockIdx.x;
+  int32_t* desc = a.desc + 4 * (int64_t)w;
+  if (tid == 0) desc[0] = 0;
+  if (w >= parts) return;
+  // The first `rest` workgroups have one unit more.
+  const int share = (unsigned)total / (unsigned)parts, rest = total - share * parts;
+  int u = w * share + (w < rest ? w : rest);
+  const int u_end = u + share + (w < rest ? 1 : 0);
   if (upto - mine <= u && u < upto) {
-    int64_t at = upto - mine;
+    int at = upto - mine;
     for (int r = r0; r < r1; ++r) {
-      const int64_t n = (int64_t)units_of(request_of(a, r)) * a.c.heads;
+      const Request q = request_of(a, r);
+      const int n = units_of(q) * a.c.heads;
       if (u < at + n) {
         found[0] = r;
         found[1] = u - at;
+        found_request = q;
         break;
       }
       at += n;
     }
   }
   __syncthreads();
-  int r = __builtin_amdgcn_readfirstlane((int)found[0]);
-  // Units of one request fit 32 bits: fewer than 2^31 / 128 times 1024 heads is 2^34, so 64.
-  int64_t off = ((int64_t)__builtin_amdgcn_readfirstlane((int)(found[1] >> 32)) << 32) |
-                (uint32_t)__builtin_amdgcn_readfirstlane((int)found[1]);
-  if (tid == 0) desc[0] = 0;
 
-  Request req = request_of(a, r);
-  int units = units_of(req);
-  while (u < u_end) {
-    while (off >= (int64_t)units * a.c.heads) {
-      off -= (int64_t)units * a.c.heads;
-      req = request_of(a, ++r);
-      units = units_of(req);
+  // ---- pieces: the units of one request and key/value head that the workgroup has. While one is
+  // worked on, the next one's page ids are on their way, and while its sums are joined and written,
+  // the next one's codes.
+  struct Piece {
+    Request req;
+    int r, head, units, unit0, unit1, u;
+  };
+  const auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  const auto uniform_request = [&](const Request& q) {
+    return Request{uniform(q.t0), uniform(q.n), uniform(q.first), uniform(q.from), uniform(q.end)};
+  };
+  int at_r = uniform(found[0]), off = uniform(found[1]);
+  Request at_req = uniform_request(found_request);
+  const auto next_piece = [&]() {
+    Piece p;
+    p.units = units_of(at_req);
+    while (off >= p.units * a.c.heads) {
+      off -= p.units * a.c.heads;
+      at_req = uniform_request(request_of(a, ++at_r));
+      p.units = units_of(at_req);
     }
-    const int head = (int)(off / units), unit0 = (int)(off % units);
-    const int64_t left = u_end - u;
-    const int unit1 = left < units - unit0 ? unit0 + (int)left : units;
+    p.req = at_req;
+    p.r = at_r;
+    p.head = (unsigned)off / (unsigned)p.units;
+    p.unit0 = off - p.head * p.units;
+    p.unit1 = u_end - u < p.units - p.unit0 ? p.unit0 + u_end - u : p.units;
+    p.u = u;
+    u += p.unit1 - p.unit0;
+    off += p.unit1 - p.unit0;
+    return p;
+  };
+
+  // ---- loading, the wavefront's quarter of a piece: positions first_of .. stop_of
+  const int page_mask = (1 << a.c.page_shift) - 1;
+  const int32_t pages = (int32_t)(a.c.slots >> a.c.page_shift);
+  constexpr int kTile = CG * kBlock;
+  const auto first_of = [&](const Piece& p) {
+    return p.req.from + p.unit0 * kUnit + wave * (p.unit1 - p.unit0) * kBlock;
+  };
+  const auto stop_of = [&](const Piece& p) {
+    return min(p.req.end, first_of(p) + (p.unit1 - p.unit0) * kBlock);
+  };
+  // Lane i has the page of positions 16 i .. 16 i + 15 of a tile (i < 2 CG).
+  const auto load_ids = [&](const Piece& p, int32_t base) {
+    const int32_t at = base + 16 * lane;
+    const int32_t id = lane < 2 * CG && at < stop_of(p)
+                           ? a.table[(int64_t)p.r * a.width + (at >> a.c.page_shift)] : -1;
+    return id < pages ? id : -1;
+  };
+  // Rows of a block: keys' lanes (col, grp) have position 8 (col / 4) + col % 4 (+ 4) and channels
+  // grp D/4 ..; values' lanes positions 8 grp .. 8 grp + 7. A hidden page's are read from page 0.
+  const bool one_page = a.c.page_shift >= 5;       // a block lies in one
+  const auto row_of = [&](const Piece& p, int32_t id, int32_t at) {
+    return (((int64_t)(id < 0 ? 0 : id) * a.c.heads + p.head) << a.c.page_shift) + (at & page_mask);
+  };
+  uint32_t kw[CG][2][D / 32], vw[CG][D / 16];
+  u32x4 ks, vs;
+  const auto load_keys = [&](const Piece& p, int b, int32_t at, int32_t ids) {
+    const uint8_t* from;
+    const int k_at = 8 * (col >> 2);
+    if (one_page)
+      from = a.c.k_codes + row_of(p, __builtin_amdgcn_readlane(ids, 2 * b), at) * (D / 2) +
+             ((k_at + (col & 3)) * (D / 2) + grp * (D / 8));
+    else
+      from = a.c.k_codes + (row_of(p, __shfl(ids, 2 * b + (col >> 3)), at + k_at) + (col & 3)) * (D / 2) +
+             grp * (D / 8);
+    load_words(from, kw[b][0]);
+    load_words(from + 4 * (D / 2), kw[b][1]);
+  };
+  const auto load_values = [&](const Piece& p, int b, int32_t at, int32_t ids) {
+    const uint8_t* from;
+    if (one_page)
+      from = a.c.v_codes + row_of(p, __builtin_amdgcn_readlane(ids, 2 * b), at) * (D / 2) +
+             (8 * grp * (D / 2) + col * (D / 4));
+    else
+      from = a.c.v_codes + row_of(p, __shfl(ids, 2 * b + (grp >> 1)), at + 8 * grp) * (D / 2) + col * (D / 4);
+    load_words(from, vw[b]);
+  };
+  const auto load_scales = [&](const Piece& p, int32_t base, int32_t ids) {
+    const int64_t row = row_of(p, __shfl(ids, 2 * blk + (grp >> 1)), base + kBlock * blk + 8 * grp);
+    ks = *reinterpret_cast<const u32x4*>(a.c.k_scales + row);
+    vs = *reinterpret_cast<const u32x4*>(a.c.v_scales + row);
+  };
+  const auto load_first_tile = [&](const Piece& p, int32_t ids) {
+    const int32_t base = first_of(p), stop = stop_of(p);
+    if (base >= stop) return;
+#pragma unroll
+    for (int b = 0; b < CG; ++b)
+      if (base + b * kBlock < stop) {
+        load_keys(p, b, base + b * kBlock, ids);
+        load_values(p, b, base + b * kBlock, ids);
+      }
+    load_scales(p, base, ids);
+  };
+
+  Piece now = next_piece();
+  int32_t ids = load_ids(now, first_of(now));
+  load_first_tile(now, ids);
+  for (;;) {
+    const Request& req = now.req;
+    const int head = now.head, unit0 = now.unit0, unit1 = now.unit1, units = now.units;
     const int rows = req.n * a.group;
+    const int32_t stop = stop_of(now);
+    int32_t next_ids = load_ids(now, first_of(now) + kTile);
 
     // ---- queries: the B operand, scaled by a power of two so that float16 holds them
     half8v qf[NT][kChunks], ql[QSPLIT ? NT : 1][kChunks];
@@ -255,7 +346,7 @@ void k_kv4_decode(AttnArgs a) {
     f32x4 o[NT][kCh];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const int row = nt * 16 + col;
+      const int row = nt * kCols + col % kCols;
       const int token = row / a.group;
       float x[D / 4];
       const int64_t at = (int64_t)(req.t0 + token) * a.q_stride +
@@ -291,94 +382,66 @@ void k_kv4_decode(AttnArgs a) {
       for (int i = 0; i < kCh; ++i) o[nt][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
-    // ---- the wavefront's tiles of the piece
-    const int32_t* table = a.table + (int64_t)r * a.width;
-    const int page_mask = (1 << a.c.page_shift) - 1;
-    const int64_t pages = a.c.slots >> a.c.page_shift;
-    // Keys: lane (col, grp) has position 8 (col / 4) + col % 4 (+ 4), channels grp D/4 ..;
-    // values and scales: positions 8 grp .. 8 grp + 7. A tile lies in one page, or (16 positions a
-    // page) in two.
-    const bool one_page = a.c.page_shift >= 5;
-    const int k_at = 8 * (col >> 2), v_at = 8 * grp;
-    const auto load_ids = [&](int32_t base) {
-      const int32_t kp = one_page ? base : base + k_at, vp = one_page ? base : base + v_at;
-      const int32_t v = vp < req.end ? table[vp >> a.c.page_shift] : -1;
-      const int32_t k = one_page ? v : kp < req.end ? table[kp >> a.c.page_shift] : -1;
-      return int2{k, v};
-    };
-    const auto load_tile = [&](int32_t base, int2 ids, RawTile<D>& t) {
-      const uint8_t *kr, *vr;
-      const uint16_t *ks, *vs;
-      if (one_page) {
-        const int32_t id = __builtin_amdgcn_readfirstlane(ids.y);
-        t.valid = id >= 0 && id < pages;
-        const int64_t row = (((int64_t)(t.valid ? id : 0) * a.c.heads + head) << a.c.page_shift) + (base & page_mask);
-        kr = a.c.k_codes + row * (D / 2) + ((k_at + (col & 3)) * (D / 2) + grp * (D / 8));
-        vr = a.c.v_codes + row * (D / 2) + (v_at * (D / 2) + col * (D / 4));
-        ks = a.c.k_scales + row + v_at;
-        vs = a.c.v_scales + row + v_at;
-      } else {
-        const auto row_of = [&](int32_t id, int32_t p) {       // hidden: any page, masked below
-          const int32_t page = id >= 0 && id < pages ? id : 0;
-          return (((int64_t)page * a.c.heads + head) << a.c.page_shift) + (p & page_mask);
-        };
-        t.valid = ids.y >= 0 && ids.y < pages;
-        const int64_t k_row = row_of(ids.x, base + k_at), v_row = row_of(ids.y, base + v_at);
-        kr = a.c.k_codes + (k_row + (col & 3)) * (D / 2) + grp * (D / 8);
-        vr = a.c.v_codes + v_row * (D / 2) + col * (D / 4);
-        ks = a.c.k_scales + v_row;
-        vs = a.c.v_scales + v_row;
-      }
-      load_words(kr, t.k[0]);
-      load_words(kr + 4 * (D / 2), t.k[1]);
-      load_words(vr, t.v);
-      t.ks = *reinterpret_cast<const u32x4*>(ks);
-      t.vs = *reinterpret_cast<const u32x4*>(vs);
-    };
-    const auto tile = [&](int32_t base, const RawTile<D>& t) {
-      f32x4 s[NT][2];
+    // ---- the next piece and its first page ids
+    const bool another = u < u_end;
+    Piece then = now;
+    int32_t then_ids = -1;
+    if (another) {
+      then = next_piece();
+      then_ids = load_ids(then, first_of(then));
+    }
+
+    for (int32_t base = first_of(now); base < stop; base += kTile) {
+      const bool more = base + kTile < stop;
+      float s[NT][8];
 #pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
-        half8v kf[kChunks];
+      for (int b = 0; b < CG; ++b) {
+        if (b && base + b * kBlock >= stop) break;
+        half8v kf[2][kChunks];
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c) kf[c] = values_of(t.k[hf][c]);
+        for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+          for (int c = 0; c < kChunks; ++c) kf[hf][c] = values_of(kw[b][hf][c]);
+        if (base + kTile + b * kBlock < stop) load_keys(now, b, base + kTile + b * kBlock, next_ids);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+          f32x4 acc[2] = {};
 #pragma unroll
-          for (int c = 0; c < kChunks; ++c) {
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[c], qf[nt][c], acc, 0, 0, 0);
-            if constexpr (QSPLIT)
-              acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[c], ql[nt][c], acc, 0, 0, 0);
+          for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+              acc[hf] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[hf][c], qf[nt][c], acc[hf], 0, 0, 0);
+              if constexpr (QSPLIT)
+                acc[hf] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[hf][c], ql[nt][c], acc[hf], 0, 0, 0);
+            }
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float x = acc[j >> 2][j & 3];
+            s[nt][j] = b == 0 || blk == b ? x : s[nt][j];
           }
-          s[nt][hf] = acc;
         }
       }
-      // Whether every row sees all 32 positions.
-      const bool full = base >= req.from && base + kTile <= req.end && base + kTile - 1 <= req.first &&
+      // Whether every row sees all positions of the tile.
+      const bool full = base + kTile <= stop && base + kTile - 1 <= req.first &&
                         (!a.window || base > (int64_t)req.first + req.n - 1 - a.window) &&
-                        __builtin_amdgcn_ballot_w64(t.valid == 0) == 0;
+                        !__builtin_amdgcn_ballot_w64(lane < 2 * CG && ids < 0);
       bf16x8 hi[NT], lo[NT];
-      float vscale[8], kscale[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        kscale[j] = scale_at(t.ks, j);
-        vscale[j] = scale_at(t.vs, j);
-      }
       const auto weigh = [&](auto all_seen) {
         constexpr bool kAll = decltype(all_seen)::value;
+        const int32_t at = base + kBlock * blk + 8 * grp;
+        bool page_seen = true;
+        if constexpr (!kAll) page_seen = __shfl(ids, 2 * blk + (grp >> 1)) >= 0;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           float x[8];
           bool seen[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            x[j] = s[nt][j >> 2][j & 3] * kscale[j];
+            x[j] = s[nt][j] * scale_at(ks, j);
             if constexpr (!kAll) {
-              const int32_t pos = base + 8 * grp + j;
               // Rows past the request's see what any position allows; they are not written.
-              seen[j] = t.valid && pos < req.end && pos <= last[nt] &&
-                        (!a.window || last[nt] == INT32_MAX || pos > (int64_t)last[nt] - a.window);
+              seen[j] = page_seen && at + j < stop && at + j <= last[nt] &&
+                        (!a.window || last[nt] == INT32_MAX || at + j > (int64_t)last[nt] - a.window);
               x[j] = seen[j] ? x[j] : kNone;
             }
           }
@@ -401,63 +464,66 @@ void k_kv4_decode(AttnArgs a) {
             float e = exp2_fast(__builtin_fmaf(x[j], qs[nt], -ref[nt]));
             if constexpr (!kAll) e = seen[j] ? e : 0.0f;
             sum[nt] += e;
-            w[j] = e * (kAll || seen[j] ? vscale[j] : 0.0f);
+            w[j] = e * (kAll || seen[j] ? scale_at(vs, j) : 0.0f);
           }
           split_weights(w, hi[nt], lo[nt]);
         }
       };
       if (full) weigh(std::true_type{});
       else weigh(std::false_type{});
+      if (more) load_scales(now, base + kTile, next_ids);
       // O^T += V^T P^T: MFMA i has channel D/16 m + i in row m.
 #pragma unroll
-      for (int b = 0; b < (D == 256 ? 2 : 1); ++b) {
-        uint32_t even[4], odd[4];
-        if (b == 0) pair_positions<D, 0>(t.v, even, odd);
-        else pair_positions<D, D == 256 ? 1 : 0>(t.v, even, odd);
-        bf16x8 vf[D == 64 ? 4 : 8];
-        vf[0] = values_at<0>(even);
-        vf[1] = values_at<0>(odd);
-        vf[2] = values_at<1>(even);
-        vf[3] = values_at<1>(odd);
-        if constexpr (D != 64) {
-          vf[4] = values_at<2>(even);
-          vf[5] = values_at<2>(odd);
-          vf[6] = values_at<3>(even);
-          vf[7] = values_at<3>(odd);
-        }
+      for (int b = 0; b < CG; ++b) {
+        if (b && base + b * kBlock >= stop) break;
+        bf16x8 bh[NT], bl[NT];
 #pragma unroll
-        for (int i = 0; i < (D == 64 ? 4 : 8); ++i)
+        for (int nt = 0; nt < NT; ++nt) {
+          bh[nt] = hi[nt];
+          bl[nt] = lo[nt];
+          if constexpr (CG > 1) {
+            const uint32_t mask = blk == b ? ~0u : 0u;
+            bh[nt] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, hi[nt]) & mask);
+            bl[nt] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, lo[nt]) & mask);
+          }
+        }
+        const auto half_of = [&](auto which) {       // 8 channels a lane (D = 64: 4)
+          constexpr int h = decltype(which)::value, kN = D == 64 ? 4 : 8;
+          uint32_t even[4], odd[4];
+          pair_positions<D, h>(vw[b], even, odd);
+          bf16x8 vf[kN];
+          vf[0] = values_at<0>(even);
+          vf[1] = values_at<0>(odd);
+          vf[2] = values_at<1>(even);
+          vf[3] = values_at<1>(odd);
+          if constexpr (D != 64) {
+            vf[4] = values_at<2>(even);
+            vf[5] = values_at<2>(odd);
+            vf[6] = values_at<3>(even);
+            vf[7] = values_at<3>(odd);
+          }
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
-            f32x4& acc = o[nt][8 * b + i];
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i], lo[nt], acc, 0, 0, 0);
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i], hi[nt], acc, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < kN; ++i)
+              o[nt][8 * h + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i], bl[nt], o[nt][8 * h + i], 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < kN; ++i)
+              o[nt][8 * h + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i], bh[nt], o[nt][8 * h + i], 0, 0, 0);
           }
+        };
+        half_of(std::integral_constant<int, 0>{});
+        if constexpr (D == 256) half_of(std::integral_constant<int, 1>{});
+        if (base + kTile + b * kBlock < stop) load_values(now, b, base + kTile + b * kBlock, next_ids);
       }
-    };
-    {
-      const int32_t stop = req.end < req.from + unit1 * kUnit ? req.end : req.from + unit1 * kUnit;
-      int32_t base = req.from + unit0 * kUnit + wave * kTile;
-      // kAhead tiles are in flight while one is used, and the page id of the next is known.
-      RawTile<D> t[kAhead + 1];
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k)
-        if (base + k * kUnit < stop) load_tile(base + k * kUnit, load_ids(base + k * kUnit), t[k]);
-      int2 ids = load_ids(base + kAhead * kUnit);
-      for (; base < stop; base += (kAhead + 1) * kUnit)
-#pragma unroll
-        for (int k = 0; k < kAhead + 1; ++k) {
-          const int32_t at = base + k * kUnit;
-          if (k && at >= stop) break;
-          if (at + kAhead * kUnit < stop) load_tile(at + kAhead * kUnit, ids, t[(k + kAhead) % (kAhead + 1)]);
-          ids = load_ids(at + (kAhead + 1) * kUnit);
-          tile(at, t[k]);
-        }
+      ids = next_ids;
+      if (more) next_ids = load_ids(now, base + 2 * kTile);
     }
 
     // ---- the wavefronts' sums together, and out
+    if (another) load_first_tile(then, then_ids);
     const bool whole = unit0 == 0 && unit1 == units;
-    const int64_t slot = 2 * w + (unit0 == 0 ? 1 : 0);
+    const int64_t slot = 2 * (int64_t)w + (unit0 == 0 ? 1 : 0);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const float total_sum = column_sum(sum[nt]);
@@ -469,34 +535,40 @@ void k_kv4_decode(AttnArgs a) {
     __syncthreads();
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      float best = kNone;
+      // The row's sums are in CG columns of each wavefront.
+      const auto largest = [&](int row) {
+        float top = kNone;
 #pragma unroll
-      for (int i = 0; i < kDecWaves; ++i) best = fmaxf(best, ref_s[i][nt * 16 + col]);
-      const float f = exp2_fast(ref[nt] - best);
+        for (int k = 0; k < kDecWaves; ++k)
+#pragma unroll
+          for (int g = 0; g < CG; ++g) top = fmaxf(top, ref_s[k][nt * 16 + g * kCols + row]);
+        return top;
+      };
+      const float f = exp2_fast(ref[nt] - largest(col % kCols));
 #pragma unroll
       for (int h = 0; h < 4; ++h)
 #pragma unroll
         for (int i = 0; i < kCh; ++i) merged[wave][col][(4 * grp + h) * kCh + i] = o[nt][i][h] * f;
       __syncthreads();
-      for (int i = tid; i < 16 * (D / 4); i += kDecThreads) {
-        const int c = i / (D / 4), ch = i % (D / 4) * 4, row = nt * 16 + c;
+      for (int i = tid; i < kCols * (D / 4); i += kDecThreads) {
+        const int c = i / (D / 4), ch = i % (D / 4) * 4, row = nt * kCols + c;
         if (row >= rows) continue;
-        float top = kNone, l = 0.0f;
-#pragma unroll
-        for (int k = 0; k < kDecWaves; ++k) top = fmaxf(top, ref_s[k][row]);
+        const float top = largest(c);
+        float l = 0.0f;
         f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int k = 0; k < kDecWaves; ++k) {
-          l += sum_s[k][row] * exp2_fast(ref_s[k][row] - top);
-          v += *reinterpret_cast<const f32x4*>(&merged[k][c][ch]);
-        }
+        for (int k = 0; k < kDecWaves; ++k)
+#pragma unroll
+          for (int g = 0; g < CG; ++g) {
+            const int at = nt * 16 + g * kCols + c;
+            l += sum_s[k][at] * exp2_fast(ref_s[k][at] - top);
+            v += *reinterpret_cast<const f32x4*>(&merged[k][g * kCols + c][ch]);
+          }
         if (whole) {
           const float inv = l > 0.0f ? 1.0f / l : 0.0f;
           const int64_t at = (int64_t)(req.t0 + row / a.group) * (a.c.heads * a.group) +
                              head * a.group + row % a.group;
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            store_element(a.out, a.out_dtype, at * D + ch + j, l > 0.0f ? v[j] * inv : 0.0f);
+          store_four(a.out, a.out_dtype, at * D + ch, l > 0.0f ? v * inv : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
           if (a.lse && ch == 0) a.lse[at] = l > 0.0f ? (top + __log2f(l)) * kLn2 : -INFINITY;
         } else {
           *reinterpret_cast<f32x4*>(a.part_o + (slot * kRows + row) * D + ch) = v;
@@ -511,16 +583,16 @@ void k_kv4_decode(AttnArgs a) {
     if (!whole && unit0 == 0 && tid == 0) {
       // The piece begins here: parts 2 w + 1, then 2 (w + 1), ... of the workgroups up to the one
       // that has the last unit.
-      const int64_t end_unit = u + units;
-      const int64_t w1 = (end_unit * parts - 1) / total;
-      desc[0] = (int32_t)(w1 - w + 1);
-      desc[1] = r;
+      const int last_unit = now.u + units - 1, more_units = rest * (share + 1);
+      const int w1 = last_unit < more_units ? last_unit / (share + 1) : rest + (last_unit - more_units) / share;
+      desc[0] = w1 - w + 1;
+      desc[1] = now.r;
       desc[2] = head;
       desc[3] = rows;
     }
-    const int done = unit1 - unit0;
-    u += done;
-    off += done;
+    if (!another) break;
+    now = then;
+    ids = then_ids;
   }
 }
 
@@ -564,8 +636,7 @@ __global__ __launch_bounds__(kDecThreads) void k_kv4_join(AttnArgs a, int kRows)
   const int64_t at = (int64_t)(req.t0 + row / a.group) * (a.c.heads * a.group) +
                      desc[2] * a.group + row % a.group;
   const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-  for (int j = 0; j < 4; ++j)
-    store_element(a.out, a.out_dtype, at * D + 4 * ch + j, l > 0.0f ? v[j] * inv : 0.0f);
+  store_four(a.out, a.out_dtype, at * D + 4 * ch, l > 0.0f ? v * inv : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
   if (a.lse && ch == 0) a.lse[at] = l > 0.0f ? (top + __log2f(l)) * kLn2 : -INFINITY;
 }
 
@@ -1024,9 +1095,9 @@ constexpr int kPromptGrid = 1024;     // workgroups that the splits of few rows 
 constexpr int kDecParts = 512;      // workgroups of the decode kernel: two a CU
 constexpr int64_t kDescBytes = 16 * kDecParts;
 
-template <int D, int NT>
+template <int D, int NT, int CG>
 int32_t launch_decode(AttnArgs a, void* work, hipStream_t stream) {
-  constexpr int kRows = 16 * NT;
+  constexpr int kRows = 16 * NT / CG;
   uint8_t* at = static_cast<uint8_t*>(work);
   a.parts = kDecParts;
   a.desc = reinterpret_cast<int32_t*>(at);
@@ -1035,9 +1106,9 @@ int32_t launch_decode(AttnArgs a, void* work, hipStream_t stream) {
   static_assert(kDescBytes + (int64_t)2 * kDecParts * kRows * (D + 2) * 4 <= LOGBQ_KV4_WORKSPACE_BYTES,
                 "the workspace holds every part");
   if (a.q_dtype == LOGBQ_DTYPE_F32)
-    hipLaunchKernelGGL((k_kv4_decode<D, NT, true>), dim3(kDecParts), dim3(kDecThreads), 0, stream, a);
+    hipLaunchKernelGGL((k_kv4_decode<D, NT, CG, true>), dim3(kDecParts), dim3(kDecThreads), 0, stream, a);
   else
-    hipLaunchKernelGGL((k_kv4_decode<D, NT, false>), dim3(kDecParts), dim3(kDecThreads), 0, stream, a);
+    hipLaunchKernelGGL((k_kv4_decode<D, NT, CG, false>), dim3(kDecParts), dim3(kDecThreads), 0, stream, a);
   if (launch_status() != LOGBQ_OK) return LOGBQ_ERR_HIP;
   hipLaunchKernelGGL(k_kv4_join<D>, dim3(kDecParts, kRows), dim3(kDecThreads), 0, stream, a, kRows);
   return launch_status();
@@ -1074,11 +1145,13 @@ int32_t launch_prompt(AttnArgs a, void* work, hipStream_t stream) {
 template <int D>
 int32_t launch_attention(const AttnArgs& a, int64_t max_new, void* work, hipStream_t stream) {
   const int64_t rows = max_new > INT32_MAX ? INT32_MAX : max_new * a.group;
-  if (rows <= 16) return launch_decode<D, 1>(a, work, stream);
-  if (rows <= 32) return launch_decode<D, 2>(a, work, stream);
-  if (D < 256 && rows <= 64) return launch_decode<D, D < 256 ? 4 : 2>(a, work, stream);
+  if (rows <= 4) return launch_decode<D, 1, 4>(a, work, stream);
+  if (rows <= 8) return launch_decode<D, 1, 2>(a, work, stream);
+  if (rows <= 16) return launch_decode<D, 1, 1>(a, work, stream);
+  if (rows <= 32) return launch_decode<D, 2, 1>(a, work, stream);
+  if (D == 64 && rows <= 64) return launch_decode<D, D == 64 ? 4 : 2, 1>(a, work, stream);
   // A prompt among them: decode requests apart from the longer ones.
-  const int32_t status = launch_decode<D, 1>(a, work, stream);
+  const int32_t status = launch_decode<D, 1, 1>(a, work, stream);
   if (status != LOGBQ_OK) return status;
   return launch_prompt<D, kPromptBlocks>(a, work, stream);
 }
@@ -1104,6 +1177,8 @@ int32_t logbq_kv4_attention(const void* q_dev, int64_t q_stride, int32_t q_dtype
   if (q_heads % c.heads || q_heads / c.heads > 16) return LOGBQ_ERR_UNSUPPORTED;
   if (tokens >= INT32_MAX || requests >= INT32_MAX || width > (1 << 30) / cache->page)
     return LOGBQ_ERR_UNSUPPORTED;
+  // Units of 128 positions of one head, and at least one a request, fit 31 bits.
+  if ((double)requests * c.heads * ((double)width * cache->page / 128 + 1) >= INT32_MAX) return LOGBQ_ERR_UNSUPPORTED;
   if (tokens == 0 || requests == 0 || max_new == 0) return LOGBQ_OK;
   if (!q_dev || !out_dev || !seq_lens_dev || !q_starts_dev || !work_dev || (width > 0 && !table_dev))
     return LOGBQ_ERR_INVALID_ARG;
