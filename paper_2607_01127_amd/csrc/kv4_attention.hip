@@ -30,6 +30,7 @@ struct AttnArgs {
   Kv4 c;
   int64_t q_stride;
   int32_t width, tokens, requests, group, window, q_dtype, out_dtype, parts;
+  int32_t unit;           // positions that the workgroups' shares are counted in
   float scale;
 };
 
@@ -40,6 +41,14 @@ constexpr float kLn2 = 0.69314718055994530942f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// The same number, but one that the compiler cannot compute ahead of a loop: what is derived from it
+// takes no registers across the loop. (A spilled value is worse than a recomputed one: its load
+// comes back only after all the loads of codes before it.)
+__device__ __forceinline__ int here(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // A request as the kernels see it.
 struct Request {
   int32_t t0, n;          // first token, number of tokens
@@ -48,11 +57,15 @@ struct Request {
 };
 
 __device__ __forceinline__ Request request_of(const AttnArgs& a, int r) {
+  // Lengths do not change while a kernel runs; through the constant address space a uniform index
+  // loads them by the scalar path, apart from the codes that are on their way.
+  typedef const __attribute__((address_space(4))) int32_t* Constant;
+  const Constant q_starts = (Constant)(uintptr_t)a.q_starts, seq_lens = (Constant)(uintptr_t)a.seq_lens;
   Request q;
-  int32_t t0 = a.q_starts[r], t1 = a.q_starts[r + 1];
+  int32_t t0 = q_starts[r], t1 = q_starts[r + 1];
   t0 = t0 < 0 ? 0 : t0 > a.tokens ? a.tokens : t0;
   t1 = t1 < t0 ? t0 : t1 > a.tokens ? a.tokens : t1;
-  const int32_t len = a.seq_lens[r] > 0 ? a.seq_lens[r] : 0;
+  const int32_t len = seq_lens[r] > 0 ? seq_lens[r] : 0;
   const int64_t span = a.c.slots > 0 ? (int64_t)a.width << a.c.page_shift : 0;
   q.t0 = t0;
   q.n = t1 - t0;
@@ -83,7 +96,7 @@ __device__ __forceinline__ Request request_of(const AttnArgs& a, int r) {
 constexpr int kDecThreads = 256;
 constexpr int kDecWaves = kDecThreads / 64;
 constexpr int kBlock = 32;                         // positions of a block
-constexpr int kUnit = kBlock * kDecWaves;          // positions that workgroups' shares are counted in
+constexpr int kUnit = kBlock * kDecWaves;          // shares are counted in one or more of these
 
 template <int N>
 __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[N]) {
@@ -171,7 +184,7 @@ __device__ __forceinline__ float column_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
-template <int D, int NT, int CG, bool QSPLIT>
+template <int D, int NT, int CG, bool QSPLIT, bool ONE_PAGE>
 __global__ __launch_bounds__(kDecThreads, (D / 64 * NT <= 2 ? 2 : 1))
 void k_kv4_decode(AttnArgs a) {
   static_assert(NT == 1 || CG == 1, "columns are shared only within one tile of 16");
@@ -179,6 +192,10 @@ void k_kv4_decode(AttnArgs a) {
   constexpr int kRows = kCols * NT, kChunks = D / 32, kCh = D / 16;
   __shared__ float merged[kDecWaves][16][D + 4];
   __shared__ float ref_s[kDecWaves][16 * NT], sum_s[kDecWaves][16 * NT];
+  // The queries' operands, one copy a wavefront: they are read again for each tile, as the registers
+  // are needed for codes in flight.
+  __shared__ half8v q_hi[kDecWaves][NT][kChunks][64];
+  __shared__ half8v q_lo[QSPLIT ? kDecWaves : 1][NT][kChunks][64];
   __shared__ int32_t scan[kDecWaves];
   __shared__ int32_t found[2];
   __shared__ Request found_request;
@@ -188,7 +205,7 @@ void k_kv4_decode(AttnArgs a) {
   // ---- this workgroup's part of all requests' units (the host has seen that they fit 31 bits)
   const auto units_of = [&](const Request& q) -> int {
     if (q.n <= 0 || q.n * (int64_t)a.group > kRows) return 0;
-    return q.end > q.from ? (q.end - q.from + kUnit - 1) / kUnit : 1;    // at least zeros to write
+    return q.end > q.from ? (unsigned)(q.end - q.from + a.unit - 1) / (unsigned)a.unit : 1;    // at least zeros to write
   };
   const int per = (a.requests + kDecThreads - 1) / kDecThreads;
   const int r0 = tid * per < a.requests ? tid * per : a.requests;
@@ -270,10 +287,10 @@ void k_kv4_decode(AttnArgs a) {
   const int32_t pages = (int32_t)(a.c.slots >> a.c.page_shift);
   constexpr int kTile = CG * kBlock;
   const auto first_of = [&](const Piece& p) {
-    return p.req.from + p.unit0 * kUnit + wave * (p.unit1 - p.unit0) * kBlock;
+    return p.req.from + p.unit0 * a.unit + wave * (p.unit1 - p.unit0) * (a.unit / kDecWaves);
   };
   const auto stop_of = [&](const Piece& p) {
-    return min(p.req.end, first_of(p) + (p.unit1 - p.unit0) * kBlock);
+    return min(p.req.end, first_of(p) + (p.unit1 - p.unit0) * (a.unit / kDecWaves));
   };
   // Lane i has the page of positions 16 i .. 16 i + 15 of a tile (i < 2 CG).
   const auto load_ids = [&](const Piece& p, int32_t base) {
@@ -284,35 +301,39 @@ void k_kv4_decode(AttnArgs a) {
   };
   // Rows of a block: keys' lanes (col, grp) have position 8 (col / 4) + col % 4 (+ 4) and channels
   // grp D/4 ..; values' lanes positions 8 grp .. 8 grp + 7. A hidden page's are read from page 0.
-  const bool one_page = a.c.page_shift >= 5;       // a block lies in one
+  // ONE_PAGE: pages have 32 positions or more, so a block lies in one.
   const auto row_of = [&](const Piece& p, int32_t id, int32_t at) {
     return (((int64_t)(id < 0 ? 0 : id) * a.c.heads + p.head) << a.c.page_shift) + (at & page_mask);
   };
   uint32_t kw[CG][2][D / 32], vw[CG][D / 16];
   u32x4 ks, vs;
+  const int key_offset = (8 * (col >> 2) + (col & 3)) * (D / 2) + grp * (D / 8);
+  const int value_offset = 8 * grp * (D / 2) + col * (D / 4);
   const auto load_keys = [&](const Piece& p, int b, int32_t at, int32_t ids) {
     const uint8_t* from;
-    const int k_at = 8 * (col >> 2);
-    if (one_page)
-      from = a.c.k_codes + row_of(p, __builtin_amdgcn_readlane(ids, 2 * b), at) * (D / 2) +
-             ((k_at + (col & 3)) * (D / 2) + grp * (D / 8));
-    else
-      from = a.c.k_codes + (row_of(p, __shfl(ids, 2 * b + (col >> 3)), at + k_at) + (col & 3)) * (D / 2) +
-             grp * (D / 8);
+    if constexpr (ONE_PAGE) {
+      from = a.c.k_codes + row_of(p, __builtin_amdgcn_readlane(ids, 2 * b), at) * (D / 2) + key_offset;
+    } else {
+      const int l = here(lane), c = l & 15, g = l >> 4;
+      from = a.c.k_codes + (c & 3) * (D / 2) + g * (D / 8) +
+             row_of(p, __shfl(ids, 2 * b + (c >> 3)), at + 8 * (c >> 2)) * (D / 2);
+    }
     load_words(from, kw[b][0]);
     load_words(from + 4 * (D / 2), kw[b][1]);
   };
   const auto load_values = [&](const Piece& p, int b, int32_t at, int32_t ids) {
     const uint8_t* from;
-    if (one_page)
-      from = a.c.v_codes + row_of(p, __builtin_amdgcn_readlane(ids, 2 * b), at) * (D / 2) +
-             (8 * grp * (D / 2) + col * (D / 4));
-    else
-      from = a.c.v_codes + row_of(p, __shfl(ids, 2 * b + (grp >> 1)), at + 8 * grp) * (D / 2) + col * (D / 4);
+    if constexpr (ONE_PAGE) {
+      from = a.c.v_codes + row_of(p, __builtin_amdgcn_readlane(ids, 2 * b), at) * (D / 2) + value_offset;
+    } else {
+      const int l = here(lane), c = l & 15, g = l >> 4;
+      from = a.c.v_codes + row_of(p, __shfl(ids, 2 * b + (g >> 1)), at + 8 * g) * (D / 2) + c * (D / 4);
+    }
     load_words(from, vw[b]);
   };
   const auto load_scales = [&](const Piece& p, int32_t base, int32_t ids) {
-    const int64_t row = row_of(p, __shfl(ids, 2 * blk + (grp >> 1)), base + kBlock * blk + 8 * grp);
+    const int l = here(lane), b = (l & 15) / kCols, g = l >> 4;
+    const int64_t row = row_of(p, __shfl(ids, 2 * b + (g >> 1)), base + kBlock * b + 8 * g);
     ks = *reinterpret_cast<const u32x4*>(a.c.k_scales + row);
     vs = *reinterpret_cast<const u32x4*>(a.c.v_scales + row);
   };
@@ -328,18 +349,37 @@ void k_kv4_decode(AttnArgs a) {
     load_scales(p, base, ids);
   };
 
+  // Queries as they are: column c of a group has row nt kCols + c, lane group grp channels grp D/4 ...
+  constexpr int kQueryWords = QSPLIT ? D / 4 : D / 8;
+  uint32_t qw[NT][kQueryWords];
+  const auto load_queries = [&](const Piece& p) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int lane_here = here(lane), row = nt * kCols + lane_here % kCols;
+      const int64_t at = (int64_t)(p.req.t0 + row / a.group) * a.q_stride +
+                         (int64_t)(p.head * a.group + row % a.group) * D + (lane_here >> 4) * (D / 4);
+      if (row < p.req.n * a.group) {
+        load_words(static_cast<const uint8_t*>(a.q) + at * (QSPLIT ? 4 : 2), qw[nt]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kQueryWords; ++i) qw[nt][i] = 0;
+      }
+    }
+  };
+
+  // Loads come back in the order in which they were asked for, so page ids are asked for first and
+  // queries before codes.
   Piece now = next_piece();
-  int32_t ids = load_ids(now, first_of(now));
+  int32_t ids = load_ids(now, first_of(now)), next_ids = load_ids(now, first_of(now) + kTile);
+  load_queries(now);
   load_first_tile(now, ids);
   for (;;) {
     const Request& req = now.req;
     const int head = now.head, unit0 = now.unit0, unit1 = now.unit1, units = now.units;
     const int rows = req.n * a.group;
     const int32_t stop = stop_of(now);
-    int32_t next_ids = load_ids(now, first_of(now) + kTile);
 
     // ---- queries: the B operand, scaled by a power of two so that float16 holds them
-    half8v qf[NT][kChunks], ql[QSPLIT ? NT : 1][kChunks];
     float qs[NT];             // what scores are multiplied by, in powers of two
     float ref[NT], sum[NT];
     int32_t last[NT];         // last position that the row sees
@@ -349,15 +389,19 @@ void k_kv4_decode(AttnArgs a) {
       const int row = nt * kCols + col % kCols;
       const int token = row / a.group;
       float x[D / 4];
-      const int64_t at = (int64_t)(req.t0 + token) * a.q_stride +
-                         (int64_t)(head * a.group + row % a.group) * D + grp * (D / 4);
-      if (row < rows) {
-        if (a.q_dtype == LOGBQ_DTYPE_F32) load_row<LOGBQ_DTYPE_F32>(a.q, at, x);
-        else if (a.q_dtype == LOGBQ_DTYPE_F16) load_row<LOGBQ_DTYPE_F16>(a.q, at, x);
-        else load_row<LOGBQ_DTYPE_BF16>(a.q, at, x);
-      } else {
 #pragma unroll
-        for (int i = 0; i < D / 4; ++i) x[i] = 0.0f;
+      for (int i = 0; i < kQueryWords; ++i) {
+        const uint32_t w = qw[nt][i];
+        if constexpr (QSPLIT) {
+          x[i] = __uint_as_float(w);
+        } else if (a.q_dtype == LOGBQ_DTYPE_BF16) {
+          x[2 * i] = __uint_as_float(w << 16);
+          x[2 * i + 1] = __uint_as_float(w & 0xffff0000u);
+        } else {
+          const half2v h = __builtin_bit_cast(half2v, w);
+          x[2 * i] = (float)h.x;
+          x[2 * i + 1] = (float)h.y;
+        }
       }
       float most = 0.0f;
 #pragma unroll
@@ -368,13 +412,17 @@ void k_kv4_decode(AttnArgs a) {
       const float down = ldexpf(a.scale < 0.0f ? -1.0f : 1.0f, -e);
       qs[nt] = __builtin_fabsf(a.scale) * kLog2e * ldexpf(1.0f, e);
 #pragma unroll
-      for (int s = 0; s < kChunks; ++s)
+      for (int s = 0; s < kChunks; ++s) {
+        half8v hi, lo;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const float y = x[8 * s + j] * down;
-          qf[nt][s][j] = (half_t)y;
-          if constexpr (QSPLIT) ql[nt][s][j] = (half_t)(y - (float)(half_t)y);
+          hi[j] = (half_t)y;
+          lo[j] = (half_t)(y - (float)(half_t)y);
         }
+        q_hi[wave][nt][s][lane] = hi;
+        if constexpr (QSPLIT) q_lo[wave][nt][s][lane] = lo;
+      }
       ref[nt] = kNone;
       sum[nt] = 0.0f;
       last[nt] = row < rows ? req.first + token : INT32_MAX;
@@ -385,15 +433,18 @@ void k_kv4_decode(AttnArgs a) {
     // ---- the next piece and its first page ids
     const bool another = u < u_end;
     Piece then = now;
-    int32_t then_ids = -1;
+    int32_t then_ids = -1, then_next = -1;
     if (another) {
       then = next_piece();
       then_ids = load_ids(then, first_of(then));
+      then_next = load_ids(then, first_of(then) + kTile);
     }
 
     for (int32_t base = first_of(now); base < stop; base += kTile) {
       const bool more = base + kTile < stop;
+      const int32_t after_ids = load_ids(now, base + 2 * kTile);
       float s[NT][8];
+      const int q_lane = here(lane);
 #pragma unroll
       for (int b = 0; b < CG; ++b) {
         if (b && base + b * kBlock >= stop) break;
@@ -403,20 +454,22 @@ void k_kv4_decode(AttnArgs a) {
 #pragma unroll
           for (int c = 0; c < kChunks; ++c) kf[hf][c] = values_of(kw[b][hf][c]);
         if (base + kTile + b * kBlock < stop) load_keys(now, b, base + kTile + b * kBlock, next_ids);
+        f32x4 acc[NT][2] = {};
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          f32x4 acc[2] = {};
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int c = 0; c < kChunks; ++c)
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf) {
-              acc[hf] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[hf][c], qf[nt][c], acc[hf], 0, 0, 0);
+              acc[nt][hf] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[hf][c], q_hi[wave][nt][c][q_lane], acc[nt][hf], 0, 0, 0);
               if constexpr (QSPLIT)
-                acc[hf] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[hf][c], ql[nt][c], acc[hf], 0, 0, 0);
+                acc[nt][hf] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[hf][c], q_lo[wave][nt][c][q_lane], acc[nt][hf], 0, 0, 0);
             }
 #pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const float x = acc[j >> 2][j & 3];
+            const float x = acc[nt][j >> 2][j & 3];
             s[nt][j] = b == 0 || blk == b ? x : s[nt][j];
           }
         }
@@ -488,48 +541,46 @@ void k_kv4_decode(AttnArgs a) {
           }
         }
         const auto half_of = [&](auto which) {       // 8 channels a lane (D = 64: 4)
-          constexpr int h = decltype(which)::value, kN = D == 64 ? 4 : 8;
+          constexpr int h = decltype(which)::value;
           uint32_t even[4], odd[4];
           pair_positions<D, h>(vw[b], even, odd);
-          bf16x8 vf[kN];
-          vf[0] = values_at<0>(even);
-          vf[1] = values_at<0>(odd);
-          vf[2] = values_at<1>(even);
-          vf[3] = values_at<1>(odd);
-          if constexpr (D != 64) {
-            vf[4] = values_at<2>(even);
-            vf[5] = values_at<2>(odd);
-            vf[6] = values_at<3>(even);
-            vf[7] = values_at<3>(odd);
-          }
+          const auto channels = [&](auto byte) {       // 2 byte .. 2 byte + 3 of them
+            constexpr int B = decltype(byte)::value;
+            const bf16x8 vf[4] = {values_at<B>(even), values_at<B>(odd), values_at<B + 1>(even), values_at<B + 1>(odd)};
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
+            for (int nt = 0; nt < NT; ++nt) {
+              f32x4* acc = &o[nt][8 * h + 2 * B];
 #pragma unroll
-            for (int i = 0; i < kN; ++i)
-              o[nt][8 * h + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i], bl[nt], o[nt][8 * h + i], 0, 0, 0);
+              for (int i = 0; i < 4; ++i) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i], bl[nt], acc[i], 0, 0, 0);
 #pragma unroll
-            for (int i = 0; i < kN; ++i)
-              o[nt][8 * h + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i], bh[nt], o[nt][8 * h + i], 0, 0, 0);
-          }
+              for (int i = 0; i < 4; ++i) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i], bh[nt], acc[i], 0, 0, 0);
+            }
+          };
+          channels(std::integral_constant<int, 0>{});
+          if constexpr (D != 64) channels(std::integral_constant<int, 2>{});
         };
         half_of(std::integral_constant<int, 0>{});
         if constexpr (D == 256) half_of(std::integral_constant<int, 1>{});
         if (base + kTile + b * kBlock < stop) load_values(now, b, base + kTile + b * kBlock, next_ids);
       }
       ids = next_ids;
-      if (more) next_ids = load_ids(now, base + 2 * kTile);
+      next_ids = after_ids;
     }
 
     // ---- the wavefronts' sums together, and out
-    if (another) load_first_tile(then, then_ids);
+    if (another) {
+      load_queries(then);
+      load_first_tile(then, then_ids);
+    }
+    const int thread = here(tid), l = thread & 63, mcol = l & 15, mgrp = l >> 4;
     const bool whole = unit0 == 0 && unit1 == units;
     const int64_t slot = 2 * (int64_t)w + (unit0 == 0 ? 1 : 0);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const float total_sum = column_sum(sum[nt]);
-      if (grp == 0) {
-        ref_s[wave][nt * 16 + col] = ref[nt];
-        sum_s[wave][nt * 16 + col] = total_sum;
+      if (mgrp == 0) {
+        ref_s[wave][nt * 16 + mcol] = ref[nt];
+        sum_s[wave][nt * 16 + mcol] = total_sum;
       }
     }
     __syncthreads();
@@ -544,37 +595,37 @@ void k_kv4_decode(AttnArgs a) {
           for (int g = 0; g < CG; ++g) top = fmaxf(top, ref_s[k][nt * 16 + g * kCols + row]);
         return top;
       };
-      const float f = exp2_fast(ref[nt] - largest(col % kCols));
+      const float f = exp2_fast(ref[nt] - largest(mcol % kCols));
 #pragma unroll
       for (int h = 0; h < 4; ++h)
 #pragma unroll
-        for (int i = 0; i < kCh; ++i) merged[wave][col][(4 * grp + h) * kCh + i] = o[nt][i][h] * f;
+        for (int i = 0; i < kCh; ++i) merged[wave][mcol][(4 * mgrp + h) * kCh + i] = o[nt][i][h] * f;
       __syncthreads();
-      for (int i = tid; i < kCols * (D / 4); i += kDecThreads) {
+      for (int i = thread; i < kCols * (D / 4); i += kDecThreads) {
         const int c = i / (D / 4), ch = i % (D / 4) * 4, row = nt * kCols + c;
         if (row >= rows) continue;
         const float top = largest(c);
-        float l = 0.0f;
+        float den = 0.0f;
         f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int k = 0; k < kDecWaves; ++k)
 #pragma unroll
           for (int g = 0; g < CG; ++g) {
             const int at = nt * 16 + g * kCols + c;
-            l += sum_s[k][at] * exp2_fast(ref_s[k][at] - top);
+            den += sum_s[k][at] * exp2_fast(ref_s[k][at] - top);
             v += *reinterpret_cast<const f32x4*>(&merged[k][g * kCols + c][ch]);
           }
         if (whole) {
-          const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+          const float inv = den > 0.0f ? 1.0f / den : 0.0f;
           const int64_t at = (int64_t)(req.t0 + row / a.group) * (a.c.heads * a.group) +
                              head * a.group + row % a.group;
-          store_four(a.out, a.out_dtype, at * D + ch, l > 0.0f ? v * inv : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
-          if (a.lse && ch == 0) a.lse[at] = l > 0.0f ? (top + __log2f(l)) * kLn2 : -INFINITY;
+          store_four(a.out, a.out_dtype, at * D + ch, den > 0.0f ? v * inv : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+          if (a.lse && ch == 0) a.lse[at] = den > 0.0f ? (top + __log2f(den)) * kLn2 : -INFINITY;
         } else {
           *reinterpret_cast<f32x4*>(a.part_o + (slot * kRows + row) * D + ch) = v;
           if (ch == 0) {
             a.part_rl[(slot * kRows + row) * 2] = top;
-            a.part_rl[(slot * kRows + row) * 2 + 1] = l;
+            a.part_rl[(slot * kRows + row) * 2 + 1] = den;
           }
         }
       }
@@ -593,6 +644,7 @@ void k_kv4_decode(AttnArgs a) {
     if (!another) break;
     now = then;
     ids = then_ids;
+    next_ids = then_next;
   }
 }
 
@@ -1105,11 +1157,20 @@ int32_t launch_decode(AttnArgs a, void* work, hipStream_t stream) {
   a.part_o = a.part_rl + 2 * kDecParts * kRows * 2;
   static_assert(kDescBytes + (int64_t)2 * kDecParts * kRows * (D + 2) * 4 <= LOGBQ_KV4_WORKSPACE_BYTES,
                 "the workspace holds every part");
-  if (a.q_dtype == LOGBQ_DTYPE_F32)
-    hipLaunchKernelGGL((k_kv4_decode<D, NT, CG, true>), dim3(kDecParts), dim3(kDecThreads), 0, stream, a);
-  else
-    hipLaunchKernelGGL((k_kv4_decode<D, NT, CG, false>), dim3(kDecParts), dim3(kDecThreads), 0, stream, a);
+  // Requests of at most 512 positions are not split, which saves the second launch (one of 500
+  // positions: 9.3 us a call, 13.3 with it).
+  const int64_t span = (int64_t)a.width << a.c.page_shift;
+  const bool whole = span <= 4 * kUnit;
+  a.unit = whole && span > kUnit ? (int)(span + kUnit - 1) / kUnit * kUnit : kUnit;
+  const bool split = a.q_dtype == LOGBQ_DTYPE_F32, one_page = a.c.page_shift >= 5;
+#define DECODE(SPLIT, ONE_PAGE)                                                                      \
+  if (split == SPLIT && one_page == ONE_PAGE)                                                        \
+    hipLaunchKernelGGL((k_kv4_decode<D, NT, CG, SPLIT, ONE_PAGE>), dim3(kDecParts), dim3(kDecThreads), \
+                       0, stream, a)
+  DECODE(false, false); DECODE(false, true); DECODE(true, false); DECODE(true, true);
+#undef DECODE
   if (launch_status() != LOGBQ_OK) return LOGBQ_ERR_HIP;
+  if (whole) return LOGBQ_OK;
   hipLaunchKernelGGL(k_kv4_join<D>, dim3(kDecParts, kRows), dim3(kDecThreads), 0, stream, a, kRows);
   return launch_status();
 }
@@ -1145,11 +1206,17 @@ int32_t launch_prompt(AttnArgs a, void* work, hipStream_t stream) {
 template <int D>
 int32_t launch_attention(const AttnArgs& a, int64_t max_new, void* work, hipStream_t stream) {
   const int64_t rows = max_new > INT32_MAX ? INT32_MAX : max_new * a.group;
-  if (rows <= 4) return launch_decode<D, 1, 4>(a, work, stream);
+  // Tiles of four blocks have twice the codes in flight of tiles of two, but take longer to start:
+  // for shares of 20 units or more, and for long requests (D = 128: 128 requests of 3000 to 9000
+  // 167 us against 183, one of 131071 40.6 against 42.4, 32 of 300 to 4100 39.7 against 35.7). Their
+  // registers do not hold split queries as well from D = 128.
+  const int64_t span = (int64_t)a.width << a.c.page_shift;
+  const bool large = (double)a.requests * a.c.heads * span >= 20.0 * kUnit * kDecParts || span >= 32768;
+  if (rows <= 4 && large && (D == 64 || a.q_dtype != LOGBQ_DTYPE_F32)) return launch_decode<D, 1, 4>(a, work, stream);
   if (rows <= 8) return launch_decode<D, 1, 2>(a, work, stream);
   if (rows <= 16) return launch_decode<D, 1, 1>(a, work, stream);
-  if (rows <= 32) return launch_decode<D, 2, 1>(a, work, stream);
-  if (D == 64 && rows <= 64) return launch_decode<D, D == 64 ? 4 : 2, 1>(a, work, stream);
+  if (D < 256 && rows <= 32) return launch_decode<D, D < 256 ? 2 : 1, 1>(a, work, stream);
+  if (D == 64 && rows <= 64) return launch_decode<D, D == 64 ? 4 : 1, 1>(a, work, stream);
   // A prompt among them: decode requests apart from the longer ones.
   const int32_t status = launch_decode<D, 1, 1>(a, work, stream);
   if (status != LOGBQ_OK) return status;
