@@ -706,7 +706,7 @@ __global__ __launch_bounds__(kDecThreads) void k_kv4_join(AttnArgs a, int kRows)
 // second product as two bfloat16 numbers, for the reason given above.
 constexpr int kPromptThreads = 256;
 constexpr int kPromptTile = 64;
-constexpr int kPromptMinRows = 17;           // fewer go through the decode kernel
+constexpr int kPromptMinRows = 17;           // fewer go through the decode kernel, if it is launched
 
 // Offset of a slot of a value fragment: the lanes of a converting wavefront differ in the chunk of
 // positions and the half, which the exclusive or spreads over the banks.
@@ -716,7 +716,7 @@ __device__ __forceinline__ int value_slot(int frag, int chunk, int half, int cha
 
 template <int D, int NB, bool QSPLIT>
 __global__ __launch_bounds__(kPromptThreads, D / 64 * NB <= 2 ? 2 : 1)
-void k_kv4_prompt(AttnArgs a, int splits) {
+void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
   constexpr int kRows = 128 * NB, kKc = D / 16, kCb = D / 32, kItems = D == 256 ? 2 : 1;
   __shared__ half8v kbuf[2][2 * kKc * 64];
   __shared__ bf16x8 vbuf[2][kCb * 4 * 64];
@@ -730,7 +730,7 @@ void k_kv4_prompt(AttnArgs a, int splits) {
   // prompt see more positions
   const auto tiles_of = [&](const Request& q) -> int64_t {
     const int64_t rows = (int64_t)q.n * a.group;
-    return rows < kPromptMinRows ? 0 : (rows + kRows - 1) / kRows;
+    return rows < min_rows ? 0 : (rows + kRows - 1) / kRows;
   };
   const int head = blockIdx.x % a.c.heads;
   const int64_t unit = gridDim.x / a.c.heads - 1 - blockIdx.x / a.c.heads;
@@ -1176,11 +1176,11 @@ int32_t launch_decode(AttnArgs a, void* work, hipStream_t stream) {
 }
 
 template <int D, int NB>
-int32_t launch_prompt(AttnArgs a, void* work, hipStream_t stream) {
+int32_t launch_prompt(AttnArgs a, int min_rows, void* work, hipStream_t stream) {
   constexpr int kRows = 128 * NB;
-  // As many row tiles as the requests can have; each has at least kPromptMinRows rows.
+  // As many row tiles as the requests can have; each has at least min_rows rows.
   const int64_t rows = (int64_t)a.tokens * a.group;
-  const int64_t short_ones = rows / kPromptMinRows < a.requests ? rows / kPromptMinRows : a.requests;
+  const int64_t short_ones = rows / min_rows < a.requests ? rows / min_rows : a.requests;
   const int64_t tiles = (rows / kRows + short_ones) * a.c.heads;
   if (tiles == 0) return LOGBQ_OK;
   if (tiles > INT32_MAX) return LOGBQ_ERR_UNSUPPORTED;
@@ -1194,9 +1194,9 @@ int32_t launch_prompt(AttnArgs a, void* work, hipStream_t stream) {
                 "the workspace holds every part");
   const dim3 grid((unsigned)tiles, (unsigned)splits);
   if (a.q_dtype == LOGBQ_DTYPE_F32)
-    hipLaunchKernelGGL((k_kv4_prompt<D, NB, true>), grid, dim3(kPromptThreads), 0, stream, a, (int)splits);
+    hipLaunchKernelGGL((k_kv4_prompt<D, NB, true>), grid, dim3(kPromptThreads), 0, stream, a, (int)splits, min_rows);
   else
-    hipLaunchKernelGGL((k_kv4_prompt<D, NB, false>), grid, dim3(kPromptThreads), 0, stream, a, (int)splits);
+    hipLaunchKernelGGL((k_kv4_prompt<D, NB, false>), grid, dim3(kPromptThreads), 0, stream, a, (int)splits, min_rows);
   if (splits == 1 || launch_status() != LOGBQ_OK) return launch_status();
   hipLaunchKernelGGL(k_kv4_prompt_join<D>, dim3((unsigned)tiles, kRows / (kPromptThreads / (D / 4))),
                      dim3(kPromptThreads), 0, stream, a, (int)splits, kRows);
@@ -1217,10 +1217,11 @@ int32_t launch_attention(const AttnArgs& a, int64_t max_new, void* work, hipStre
   if (rows <= 16) return launch_decode<D, 1, 1>(a, work, stream);
   if (D < 256 && rows <= 32) return launch_decode<D, D < 256 ? 2 : 1, 1>(a, work, stream);
   if (D == 64 && rows <= 64) return launch_decode<D, D == 64 ? 4 : 1, 1>(a, work, stream);
-  // A prompt among them: decode requests apart from the longer ones.
+  // A prompt among them: decode requests apart from the longer ones. One request is taken as a prompt.
+  if (a.requests == 1) return launch_prompt<D, kPromptBlocks>(a, 1, work, stream);
   const int32_t status = launch_decode<D, 1, 1>(a, work, stream);
   if (status != LOGBQ_OK) return status;
-  return launch_prompt<D, kPromptBlocks>(a, work, stream);
+  return launch_prompt<D, kPromptBlocks>(a, kPromptMinRows, work, stream);
 }
 
 }  // namespace

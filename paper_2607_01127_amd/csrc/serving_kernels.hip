@@ -155,10 +155,9 @@ __global__ __launch_bounds__(kTabThreads) void k_batch_tables(TabArgs a) {
 
 // ------------------------------------------------------------------ the 4-bit cache
 // 16 lanes take a row: lane c has channels c D/16 .. (c + 1) D/16 - 1, which are one group of the
-// value layout. A wavefront takes 4 consecutive tokens of one head.
+// value layout. A workgroup takes 16 consecutive tokens of one head.
 constexpr int kRowLanes = 16;
 constexpr int kRowThreads = 256;
-constexpr int kRowTokens = 4;
 
 // N codes of 4 bits as N / 8 words (N = 4: the low half of one word).
 template <int N>
@@ -180,9 +179,11 @@ __device__ __forceinline__ void load_codes(const uint8_t* from, uint32_t (&w)[(N
 
 // Largest value of the 16 lanes of a row.
 __device__ __forceinline__ uint32_t row_max(uint32_t v) {
-#pragma unroll
-  for (int d = 1; d < kRowLanes; d <<= 1) v = max(v, (uint32_t)__shfl_xor((int)v, d));
-  return v;
+  // Rotations within 16 lanes by 8, 4, 2 and 1.
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x128, 0xf, 0xf, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x124, 0xf, 0xf, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x122, 0xf, 0xf, true));
+  return max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x121, 0xf, 0xf, true));
 }
 
 // Codes of one row: the scale is the smallest bfloat16 s with 6 s >= max |x|, found from the
@@ -225,10 +226,8 @@ __global__ __launch_bounds__(kRowThreads) void k_kv4_append(const void* k, int64
                                                             const void* v, int64_t v_stride,
                                                             int64_t tokens, Kv4 c,
                                                             const int64_t* slots) {
-  const int64_t unit = ((int64_t)blockIdx.x * kRowThreads + threadIdx.x) >> 6;
-  const int group = threadIdx.x & (kRowLanes - 1), sub = (threadIdx.x >> 4) & (kRowTokens - 1);
-  const int head = (int)(unit % c.heads);
-  const int64_t t = unit / c.heads * kRowTokens + sub;
+  const int group = threadIdx.x & (kRowLanes - 1), head = blockIdx.y;
+  const int64_t t = (int64_t)blockIdx.x * (kRowThreads / kRowLanes) + (threadIdx.x >> 4);
   const int64_t slot = t < tokens ? slots[t] : -1;
   if (slot < 0 || slot >= c.slots) return;        // whole rows of 16 lanes leave together
   const int64_t at = (int64_t)head * D + group * (D / 16);
@@ -257,10 +256,8 @@ __device__ __forceinline__ void read_row(const Kv4& c, int64_t slot, bool held, 
 template <int D>
 __global__ __launch_bounds__(kRowThreads) void k_kv4_read(Kv4 c, const int64_t* slots, int64_t tokens,
                                                           void* k, void* v, int32_t dtype) {
-  const int64_t unit = ((int64_t)blockIdx.x * kRowThreads + threadIdx.x) >> 6;
-  const int group = threadIdx.x & (kRowLanes - 1), sub = (threadIdx.x >> 4) & (kRowTokens - 1);
-  const int head = (int)(unit % c.heads);
-  const int64_t t = unit / c.heads * kRowTokens + sub;
+  const int group = threadIdx.x & (kRowLanes - 1), head = blockIdx.y;
+  const int64_t t = (int64_t)blockIdx.x * (kRowThreads / kRowLanes) + (threadIdx.x >> 4);
   if (t >= tokens) return;
   const int64_t slot = slots[t];
   const bool held = slot >= 0 && slot < c.slots;
@@ -691,11 +688,9 @@ __global__ __launch_bounds__(kLpThreads) void k_token_logprobs(LpArgs a) {
 }
 
 // ------------------------------------------------------------------ host side
-// Workgroups for `tokens` tokens of all heads, or 0 if they are too many for one launch.
-unsigned row_grid(int64_t tokens, int32_t heads) {
-  const int64_t units = (tokens + kRowTokens - 1) / kRowTokens * heads;
-  const int64_t grid = (units + kRowThreads / 64 - 1) / (kRowThreads / 64);
-  return grid > INT32_MAX ? 0u : (unsigned)grid;
+// Workgroups for the rows of `tokens` (fewer than 2^31) tokens.
+dim3 row_grid(int64_t tokens, int32_t heads) {
+  return dim3((unsigned)((tokens + kRowThreads / kRowLanes - 1) / (kRowThreads / kRowLanes)), (unsigned)heads);
 }
 
 constexpr int64_t kMaxTokens = (int64_t)1 << 31;
@@ -745,11 +740,10 @@ int32_t logbq_kv4_append(const void* k_dev, int64_t k_stride, const void* v_dev,
   if (k_stride > INT64_MAX / 8 / tokens || v_stride > INT64_MAX / 8 / tokens) return LOGBQ_ERR_UNSUPPORTED;
   if (!aligned16(k_dev) || !aligned16(v_dev) || k_stride * bytes % 16 || v_stride * bytes % 16)
     return LOGBQ_ERR_UNSUPPORTED;
-  const unsigned grid = row_grid(tokens, c.heads);
-  if (!grid) return LOGBQ_ERR_UNSUPPORTED;
+  const dim3 grid = row_grid(tokens, c.heads);
 #define APPEND(D, DT)                                                                          \
   if (cache->dim == D && dtype == DT)                                                          \
-    hipLaunchKernelGGL((k_kv4_append<D, DT>), dim3(grid), dim3(kRowThreads), 0,                \
+    hipLaunchKernelGGL((k_kv4_append<D, DT>), grid, dim3(kRowThreads), 0,                \
                        (hipStream_t)stream, k_dev, k_stride, v_dev, v_stride, tokens, c, slots_dev)
   APPEND(64, LOGBQ_DTYPE_F32); APPEND(64, LOGBQ_DTYPE_F16); APPEND(64, LOGBQ_DTYPE_BF16);
   APPEND(128, LOGBQ_DTYPE_F32); APPEND(128, LOGBQ_DTYPE_F16); APPEND(128, LOGBQ_DTYPE_BF16);
@@ -768,11 +762,10 @@ int32_t logbq_kv4_read(const logbq_kv4* cache, const int64_t* slots_dev, int64_t
   if (tokens == 0) return LOGBQ_OK;
   if (!k_dev || !v_dev || !slots_dev) return LOGBQ_ERR_INVALID_ARG;
   if (!aligned16(k_dev) || !aligned16(v_dev)) return LOGBQ_ERR_UNSUPPORTED;
-  const unsigned grid = row_grid(tokens, c.heads);
-  if (!grid) return LOGBQ_ERR_UNSUPPORTED;
+  const dim3 grid = row_grid(tokens, c.heads);
 #define READ(D)                                                                                   \
   if (cache->dim == D)                                                                            \
-    hipLaunchKernelGGL((k_kv4_read<D>), dim3(grid), dim3(kRowThreads), 0, (hipStream_t)stream, c, \
+    hipLaunchKernelGGL((k_kv4_read<D>), grid, dim3(kRowThreads), 0, (hipStream_t)stream, c, \
                        slots_dev, tokens, k_dev, v_dev, dtype)
   READ(64); READ(128); READ(256);
 #undef READ

@@ -151,7 +151,7 @@ def _check(status: int, where: str):
         raise LogbqError(status, where)
 
 
-_current_stream = None
+_current_stream = None      # set at the first call
 
 
 def _current_stream_getter():
@@ -169,7 +169,7 @@ def _stream(stream):
         global _current_stream
         if _current_stream is None:
             _current_stream = _current_stream_getter()
-        return c_void_p(_current_stream())
+        return _current_stream()
     if isinstance(stream, int):
         return c_void_p(stream)
     return c_void_p(stream.cuda_stream)
