@@ -1042,16 +1042,20 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
         else weigh(std::false_type{});
       }
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < 2; ++h) {
+        bf16x8 vf[kCb];
 #pragma unroll
-        for (int c = 0; c < kCb; ++c) {
-          const bf16x8 vf = vbuf[buf][value_slot(c * 4 + 2 * pb + h, 2 * pb + h, half, col)];
+        for (int c = 0; c < kCb; ++c) vf[c] = vbuf[buf][value_slot(c * 4 + 2 * pb + h, 2 * pb + h, half, col)];
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb) {
-            o[nb][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, lo[nb][h], o[nb][c], 0, 0, 0);
-            o[nb][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, hi[nb][h], o[nb][c], 0, 0, 0);
-          }
+        for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+          for (int c = 0; c < kCb; ++c)
+            o[nb][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[c], lo[nb][h], o[nb][c], 0, 0, 0);
+#pragma unroll
+          for (int c = 0; c < kCb; ++c)
+            o[nb][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[c], hi[nb][h], o[nb][c], 0, 0, 0);
         }
+      }
     }
   };
 
