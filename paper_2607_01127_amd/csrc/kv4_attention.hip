@@ -714,7 +714,7 @@ __device__ __forceinline__ int value_slot(int frag, int chunk, int half, int cha
   return frag * 64 + ((half * 32 + channel) ^ (chunk * 2 + half));
 }
 
-template <int D, int NB, bool QSPLIT>
+template <int D, int NB, bool QSPLIT, bool ONE_PAGE>
 __global__ __launch_bounds__(kPromptThreads, D / 64 * NB <= 2 ? 2 : 1)
 void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
   constexpr int kRows = 128 * NB, kKc = D / 16, kCb = D / 32, kItems = D == 256 ? 2 : 1;
@@ -857,39 +857,41 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
     u32x4 k[kItems], v[kItems];
     uint16_t ks, lane_ks, lane_vs;           // of its keys' position, and of position `lane`
     uint64_t valid;                          // positions of the tile that can be seen
-    bool key_ok, value_ok;
+    bool key_ok;
   };
   const auto load_ids = [&](int base) {
     Ids ids;
     const auto id_at = [&](int p) { return p < kv_end ? table[p >> a.c.page_shift] : -1; };
-    ids.lane = id_at(base + lane);
-    ids.key = id_at(base + key_pos);
-    ids.value = id_at(base + 8 * v_block);
+    ids.lane = id_at(ONE_PAGE ? base : base + lane);
+    ids.key = ONE_PAGE ? ids.lane : id_at(base + key_pos);
+    ids.value = ONE_PAGE ? ids.lane : id_at(base + 8 * v_block);
     return ids;
   };
   const auto load_raw = [&](int base, const Ids& ids) {
     Raw t;
-    const auto row_of = [&](int32_t id, int p) {
-      const int32_t page = id >= 0 && id < pages ? id : 0;
-      return (((int64_t)page * a.c.heads + head) << a.c.page_shift) + (p & page_mask);
-    };
+    // A row's place: scalar for the tile where it lies in one page, with a lane's offset.
+    const int32_t tile_id = __builtin_amdgcn_readfirstlane(ids.lane);
+    const int32_t tile_page = tile_id >= 0 && tile_id < pages ? tile_id : 0;
+    const int64_t tile_row = (((int64_t)tile_page * a.c.heads + head) << a.c.page_shift) + (base & page_mask);
     const auto ok = [&](int32_t id) { return id >= 0 && id < pages; };
-    const int64_t lr = row_of(ids.lane, base + lane);
-    t.lane_ks = a.c.k_scales[lr];
-    t.lane_vs = a.c.v_scales[lr];
-    t.valid = __builtin_amdgcn_ballot_w64(ok(ids.lane));
+    const auto place = [&](const auto* buffer, int row_size, int32_t id, int p, int offset) {
+      if constexpr (ONE_PAGE) return buffer + tile_row * row_size + (p * row_size + offset);
+      const int32_t page = ok(id) ? id : 0;
+      const int64_t row = (((int64_t)page * a.c.heads + head) << a.c.page_shift) + ((base + p) & page_mask);
+      return buffer + row * row_size + offset;
+    };
+    t.lane_ks = *place(a.c.k_scales, 1, ids.lane, lane, 0);
+    t.lane_vs = *place(a.c.v_scales, 1, ids.lane, lane, 0);
+    t.valid = __builtin_amdgcn_ballot_w64(ok(ids.lane) && base + lane < kv_end);
     t.key_ok = ok(ids.key);
-    t.value_ok = ok(ids.value);
     if (has_keys) {
-      const int64_t kr = row_of(ids.key, base + key_pos);
-      t.ks = a.c.k_scales[kr];
+      t.ks = *place(a.c.k_scales, 1, ids.key, key_pos, 0);
 #pragma unroll
       for (int i = 0; i < kItems; ++i)
-        t.k[i] = *reinterpret_cast<const u32x4*>(a.c.k_codes + kr * (D / 2) + (key_item + 4 * i) * 16);
+        t.k[i] = *reinterpret_cast<const u32x4*>(place(a.c.k_codes, D / 2, ids.key, key_pos, (key_item + 4 * i) * 16));
     }
     if (has_values) {
-      const int64_t vr = row_of(ids.value, base + 8 * v_block);
-      const uint8_t* from = a.c.v_codes + vr * (D / 2) + v_group * (D / 4) + v_half * (D / 8);
+      const uint8_t* from = place(a.c.v_codes, D / 2, ids.value, 8 * v_block, v_group * (D / 4) + v_half * (D / 8));
 #pragma unroll
       for (int i = 0; i < kItems; ++i) t.v[i] = *reinterpret_cast<const u32x4*>(from + 16 * i);
     }
@@ -1197,10 +1199,13 @@ int32_t launch_prompt(AttnArgs a, int min_rows, void* work, hipStream_t stream) 
   static_assert(16 * kPromptGrid + (int64_t)kPromptGrid * kRows * (D + 2) * 4 <= LOGBQ_KV4_WORKSPACE_BYTES,
                 "the workspace holds every part");
   const dim3 grid((unsigned)tiles, (unsigned)splits);
-  if (a.q_dtype == LOGBQ_DTYPE_F32)
-    hipLaunchKernelGGL((k_kv4_prompt<D, NB, true>), grid, dim3(kPromptThreads), 0, stream, a, (int)splits, min_rows);
-  else
-    hipLaunchKernelGGL((k_kv4_prompt<D, NB, false>), grid, dim3(kPromptThreads), 0, stream, a, (int)splits, min_rows);
+  const bool split = a.q_dtype == LOGBQ_DTYPE_F32, one_page = a.c.page_shift >= 6;
+#define PROMPT(SPLIT, ONE_PAGE)                                                                     \
+  if (split == SPLIT && one_page == ONE_PAGE)                                                       \
+    hipLaunchKernelGGL((k_kv4_prompt<D, NB, SPLIT, ONE_PAGE>), grid, dim3(kPromptThreads), 0, stream, \
+                       a, (int)splits, min_rows)
+  PROMPT(false, false); PROMPT(false, true); PROMPT(true, false); PROMPT(true, true);
+#undef PROMPT
   if (splits == 1 || launch_status() != LOGBQ_OK) return launch_status();
   hipLaunchKernelGGL(k_kv4_prompt_join<D>, dim3((unsigned)tiles, kRows / (kPromptThreads / (D / 4))),
                      dim3(kPromptThreads), 0, stream, a, (int)splits, kRows);
