@@ -514,8 +514,11 @@ int32_t logbq_kv4_read(const logbq_kv4* cache, const int64_t* slots_dev, int64_t
  * Token i of n new ones of a request of length s has position p = s - n + i and sees positions
  * max(0, p - window + 1) .. p (0 .. p without a window). A token that sees nothing has output 0
  * and lse -inf. Products of q are taken in float16 (float32 queries as a sum of two float16
- * values), all sums and the softmax in float32; its weights are rounded to 11 bits at least for the
- * product with the values.
+ * values), all sums and the softmax in float32; its weights times the values' scales are rounded to
+ * 16 bits for the product with the values' codes. Requests of up to 16 query rows (tokens times
+ * q_heads / heads; 32 for dim 128, 64 for dim 64 if no request of the call has more) share their
+ * positions out over the whole chip; the others go in tiles of 128 rows, whose positions are split
+ * where there are few. Results do not change from call to call. Enqueues one to four kernels.
  * Errors: INVALID_ARG, UNSUPPORTED (dim, page, heads, dtypes, alignment, sizes, a workspace that
  * is too small), HIP.
  */
