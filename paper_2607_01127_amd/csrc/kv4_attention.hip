@@ -626,11 +626,11 @@ void k_kv4_decode(AttnArgs a) {
             v += *reinterpret_cast<const f32x4*>(&merged[k][g * kCols + c][ch]);
           }
         if (whole) {
-          const float inv = den > 0.0f ? 1.0f / den : 0.0f;
+          const float inv = den != 0.0f ? 1.0f / den : 0.0f;
           const int64_t at = (int64_t)(req.t0 + row / a.group) * (a.c.heads * a.group) +
                              head * a.group + row % a.group;
-          store_four(a.out, a.out_dtype, at * D + ch, den > 0.0f ? v * inv : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
-          if (a.lse && ch == 0) a.lse[at] = den > 0.0f ? (top + __log2f(den)) * kLn2 : -INFINITY;
+          store_four(a.out, a.out_dtype, at * D + ch, den != 0.0f ? v * inv : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+          if (a.lse && ch == 0) a.lse[at] = den != 0.0f ? (top + __log2f(den)) * kLn2 : -INFINITY;
         } else {
           *reinterpret_cast<f32x4*>(a.part_o + (slot * kRows + row) * D + ch) = v;
           if (ch == 0) {
@@ -697,9 +697,9 @@ __global__ __launch_bounds__(kDecThreads) void k_kv4_join(AttnArgs a, int kRows)
   for (int i = 1; i < kSlices; ++i) v += sums[i][ch];
   const int64_t at = (int64_t)(req.t0 + row / a.group) * (a.c.heads * a.group) +
                      desc[2] * a.group + row % a.group;
-  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-  store_four(a.out, a.out_dtype, at * D + 4 * ch, l > 0.0f ? v * inv : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
-  if (a.lse && ch == 0) a.lse[at] = l > 0.0f ? (top + __log2f(l)) * kLn2 : -INFINITY;
+  const float inv = l != 0.0f ? 1.0f / l : 0.0f;
+  store_four(a.out, a.out_dtype, at * D + 4 * ch, l != 0.0f ? v * inv : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+  if (a.lse && ch == 0) a.lse[at] = l != 0.0f ? (top + __log2f(l)) * kLn2 : -INFINITY;
 }
 
 // ------------------------------------------------------------------ prompts
@@ -1111,7 +1111,7 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
     if (row >= rows) continue;
     const int64_t at = (int64_t)(req.t0 + row / a.group) * (a.c.heads * a.group) +
                        head * a.group + row % a.group;
-    const float inv = splits > 1 ? 1.0f : l > 0.0f ? 1.0f / l : 0.0f;
+    const float inv = splits > 1 ? 1.0f : l != 0.0f ? 1.0f / l : 0.0f;
 #pragma unroll
     for (int c = 0; c < kCb; ++c)
 #pragma unroll
@@ -1127,7 +1127,7 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
         a.part_rl[(part + row - row0) * 2] = ref[nb];
         a.part_rl[(part + row - row0) * 2 + 1] = l;
       } else if (a.lse) {
-        a.lse[at] = l > 0.0f ? (ref[nb] + __log2f(l)) * kLn2 : -INFINITY;
+        a.lse[at] = l != 0.0f ? (ref[nb] + __log2f(l)) * kLn2 : -INFINITY;
       }
     }
   }
@@ -1157,9 +1157,9 @@ __global__ __launch_bounds__(kPromptThreads) void k_kv4_prompt_join(AttnArgs a, 
   }
   const int64_t at = (int64_t)(req.t0 + row / a.group) * (a.c.heads * a.group) +
                      head * a.group + row % a.group;
-  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-  store_four(a.out, a.out_dtype, at * D + ch, l > 0.0f ? v * inv : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
-  if (a.lse && ch == 0) a.lse[at] = l > 0.0f ? (top + __log2f(l)) * kLn2 : -INFINITY;
+  const float inv = l != 0.0f ? 1.0f / l : 0.0f;
+  store_four(a.out, a.out_dtype, at * D + ch, l != 0.0f ? v * inv : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+  if (a.lse && ch == 0) a.lse[at] = l != 0.0f ? (top + __log2f(l)) * kLn2 : -INFINITY;
 }
 
 // ------------------------------------------------------------------ host side

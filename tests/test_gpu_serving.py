@@ -322,6 +322,27 @@ def test_attention_wide_values(new):
     assert torch.allclose(res * 2.0 ** 40, big, rtol=1e-5, atol=1e-5)
 
 
+@pytest.mark.parametrize("lens,new", [([300, 0], [1, 1]), ([5000, 70], [1, 1]), ([45, 7, 0], [40, 3, 1]),
+                                      ([2000], [40]), ([2000], [1000])])
+def test_attention_nan_queries(lens, new):
+    """A query with a NaN has a NaN result wherever it sees a position, and zeros where it sees none;
+    the other rows' results stay as they are."""
+    say("nan queries", lens, new)
+    rng = np.random.default_rng(22)
+    buffers, q, out, lse, table, lens, starts = attend(rng, lens, new, 2, 4, 128, 16)
+    bad = torch.zeros(q.shape[:2], dtype=torch.bool, device=DEV)
+    bad[0, 1] = bad[-1, 6] = bad[q.shape[0] // 2, 3] = True
+    held = torch.where(bad[..., None] & (torch.arange(128, device=DEV) == 77), math.nan, q)
+    got_lse = torch.empty_like(lse)
+    got = L.kv4_attention(held, buffers, dev(table), dev(lens.astype(np.int32)), dev(starts),
+                          int(max(new)), out=torch.empty_like(out), lse=got_lse)
+    nan = bad & (lse > -math.inf)
+    assert torch.equal(torch.isnan(got_lse), nan)
+    assert torch.equal(got_lse[~nan], lse[~nan]) and torch.equal(got[~nan], out[~nan])
+    # A channel whose codes are all 0 could be 0 in no product: NaN times 0 is NaN.
+    assert bool(torch.isnan(got[nan]).all())
+
+
 def test_attention_garbage_beyond_the_lengths():
     """What lies past a request's length (poisoned scales) reaches no output."""
     say("garbage")
