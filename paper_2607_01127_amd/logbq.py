@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from contextlib import nullcontext
 from ctypes import POINTER, c_double, c_float, c_int32, c_int64, c_uint8, c_uint16, c_void_p
 from typing import NamedTuple
 
@@ -491,6 +492,20 @@ def _kv4_struct(cache) -> Kv4Struct:
                      2 * half, 0)
 
 
+_as_it_is = nullcontext()
+
+
+def _made_on(stream):
+    """A context whose new tensors belong to the stream that a call is given: memory that the
+    current stream still uses is not handed out, and what is filled is filled in order."""
+    if stream is None:
+        return _as_it_is
+    import torch
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+    return torch.cuda.stream(stream)
+
+
 def _rows(x, heads, dim, name):
     """Elements between the tokens of x [tokens][heads][dim], whose heads and channels are
     contiguous."""
@@ -523,9 +538,10 @@ def batch_tables(cached, new, free_pages, table, page: int, tokens: int, out=Non
     _device_array(table, i32, (n, width), "table")
     if out is None:
         e = dict(device=cached.device, dtype=i32)
-        out = dict(slots=torch.empty(tokens, device=cached.device, dtype=torch.int64),
-                   positions=torch.empty(tokens, **e), q_starts=torch.empty(n + 1, **e),
-                   seq_lens=torch.empty(n, **e), info=torch.empty(4, **e))
+        with _made_on(stream):
+            out = dict(slots=torch.empty(tokens, device=cached.device, dtype=torch.int64),
+                       positions=torch.empty(tokens, **e), q_starts=torch.empty(n + 1, **e),
+                       seq_lens=torch.empty(n, **e), info=torch.empty(4, **e))
     else:
         _device_array(out["slots"], torch.int64, (tokens,), "slots")
         _device_array(out["positions"], i32, (tokens,), "positions")
@@ -562,8 +578,9 @@ def kv4_read(cache, slots, dtype=None, stream=None):
     c = _kv4_struct(cache)
     _device_array(slots, torch.int64, (slots.numel(),), "slots")
     shape = (slots.numel(), c.heads, c.dim)
-    k = torch.empty(shape, dtype=dtype or torch.float16, device=slots.device)
-    v = torch.empty_like(k)
+    with _made_on(stream):
+        k = torch.empty(shape, dtype=dtype or torch.float16, device=slots.device)
+        v = torch.empty_like(k)
     _check(lib().logbq_kv4_read(ctypes.byref(c), slots.data_ptr(), shape[0], k.data_ptr(),
                                 v.data_ptr(), _dtype_code(k.dtype), _stream(stream)),
            "logbq_kv4_read")
@@ -591,13 +608,15 @@ def kv4_attention(q, cache, table, seq_lens, q_starts, max_new: int, scale=None,
     _device_array(seq_lens, i32, (n,), "seq_lens")
     _device_array(q_starts, i32, (n + 1,), "q_starts")
     if out is None:
-        out = torch.empty((tokens, q_heads, c.dim), dtype=torch.float16, device=q.device)
+        with _made_on(stream):
+            out = torch.empty((tokens, q_heads, c.dim), dtype=torch.float16, device=q.device)
     else:
         _device_array(out, out.dtype, (tokens, q_heads, c.dim), "out")
     if lse is not None:
         _device_array(lse, torch.float32, (tokens, q_heads), "lse")
     if workspace is None:
-        workspace = torch.empty(KV4_WORKSPACE_BYTES, dtype=torch.uint8, device=q.device)
+        with _made_on(stream):
+            workspace = torch.empty(KV4_WORKSPACE_BYTES, dtype=torch.uint8, device=q.device)
     _check(lib().logbq_kv4_attention(
         q.data_ptr(), q_stride, _dtype_code(q.dtype), tokens, q_heads, ctypes.byref(c),
         table.data_ptr(), n, width, seq_lens.data_ptr(), q_starts.data_ptr(), max_new,
@@ -621,16 +640,18 @@ def token_logprobs(logits, targets, top: int = 0, out=None, workspace=None, stre
     _device_array(targets, torch.int64, (tokens,), "targets")
     if out is None:
         f = dict(dtype=torch.float32, device=logits.device)
-        out = dict(logprob=torch.empty(tokens, **f), entropy=torch.empty(tokens, **f),
-                   top_index=torch.empty((tokens, top), dtype=torch.int32, device=logits.device),
-                   top_logprob=torch.empty((tokens, top), **f))
+        with _made_on(stream):
+            out = dict(logprob=torch.empty(tokens, **f), entropy=torch.empty(tokens, **f),
+                       top_index=torch.empty((tokens, top), dtype=torch.int32, device=logits.device),
+                       top_logprob=torch.empty((tokens, top), **f))
     else:
         _device_array(out["logprob"], torch.float32, (tokens,), "logprob")
         _device_array(out["entropy"], torch.float32, (tokens,), "entropy")
         _device_array(out["top_index"], torch.int32, (tokens, top), "top_index")
         _device_array(out["top_logprob"], torch.float32, (tokens, top), "top_logprob")
     if workspace is None:
-        workspace = torch.zeros(LOGPROBS_WORKSPACE_BYTES, dtype=torch.uint8, device=logits.device)
+        with _made_on(stream):
+            workspace = torch.zeros(LOGPROBS_WORKSPACE_BYTES, dtype=torch.uint8, device=logits.device)
     _check(lib().logbq_token_logprobs(
         logits.data_ptr(), _dtype_code(logits.dtype), tokens, vocab,
         logits.stride(0) if tokens > 1 else vocab, targets.data_ptr(), top,

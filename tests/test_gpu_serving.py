@@ -523,6 +523,43 @@ def test_logprobs_strided_streams_and_graph():
         assert all(torch.equal(want[n], out[n]) for n in out), i
 
 
+def test_results_and_workspaces_of_a_given_stream():
+    """What a call makes for itself belongs to the stream that it is given, as a Stream or as a
+    number: it is filled there in order, and memory that the current stream still writes is not
+    taken."""
+    say("given stream")
+    rng = np.random.default_rng(23)
+    x, t = torch.randn((2, 70001), device=DEV), torch.tensor([5, 70000], device=DEV)
+    buffers, q, out, _, table, lens, starts = attend(rng, [900, 65], [1, 1], 2, 4, 128, 64)
+    args = (dev(table), dev(lens.astype(np.int32)), dev(starts), 1)
+    want, slots = L.token_logprobs(x, t, 11), dev(np.arange(500))
+    rows = L.kv4_read(buffers, slots)
+    i32 = lambda v: dev(np.asarray(v, dtype=np.int32))  # noqa: E731
+    tables = lambda s: L.batch_tables(i32([3, 0]), i32([1, 9]), i32([5, 6]), i32([[1, 0], [0, 0]]),  # noqa: E731
+                                      16, 10, stream=s)
+    made = tables(None)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for stream in (side, side.cuda_stream, 0):
+        # The blocks that the current stream frees are being written for a while yet.
+        big = torch.empty(1 << 30, dtype=torch.uint8, device=DEV)
+        used = [torch.empty(n, dtype=torch.uint8, device=DEV) for n in (L.KV4_WORKSPACE_BYTES, L.LOGPROBS_WORKSPACE_BYTES)]
+        for _ in range(20):
+            big.fill_(255)
+        for u in used:
+            u.fill_(255)
+        del used
+        got = [L.token_logprobs(x, t, 11, stream=stream), L.kv4_attention(q, buffers, *args, stream=stream),
+               L.kv4_read(buffers, slots, stream=stream)]
+        torch.cuda.synchronize()
+        got.append(tables(stream))
+        torch.cuda.synchronize()
+        assert all(torch.equal(want[n], got[0][n]) for n in want)
+        assert torch.equal(got[1], out)
+        assert all(torch.equal(a, b) for a, b in zip(got[2], rows))
+        assert all(torch.equal(made[n], got[3][n]) for n in made)
+
+
 # ------------------------------------------------------------------ together
 
 def test_step_of_appended_tokens():
