@@ -472,6 +472,12 @@ def _device_array(x, dtype, shape, name):
                          f"{tuple(x.shape)} {x.dtype} on {x.device}")
 
 
+def _device_workspace(x):
+    """Raises unless x is a contiguous device tensor; the calls check its size."""
+    if not (x.is_cuda and x.is_contiguous()):
+        raise ValueError(f"workspace must be a contiguous device tensor, not {tuple(x.shape)} on {x.device}")
+
+
 def _kv4_struct(cache) -> Kv4Struct:
     import torch
     kc, ks, vc, vs = cache
@@ -617,6 +623,8 @@ def kv4_attention(q, cache, table, seq_lens, q_starts, max_new: int, scale=None,
     if workspace is None:
         with _made_on(stream):
             workspace = torch.empty(KV4_WORKSPACE_BYTES, dtype=torch.uint8, device=q.device)
+    else:
+        _device_workspace(workspace)
     _check(lib().logbq_kv4_attention(
         q.data_ptr(), q_stride, _dtype_code(q.dtype), tokens, q_heads, ctypes.byref(c),
         table.data_ptr(), n, width, seq_lens.data_ptr(), q_starts.data_ptr(), max_new,
@@ -652,6 +660,8 @@ def token_logprobs(logits, targets, top: int = 0, out=None, workspace=None, stre
     if workspace is None:
         with _made_on(stream):
             workspace = torch.zeros(LOGPROBS_WORKSPACE_BYTES, dtype=torch.uint8, device=logits.device)
+    else:
+        _device_workspace(workspace)
     _check(lib().logbq_token_logprobs(
         logits.data_ptr(), _dtype_code(logits.dtype), tokens, vocab,
         logits.stride(0) if tokens > 1 else vocab, targets.data_ptr(), top,

@@ -560,6 +560,23 @@ def test_results_and_workspaces_of_a_given_stream():
         assert all(torch.equal(made[n], got[3][n]) for n in made)
 
 
+def test_workspaces_that_are_refused():
+    """Host memory and strided views are no workspace: the call raises before anything runs."""
+    say("workspaces")
+    rng = np.random.default_rng(24)
+    buffers, q, _, _, table, lens, starts = attend(rng, [40], [1], 2, 4, 64, 16)
+    args = (dev(table), dev(lens.astype(np.int32)), dev(starts), 1)
+    x, t = torch.randn((2, 50), device=DEV), torch.tensor([5, 7], device=DEV)
+    u8 = torch.uint8
+    for bad in (torch.zeros(L.LOGPROBS_WORKSPACE_BYTES, dtype=u8),
+                torch.zeros(1, dtype=u8, device=DEV).expand(L.KV4_WORKSPACE_BYTES),
+                torch.zeros(2 * L.LOGPROBS_WORKSPACE_BYTES, dtype=u8, device=DEV)[::2]):
+        with pytest.raises(ValueError, match="workspace"):
+            L.kv4_attention(q, buffers, *args, workspace=bad)
+        with pytest.raises(ValueError, match="workspace"):
+            L.token_logprobs(x, t, 3, workspace=bad)
+
+
 # ------------------------------------------------------------------ together
 
 def test_step_of_appended_tokens():
