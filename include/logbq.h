@@ -465,10 +465,11 @@ int32_t logbq_batch_tables(const int32_t* cached_dev, const int32_t* new_dev, in
  *   k_dev, v_dev : device, row t of head h at element t * stride + h * dim; 16-byte aligned, and
  *                  so is every row (stride in elements, at least heads * dim).
  *   dtype        : logbq_dtype of both.
+ *   tokens       : fewer than 2^28 - 16.
  *   cache        : host, the buffers; codes and scales of the slots are written.
  *   slots_dev    : device, [tokens] int64. A token whose slot is negative or past the cache is
  *                  left out. Two tokens with one slot: either may be kept.
- * Errors: INVALID_ARG, UNSUPPORTED (dim, page, dtype, alignment, stride), HIP.
+ * Errors: INVALID_ARG, UNSUPPORTED (dim, page, dtype, tokens, alignment, stride), HIP.
  */
 int32_t logbq_kv4_append(const void* k_dev, int64_t k_stride, const void* v_dev, int64_t v_stride,
                          int32_t dtype, int64_t tokens, const logbq_kv4* cache,
@@ -477,6 +478,7 @@ int32_t logbq_kv4_append(const void* k_dev, int64_t k_stride, const void* v_dev,
 /*
  * logbq_kv4_read -- the values that the cache holds in given slots, e.g. to export a prefix.
  *   slots_dev    : device, [tokens] int64; a slot that is negative or past the cache gives zeros.
+ *   tokens       : fewer than 2^28 - 16.
  *   k_dev, v_dev : device, [tokens][heads][dim], written; 16-byte aligned.
  *   dtype        : logbq_dtype of both. Exact in float32, and in float16 within its range;
  *                  rounded to nearest in bfloat16.
@@ -539,6 +541,7 @@ int32_t logbq_kv4_attention(const void* q_dev, int64_t q_stride, int32_t q_dtype
  * `tokens` rows of logits.
  *   logits_dev : device, row t at element t * stride, vocab elements; aligned to its type.
  *   dtype      : logbq_dtype.
+ *   tokens     : fewer than 2^24.
  *   targets_dev : device, [tokens] int64; a target outside 0 .. vocab - 1 asks for nothing and
  *                 gives log probability 0.
  *   top        : 0 .. LOGBQ_LOGPROBS_MAX_TOP, at most vocab.
@@ -555,7 +558,7 @@ int32_t logbq_kv4_attention(const void* q_dev, int64_t q_stride, int32_t q_dtype
  * ranks above every number.
  * Sums are float32.
  * Errors: INVALID_ARG (null pointer, negative size, top > vocab), UNSUPPORTED (dtype, alignment,
- * vocab >= 2^31, top, stride, a workspace that is too small), HIP.
+ * tokens, vocab >= 2^31, top, stride, a workspace that is too small), HIP.
  */
 int32_t logbq_token_logprobs(const void* logits_dev, int32_t dtype, int64_t tokens, int64_t vocab,
                              int64_t stride, const int64_t* targets_dev, int32_t top,

@@ -698,12 +698,14 @@ __global__ __launch_bounds__(kLpThreads) void k_token_logprobs(LpArgs a) {
 }
 
 // ------------------------------------------------------------------ host side
-// Workgroups for the rows of `tokens` (fewer than 2^31) tokens.
+// Workgroups for the rows of `tokens` (fewer than kMaxTokens) tokens.
 dim3 row_grid(int64_t tokens, int32_t heads) {
   return dim3((unsigned)((tokens + kRowThreads / kRowLanes - 1) / (kRowThreads / kRowLanes)), (unsigned)heads);
 }
 
-constexpr int64_t kMaxTokens = (int64_t)1 << 31;
+// A launch has fewer than 2^32 threads a dimension.
+constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - 1;
+constexpr int64_t kMaxTokens = ((int64_t)1 << 32) / kRowLanes - kRowThreads / kRowLanes;
 
 }  // namespace
 
@@ -816,12 +818,12 @@ int32_t logbq_token_logprobs(const void* logits_dev, int32_t dtype, int64_t toke
   splits = splits > kLpMaxSplits ? kLpMaxSplits : splits;
   splits = splits > most ? most : splits;
   a.splits = splits < 1 ? 1 : (int32_t)splits;
-  if (tokens * a.splits > INT32_MAX) return LOGBQ_ERR_UNSUPPORTED;
+  const int threads = tokens * a.splits < kLpManyRows ? 512 : 256;
+  if (tokens * a.splits * threads > kMaxThreads) return LOGBQ_ERR_UNSUPPORTED;
 #define LOGPROBS(DT, THREADS)                                                                     \
   if (dtype == DT && threads == THREADS)                                                          \
     hipLaunchKernelGGL((k_token_logprobs<DT, THREADS>), dim3((unsigned)(tokens * a.splits)),      \
                        dim3(THREADS), 0, (hipStream_t)stream, a)
-  const int threads = tokens * a.splits < kLpManyRows ? 512 : 256;
   LOGPROBS(LOGBQ_DTYPE_F32, 256); LOGPROBS(LOGBQ_DTYPE_F16, 256); LOGPROBS(LOGBQ_DTYPE_BF16, 256);
   LOGPROBS(LOGBQ_DTYPE_F32, 512); LOGPROBS(LOGBQ_DTYPE_F16, 512); LOGPROBS(LOGBQ_DTYPE_BF16, 512);
 #undef LOGPROBS

@@ -118,6 +118,15 @@ def test_logprobs_refusals(change, status):
     assert L.lib().logbq_token_logprobs(*f.values(), None) == status
 
 
+def test_more_rows_than_a_launch_holds_are_refused():
+    h, c = L.lib(), cache()
+    most = (1 << 28) - 16
+    assert h.logbq_kv4_append(A, 256, A, 256, 1, most, c, A, None) == NO
+    assert h.logbq_kv4_read(c, A, most, A, A, 1, None) == NO
+    assert h.logbq_token_logprobs(A, 0, 1 << 24, 10, 10, A, 0, A, A, None, None, A,
+                                  L.LOGPROBS_WORKSPACE_BYTES, None) == NO
+
+
 def test_binding_refuses_host_tensors_and_wrong_shapes():
     i32 = torch.zeros(3, dtype=torch.int32)
     with pytest.raises(ValueError):
