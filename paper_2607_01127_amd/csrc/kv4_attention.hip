@@ -101,7 +101,7 @@ __device__ __forceinline__ Request request_of(const AttnArgs& a, int r) {
 // Bound by HBM latency and bandwidth: codes come from pages in any order, which a plain read of
 // 4 KiB chunks in random order takes 150 us for 813 MB (in order: 140). Measured, 8 heads x 4
 // queries x 128 channels, float16: 128 requests of 3000 to 9000 positions (813 MB) 164 us, 5.0 TB/s;
-// one of 131071 (138 MB) 40 us; 32 of 300 to 4100 (74 MB) 35 us, of which about 9 us pass before the
+// one of 131071 (138 MB) 40 us; 32 of 300 to 4100 (74 MB) 34 us, of which about 9 us pass before the
 // first codes are used and 5 in the join.
 constexpr int kDecThreads = 256;
 constexpr int kDecWaves = kDecThreads / 64;
@@ -717,7 +717,7 @@ __global__ __launch_bounds__(kDecThreads) void k_kv4_join(AttnArgs a, int kRows)
 //
 // Bound by instruction issue: about 500 vector instructions and 24 MFMAs a wavefront's tile, issue
 // slots 86 % busy. Measured, 8 heads x 4 queries x 128 channels, float16: a prompt of 6001 tokens
-// (295 GFLOP) 464 us, 636 TFLOP/s, or 954 with the second bfloat16 number's products. Weights in one
+// (295 GFLOP) 450 us, 656 TFLOP/s, or 984 with the second bfloat16 number's products. Weights in one
 // float16 took 415 us, but lost what lies 2^-22 below a row's largest.
 constexpr int kPromptThreads = 256;
 constexpr int kPromptTile = 64;
