@@ -470,7 +470,7 @@ __device__ __forceinline__ void join_lanes(LpSums& p) {
 }
 
 // Accesses to what other workgroups of the launch wrote or will read: coherent over the chip's
-// L2 caches one by one, so that no cache has to be written back as a whole.
+// L2 caches, one by one.
 template <typename T>
 __device__ __forceinline__ T load_shared(const T* p) {
   return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -564,7 +564,8 @@ __global__ __launch_bounds__(kLpThreads) void k_token_logprobs(LpArgs a) {
     const bool first = from == v0;
     if ((steps & (steps - 1)) == 0) {
       // -kLargest is also the maximum of none.
-      maxima[wave][lane] = logit_key(sums.m > -kLargest ? sums.m : -INFINITY);
+      __hip_atomic_store(&maxima[wave][lane], logit_key(sums.m > -kLargest ? sums.m : -INFINITY),
+                         __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
       if (first) __syncthreads();
       if ((31 - __builtin_clz(steps)) % kLpWaves == wave) {
         uint32_t key[kLpWaves];
@@ -634,17 +635,21 @@ __global__ __launch_bounds__(kLpThreads) void k_token_logprobs(LpArgs a) {
 
   if (a.splits > 1) {
     LpPart* parts = a.parts + row * a.splits;
-    // All stores have arrived before the part counts itself.
     if (lane == 0) {
       store_shared(&parts[part].m, sums.m);
       store_shared(&parts[part].s, sums.s);
       store_shared(&parts[part].t, sums.t);
     }
     if (lane < a.top) store_shared(&parts[part].keys[lane], lane < best.held ? best.keys[lane] : (uint64_t)0);
-    __builtin_amdgcn_s_waitcnt(0);
+    // Every lane's stores are released before the part counts itself, and the workgroup that counts
+    // last acquires those of all parts.
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
+    __builtin_amdgcn_wave_barrier();
     uint32_t before = 0;
     if (lane == 0) before = __hip_atomic_fetch_add(a.arrived + row, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (__builtin_amdgcn_readfirstlane(before) != (uint32_t)a.splits - 1) return;
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
     // All parts are there: a lane takes the sums of one (a.splits <= 64), and every 64th key.
     constexpr int kMost = kLpMaxSplits * kLpTop / 64;
     uint64_t k[kMost], first = 0;
