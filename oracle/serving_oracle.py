@@ -155,19 +155,20 @@ def token_logprobs(x, targets, top):
     for r in range(rows):
         row = x[r]
         bad = np.isnan(row).any() or np.isposinf(row).any() or np.isneginf(row).all()
+        # Differences from the maximum, as m + log s would round log s away where m is huge.
         if bad:
-            lse = ent[r] = np.nan
+            d, log_s, ent[r] = np.full(vocab, np.nan), np.nan, np.nan
         else:
-            m = row.max()
-            e = np.exp(row - m)
-            lse = m + math.log(e.sum())
+            d = row - row.max()
+            e = np.exp(d)
+            log_s = math.log(e.sum())
             keep = e > 0
-            ent[r] = lse - (e[keep] * row[keep]).sum() / e.sum()
+            ent[r] = log_s - (e[keep] * d[keep]).sum() / e.sum()
         t = int(targets[r])
         with np.errstate(invalid="ignore"):
-            lp[r] = row[t] - lse if 0 <= t < vocab else 0.0
+            lp[r] = d[t] - log_s if 0 <= t < vocab else 0.0
             # NaN first, then larger values, equal ones by index.
             order = np.lexsort((np.arange(vocab), np.where(np.isnan(row), 0.0, -row), ~np.isnan(row)))
             index[r] = order[:top]
-            best[r] = row[order[:top]] - lse
+            best[r] = d[order[:top]] - log_s
     return lp, ent, index, best

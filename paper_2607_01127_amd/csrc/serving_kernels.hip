@@ -410,40 +410,29 @@ __device__ __forceinline__ void vector_values(const u32x4& v, float* x) {
 
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
-constexpr float kLn2Low = -1.90465429e-9f;             // ln 2 - float(ln 2)
 constexpr float kLargest = 3.4028235e38f;
-// Up to here m log2 e is a float32 number, and u is one fma about it; past it the difference comes
-// first.
-constexpr float kFmaMost = 1e38f;
 
-// Adds terms whose largest is at most m. 2^-1000 is 0 in float32, so the lower limit on u only keeps
-// 0 times -inf out of t; it is taken where a logit of -inf has shown itself there. A NaN or a
-// difference of infinities reaches s.
+// Adds terms whose largest is at most m. The difference comes before the product with log2 e, so the
+// maximum's own term is exactly 1 and an offset common to all logits changes nothing; one fma of x
+// about the rounded m log2 e would leave that product's rounding in every term, which from 1e9 on is
+// more than any sum holds. 2^-1000 is 0 in float32, so the lower limit on u only keeps 0 times -inf
+// out of t; it is taken where a logit of -inf (or one that far below m) has shown itself there. A NaN
+// or a difference of infinities reaches s.
 template <int N>
 __device__ __forceinline__ void add_terms(const float (&x)[N], LpSums& p) {
   float s = 0.0f, t = 0.0f;
-  if (__builtin_fabsf(p.m) < kFmaMost) {
-    const float mc = p.m * kLog2e;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float u = (x[i] - p.m) * kLog2e, e = __builtin_amdgcn_exp2f(u);
+    s += e;
+    t = __builtin_fmaf(e, u, t);
+  }
+  if (t != t) {
+    t = 0.0f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float u = __builtin_fmaf(x[i], kLog2e, -mc), e = __builtin_amdgcn_exp2f(u);
-      s += e;
-      t = __builtin_fmaf(e, u, t);
-    }
-    if (t != t) {
-      t = 0.0f;
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float u = __builtin_fmaf(x[i], kLog2e, -mc);
-        t += __builtin_amdgcn_exp2f(u) * fmaxf(u, -1000.0f);
-      }
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float u = (x[i] - p.m) * kLog2e, e = __builtin_amdgcn_exp2f(u);
-      s += e;
-      t += e * fmaxf(u, -1000.0f);
+      const float u = (x[i] - p.m) * kLog2e;
+      t = __builtin_fmaf(__builtin_amdgcn_exp2f(u), fmaxf(u, -1000.0f), t);
     }
   }
   p.s += s;
@@ -451,9 +440,7 @@ __device__ __forceinline__ void add_terms(const float (&x)[N], LpSums& p) {
 }
 // Sums about m, about `to` >= m.
 __device__ __forceinline__ void move_sums(LpSums& p, float to) {
-  const float u = __builtin_fabsf(to) < kFmaMost && __builtin_fabsf(p.m) < kFmaMost
-                      ? p.m * kLog2e - to * kLog2e : (p.m - to) * kLog2e;
-  const float f = __builtin_amdgcn_exp2f(u);
+  const float u = (p.m - to) * kLog2e, f = __builtin_amdgcn_exp2f(u);
   p.t = f * (p.t + p.s * fmaxf(u, -1000.0f));
   p.s *= f;
   p.m = to;
@@ -681,15 +668,9 @@ __global__ __launch_bounds__(kLpThreads) void k_token_logprobs(LpArgs a) {
     if (lane == 0) store_shared(a.arrived + row, 0u);
   }
 
-  // x - L for a logit x, with L = m + ln s: the sums are about m log2 e as rounded, and its product
-  // with ln 2 is taken to twice the precision.
+  // x - L for a logit x, with L = m + ln s.
   const float log2_s = __log2f(sums.s);
-  const bool by_fma = __builtin_fabsf(sums.m) < kFmaMost;
-  const float mc = sums.m * kLog2e;
-  const auto log_probability = [&](float x) {
-    return by_fma ? __builtin_fmaf(-mc, kLn2, x) - __builtin_fmaf(mc, kLn2Low, kLn2 * log2_s)
-                  : x - sums.m - kLn2 * log2_s;
-  };
+  const auto log_probability = [&](float x) { return (x - sums.m) - kLn2 * log2_s; };
   if (tid == 0) {
     const int64_t target = a.targets[row];
     a.logprob[row] = target >= 0 && target < a.vocab ? log_probability(load_element<DT>(base, target)) : 0.0f;

@@ -41,7 +41,7 @@ def check(x, targets, top):
                             ("entropy", ent, eps * (2 + ent))):
         have = host(got[name])
         assert np.isfinite(have).all(), (name, have)
-        assert float(np.max(np.abs(have - want) - tol)) <= 0.0, (name, have, want)
+        assert float(np.max(np.abs(have - want) - tol, initial=-1.0)) <= 0.0, (name, have, want)
     assert np.array_equal(got["top_index"].cpu().numpy(), index)
     return got
 
