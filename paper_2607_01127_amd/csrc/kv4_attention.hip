@@ -914,9 +914,10 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
   };
   int ek = -200;                        // exponent that the keys' scales are divided by
   const auto convert = [&](const Raw& t, int buf) {
-    // The exponent first; every wavefront sees all 64 scales, so all come to the same one.
+    // The exponent first; every wavefront sees all 64 scales, so all come to the same one. Positions
+    // that no row sees have no part in it.
     const bool seen = (t.valid >> lane) & 1;
-    const int xk = seen ? (int)(t.lane_ks >> 7) - 127 : -127;
+    const int xk = seen ? (int)(t.lane_ks >> 7) - 127 : -1000;
     if (__builtin_amdgcn_ballot_w64(xk - ek > 12)) {
       int mk = xk;
       for (int d = 1; d < 64; d <<= 1) mk = max(mk, __shfl_xor(mk, d));
@@ -984,7 +985,7 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
 
   // ---- a tile's products and softmax
   const auto compute = [&](int base, uint64_t valid, int ek_of, int buf) {
-    if (!has_rows || base > place_hi ||
+    if (!has_rows || valid == 0 || base > place_hi ||
         (a.window && base + kPromptTile - 1 <= (int64_t)place_lo - a.window))
       return;
     const bool full = base + kPromptTile - 1 <= place_lo && valid == ~0ull &&
@@ -1031,7 +1032,9 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
           float top = s[nb][0];
 #pragma unroll
           for (int i = 1; i < 16; ++i) top = fmaxf(top, s[nb][i]);
-          const float reach = top * f;
+          // A row that sees none of the tile keeps its reference: kNone is no score, and a tile's
+          // factor could bring it above those of later tiles.
+          const float reach = !kAll && top == kNone ? kNone : top * f;
           if (__builtin_amdgcn_ballot_w64(reach - ref[nb] > 8.0f)) {
             const float most = fmaxf(reach, __shfl_xor(reach, 32));
             const float next = most - ref[nb] > 8.0f ? most : ref[nb];
