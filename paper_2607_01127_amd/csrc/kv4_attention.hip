@@ -990,7 +990,6 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
       return;
     const bool full = base + kPromptTile - 1 <= place_lo && valid == ~0ull &&
                       (!a.window || base > (int64_t)place_hi - a.window);
-    const float up = exp2_fast((float)ek_of);
 #pragma unroll
     for (int pb = 0; pb < 2; ++pb) {
       float16v s[NB];
@@ -1016,7 +1015,8 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
       const uint32_t bits = (uint32_t)(valid >> (32 * pb)) >> (4 * half);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        const float f = qs[nb] * up;
+        // By ldexp, as 2^ek alone may be below float32's normal numbers.
+        const float f = ldexpf(qs[nb], ek_of);
         const auto weigh = [&](auto all_seen) {
           constexpr bool kAll = decltype(all_seen)::value;
           bool seen[16];

@@ -54,3 +54,16 @@ def test_zero_keys_outside_the_window(dim):
         q = dev(qv * (1 + 0.01 * rng.standard_normal((290, 1, dim))), torch.float32)
         for dtype in ("f16", "bf16", "f32"):
             attend(q.to(TYPES[dtype]), cache, [[0, 1, 2, 3, 4]], [290], [290], page, scale=scale, window=16)
+
+
+def test_tiny_keys_and_large_queries():
+    """Keys whose scales are below 2^-117: a tile's factor has to stay a number other than 0."""
+    print("tiny keys", flush=True)
+    rng = np.random.default_rng(5)
+    for dim in (64, 128, 256):
+        k = rng.standard_normal((4, 1, 64, dim)) * 2.0 ** -122
+        cache = cache_of(k, rng.standard_normal(k.shape))
+        q = dev(rng.standard_normal((200, 2, dim)) * 2.0 ** 122, torch.float32)
+        for dtype in ("bf16", "f32"):
+            for new in ([200], [1]):
+                attend(q[:new[0]].to(TYPES[dtype]), cache, [[2, 0, 3, 1]], [240], new, 64)
