@@ -41,6 +41,17 @@ constexpr float kLn2 = 0.69314718055994530942f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// The exponent of a score x f about a reference. The reference is such a product, rounded; with this one
+// rounded too the largest gives 0 whatever its size. One fma in their place leaves the reference's own
+// rounding in the exponent: half an ulp of the score, which from 2^31 on is more than float32's range.
+template <bool ROUNDED = true>
+__device__ __forceinline__ float exponent(float x, float f, float ref) {
+#pragma clang fp contract(off)
+  if (!ROUNDED) return __builtin_fmaf(x, f, -ref);
+  const float y = x * f;
+  return y - ref;
+}
+
 // The same number, but one that the compiler cannot compute ahead of a loop: what is derived from it
 // takes no registers across the loop. (A spilled value is worse than a recomputed one: its load
 // comes back only after all the loads of codes before it.)
@@ -524,7 +535,7 @@ void k_kv4_decode(AttnArgs a) {
           float w[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            float e = exp2_fast(__builtin_fmaf(x[j], qs[nt], -ref[nt]));
+            float e = exp2_fast(exponent(x[j], qs[nt], ref[nt]));
             if constexpr (!kAll) e = seen[j] ? e : 0.0f;
             sum[nt] += e;
             w[j] = e * (kAll || seen[j] ? scale_at(vs, j) : 0.0f);
@@ -715,12 +726,18 @@ __global__ __launch_bounds__(kDecThreads) void k_kv4_join(AttnArgs a, int kRows)
 // goes back into the scores' factor. The values' scales multiply the weights, which go into the
 // second product as two bfloat16 numbers, for the reason given above.
 //
+// An exponent is one fma, of which a wavefront's tile has 32. Where a reference has passed kFar, up to which
+// the reference's rounding is 2^-4 at most, the workgroup goes over its positions again with rounded
+// products. (Rounded ones throughout are 32 instructions more a tile; both ways in one loop, behind a
+// branch, cost every prompt 2 %, a second loop nothing.)
+//
 // Bound by instruction issue: about 500 vector instructions and 24 MFMAs a wavefront's tile, issue
 // slots 86 % busy. Measured, 8 heads x 4 queries x 128 channels, float16: a prompt of 6001 tokens
 // (295 GFLOP) 450 us, 656 TFLOP/s, or 984 with the second bfloat16 number's products. Weights in one
 // float16 took 415 us, but lost what lies 2^-22 below a row's largest.
 constexpr int kPromptThreads = 256;
 constexpr int kPromptTile = 64;
+constexpr float kFar = 1048576.0f;
 constexpr int kPromptMinRows = 17;           // fewer go through the decode kernel, if it is launched
 
 // Offset of a slot of a value fragment: the lanes of a converting wavefront differ in the chunk of
@@ -844,13 +861,7 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
         qf[nb][c][j] = (half_t)y;
         if constexpr (QSPLIT) ql[nb][c][j] = (half_t)(y - (float)(half_t)y);
       }
-    ref[nb] = kNone;
-    sum[nb] = 0.0f;
     last[nb] = row < rows ? req.first + token : INT32_MAX;
-#pragma unroll
-    for (int c = 0; c < kCb; ++c)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o[nb][c][i] = 0.0f;
   }
 
   // ---- loading and converting a tile. A thread has 32 channels of one position's keys (D = 256:
@@ -984,7 +995,9 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
   };
 
   // ---- a tile's products and softmax
-  const auto compute = [&](int base, uint64_t valid, int ek_of, int buf) {
+  bool far = false;                     // a reference of the wavefront has passed kFar
+  const auto compute = [&](int base, uint64_t valid, int ek_of, int buf, auto rounded) {
+    constexpr bool kRounded = decltype(rounded)::value;
     if (!has_rows || valid == 0 || base > place_hi ||
         (a.window && base + kPromptTile - 1 <= (int64_t)place_lo - a.window))
       return;
@@ -1026,19 +1039,20 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
               const int at = 8 * (i >> 2) + (i & 3), pos = base + 32 * pb + 4 * half + at;
               seen[i] = ((bits >> at) & 1u) && pos <= last[nb] &&
                         (!a.window || last[nb] == INT32_MAX || pos > (int64_t)last[nb] - a.window);
-              s[nb][i] = seen[i] ? s[nb][i] : kNone;
+              s[nb][i] = seen[i] ? s[nb][i] : -INFINITY;
             }
           }
           float top = s[nb][0];
 #pragma unroll
           for (int i = 1; i < 16; ++i) top = fmaxf(top, s[nb][i]);
-          // A row that sees none of the tile keeps its reference: kNone is no score, and a tile's
-          // factor could bring it above those of later tiles.
-          const float reach = !kAll && top == kNone ? kNone : top * f;
+          // A row that sees none of the tile keeps its reference.
+          const float reach = !kAll && top == -INFINITY ? kNone : top * f;
           if (__builtin_amdgcn_ballot_w64(reach - ref[nb] > 8.0f)) {
             const float most = fmaxf(reach, __shfl_xor(reach, 32));
             const float next = most - ref[nb] > 8.0f ? most : ref[nb];
             const float g = exp2_fast(ref[nb] - next);
+            if constexpr (!kRounded)
+              far |= __builtin_amdgcn_ballot_w64(next != kNone && __builtin_fabsf(next) > kFar) != 0;
             ref[nb] = next;
             sum[nb] *= g;
 #pragma unroll
@@ -1050,7 +1064,7 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
               const int i = 8 * h + j;
-              float e = exp2_fast(__builtin_fmaf(s[nb][i], f, -ref[nb]));
+              float e = exp2_fast(exponent<kRounded>(s[nb][i], f, ref[nb]));
               if constexpr (!kAll) e = seen[i] ? e : 0.0f;
               sum[nb] += e;
               w[j] = e * vs[i >> 2][i & 3];
@@ -1079,7 +1093,17 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
     }
   };
 
-  if (tile0 < tile1) {
+  const auto go_over = [&](auto rounded) {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      ref[nb] = kNone;
+      sum[nb] = 0.0f;
+#pragma unroll
+      for (int c = 0; c < kCb; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[nb][c][i] = 0.0f;
+    }
+    if (tile0 >= tile1) return;
     const int stop = kv_from + tile1 * kPromptTile;
     int base = kv_from + tile0 * kPromptTile;
     Raw raw = load_raw(base, load_ids(base));
@@ -1094,7 +1118,7 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
         raw = load_raw(base + kPromptTile, ids);
         ids = load_ids(base + 2 * kPromptTile);
       }
-      compute(base, valid, ek_of, buf);
+      compute(base, valid, ek_of, buf, rounded);
       if (more) {
         convert(raw, buf ^ 1);
         valid = raw.valid;
@@ -1103,7 +1127,9 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
       buf ^= 1;
       __syncthreads();
     }
-  }
+  };
+  go_over(std::false_type{});
+  if (__syncthreads_or(far)) go_over(std::true_type{});
 
   // ---- out: a lane has 4 consecutive channels of its row at a time
   if (!has_rows) return;
