@@ -722,14 +722,16 @@ __global__ __launch_bounds__(kDecThreads) void k_kv4_join(AttnArgs a, int kRows)
 // tile's codes are loaded before this one's products and converted after them, one barrier a tile.
 //
 // Converted keys carry their rows' scales (a code has at most 2 significant bits and a scale 8, so
-// the product is exact in float16) divided by a power of two that keeps the largest below 2^13; it
-// goes back into the scores' factor. The values' scales multiply the weights, which go into the
-// second product as two bfloat16 numbers, for the reason given above.
+// the product is exact in float16) divided by a power of two that brings all of the tile's into
+// [2^-13, 2^13); it goes back into the scores' factor. The values' scales multiply the weights, which
+// go into the second product as two bfloat16 numbers, for the reason given above. An exponent is one
+// fma, of which a wavefront's tile has 32.
 //
-// An exponent is one fma, of which a wavefront's tile has 32. Where a reference has passed kFar, up to which
-// the reference's rounding is 2^-4 at most, the workgroup goes over its positions again with rounded
-// products. (Rounded ones throughout are 32 instructions more a tile; both ways in one loop, behind a
-// branch, cost every prompt 2 %, a second loop nothing.)
+// Two things do not go this way, and a workgroup that meets one goes over its positions again with care:
+// a tile whose keys' scales span more than 26 binades (a few keys far larger than the rest, a scale that
+// is no number), of which the positions with the largest are taken first and the tile comes again for the
+// others; and a reference past kFar, up to which its rounding is 2^-4 at most, about which the product is
+// rounded too. (Both in the one loop cost every prompt 2 to 7 %, a second loop nothing.)
 //
 // Bound by instruction issue: about 500 vector instructions and 24 MFMAs a wavefront's tile, issue
 // slots 86 % busy. Measured, 8 heads x 4 queries x 128 channels, float16: a prompt of 6001 tokens
@@ -753,6 +755,7 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
   __shared__ half8v kbuf[2][2 * kKc * 64];
   __shared__ bf16x8 vbuf[2][kCb * 4 * 64];
   __shared__ float vscale[2][kPromptTile];
+  __shared__ uint64_t rest_of[2];
   __shared__ int64_t scan[4];
   __shared__ int64_t found[2];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -924,16 +927,31 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
     return t;
   };
   int ek = -200;                        // exponent that the keys' scales are divided by
-  const auto convert = [&](const Raw& t, int buf) {
+  bool again = false;                   // the wavefront has met what is to be taken with care
+  // With care, returns the positions that are left for another time; rest_of has the same, from one
+  // wavefront, for the number of times that all go round, which no change of the cache meanwhile may
+  // set apart.
+  const auto convert = [&](const Raw& t, int buf, auto careful) {
+    constexpr bool kCareful = decltype(careful)::value;
     // The exponent first; every wavefront sees all 64 scales, so all come to the same one. Positions
-    // that no row sees have no part in it.
+    // that no row sees, and scales of 0, have no part in it.
     const bool seen = (t.valid >> lane) & 1;
-    const int xk = seen ? (int)(t.lane_ks >> 7) - 127 : -1000;
-    if (__builtin_amdgcn_ballot_w64(xk - ek > 12)) {
-      int mk = xk;
-      for (int d = 1; d < 64; d <<= 1) mk = max(mk, __shfl_xor(mk, d));
-      ek = mk - 10;
+    const bool counts = seen && (t.lane_ks & 0x7fff);
+    const int xk = (int)(t.lane_ks >> 7 & 0xff) - 127;
+    uint64_t rest = 0;
+    if (__builtin_amdgcn_ballot_w64(counts && (unsigned)(xk - ek + 13) > 25u)) {
+      int most = counts ? xk : -1000, least = counts ? xk : 1000;
+      for (int d = 1; d < 64; d <<= 1) {
+        most = max(most, __shfl_xor(most, d));
+        least = min(least, __shfl_xor(least, d));
+      }
+      if constexpr (!kCareful) again |= __builtin_amdgcn_readfirstlane(most - least) > 25;
+      least = max(least, most - 25);
+      if constexpr (kCareful) rest = __builtin_amdgcn_ballot_w64(counts && xk < least);
+      ek = __builtin_amdgcn_readfirstlane((most + least + 1) >> 1);
     }
+    if constexpr (kCareful)
+      if (tid == 0) rest_of[buf] = rest;
     if (wave == 0) vscale[buf][lane] = seen ? bf16_value(t.lane_vs) : 0.0f;
     if (has_keys) {
       const half_t s = (half_t)(t.key_ok ? ldexpf(bf16_value(t.ks), -ek) : 0.0f);
@@ -992,12 +1010,12 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
         }
       }
     }
+    return rest;
   };
 
   // ---- a tile's products and softmax
-  bool far = false;                     // a reference of the wavefront has passed kFar
-  const auto compute = [&](int base, uint64_t valid, int ek_of, int buf, auto rounded) {
-    constexpr bool kRounded = decltype(rounded)::value;
+  const auto compute = [&](int base, uint64_t valid, int ek_of, int buf, auto careful) {
+    constexpr bool kCareful = decltype(careful)::value;
     if (!has_rows || valid == 0 || base > place_hi ||
         (a.window && base + kPromptTile - 1 <= (int64_t)place_lo - a.window))
       return;
@@ -1051,8 +1069,8 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
             const float most = fmaxf(reach, __shfl_xor(reach, 32));
             const float next = most - ref[nb] > 8.0f ? most : ref[nb];
             const float g = exp2_fast(ref[nb] - next);
-            if constexpr (!kRounded)
-              far |= __builtin_amdgcn_ballot_w64(next != kNone && __builtin_fabsf(next) > kFar) != 0;
+            if constexpr (!kCareful)
+              again |= __builtin_amdgcn_ballot_w64(next != kNone && __builtin_fabsf(next) > kFar) != 0;
             ref[nb] = next;
             sum[nb] *= g;
 #pragma unroll
@@ -1064,7 +1082,7 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
               const int i = 8 * h + j;
-              float e = exp2_fast(exponent<kRounded>(s[nb][i], f, ref[nb]));
+              float e = exp2_fast(exponent<kCareful>(s[nb][i], f, ref[nb]));
               if constexpr (!kAll) e = seen[i] ? e : 0.0f;
               sum[nb] += e;
               w[j] = e * vs[i >> 2][i & 3];
@@ -1093,7 +1111,8 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
     }
   };
 
-  const auto go_over = [&](auto rounded) {
+  const auto go_over = [&](auto careful) {
+    constexpr bool kCareful = decltype(careful)::value;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       ref[nb] = kNone;
@@ -1108,28 +1127,38 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
     int base = kv_from + tile0 * kPromptTile;
     Raw raw = load_raw(base, load_ids(base));
     Ids ids = load_ids(base + kPromptTile);
-    convert(raw, 0);
-    uint64_t valid = raw.valid;
+    uint64_t valid = raw.valid & ~convert(raw, 0, careful);
     int buf = 0, ek_of = ek;
     __syncthreads();
-    for (; base < stop; base += kPromptTile) {
-      const bool more = base + kPromptTile < stop;
-      if (more) {
-        raw = load_raw(base + kPromptTile, ids);
-        ids = load_ids(base + 2 * kPromptTile);
+    while (base < stop) {
+      int next = base + kPromptTile;
+      if (next < stop) {
+        raw = load_raw(next, ids);
+        ids = load_ids(next + kPromptTile);
       }
-      compute(base, valid, ek_of, buf, rounded);
-      if (more) {
-        convert(raw, buf ^ 1);
-        valid = raw.valid;
+      compute(base, valid, ek_of, buf, careful);
+      if constexpr (kCareful) {
+        const uint64_t held = rest_of[buf];
+        const uint64_t rest = (uint64_t)__builtin_amdgcn_readfirstlane((int)(held >> 32)) << 32 |
+                              (uint32_t)__builtin_amdgcn_readfirstlane((int)held);
+        if (rest) {                     // the tile again, for these
+          next = base;
+          raw = load_raw(base, load_ids(base));
+          raw.valid = rest;
+          ids = load_ids(base + kPromptTile);
+        }
+      }
+      if (next < stop) {
+        valid = raw.valid & ~convert(raw, buf ^ 1, careful);
         ek_of = ek;
       }
+      base = next;
       buf ^= 1;
       __syncthreads();
     }
   };
   go_over(std::false_type{});
-  if (__syncthreads_or(far)) go_over(std::true_type{});
+  if (__syncthreads_or(again)) go_over(std::true_type{});
 
   // ---- out: a lane has 4 consecutive channels of its row at a time
   if (!has_rows) return;
