@@ -1085,7 +1085,7 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
               float e = exp2_fast(exponent<kCareful>(s[nb][i], f, ref[nb]));
               if constexpr (!kAll) e = seen[i] ? e : 0.0f;
               sum[nb] += e;
-              w[j] = e * vs[i >> 2][i & 3];
+              w[j] = kAll || seen[i] ? e * vs[i >> 2][i & 3] : 0.0f;
             }
             split_weights(w, hi[nb][h], lo[nb][h]);
           }
