@@ -505,7 +505,8 @@ int32_t logbq_kv4_read(const logbq_kv4* cache, const int64_t* slots_dev, int64_t
  *   seq_lens_dev : device, [requests] int32, cached tokens with this step's, which are already
  *                appended.
  *   q_starts_dev : device, [requests + 1] int32, first token of each request.
- *   max_new    : upper bound of a request's tokens (host). Tokens past it may be left out.
+ *   max_new    : upper bound of a request's tokens (host). Tokens of a request past it are left out:
+ *                nothing is written for them, and the others are as they would be beside them.
  *   scale      : factor on the products q . k.
  *   window     : a token sees itself and the window - 1 positions before it; 0: all.
  *   out_dev    : device, [tokens][q_heads][dim], written for the tokens that belong to a request.

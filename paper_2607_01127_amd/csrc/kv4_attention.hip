@@ -29,7 +29,7 @@ struct AttnArgs {
   int32_t* desc;          // [parts][4]: what the join has to sum
   Kv4 c;
   int64_t q_stride;
-  int32_t width, tokens, requests, group, window, q_dtype, out_dtype, parts;
+  int32_t width, tokens, requests, group, window, max_new, q_dtype, out_dtype, parts;
   int32_t unit;           // positions that the workgroups' shares are counted in
   float scale;
 };
@@ -62,7 +62,7 @@ __device__ __forceinline__ int here(int x) {
 
 // A request as the kernels see it.
 struct Request {
-  int32_t t0, n;          // first token, number of tokens
+  int32_t t0, n;          // first token, number of tokens (at most max_new)
   int32_t first;          // position of the first token
   int32_t from, end;      // positions that some token sees: [from, end), from a multiple of 32
 };
@@ -79,9 +79,9 @@ __device__ __forceinline__ Request request_of(const AttnArgs& a, int r) {
   const int32_t len = seq_lens[r] > 0 ? seq_lens[r] : 0;
   const int64_t span = a.c.slots > 0 ? (int64_t)a.width << a.c.page_shift : 0;
   q.t0 = t0;
-  q.n = t1 - t0;
-  q.first = len - q.n;
-  q.end = len < span ? len : (int32_t)span;
+  q.n = t1 - t0 < a.max_new ? t1 - t0 : a.max_new;
+  q.first = len - (t1 - t0);
+  q.end = q.first + q.n < span ? q.first + q.n : (int32_t)span;
   int64_t from = a.window ? (int64_t)q.first - a.window + 1 : 0;
   q.from = from > 0 ? (int32_t)from & ~31 : 0;
   return q;
@@ -1354,6 +1354,7 @@ int32_t logbq_kv4_attention(const void* q_dev, int64_t q_stride, int32_t q_dtype
   a.requests = (int32_t)requests;
   a.group = q_heads / c.heads;
   a.window = window;
+  a.max_new = max_new < INT32_MAX ? (int32_t)max_new : INT32_MAX;
   a.q_dtype = q_dtype;
   a.out_dtype = out_dtype;
   a.scale = scale;
