@@ -1254,15 +1254,18 @@ int32_t launch_decode(AttnArgs a, void* work, hipStream_t stream) {
   return launch_status();
 }
 
+// As many row tiles as the requests can have; each request has at least min_rows rows.
+int64_t prompt_tiles(const AttnArgs& a, int min_rows, int rows_of_tile) {
+  const int64_t rows = (int64_t)a.tokens * a.group;
+  const int64_t short_ones = rows / min_rows < a.requests ? rows / min_rows : a.requests;
+  return (rows / rows_of_tile + short_ones) * a.c.heads;
+}
+
 template <int D, int NB>
 int32_t launch_prompt(AttnArgs a, int min_rows, void* work, hipStream_t stream) {
   constexpr int kRows = 128 * NB;
-  // As many row tiles as the requests can have; each has at least min_rows rows.
-  const int64_t rows = (int64_t)a.tokens * a.group;
-  const int64_t short_ones = rows / min_rows < a.requests ? rows / min_rows : a.requests;
-  const int64_t tiles = (rows / kRows + short_ones) * a.c.heads;
+  const int64_t tiles = prompt_tiles(a, min_rows, kRows);
   if (tiles == 0) return LOGBQ_OK;
-  if (tiles > INT32_MAX) return LOGBQ_ERR_UNSUPPORTED;
   int64_t splits = kPromptGrid / tiles;
   // A split has four tiles at least where the block table is full.
   const int64_t most = ((int64_t)a.width << a.c.page_shift) / (4 * kPromptTile);
@@ -1304,10 +1307,14 @@ int32_t launch_attention(const AttnArgs& a, int64_t max_new, void* work, hipStre
   if (D < 256 && rows <= 32) return launch_decode<D, D < 256 ? 2 : 1, 1>(a, work, stream);
   if (D == 64 && rows <= 64) return launch_decode<D, D == 64 ? 4 : 1, 1>(a, work, stream);
   // A prompt among them: decode requests apart from the longer ones. One request is taken as a prompt.
-  if (a.requests == 1) return launch_prompt<D, kPromptBlocks>(a, 1, work, stream);
+  // A launch has fewer than 2^32 threads a dimension, which is seen to before anything is enqueued.
+  const int min_rows = a.requests == 1 ? 1 : kPromptMinRows;
+  if (prompt_tiles(a, min_rows, 128 * kPromptBlocks) > (((int64_t)1 << 32) - 1) / kPromptThreads)
+    return LOGBQ_ERR_UNSUPPORTED;
+  if (a.requests == 1) return launch_prompt<D, kPromptBlocks>(a, min_rows, work, stream);
   const int32_t status = launch_decode<D, 1, 1>(a, work, stream);
   if (status != LOGBQ_OK) return status;
-  return launch_prompt<D, kPromptBlocks>(a, kPromptMinRows, work, stream);
+  return launch_prompt<D, kPromptBlocks>(a, min_rows, work, stream);
 }
 
 }  // namespace
