@@ -467,8 +467,10 @@ int32_t logbq_batch_tables(const int32_t* cached_dev, const int32_t* new_dev, in
  *   dtype        : logbq_dtype of both.
  *   tokens       : fewer than 2^28 - 16.
  *   cache        : host, the buffers; codes and scales of the slots are written.
- *   slots_dev    : device, [tokens] int64. A token whose slot is negative or past the cache is
- *                  left out. Two tokens with one slot: either may be kept.
+ *   slots_dev    : device, [tokens] int64, distinct. A token whose slot is negative or past the
+ *                  cache is left out. What a slot holds that two tokens name is not specified: its
+ *                  codes and scales, of keys and values and of each head, are stored one by one and
+ *                  may be of either token. No other slot is touched.
  * Errors: INVALID_ARG, UNSUPPORTED (dim, page, dtype, tokens, alignment, stride), HIP.
  */
 int32_t logbq_kv4_append(const void* k_dev, int64_t k_stride, const void* v_dev, int64_t v_stride,

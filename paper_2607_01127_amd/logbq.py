@@ -564,8 +564,8 @@ def batch_tables(cached, new, free_pages, table, page: int, tokens: int, out=Non
 
 def kv4_append(k, v, cache, slots, stream=None):
     """logbq_kv4_append: keys and values [tokens][heads][dim] (float32, float16 or bfloat16; the
-    tokens may be strided) quantized into `slots` (int64 [tokens]; negative: left out) of a
-    Kv4Cache."""
+    tokens may be strided) quantized into `slots` (int64 [tokens]; negative: left out; what a slot
+    holds that two tokens name is not specified) of a Kv4Cache."""
     import torch
     c = _kv4_struct(cache)
     k_stride, v_stride = _rows(k, c.heads, c.dim, "k"), _rows(v, c.heads, c.dim, "v")
