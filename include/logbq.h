@@ -450,8 +450,9 @@ typedef struct logbq_kv4 {
  *                   needs more than `width` pages) and 4 (`tokens` is less than the sum of new).
  * A token without a page has slot -1, and a missing page's entry is -1. Lengths, positions and
  * sums saturate at 2^31 - 1.
- * A second call on the same input lengths gives the same results.
- * Errors: INVALID_ARG (null pointer, negative size), UNSUPPORTED (page, requests > 4096, width or
+ * A second call on the same input lengths gives the same results. No output may overlap an input
+ * (cached_dev, new_dev, free_dev).
+ * Errors: INVALID_ARG (null pointer, negative size, overlap), UNSUPPORTED (page, requests > 4096, width or
  * free_count or tokens above 2^31 - 1), HIP.
  */
 int32_t logbq_batch_tables(const int32_t* cached_dev, const int32_t* new_dev, int64_t requests,

@@ -689,6 +689,18 @@ dim3 row_grid(int64_t tokens, int32_t heads) {
   return dim3((unsigned)((tokens + kRowThreads / kRowLanes - 1) / (kRowThreads / kRowLanes)), (unsigned)heads);
 }
 
+// Whether a call would write what it reads: its workgroups have no order among them.
+struct Range { const void* at; int64_t bytes; };
+template <int N, int M>
+bool any_overlap(const Range (&in)[N], const Range (&out)[M]) {
+  for (const Range& i : in)
+    for (const Range& o : out)
+      if (i.bytes > 0 && o.bytes > 0 && (uintptr_t)i.at < (uintptr_t)o.at + o.bytes &&
+          (uintptr_t)o.at < (uintptr_t)i.at + i.bytes)
+        return true;
+  return false;
+}
+
 // A launch has fewer than 2^32 threads a dimension.
 constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - 1;
 constexpr int64_t kMaxTokens = ((int64_t)1 << 32) / kRowLanes - kRowThreads / kRowLanes;
@@ -711,6 +723,10 @@ int32_t logbq_batch_tables(const int32_t* cached_dev, const int32_t* new_dev, in
   if (requests > 0 && width > 0 && !table_dev) return LOGBQ_ERR_INVALID_ARG;
   if (free_count > 0 && !free_dev) return LOGBQ_ERR_INVALID_ARG;
   if (tokens > 0 && (!slots_dev || !positions_dev)) return LOGBQ_ERR_INVALID_ARG;
+  const Range in[] = {{cached_dev, 4 * requests}, {new_dev, 4 * requests}, {free_dev, 4 * free_count}};
+  const Range out[] = {{table_dev, 4 * requests * width}, {slots_dev, 8 * tokens}, {positions_dev, 4 * tokens},
+                       {q_starts_dev, 4 * (requests + 1)}, {seq_lens_dev, 4 * requests}, {info_dev, 16}};
+  if (any_overlap(in, out)) return LOGBQ_ERR_INVALID_ARG;
   TabArgs a = {cached_dev, new_dev, free_dev, table_dev, slots_dev, positions_dev, q_starts_dev,
                seq_lens_dev, info_dev, width, free_count, tokens, (int32_t)requests,
                __builtin_ctz((unsigned)page)};
