@@ -57,7 +57,8 @@ class Decoder:
         self.embedding = torch.randn((s.vocab, s.hidden), generator=g, device=device).half()
         self.head = (torch.randn((s.vocab, s.hidden), generator=g, device=device) * s.hidden ** -0.5).half()
         self.rotation = 10000.0 ** (-torch.arange(0, s.dim, 2, device=device).float() / s.dim)
-        self.free = torch.randperm(pages, generator=g, device=device).int()      # ids of free pages
+        self.free = torch.randperm(pages, generator=g, device=device).int()      # ids of pages
+        self.used = 0                      # the first of them, which its batches have taken
         self.kv_work = torch.empty(L.KV4_WORKSPACE_BYTES, dtype=torch.uint8, device=device)
         self.lp_work = torch.zeros(L.LOGPROBS_WORKSPACE_BYTES, dtype=torch.uint8, device=device)
 
@@ -89,12 +90,12 @@ class Decoder:
 
 
 class Batch:
-    """Requests that are served together. The host keeps their lengths, and the first free page."""
+    """Requests that are served together. The host keeps their lengths. Pages are taken from the decoder
+    for good, so that batches of one decoder may live side by side."""
 
     def __init__(self, decoder: Decoder, requests: int, most: int):
         self.decoder = decoder
         self.lengths = [0] * requests
-        self.used = 0                      # pages taken from the decoder's free list
         width = -(-most // decoder.page)
         self.table = torch.full((requests, width), -1, dtype=torch.int32, device=decoder.device)
 
@@ -107,11 +108,11 @@ class Batch:
         tokens = torch.tensor(sum(new_tokens, []), dtype=torch.int64).to(d.device)
         pages = sum(-(-(a + b) // page) - -(-a // page) for a, b in zip(self.lengths, new))
         total = [a + b for a, b in zip(self.lengths, new)]
-        if max(total) > self.table.shape[1] * page or self.used + pages > d.free.numel():
+        if max(total) > self.table.shape[1] * page or d.used + pages > d.free.numel():
             raise ValueError("the cache or the block table is too small for this step")
-        tables = L.batch_tables(ints[0], ints[1], d.free[self.used:], self.table, page, len(tokens))
+        tables = L.batch_tables(ints[0], ints[1], d.free[d.used:], self.table, page, len(tokens))
         logits = d.step(tokens, dict(tables, table=self.table), max(new))
-        self.lengths, self.used = total, self.used + pages
+        self.lengths, d.used = total, d.used + pages
         return logits
 
     def generate(self, prompts, steps: int, top: int = 5):

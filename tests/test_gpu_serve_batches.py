@@ -1,0 +1,31 @@
+"""The serving example: batches of one decoder that live side by side, and what its calls refuse."""
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+def test_batches_of_one_decoder_do_not_share_pages():
+    """Two batches in turn on one decoder give bit for bit what each gives on a decoder of its own: the
+    pages are others, the positions and values are not."""
+    from paper_2607_01127_amd.serve_example import Batch, Decoder, Shape
+    print("two batches", flush=True)
+    shape = Shape(layers=1)
+    texts = [[list(range(40)), [7, 8, 9]], [list(range(100, 163)), [5]]]
+    steps = [[[1], [2]], [[3], [4]], [[5, 6, 7], [8]]]
+
+    def logits(batch, text):
+        yield batch.step(text)
+        for s in steps:
+            yield batch.step(s)
+
+    alone = [list(logits(Batch(Decoder(shape, pages=40, page=16, seed=6), 2, 128), t)) for t in texts]
+    both = Decoder(shape, pages=40, page=16, seed=6)
+    together = zip(*(logits(Batch(both, 2, 128), t) for t in texts))
+    for i, pair in enumerate(together):
+        for k in range(2):
+            assert torch.equal(pair[k], alone[k][i]), (i, k)
+    used = sum(-(-(len(t) + sum(len(s[r]) for s in steps)) // 16) for text in texts for r, t in enumerate(text))
+    assert both.used == used
+    with pytest.raises(ValueError):
+        Batch(both, 1, 1000).step([list(range(16 * (40 - used) + 1))])
