@@ -117,7 +117,10 @@ class Batch:
 
     def generate(self, prompts, steps: int, top: int = 5):
         """Greedy continuation: the chosen tokens [requests][steps] (a list of lists), their log
-        probabilities and entropies, and the alternatives of the last step."""
+        probabilities and entropies, and the alternatives of the last step. Each request begins with a
+        token at least."""
+        if steps < 1 or not all(prompts):
+            raise ValueError("generate needs a step and a token of each prompt")
         d = self.decoder
         logits = self.step(prompts)
         ends = torch.tensor([len(p) for p in prompts]).cumsum(0) - 1
@@ -138,8 +141,8 @@ class Batch:
         """Log probabilities of the texts' own tokens but the first (float32 [sum of lengths - 1])."""
         logits = self.step(texts)
         keep = torch.tensor([i for i, last in enumerate(j + 1 == len(t) for t in texts for j in range(len(t)))
-                             if not last]).to(logits.device)
-        targets = torch.tensor([token for t in texts for token in t[1:]]).to(logits.device)
+                             if not last], dtype=torch.int64).to(logits.device)
+        targets = torch.tensor([token for t in texts for token in t[1:]], dtype=torch.int64).to(logits.device)
         return L.token_logprobs(logits[keep], targets, workspace=self.decoder.lp_work)["logprob"]
 
 

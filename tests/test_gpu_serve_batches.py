@@ -29,3 +29,20 @@ def test_batches_of_one_decoder_do_not_share_pages():
     assert both.used == used
     with pytest.raises(ValueError):
         Batch(both, 1, 1000).step([list(range(16 * (40 - used) + 1))])
+
+
+def test_empty_prompts_and_single_tokens():
+    """An empty prompt has no last token whose logits could be continued (they would be the request's
+    before it); texts of one token have nothing to score."""
+    from paper_2607_01127_amd.serve_example import Batch, Decoder, Shape
+    print("empty prompts", flush=True)
+    d = Decoder(Shape(layers=1), pages=16, page=16, seed=6)
+    for prompts in ([[1, 2], []], [[], [1, 2]], [[]]):
+        with pytest.raises(ValueError):
+            Batch(d, len(prompts), 64).generate(prompts, 2)
+    with pytest.raises(ValueError):
+        Batch(d, 1, 64).generate([[1, 2]], 0)
+    assert d.used == 0
+    assert Batch(d, 2, 64).score([[3], [4]]).shape == (0,)
+    whole, part = Batch(d, 2, 64).score([[3, 4], [5]]), Batch(d, 1, 64).score([[3, 4]])
+    assert whole.shape == (1,) and float((whole - part).abs()) < 1e-3
