@@ -714,10 +714,10 @@ __global__ __launch_bounds__(kDecThreads) void k_kv4_join(AttnArgs a, int kRows)
 }
 
 // ------------------------------------------------------------------ prompts
-// A workgroup takes 128 NB query rows (tokens x the query heads of one key/value head) and goes over
+// A workgroup takes 128 query rows (tokens x the query heads of one key/value head) and goes over
 // the positions they see, 64 at a time. All four wavefronts turn the 64 positions' codes into
 // float16 operands in LDS, in the order in which the MFMAs read them; each wavefront then has
-// 32 NB rows: S^T = K Q^T and O^T = V^T P^T with 32x32x16 MFMAs, where a lane's 8 weights of 16
+// 32 rows: S^T = K Q^T and O^T = V^T P^T with 32x32x16 MFMAs, where a lane's 8 weights of 16
 // positions are the second product's B operand as they are. Tiles are double buffered: the next
 // tile's codes are loaded before this one's products and converted after them, one barrier a tile.
 //
@@ -739,6 +739,7 @@ __global__ __launch_bounds__(kDecThreads) void k_kv4_join(AttnArgs a, int kRows)
 // float16 took 415 us, but lost what lies 2^-22 below a row's largest.
 constexpr int kPromptThreads = 256;
 constexpr int kPromptTile = 64;
+constexpr int kPromptRows = 128;             // 32 a wavefront
 constexpr float kFar = 1048576.0f;
 constexpr int kPromptMinRows = 17;           // fewer go through the decode kernel, if it is launched
 
@@ -748,10 +749,10 @@ __device__ __forceinline__ int value_slot(int frag, int chunk, int half, int cha
   return frag * 64 + ((half * 32 + channel) ^ (chunk * 2 + half));
 }
 
-template <int D, int NB, bool QSPLIT, bool ONE_PAGE>
-__global__ __launch_bounds__(kPromptThreads, D / 64 * NB <= 2 ? 2 : 1)
+template <int D, bool QSPLIT, bool ONE_PAGE>
+__global__ __launch_bounds__(kPromptThreads, D <= 128 ? 2 : 1)
 void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
-  constexpr int kRows = 128 * NB, kKc = D / 16, kCb = D / 32, kItems = D == 256 ? 2 : 1;
+  constexpr int kRows = kPromptRows, kKc = D / 16, kCb = D / 32, kItems = D == 256 ? 2 : 1;
   __shared__ half8v kbuf[2][2 * kKc * 64];
   __shared__ bf16x8 vbuf[2][kCb * 4 * 64];
   __shared__ float vscale[2][kPromptTile];
@@ -822,18 +823,17 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
   const int tile1 = (int)((int64_t)tiles * (blockIdx.y + 1) / splits);
 
   // ---- queries
-  half8v qf[NB][kKc], ql[QSPLIT ? NB : 1][QSPLIT ? kKc : 1];
-  float qs[NB], ref[NB], sum[NB];
-  int32_t last[NB];
-  float16v o[NB][kCb];
-  const int wave_row = row0 + wave * 32 * NB;
+  half8v qf[kKc], ql[QSPLIT ? kKc : 1];
+  float qs, ref, sum;
+  int32_t last;
+  float16v o[kCb];
+  const int wave_row = row0 + wave * 32;
   const bool has_rows = wave_row < rows;
-  const int wave_end = wave_row + 32 * NB < rows ? wave_row + 32 * NB : rows;
+  const int wave_end = wave_row + 32 < rows ? wave_row + 32 : rows;
   const int place_lo = req.first + wave_row / a.group;              // of the wavefront's rows
   const int place_hi = req.first + (wave_end - 1) / a.group;
-#pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    const int row = wave_row + nb * 32 + col;
+  {
+    const int row = wave_row + col;
     const int token = row / a.group;
     const int64_t at = (int64_t)(req.t0 + token) * a.q_stride +
                        (int64_t)(head * a.group + row % a.group) * D + half * 8;
@@ -855,16 +855,16 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
     most = fmaxf(most, __shfl_xor(most, 32));
     const int e = most > 0.0f && most < INFINITY ? (int)(__float_as_uint(most) >> 23) - 127 : 0;
     const float down = ldexpf(a.scale < 0.0f ? -1.0f : 1.0f, -e);
-    qs[nb] = __builtin_fabsf(a.scale) * kLog2e * ldexpf(1.0f, e);
+    qs = __builtin_fabsf(a.scale) * kLog2e * ldexpf(1.0f, e);
 #pragma unroll
     for (int c = 0; c < kKc; ++c)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float y = x[c][j] * down;
-        qf[nb][c][j] = (half_t)y;
-        if constexpr (QSPLIT) ql[nb][c][j] = (half_t)(y - (float)(half_t)y);
+        qf[c][j] = (half_t)y;
+        if constexpr (QSPLIT) ql[c][j] = (half_t)(y - (float)(half_t)y);
       }
-    last[nb] = row < rows ? req.first + token : INT32_MAX;
+    last = row < rows ? req.first + token : INT32_MAX;
   }
 
   // ---- loading and converting a tile. A thread has 32 channels of one position's keys (D = 256:
@@ -1023,105 +1023,91 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
                       (!a.window || base > (int64_t)place_hi - a.window);
 #pragma unroll
     for (int pb = 0; pb < 2; ++pb) {
-      float16v s[NB];
+      float16v s;
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[nb][i] = 0.0f;
+      for (int i = 0; i < 16; ++i) s[i] = 0.0f;
 #pragma unroll
       for (int c = 0; c < kKc; ++c) {
         const half8v kf = kbuf[buf][(pb * kKc + c) * 64 + lane];
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          s[nb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[nb][c], s[nb], 0, 0, 0);
-          if constexpr (QSPLIT)
-            s[nb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, ql[nb][c], s[nb], 0, 0, 0);
-        }
+        s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[c], s, 0, 0, 0);
+        if constexpr (QSPLIT)
+          s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, ql[c], s, 0, 0, 0);
       }
-      bf16x8 hi[NB][2], lo[NB][2];
+      bf16x8 hi[2], lo[2];
       f32x4 vs[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         vs[i] = *reinterpret_cast<const f32x4*>(&vscale[buf][32 * pb + 8 * i + 4 * half]);
       const uint32_t bits = (uint32_t)(valid >> (32 * pb)) >> (4 * half);
+      // By ldexp, as 2^ek alone may be below float32's normal numbers.
+      const float f = ldexpf(qs, ek_of);
+      const auto weigh = [&](auto all_seen) {
+        constexpr bool kAll = decltype(all_seen)::value;
+        bool seen[16];
+        if constexpr (!kAll) {
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        // By ldexp, as 2^ek alone may be below float32's normal numbers.
-        const float f = ldexpf(qs[nb], ek_of);
-        const auto weigh = [&](auto all_seen) {
-          constexpr bool kAll = decltype(all_seen)::value;
-          bool seen[16];
-          if constexpr (!kAll) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int at = 8 * (i >> 2) + (i & 3), pos = base + 32 * pb + 4 * half + at;
-              seen[i] = ((bits >> at) & 1u) && pos <= last[nb] &&
-                        (!a.window || last[nb] == INT32_MAX || pos > (int64_t)last[nb] - a.window);
-              s[nb][i] = seen[i] ? s[nb][i] : -INFINITY;
-            }
+          for (int i = 0; i < 16; ++i) {
+            const int at = 8 * (i >> 2) + (i & 3), pos = base + 32 * pb + 4 * half + at;
+            seen[i] = ((bits >> at) & 1u) && pos <= last &&
+                      (!a.window || last == INT32_MAX || pos > (int64_t)last - a.window);
+            s[i] = seen[i] ? s[i] : -INFINITY;
           }
-          float top = s[nb][0];
+        }
+        float top = s[0];
 #pragma unroll
-          for (int i = 1; i < 16; ++i) top = fmaxf(top, s[nb][i]);
-          // A row that sees none of the tile keeps its reference.
-          const float reach = !kAll && top == -INFINITY ? kNone : top * f;
-          if (__builtin_amdgcn_ballot_w64(reach - ref[nb] > 8.0f)) {
-            const float most = fmaxf(reach, __shfl_xor(reach, 32));
-            const float next = most - ref[nb] > 8.0f ? most : ref[nb];
-            const float g = exp2_fast(ref[nb] - next);
-            if constexpr (!kCareful)
-              again |= __builtin_amdgcn_ballot_w64(next != kNone && __builtin_fabsf(next) > kFar) != 0;
-            ref[nb] = next;
-            sum[nb] *= g;
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+        // A row that sees none of the tile keeps its reference.
+        const float reach = !kAll && top == -INFINITY ? kNone : top * f;
+        if (__builtin_amdgcn_ballot_w64(reach - ref > 8.0f)) {
+          const float most = fmaxf(reach, __shfl_xor(reach, 32));
+          const float next = most - ref > 8.0f ? most : ref;
+          const float g = exp2_fast(ref - next);
+          if constexpr (!kCareful)
+            again |= __builtin_amdgcn_ballot_w64(next != kNone && __builtin_fabsf(next) > kFar) != 0;
+          ref = next;
+          sum *= g;
 #pragma unroll
-            for (int c = 0; c < kCb; ++c) o[nb][c] *= g;
+          for (int c = 0; c < kCb; ++c) o[c] *= g;
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float w[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int i = 8 * h + j;
+            float e = exp2_fast(exponent<kCareful>(s[i], f, ref));
+            if constexpr (!kAll) e = seen[i] ? e : 0.0f;
+            sum += e;
+            w[j] = kAll || seen[i] ? e * vs[i >> 2][i & 3] : 0.0f;
           }
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            float w[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const int i = 8 * h + j;
-              float e = exp2_fast(exponent<kCareful>(s[nb][i], f, ref[nb]));
-              if constexpr (!kAll) e = seen[i] ? e : 0.0f;
-              sum[nb] += e;
-              w[j] = kAll || seen[i] ? e * vs[i >> 2][i & 3] : 0.0f;
-            }
-            split_weights(w, hi[nb][h], lo[nb][h]);
-          }
-        };
-        if (full) weigh(std::true_type{});
-        else weigh(std::false_type{});
-      }
+          split_weights(w, hi[h], lo[h]);
+        }
+      };
+      if (full) weigh(std::true_type{});
+      else weigh(std::false_type{});
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         bf16x8 vf[kCb];
 #pragma unroll
         for (int c = 0; c < kCb; ++c) vf[c] = vbuf[buf][value_slot(c * 4 + 2 * pb + h, 2 * pb + h, half, col)];
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
+        for (int c = 0; c < kCb; ++c)
+          o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[c], lo[h], o[c], 0, 0, 0);
 #pragma unroll
-          for (int c = 0; c < kCb; ++c)
-            o[nb][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[c], lo[nb][h], o[nb][c], 0, 0, 0);
-#pragma unroll
-          for (int c = 0; c < kCb; ++c)
-            o[nb][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[c], hi[nb][h], o[nb][c], 0, 0, 0);
-        }
+        for (int c = 0; c < kCb; ++c)
+          o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[c], hi[h], o[c], 0, 0, 0);
       }
     }
   };
 
   const auto go_over = [&](auto careful) {
     constexpr bool kCareful = decltype(careful)::value;
+    ref = kNone;
+    sum = 0.0f;
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      ref[nb] = kNone;
-      sum[nb] = 0.0f;
+    for (int c = 0; c < kCb; ++c)
 #pragma unroll
-      for (int c = 0; c < kCb; ++c)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[nb][c][i] = 0.0f;
-    }
+      for (int i = 0; i < 16; ++i) o[c][i] = 0.0f;
     if (tile0 >= tile1) return;
     const int stop = kv_from + tile1 * kPromptTile;
     int base = kv_from + tile0 * kPromptTile;
@@ -1162,31 +1148,28 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
 
   // ---- out: a lane has 4 consecutive channels of its row at a time
   if (!has_rows) return;
+  const int row = wave_row + col;
+  const float l = sum + __shfl_xor(sum, 32);
+  if (row >= rows) return;
+  const int64_t at = (int64_t)(req.t0 + row / a.group) * (a.c.heads * a.group) +
+                     head * a.group + row % a.group;
+  const float inv = splits > 1 ? 1.0f : l != 0.0f ? 1.0f / l : 0.0f;
 #pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    const int row = wave_row + nb * 32 + col;
-    const float l = sum[nb] + __shfl_xor(sum[nb], 32);
-    if (row >= rows) continue;
-    const int64_t at = (int64_t)(req.t0 + row / a.group) * (a.c.heads * a.group) +
-                       head * a.group + row % a.group;
-    const float inv = splits > 1 ? 1.0f : l != 0.0f ? 1.0f / l : 0.0f;
+  for (int c = 0; c < kCb; ++c)
 #pragma unroll
-    for (int c = 0; c < kCb; ++c)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const f32x4 v = {o[nb][c][4 * i] * inv, o[nb][c][4 * i + 1] * inv, o[nb][c][4 * i + 2] * inv,
-                         o[nb][c][4 * i + 3] * inv};
-        const int ch = 32 * c + 8 * i + 4 * half;
-        if (splits > 1) *reinterpret_cast<f32x4*>(a.part_o + (part + row - row0) * D + ch) = v;
-        else store_four(a.out, a.out_dtype, at * D + ch, v);
-      }
-    if (half == 0) {
-      if (splits > 1) {
-        a.part_rl[(part + row - row0) * 2] = ref[nb];
-        a.part_rl[(part + row - row0) * 2 + 1] = l;
-      } else if (a.lse) {
-        a.lse[at] = l != 0.0f ? (ref[nb] + __log2f(l)) * kLn2 : -INFINITY;
-      }
+    for (int i = 0; i < 4; ++i) {
+      const f32x4 v = {o[c][4 * i] * inv, o[c][4 * i + 1] * inv, o[c][4 * i + 2] * inv,
+                       o[c][4 * i + 3] * inv};
+      const int ch = 32 * c + 8 * i + 4 * half;
+      if (splits > 1) *reinterpret_cast<f32x4*>(a.part_o + (part + row - row0) * D + ch) = v;
+      else store_four(a.out, a.out_dtype, at * D + ch, v);
+    }
+  if (half == 0) {
+    if (splits > 1) {
+      a.part_rl[(part + row - row0) * 2] = ref;
+      a.part_rl[(part + row - row0) * 2 + 1] = l;
+    } else if (a.lse) {
+      a.lse[at] = l != 0.0f ? (ref + __log2f(l)) * kLn2 : -INFINITY;
     }
   }
 }
@@ -1221,10 +1204,14 @@ __global__ __launch_bounds__(kPromptThreads) void k_kv4_prompt_join(AttnArgs a, 
 }
 
 // ------------------------------------------------------------------ host side
-constexpr int kPromptBlocks = 1;      // 32-row blocks of a wavefront of the prompt kernel
 constexpr int kPromptGrid = 1024;     // workgroups that the splits of few rows aim at
 constexpr int kDecParts = 512;      // workgroups of the decode kernel: two a CU
 constexpr int64_t kDescBytes = 16 * kDecParts;
+
+// Whether a decode kernel takes split (float32) queries: with four blocks a tile its registers do not hold
+// them as well from D = 128.
+template <int D, int CG>
+constexpr bool kDecSplits = CG < 4 || D == 64;
 
 template <int D, int NT, int CG>
 int32_t launch_decode(AttnArgs a, void* work, hipStream_t stream) {
@@ -1246,7 +1233,12 @@ int32_t launch_decode(AttnArgs a, void* work, hipStream_t stream) {
   if (split == SPLIT && one_page == ONE_PAGE)                                                        \
     hipLaunchKernelGGL((k_kv4_decode<D, NT, CG, SPLIT, ONE_PAGE>), dim3(kDecParts), dim3(kDecThreads), \
                        0, stream, a)
-  DECODE(false, false); DECODE(false, true); DECODE(true, false); DECODE(true, true);
+  DECODE(false, false); DECODE(false, true);
+  if constexpr (kDecSplits<D, CG>) {
+    DECODE(true, false); DECODE(true, true);
+  } else if (split) {
+    return LOGBQ_ERR_UNSUPPORTED;
+  }
 #undef DECODE
   if (launch_status() != LOGBQ_OK) return LOGBQ_ERR_HIP;
   if (whole) return LOGBQ_OK;
@@ -1255,16 +1247,16 @@ int32_t launch_decode(AttnArgs a, void* work, hipStream_t stream) {
 }
 
 // As many row tiles as the requests can have; each request has at least min_rows rows.
-int64_t prompt_tiles(const AttnArgs& a, int min_rows, int rows_of_tile) {
+int64_t prompt_tiles(const AttnArgs& a, int min_rows) {
   const int64_t rows = (int64_t)a.tokens * a.group;
   const int64_t short_ones = rows / min_rows < a.requests ? rows / min_rows : a.requests;
-  return (rows / rows_of_tile + short_ones) * a.c.heads;
+  return (rows / kPromptRows + short_ones) * a.c.heads;
 }
 
-template <int D, int NB>
+template <int D>
 int32_t launch_prompt(AttnArgs a, int min_rows, void* work, hipStream_t stream) {
-  constexpr int kRows = 128 * NB;
-  const int64_t tiles = prompt_tiles(a, min_rows, kRows);
+  constexpr int kRows = kPromptRows;
+  const int64_t tiles = prompt_tiles(a, min_rows);
   if (tiles == 0) return LOGBQ_OK;
   int64_t splits = kPromptGrid / tiles;
   // A split has four tiles at least where the block table is full.
@@ -1282,7 +1274,7 @@ int32_t launch_prompt(AttnArgs a, int min_rows, void* work, hipStream_t stream) 
   const bool split = a.q_dtype == LOGBQ_DTYPE_F32, one_page = a.c.page_shift >= 6;
 #define PROMPT(SPLIT, ONE_PAGE)                                                                     \
   if (split == SPLIT && one_page == ONE_PAGE)                                                       \
-    hipLaunchKernelGGL((k_kv4_prompt<D, NB, SPLIT, ONE_PAGE>), grid, dim3(kPromptThreads), 0, stream, \
+    hipLaunchKernelGGL((k_kv4_prompt<D, SPLIT, ONE_PAGE>), grid, dim3(kPromptThreads), 0, stream, \
                        a, (int)splits, min_rows)
   PROMPT(false, false); PROMPT(false, true); PROMPT(true, false); PROMPT(true, true);
 #undef PROMPT
@@ -1297,11 +1289,10 @@ int32_t launch_attention(const AttnArgs& a, int64_t max_new, void* work, hipStre
   const int64_t rows = max_new > INT32_MAX ? INT32_MAX : max_new * a.group;
   // Tiles of four blocks have twice the codes in flight of tiles of two, but take longer to start:
   // for shares of 20 units or more, and for long requests (D = 128: 128 requests of 3000 to 9000
-  // 167 us against 183, one of 131071 40.6 against 42.4, 32 of 300 to 4100 39.7 against 35.7). Their
-  // registers do not hold split queries as well from D = 128.
+  // 167 us against 183, one of 131071 40.6 against 42.4, 32 of 300 to 4100 39.7 against 35.7).
   const int64_t span = (int64_t)a.width << a.c.page_shift;
   const bool large = (double)a.requests * a.c.heads * span >= 20.0 * kUnit * kDecParts || span >= 32768;
-  if (rows <= 4 && large && (D == 64 || a.q_dtype != LOGBQ_DTYPE_F32)) return launch_decode<D, 1, 4>(a, work, stream);
+  if (rows <= 4 && large && (kDecSplits<D, 4> || a.q_dtype != LOGBQ_DTYPE_F32)) return launch_decode<D, 1, 4>(a, work, stream);
   if (rows <= 8) return launch_decode<D, 1, 2>(a, work, stream);
   if (rows <= 16) return launch_decode<D, 1, 1>(a, work, stream);
   if (D < 256 && rows <= 32) return launch_decode<D, D < 256 ? 2 : 1, 1>(a, work, stream);
@@ -1309,12 +1300,12 @@ int32_t launch_attention(const AttnArgs& a, int64_t max_new, void* work, hipStre
   // A prompt among them: decode requests apart from the longer ones. One request is taken as a prompt.
   // A launch has fewer than 2^32 threads a dimension, which is seen to before anything is enqueued.
   const int min_rows = a.requests == 1 ? 1 : kPromptMinRows;
-  if (prompt_tiles(a, min_rows, 128 * kPromptBlocks) > (((int64_t)1 << 32) - 1) / kPromptThreads)
+  if (prompt_tiles(a, min_rows) > (((int64_t)1 << 32) - 1) / kPromptThreads)
     return LOGBQ_ERR_UNSUPPORTED;
-  if (a.requests == 1) return launch_prompt<D, kPromptBlocks>(a, min_rows, work, stream);
+  if (a.requests == 1) return launch_prompt<D>(a, min_rows, work, stream);
   const int32_t status = launch_decode<D, 1, 1>(a, work, stream);
   if (status != LOGBQ_OK) return status;
-  return launch_prompt<D, kPromptBlocks>(a, min_rows, work, stream);
+  return launch_prompt<D>(a, min_rows, work, stream);
 }
 
 }  // namespace

@@ -42,14 +42,7 @@ __device__ __forceinline__ float load_element(const void* p, int64_t i) {
   return bf16_value(static_cast<const uint16_t*>(p)[i]);
 }
 
-// x rounded to nearest into element i of an array of a type.
-__device__ __forceinline__ void store_element(void* p, int32_t dtype, int64_t i, float x) {
-  if (dtype == LOGBQ_DTYPE_F32) static_cast<float*>(p)[i] = x;
-  else if (dtype == LOGBQ_DTYPE_F16) static_cast<half_t*>(p)[i] = (half_t)x;
-  else static_cast<__bf16*>(p)[i] = (__bf16)x;
-}
-
-// Four consecutive elements.
+// x rounded to nearest into four consecutive elements from i of an array of a type.
 __device__ __forceinline__ void store_four(void* p, int32_t dtype, int64_t i, f32x4 x) {
   if (dtype == LOGBQ_DTYPE_F32) {
     *reinterpret_cast<f32x4*>(static_cast<float*>(p) + i) = x;
