@@ -757,6 +757,7 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
   __shared__ bf16x8 vbuf[2][kCb * 4 * 64];
   __shared__ float vscale[2][kPromptTile];
   __shared__ uint64_t rest_of[2];
+  __shared__ int again;                 // a wavefront has met what is to be taken with care
   __shared__ int64_t scan[4];
   __shared__ int64_t found[2];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -781,7 +782,10 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
     if (lane >= d) upto += x;
   }
   if (lane == 63) scan[wave] = upto;
-  if (tid == 0) found[0] = -1;
+  if (tid == 0) {
+    found[0] = -1;
+    again = 0;
+  }
   __syncthreads();
   for (int w = 0; w < wave; ++w) upto += scan[w];
   if (upto - mine <= unit && unit < upto) {
@@ -927,7 +931,7 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
     return t;
   };
   int ek = -200;                        // exponent that the keys' scales are divided by
-  bool again = false;                   // the wavefront has met what is to be taken with care
+  const auto set_again = [&] { __hip_atomic_store(&again, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); };
   // With care, returns the positions that are left for another time; rest_of has the same, from one
   // wavefront, for the number of times that all go round, which no change of the cache meanwhile may
   // set apart.
@@ -940,15 +944,13 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
     const int xk = (int)(t.lane_ks >> 7 & 0xff) - 127;
     uint64_t rest = 0;
     if (__builtin_amdgcn_ballot_w64(counts && (unsigned)(xk - ek + 13) > 25u)) {
-      int most = counts ? xk : -1000, least = counts ? xk : 1000;
-      for (int d = 1; d < 64; d <<= 1) {
-        most = max(most, __shfl_xor(most, d));
-        least = min(least, __shfl_xor(least, d));
-      }
-      if constexpr (!kCareful) again |= __builtin_amdgcn_readfirstlane(most - least) > 25;
-      least = max(least, most - 25);
-      if constexpr (kCareful) rest = __builtin_amdgcn_ballot_w64(counts && xk < least);
-      ek = __builtin_amdgcn_readfirstlane((most + least + 1) >> 1);
+      int most = counts ? xk : -1000;
+      for (int d = 1; d < 64; d <<= 1) most = max(most, __shfl_xor(most, d));
+      rest = __builtin_amdgcn_ballot_w64(counts && xk < most - 25);
+      if constexpr (!kCareful)
+        if (rest) set_again();
+      // Room for the largest to grow by 2 binades, where the smallest leaves it.
+      ek = __builtin_amdgcn_readfirstlane(most) - (__builtin_amdgcn_ballot_w64(counts && xk < most - 23) ? 12 : 10);
     }
     if constexpr (kCareful)
       if (tid == 0) rest_of[buf] = rest;
@@ -1010,7 +1012,7 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
         }
       }
     }
-    return rest;
+    return kCareful ? rest : 0;
   };
 
   // ---- a tile's products and softmax
@@ -1063,7 +1065,7 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
           const float next = most - ref > 8.0f ? most : ref;
           const float g = exp2_fast(ref - next);
           if constexpr (!kCareful)
-            again |= __builtin_amdgcn_ballot_w64(next != kNone && __builtin_fabsf(next) > kFar) != 0;
+            if (__builtin_amdgcn_ballot_w64(next != kNone && __builtin_fabsf(next) > kFar)) set_again();
           ref = next;
           sum *= g;
 #pragma unroll
@@ -1143,8 +1145,8 @@ void k_kv4_prompt(AttnArgs a, int splits, int min_rows) {
       __syncthreads();
     }
   };
-  go_over(std::false_type{});
-  if (__syncthreads_or(again)) go_over(std::true_type{});
+  go_over(std::false_type{});           // its last barrier is after the last time that `again` is set
+  if (__builtin_amdgcn_readfirstlane(again)) go_over(std::true_type{});
 
   // ---- out: a lane has 4 consecutive channels of its row at a time
   if (!has_rows) return;
