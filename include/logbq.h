@@ -519,12 +519,16 @@ int32_t logbq_kv4_read(const logbq_kv4* cache, const int64_t* slots_dev, int64_t
  *                are enough for any call.
  * Token i of n new ones of a request of length s has position p = s - n + i and sees positions
  * max(0, p - window + 1) .. p (0 .. p without a window). A token that sees nothing has output 0
- * and lse -inf. Products of q are taken in float16 (float32 queries as a sum of two float16
- * values), all sums and the softmax in float32; its weights times the values' scales are rounded to
- * 16 bits for the product with the values' codes. Requests of up to 16 query rows (tokens times
- * q_heads / heads; 32 for dim 128, 64 for dim 64 if no request of the call has more) share their
- * positions out over the whole chip; the others go in tiles of 128 rows, whose positions are split
- * where there are few. Results do not change from call to call. Enqueues one to four kernels.
+ * and lse -inf. What a token does not see reaches nothing of its own, whatever its scales hold.
+ * Products of q are taken in float16 (float32 queries as a sum of two float16 values), all sums and
+ * the softmax in float32; its weights times the values' scales are rounded to 16 bits for the
+ * product with the values' codes. Logits may have any size that float32 holds; so must the products
+ * of keys with queries brought below 2 (they do where |k| < 2^112), and 2^8 times the sum of |v|.
+ * Requests of up to 16 query rows (tokens times q_heads / heads; 32 for dim 128, 64 for dim 64 if no
+ * request of the call has more) share their positions out over the whole chip; the others go in
+ * tiles of 128 rows, whose positions are split where there are few. Which way is taken goes by
+ * max_new and width: a table no wider than the step's longest request serves short ones faster.
+ * Results do not change from call to call. Enqueues one to four kernels.
  * Errors: INVALID_ARG, UNSUPPORTED (dim, page, heads, dtypes, alignment, sizes, a workspace that
  * is too small), HIP.
  */
@@ -560,7 +564,8 @@ int32_t logbq_kv4_attention(const void* q_dev, int64_t q_stride, int32_t q_dtype
  * returned among the top ones only when fewer than `top` others are left, with log probability
  * -inf. Rows with a NaN, a +inf or nothing but -inf have log probabilities and entropy NaN; NaN
  * ranks above every number.
- * Sums are float32.
+ * Sums are float32, of terms about the row's maximum: the logits' size, or an offset common to a
+ * row, adds no error.
  * Errors: INVALID_ARG (null pointer, negative size, top > vocab), UNSUPPORTED (dtype, alignment,
  * tokens, vocab >= 2^31, top, stride, a workspace that is too small), HIP.
  */

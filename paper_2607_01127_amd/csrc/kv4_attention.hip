@@ -53,8 +53,8 @@ __device__ __forceinline__ float exponent(float x, float f, float ref) {
 }
 
 // The same number, but one that the compiler cannot compute ahead of a loop: what is derived from it
-// takes no registers across the loop. (A spilled value is worse than a recomputed one: its load
-// comes back only after all the loads of codes before it.)
+// takes no registers across the loop. (A value spilled to memory is worse than a recomputed one: its
+// load comes back only after all the loads of codes before it.)
 __device__ __forceinline__ int here(int x) {
   asm volatile("" : "+v"(x));
   return x;
@@ -731,12 +731,15 @@ __global__ __launch_bounds__(kDecThreads) void k_kv4_join(AttnArgs a, int kRows)
 // a tile whose keys' scales span more than 26 binades (a few keys far larger than the rest, a scale that
 // is no number), of which the positions with the largest are taken first and the tile comes again for the
 // others; and a reference past kFar, up to which its rounding is 2^-4 at most, about which the product is
-// rounded too. (Both in the one loop cost every prompt 2 to 7 %, a second loop nothing.)
+// rounded too. (Both in the one loop cost every prompt 2 to 7 %; as a second loop they cost a prompt of
+// 254 tokens 0.5 us and one of 6001 nothing.)
 //
-// Bound by instruction issue: about 500 vector instructions and 24 MFMAs a wavefront's tile, issue
-// slots 86 % busy. Measured, 8 heads x 4 queries x 128 channels, float16: a prompt of 6001 tokens
-// (295 GFLOP) 450 us, 656 TFLOP/s, or 984 with the second bfloat16 number's products. Weights in one
-// float16 took 415 us, but lost what lies 2^-22 below a row's largest.
+// Bound by instruction issue: about 450 vector instructions and 48 MFMAs a wavefront's tile, issue
+// slots 84 % busy. Measured, 8 heads x 4 queries x 128 channels, float16: a prompt of 6001 tokens
+// (295 GFLOP) 452 us, 653 TFLOP/s, or 979 with the second bfloat16 number's products; one of 254
+// tokens 18.2 us. Weights in one float16 took 415 us, but lost what lies 2^-22 below a row's largest.
+// Two workgroups a CU up to 128 channels, one at 256 (131 KB of LDS). Float32 queries spill 6 to 9
+// registers at 128 channels and 44 to 46 at 256.
 constexpr int kPromptThreads = 256;
 constexpr int kPromptTile = 64;
 constexpr int kPromptRows = 128;             // 32 a wavefront
@@ -1207,7 +1210,9 @@ __global__ __launch_bounds__(kPromptThreads) void k_kv4_prompt_join(AttnArgs a, 
 
 // ------------------------------------------------------------------ host side
 constexpr int kPromptGrid = 1024;     // workgroups that the splits of few rows aim at
-constexpr int kDecParts = 512;      // workgroups of the decode kernel: two a CU
+// Workgroups of the decode kernel: two a CU, except that one fits a CU at 256 channels, at 128 with 32 query
+// rows and at 64 with 64, where the second half waits for the first.
+constexpr int kDecParts = 512;
 constexpr int64_t kDescBytes = 16 * kDecParts;
 
 // Whether a decode kernel takes split (float32) queries: with four blocks a tile its registers do not hold
@@ -1226,7 +1231,9 @@ int32_t launch_decode(AttnArgs a, void* work, hipStream_t stream) {
   static_assert(kDescBytes + (int64_t)2 * kDecParts * kRows * (D + 2) * 4 <= LOGBQ_KV4_WORKSPACE_BYTES,
                 "the workspace holds every part");
   // Requests of at most 512 positions are not split, which saves the second launch (one of 500
-  // positions: 10.2 us a call from Python, 13.0 with it).
+  // positions: 10.3 us a call from Python, 13.3 with it). The host knows no length but the block table's
+  // width, so here, for the blocks of a tile and for a prompt's splits, a table that is wider than its
+  // requests are long counts as if they were.
   const int64_t span = (int64_t)a.width << a.c.page_shift;
   const bool whole = span <= 4 * kUnit;
   a.unit = whole && span > kUnit ? (int)(span + kUnit - 1) / kUnit * kUnit : kUnit;
@@ -1261,7 +1268,8 @@ int32_t launch_prompt(AttnArgs a, int min_rows, void* work, hipStream_t stream) 
   const int64_t tiles = prompt_tiles(a, min_rows);
   if (tiles == 0) return LOGBQ_OK;
   int64_t splits = kPromptGrid / tiles;
-  // A split has four tiles at least where the block table is full.
+  // A split has four tiles at least where the block table is full (254 tokens: 18.2 us; in a table of
+  // 131072 positions, in 16 splits, 43.8).
   const int64_t most = ((int64_t)a.width << a.c.page_shift) / (4 * kPromptTile);
   splits = splits > 32 ? 32 : splits;
   splits = splits > most ? most : splits;
@@ -1291,7 +1299,7 @@ int32_t launch_attention(const AttnArgs& a, int64_t max_new, void* work, hipStre
   const int64_t rows = max_new > INT32_MAX ? INT32_MAX : max_new * a.group;
   // Tiles of four blocks have twice the codes in flight of tiles of two, but take longer to start:
   // for shares of 20 units or more, and for long requests (D = 128: 128 requests of 3000 to 9000
-  // 167 us against 183, one of 131071 40.6 against 42.4, 32 of 300 to 4100 39.7 against 35.7).
+  // 163 us against 172, one of 131071 37.2 against 38.5, 32 of 300 to 4100 33.6 against 31.5).
   const int64_t span = (int64_t)a.width << a.c.page_shift;
   const bool large = (double)a.requests * a.c.heads * span >= 20.0 * kUnit * kDecParts || span >= 32768;
   if (rows <= 4 && large && (kDecSplits<D, 4> || a.q_dtype != LOGBQ_DTYPE_F32)) return launch_decode<D, 1, 4>(a, work, stream);

@@ -291,9 +291,9 @@ __device__ __forceinline__ uint32_t logit_key(float x) {
 // bound as well. A buffer that fills up keeps its best `top` keys, in order: each key's place is the
 // number of larger ones.
 //
-// Bound by HBM where rows are many (1000 rows of 100003 bfloat16, 200 MB: 40 us without
-// alternatives, 49.5 with 5, 62 with 20) and by latency where they are few (one of 131072 float32:
-// 7 us without alternatives, 15 with 20, in which the parts' join takes about 4).
+// Bound by HBM where rows are many (1000 rows of 100003 bfloat16, 200 MB: 39 us without
+// alternatives, 48.5 with 5, 58 with 20) and by latency where they are few (one of 131072 float32:
+// 7.4 us without alternatives, 15 with 20, in which the parts' join takes about 4).
 //
 // Few rows are split into parts, one workgroup each; the last one of a row to finish joins them.
 constexpr int kLpVecs = 2;
@@ -301,8 +301,8 @@ constexpr int kLpAhead = 2;                      // steps whose vectors are in f
 constexpr int kLpKeys = 192;                     // of a wavefront's buffer: more than 64 + kLpTop
 constexpr int kLpMaxSplits = 32;                 // parts of one row
 constexpr int kLpMaxParts = 512;                 // parts of all rows, where rows are split
-// Workgroups from which 256 threads fill the chip (1000 x 100003 bfloat16: 52 us with 256, 58 with 512;
-// 700 x 131072 float32: 67 with 256, 57 with 512).
+// Workgroups from which 256 threads fill the chip (1000 x 100003 bfloat16, top 5: 48.5 us with 256, 54 with
+// 512; 700 x 131072 float32, top 20: 81.5 with 256, 66.6 with 512).
 constexpr int kLpManyRows = 900;
 constexpr int kLpTop = LOGBQ_LOGPROBS_MAX_TOP;
 
@@ -814,7 +814,7 @@ int32_t logbq_token_logprobs(const void* logits_dev, int32_t dtype, int64_t toke
   a.stride = stride;
   a.vocab = (int32_t)vocab;
   a.top = top;
-  // Few rows: parts of at least 16 KiB (one row of 131072: 15.4 us; of 32 KiB: 16.9).
+  // Few rows: parts of at least 16 KiB (one row of 131072: 15.0 us; of 32 KiB: 16.6).
   const int64_t most = vocab * bytes / 16384;
   int64_t splits = kLpMaxParts / tokens;
   splits = splits > kLpMaxSplits ? kLpMaxSplits : splits;
