@@ -462,6 +462,27 @@ int32_t logbq_batch_tables(const int32_t* cached_dev, const int32_t* new_dev, in
                            int32_t* info_dev, void* stream);
 
 /*
+ * logbq_tree_tables -- ancestor masks and positions of a step's drafted trees (speculative decode), from the
+ * nodes' parents. The new tokens of a request are the nodes of its tree, in an order in which parents come
+ * before their children, at most 64.
+ *   parents_dev  : device, [tokens] int32: the parent's index among the request's tokens. A negative one, or one
+ *                  that is not before the node itself, stands for the request's last cached token.
+ *   tokens       : entries of parents_dev and of the outputs.
+ *   q_starts_dev : device, [requests + 1] int32, first token of each request.
+ *   seq_lens_dev : device, [requests] int32, cached tokens with the nodes.
+ *   masks_dev    : device, [tokens] uint64, written: bit j is set where node j of the request is the node
+ *                  itself or an ancestor.
+ *   positions_dev : device, [tokens] int32, written: the node's position in its text, seq_len - nodes + depth
+ *                  (0 where that is negative). Its slot in the cache goes by its index instead (logbq_batch_tables).
+ * Tokens of a request past its 64th have mask 0 and position 0; what belongs to no request is left as it was.
+ * No output may overlap an input or the other output.
+ * Errors: INVALID_ARG (null pointer, negative size, overlap), UNSUPPORTED (sizes), HIP.
+ */
+int32_t logbq_tree_tables(const int32_t* parents_dev, int64_t tokens, const int32_t* q_starts_dev,
+                          const int32_t* seq_lens_dev, int64_t requests, uint64_t* masks_dev,
+                          int32_t* positions_dev, void* stream);
+
+/*
  * logbq_kv4_append -- keys and values of `tokens` tokens, quantized into their slots.
  *   k_dev, v_dev : device, row t of head h at element t * stride + h * dim; 16-byte aligned, and
  *                  so is every row (stride in elements, at least heads * dim).
@@ -477,6 +498,62 @@ int32_t logbq_batch_tables(const int32_t* cached_dev, const int32_t* new_dev, in
 int32_t logbq_kv4_append(const void* k_dev, int64_t k_stride, const void* v_dev, int64_t v_stride,
                          int32_t dtype, int64_t tokens, const logbq_kv4* cache,
                          const int64_t* slots_dev, void* stream);
+
+/* Rotation of queries and keys by their positions. Pair i of a head's first 2 * pairs channels is turned by
+ * position * inv_freq[i] and multiplied by `factor`; the channels after them stay as they are.
+ *   (u, v) -> factor (u cos - v sin, v cos + u sin)
+ */
+typedef struct logbq_rotation {
+  const float* inv_freq;   /* device, [pairs]                                               */
+  int32_t pairs;           /* 0 .. dim / 2, a multiple of dim / 16; 0 turns nothing          */
+  int32_t interleaved;     /* 0: pair i is channels i and i + pairs; 1: 2 i and 2 i + 1      */
+  double factor;
+} logbq_rotation;
+
+/*
+ * logbq_qk_rotate -- RMS norm of each head of the queries and keys, and their rotation, in one pass.
+ *   q_dev, k_dev : device, row t of head h at element t * stride + h * dim; 16-byte aligned, and so is every
+ *                  row. k_heads (or q_heads) 0 leaves keys (queries) out.
+ *   q_weight_dev, k_weight_dev : device, [dim] float32, 16-byte aligned: x / sqrt(mean(x^2) + eps) * weight
+ *                  before the rotation; NULL: no norm.
+ *   dtype        : logbq_dtype of q and k.
+ *   tokens       : fewer than 2^26 - 4.
+ *   dim          : 64, 128 or 256.
+ *   eps          : finite, not negative.
+ *   positions_dev : device, [tokens] int32 (may be NULL if the rotation has no pairs).
+ *   rotation     : host. |position * inv_freq| up to 2^31 is reduced exactly.
+ *   q_out_dev, k_out_dev : device, [tokens][heads][dim] of out_dtype, written; 16-byte aligned. An output may be its
+ *                  own input (same type, no gaps between the tokens), and overlaps nothing else that the call reads
+ *                  or writes.
+ * Everything is computed in 64 bits and rounded to float32, and then to out_dtype.
+ * Errors: INVALID_ARG (null pointer, negative size, eps, overlap), UNSUPPORTED (dim, pairs, dtypes, heads > 16384
+ * (keys: 1024), tokens, alignment, stride), HIP.
+ */
+int32_t logbq_qk_rotate(const void* q_dev, int64_t q_stride, int32_t q_heads, const float* q_weight_dev,
+                        const void* k_dev, int64_t k_stride, int32_t k_heads, const float* k_weight_dev,
+                        int32_t dtype, int64_t tokens, int32_t dim, double eps,
+                        const int32_t* positions_dev, const logbq_rotation* rotation, void* q_out_dev,
+                        void* k_out_dev, int32_t out_dtype, void* stream);
+
+/*
+ * logbq_kv4_append_rotated -- logbq_qk_rotate with the keys going into the cache, and the values with them, in one
+ * launch: what logbq_kv4_append would make of float32 rotated keys, and the rotated queries.
+ *   q_dev .. dtype, eps, positions_dev, rotation : as logbq_qk_rotate; q_heads 0 leaves queries out. Keys and values
+ *                  have the cache's heads and dim.
+ *   v_dev        : device, as k_dev; values are neither normed nor turned.
+ *   cache, slots_dev : as logbq_kv4_append. A token without a slot still has its query turned.
+ *   q_out_dev    : device, [tokens][q_heads][dim] of out_dtype, written; q itself (as in logbq_qk_rotate) or
+ *                  apart from whatever else the call reads.
+ * The codes are those of the 64-bit result rounded to float32 once, so they do not depend on an order of sums.
+ * Errors: as logbq_qk_rotate and logbq_kv4_append.
+ */
+int32_t logbq_kv4_append_rotated(const void* q_dev, int64_t q_stride, int32_t q_heads,
+                                 const float* q_weight_dev, const void* k_dev, int64_t k_stride,
+                                 const float* k_weight_dev, const void* v_dev, int64_t v_stride,
+                                 int32_t dtype, int64_t tokens, double eps,
+                                 const int32_t* positions_dev, const logbq_rotation* rotation,
+                                 const logbq_kv4* cache, const int64_t* slots_dev, void* q_out_dev,
+                                 int32_t out_dtype, void* stream);
 
 /*
  * logbq_kv4_read -- the values that the cache holds in given slots, e.g. to export a prefix.
@@ -538,6 +615,71 @@ int32_t logbq_kv4_attention(const void* q_dev, int64_t q_stride, int32_t q_dtype
                             const int32_t* q_starts_dev, int64_t max_new, float scale,
                             int32_t window, void* out_dev, int32_t out_dtype, float* lse_dev,
                             void* work_dev, int64_t work_bytes, void* stream);
+
+/*
+ * logbq_kv4_tree_attention -- logbq_kv4_attention for a step whose new tokens are the nodes of drafted trees.
+ *   masks_dev : device, [tokens] uint64 (logbq_tree_tables): bit j is set where the token sees the j-th new token of
+ *               its request. Bits past the request's tokens count for nothing. Any masks do, a tree's or not.
+ *   max_new   : upper bound of a request's tokens (host), at most 64.
+ *   window    : 0, or 64 at least: a token of depth d = (bits of its mask) - 1 sees the cached positions past
+ *               cached + d - window, and all the new tokens of its mask.
+ *   The others, what is written and what a row without anything to see gets: as logbq_kv4_attention, but
+ *               requests * heads * ceil(max_new * (q_heads / heads) / 128) * (width * page / 64 + 1) < 2^31.
+ * A new token of a request sees all of its cached tokens (seq_len less its new tokens) that the window holds, and new
+ * tokens by its mask. The new tokens' keys and values lie in the cache behind the cached ones, in order, as
+ * logbq_batch_tables gives their slots. A chain (parents i - 1) gets what logbq_kv4_attention computes.
+ * Errors: as logbq_kv4_attention, and UNSUPPORTED for max_new > 64 and 0 < window < 64.
+ */
+int32_t logbq_kv4_tree_attention(const void* q_dev, int64_t q_stride, int32_t q_dtype, int64_t tokens,
+                                 int32_t q_heads, const logbq_kv4* cache, const int32_t* table_dev,
+                                 int64_t requests, int64_t width, const int32_t* seq_lens_dev,
+                                 const int32_t* q_starts_dev, const uint64_t* masks_dev, int64_t max_new,
+                                 float scale, int32_t window, void* out_dev, int32_t out_dtype,
+                                 float* lse_dev, void* work_dev, int64_t work_bytes, void* stream);
+
+/* Most ranks of an adapter. */
+#define LOGBQ_ADAPTERS_MAX_RANK 128
+
+/* Bytes of workspace that logbq_linear_adapters needs for a call of these sizes; 0 for sizes that it does not
+ * take. Host only. Grows with tokens. */
+int64_t logbq_linear_adapters_workspace(int64_t tokens, int32_t count, int32_t rank);
+
+/*
+ * logbq_linear_adapters -- low-rank adapters of many requests beside up to four projections that share their
+ * activations: out_i[t] = y_i[t] + scales[a] (x[t] A_i[a]^T) B_i[a]^T with a the adapter of t's request, and y_i what
+ * logbq_linear or logbq_linear_multi gave.
+ *   x_dev    : device, [tokens][k] float16, 16-byte aligned; k % 32 == 0.
+ *   count    : projections, 1 .. 4.
+ *   a_dev, b_dev : host arrays of device pointers, 16-byte aligned: A_i [adapters][rank][k], B_i
+ *              [adapters][n_i][rank].
+ *   n        : host array, out features of the projections (any number; 0 leaves one out).
+ *   dtype    : logbq_dtype of A and B, float16 or bfloat16.
+ *   adapters : adapters in the pool.
+ *   rank     : ranks that the pool has room for, a multiple of 8, at most LOGBQ_ADAPTERS_MAX_RANK.
+ *   ranks_dev : device, [adapters] int32: rows of A and columns of B that an adapter has (0 .. rank; what
+ *              lies past them is not used, whatever it holds). NULL: all of them have `rank`.
+ *   scales_dev : device, [adapters] float32. NULL: 1.
+ *   q_starts_dev : device, [requests + 1] int32, first token of each request.
+ *   adapter_dev : device, [requests] int32: the request's adapter; one outside the pool: none.
+ *   max_new  : upper bound of a request's tokens (host). Tokens of a request past it are left out.
+ *   y_dev, out_dev : host arrays of device pointers, [tokens][n_i] float32. out_i may be y_i (in place), and
+ *              overlaps nothing else that the call reads or writes.
+ *   work_dev : device, 16-byte aligned, logbq_linear_adapters_workspace bytes at least; overwritten. Calls that
+ *              overlap need one each.
+ * Rows of requests without an adapter are copied (in place: left alone); rows that belong to no request are left as
+ * they were. Sums are float32; x A^T goes into the second product as two float16 numbers about its largest (22
+ * bits) or as three bfloat16 ones.
+ * Results do not change from call to call. Enqueues two kernels.
+ * Errors: INVALID_ARG (null pointer, negative size, count, overlap), UNSUPPORTED (dtype, k % 32, rank, alignment,
+ * sizes, a workspace that is too small), HIP.
+ */
+int32_t logbq_linear_adapters(const uint16_t* x_dev, int64_t tokens, int64_t k, int32_t count,
+                              const void* const* a_dev, const void* const* b_dev, const int64_t* n,
+                              int32_t dtype, int64_t adapters, int32_t rank, const int32_t* ranks_dev,
+                              const float* scales_dev, const int32_t* q_starts_dev,
+                              const int32_t* adapter_dev, int64_t requests, int64_t max_new,
+                              const float* const* y_dev, float* const* out_dev, void* work_dev,
+                              int64_t work_bytes, void* stream);
 
 /* Bytes of workspace that logbq_token_logprobs needs, whatever the call. */
 #define LOGBQ_LOGPROBS_WORKSPACE_BYTES 4194304

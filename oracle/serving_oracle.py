@@ -172,3 +172,50 @@ def token_logprobs(x, targets, top):
             index[r] = order[:top]
             best[r] = d[order[:top]] - log_s
     return lp, ent, index, best
+
+
+def rotate(x, weight, positions, inv_freq, interleaved=False, factor=1.0, eps=1e-6):
+    """Rows [T][heads][D] with each head normed (weight not None) and turned by its token's position."""
+    x = np.array(x, dtype=np.float64)
+    if weight is not None:
+        x = x / np.sqrt(np.mean(x * x, axis=-1, keepdims=True) + eps) * np.asarray(weight, dtype=np.float64)
+    out = x.copy()
+    pairs = len(inv_freq)
+    for t, p in enumerate(positions):
+        for i, f in enumerate(inv_freq):
+            a, b = (2 * i, 2 * i + 1) if interleaved else (i, i + pairs)
+            angle = int(p) * float(f)
+            c, s = factor * math.cos(angle), factor * math.sin(angle)
+            out[t, :, a] = x[t, :, a] * c - x[t, :, b] * s
+            out[t, :, b] = x[t, :, b] * c + x[t, :, a] * s
+    return out
+
+
+def tree_tables(parents, q_starts, seq_lens):
+    """(masks as Python numbers, positions) of every token that belongs to a request, by walking up."""
+    masks, positions = {}, {}
+    for r, length in enumerate(seq_lens):
+        a, b = q_starts[r], q_starts[r + 1]
+        for i in range(b - a):
+            if i >= 64:
+                masks[a + i], positions[a + i] = 0, 0
+                continue
+            bits, j = 0, i
+            while j >= 0:
+                bits |= 1 << j
+                up = parents[a + j]
+                j = up if 0 <= up < j else -1
+            masks[a + i] = bits
+            positions[a + i] = max(0, max(0, length) - (b - a) + bin(bits).count("1") - 1)
+    return masks, positions
+
+
+def adapters(x, y, a, b, q_starts, adapter, ranks, scales):
+    """y [T][N] + scale (x A^T) B^T with each request's adapter; x [T][K], a [adapters][rank][K], b [adapters][N][rank]."""
+    out = np.array(y, dtype=np.float64)
+    for r, i in enumerate(adapter):
+        if 0 <= i < len(a):
+            rows = slice(q_starts[r], q_starts[r + 1])
+            h = x[rows] @ a[i][:ranks[i]].T
+            out[rows] += scales[i] * (h @ b[i][:, :ranks[i]].T)
+    return out

@@ -1,6 +1,6 @@
 """Build liblogbq.so in-tree: the host fit with g++, the gfx950 kernels with hipcc (the linears and
-the quantizer in logbq_kernels.hip, the serving operators in serving_kernels.hip
-and kv4_attention.hip). Also builds
+the quantizer in logbq_kernels.hip, the serving operators in serving_kernels.hip, kv4_attention.hip,
+kv4_tree.hip, rotate_kernels.hip and adapter_kernels.hip). Also builds
 libhbmread.so, the streaming-read kernel bench.py measures the HBM read ceiling with.
 
 The host fit is compiled without -ffast-math and with -ffp-contract=off so that its float64
@@ -10,6 +10,7 @@ disabled (-Xclang -target-feature -Xclang -packed-fp32-ops).
 import os
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -39,7 +40,8 @@ def _run(cmd, verbose):
     subprocess.run(cmd, check=True)
 
 
-KERNEL_SOURCES = ("logbq_kernels", "serving_kernels", "kv4_attention")
+KERNEL_SOURCES = ("logbq_kernels", "serving_kernels", "kv4_attention", "kv4_tree", "rotate_kernels",
+                  "adapter_kernels")
 
 
 def build(verbose: bool = False) -> str:
@@ -47,8 +49,11 @@ def build(verbose: bool = False) -> str:
     fit_o = os.path.join(BUILD, "fit.o")
     ker_o = [os.path.join(BUILD, name + ".o") for name in KERNEL_SOURCES]
     _run(["g++", *HOST_FLAGS, "-c", os.path.join(CSRC, "fit.cpp"), "-o", fit_o], verbose)
-    for name, obj in zip(KERNEL_SOURCES, ker_o):
-        _run([HIPCC, *HIP_FLAGS, "-c", os.path.join(CSRC, name + ".hip"), "-o", obj], verbose)
+    # A compiler a source; the largest takes as long as the others together.
+    with ThreadPoolExecutor(4) as pool:
+        for done in [pool.submit(_run, [HIPCC, *HIP_FLAGS, "-c", os.path.join(CSRC, name + ".hip"), "-o", obj], verbose)
+                     for name, obj in zip(KERNEL_SOURCES, ker_o)]:
+            done.result()
     tmp = LIB + ".tmp"
     _run([HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, fit_o, *ker_o], verbose)
     os.replace(tmp, LIB)

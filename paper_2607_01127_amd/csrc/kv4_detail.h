@@ -1,4 +1,5 @@
-// Private to the serving operators' kernels: element types, and the 4-bit cache as kernels take it.
+// Private to the serving operators' kernels: element types, the 4-bit cache as kernels take it, and how
+// a row becomes codes.
 #ifndef KV4_DETAIL_H
 #define KV4_DETAIL_H
 
@@ -104,10 +105,75 @@ __device__ __forceinline__ int64_t scale_index(const Kv4& c, int64_t slot, int h
   return ((page * c.heads + head) << c.page_shift) + (slot & ((1 << c.page_shift) - 1));
 }
 
+// 16 lanes take a row: lane c has channels c D/16 .. (c + 1) D/16 - 1, one group of the value layout.
+constexpr int kRowLanes = 16;
+
+// N codes of 4 bits as N / 8 words (N = 4: the low half of one word).
+template <int N>
+__device__ __forceinline__ void store_codes(uint8_t* to, const uint32_t (&w)[(N + 7) / 8]) {
+  if (N == 4) *reinterpret_cast<uint16_t*>(to) = (uint16_t)w[0];
+  else if (N == 8) *reinterpret_cast<uint32_t*>(to) = w[0];
+  else *reinterpret_cast<u32x2*>(to) = u32x2{w[0], w[(N + 7) / 8 - 1]};
+}
+
+// Largest value of the 16 lanes of a row.
+__device__ __forceinline__ uint32_t row_max(uint32_t v) {
+  // Rotations within 16 lanes by 8, 4, 2 and 1.
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x128, 0xf, 0xf, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x124, 0xf, 0xf, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x122, 0xf, 0xf, true));
+  return max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x121, 0xf, 0xf, true));
+}
+
+// Codes of one row: the scale is the smallest bfloat16 s with 6 s >= max |x|, found from the
+// truncated quotient with one exact comparison (6 s has at most 11 significant bits), and the
+// magnitudes compare |x| with t s (at most 11 bits too), so no rounding enters a code.
+template <int D, bool VALUES>
+__device__ __forceinline__ void append_row(const float (&x)[D / 16], const Kv4& c, int64_t slot, int head,
+                                           int group) {
+  constexpr int N = D / 16;
+  uint32_t top = 0;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const uint32_t u = __float_as_uint(x[j]) & 0x7fffffffu;
+    top = u < 0x7f800000u && u > top ? u : top;
+  }
+  const float size = __uint_as_float(row_max(top));
+  uint32_t s = __float_as_uint(size / 6.0f) & 0xffff0000u;
+  if (6.0f * __uint_as_float(s) < size) s += 0x10000u;
+  const float scale = __uint_as_float(s);
+  constexpr float kThr[7] = {0.25f, 0.75f, 1.25f, 1.75f, 2.5f, 3.5f, 5.0f};
+  uint32_t w[(N + 7) / 8] = {};
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const float ax = __builtin_fabsf(x[j]);
+    uint32_t mag = 0;
+#pragma unroll
+    for (int t = 0; t < 7; ++t) mag += ax >= kThr[t] * scale ? 1u : 0u;
+    mag = s ? mag : 0u;
+    const uint32_t sign = x[j] < 0.0f && mag ? 8u : 0u;
+    w[j / 8] |= (mag | sign) << (4 * (j % 8));
+  }
+  store_codes<N>((VALUES ? c.v_codes : c.k_codes) + code_offset<D, VALUES>(c, slot, head, group), w);
+  if (group == 0) (VALUES ? c.v_scales : c.k_scales)[scale_index(c, slot, head)] = (uint16_t)(s >> 16);
+}
+
 // float32 value of a code (the low 4 bits).
 __device__ __forceinline__ float code_value(uint32_t code) {
   const half2v pair = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(code, 1.0f, 0);
   return (float)pair.x;
+}
+
+// Whether a call would write what it reads: its workgroups have no order among them.
+struct Range { const void* at; int64_t bytes; };
+template <int N, int M>
+bool any_overlap(const Range (&in)[N], const Range (&out)[M]) {
+  for (const Range& i : in)
+    for (const Range& o : out)
+      if (i.bytes > 0 && o.bytes > 0 && (uintptr_t)i.at < (uintptr_t)o.at + o.bytes &&
+          (uintptr_t)o.at < (uintptr_t)i.at + i.bytes)
+        return true;
+  return false;
 }
 
 // The cache as the kernels take it; LOGBQ_OK or what is wrong with it.

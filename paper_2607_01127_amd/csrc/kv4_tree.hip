@@ -1,0 +1,710 @@
+// gfx950 kernels of attention of drafted trees over the 4-bit paged cache, and their entry point of the C
+// ABI.
+//
+//   k_kv4_tree       up to 128 query rows of a request and key/value head a workgroup, converted keys and
+//                    values in LDS, the positions of the whole batch dealt out evenly.
+//   k_kv4_tree_join  sums the parts of what more than one workgroup had.
+
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+#include <type_traits>
+
+#include "kv4_attention_detail.h"
+#include "kv4_detail.h"
+#include "logbq.h"
+
+namespace {
+
+// ------------------------------------------------------------------ tiles of 64 positions
+// All four wavefronts of a workgroup turn a tile's codes into float16 and bfloat16 operands in LDS, in the
+// order in which 32x32x16 MFMAs read them; a wavefront then has 32 query rows against 32 positions at a
+// time: S^T = K Q^T and O^T = V^T P^T, where a lane's 8 weights of 16 positions are the second product's B
+// operand as they are. Tiles are double buffered: the next tile's codes are loaded before this one's
+// products and converted after them, one barrier a tile.
+constexpr int kTileThreads = 256;
+constexpr int kTilePositions = 64;
+constexpr int kTileRows = 128;                // query rows of a workgroup at most, 32 a wavefront
+
+template <int D>
+struct TileBuffers {
+  half8v k[2][2 * (D / 16) * 64];
+  bf16x8 v[2][(D / 32) * 4 * 64];
+  float vscale[2][kTilePositions];
+  uint64_t rest[2];
+  int again;                  // a wavefront has met what is to be taken with care
+
+  __device__ __forceinline__ void set_again() {
+    __hip_atomic_store(&again, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+  }
+};
+
+// A lane's query row (lanes 32 apart share one), and its sums.
+template <int D, bool QSPLIT>
+struct QueryRow {
+  static constexpr int kKc = D / 16, kCb = D / 32;
+  half8v hi[kKc], lo[QSPLIT ? kKc : 1];
+  float qs, ref, sum;         // what scores are multiplied by, in powers of two; reference and sum of weights
+  float16v o[kCb];
+
+  // Scaled by a power of two so that float16 holds them; the sign of the scale goes into the queries.
+  __device__ __forceinline__ void load(const AttnArgs& a, int64_t at, bool present) {
+    float x[kKc][8];
+    float most = 0.0f;
+#pragma unroll
+    for (int c = 0; c < kKc; ++c) {
+      if (present) {
+        if (a.q_dtype == LOGBQ_DTYPE_F32) load_row<LOGBQ_DTYPE_F32>(a.q, at + 16 * c, x[c]);
+        else if (a.q_dtype == LOGBQ_DTYPE_F16) load_row<LOGBQ_DTYPE_F16>(a.q, at + 16 * c, x[c]);
+        else load_row<LOGBQ_DTYPE_BF16>(a.q, at + 16 * c, x[c]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[c][j] = 0.0f;
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) most = fmaxf(most, __builtin_fabsf(x[c][j]));
+    }
+    most = fmaxf(most, __shfl_xor(most, 32));
+    const int e = most > 0.0f && most < INFINITY ? (int)(__float_as_uint(most) >> 23) - 127 : 0;
+    const float down = ldexpf(a.scale < 0.0f ? -1.0f : 1.0f, -e);
+    qs = __builtin_fabsf(a.scale) * kLog2e * ldexpf(1.0f, e);
+#pragma unroll
+    for (int c = 0; c < kKc; ++c)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float y = x[c][j] * down;
+        hi[c][j] = (half_t)y;
+        if constexpr (QSPLIT) lo[c][j] = (half_t)(y - (float)(half_t)y);
+      }
+  }
+  __device__ __forceinline__ void clear() {
+    ref = kNone;
+    sum = 0.0f;
+#pragma unroll
+    for (int c = 0; c < kCb; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[c][i] = 0.0f;
+  }
+
+  // 32 positions of a tile, the first or second of it. seen_at(i): whether the row sees position
+  // i + 4 * (lane / 32) of them; it is asked only where `full` is not set.
+  template <class Seen, class Careful>
+  __device__ __forceinline__ void take(TileBuffers<D>& lds, int buf, int pb, int ek, bool full, Seen&& seen_at,
+                                       Careful) {
+    constexpr bool kCareful = Careful::value;
+    const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+    float16v s;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+#pragma unroll
+    for (int c = 0; c < kKc; ++c) {
+      const half8v kf = lds.k[buf][(pb * kKc + c) * 64 + lane];
+      s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, hi[c], s, 0, 0, 0);
+      if constexpr (QSPLIT)
+        s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, lo[c], s, 0, 0, 0);
+    }
+    bf16x8 wh[2], wl[2];
+    f32x4 vs[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      vs[i] = *reinterpret_cast<const f32x4*>(&lds.vscale[buf][32 * pb + 8 * i + 4 * half]);
+    // By ldexp, as 2^ek alone may be below float32's normal numbers.
+    const float f = ldexpf(qs, ek);
+    const auto weigh = [&](auto all_seen) {
+      constexpr bool kAll = decltype(all_seen)::value;
+      bool seen[16];
+      if constexpr (!kAll) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          seen[i] = seen_at(8 * (i >> 2) + (i & 3));
+          s[i] = seen[i] ? s[i] : -INFINITY;
+        }
+      }
+      float top = s[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+      // A row that sees none of the tile keeps its reference.
+      const float reach = !kAll && top == -INFINITY ? kNone : top * f;
+      if (__builtin_amdgcn_ballot_w64(reach - ref > 8.0f)) {
+        const float most = fmaxf(reach, __shfl_xor(reach, 32));
+        const float next = most - ref > 8.0f ? most : ref;
+        const float g = exp2_fast(ref - next);
+        if constexpr (!kCareful)
+          if (__builtin_amdgcn_ballot_w64(next != kNone && __builtin_fabsf(next) > kFar)) lds.set_again();
+        ref = next;
+        sum *= g;
+#pragma unroll
+        for (int c = 0; c < kCb; ++c) o[c] *= g;
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int i = 8 * h + j;
+          float e = exp2_fast(exponent<kCareful>(s[i], f, ref));
+          if constexpr (!kAll) e = seen[i] ? e : 0.0f;
+          sum += e;
+          w[j] = kAll || seen[i] ? e * vs[i >> 2][i & 3] : 0.0f;
+        }
+        split_weights(w, wh[h], wl[h]);
+      }
+    };
+    if (full) weigh(std::true_type{});
+    else weigh(std::false_type{});
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      bf16x8 vf[kCb];
+#pragma unroll
+      for (int c = 0; c < kCb; ++c) vf[c] = lds.v[buf][value_slot(c * 4 + 2 * pb + h, 2 * pb + h, half, col)];
+#pragma unroll
+      for (int c = 0; c < kCb; ++c)
+        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[c], wl[h], o[c], 0, 0, 0);
+#pragma unroll
+      for (int c = 0; c < kCb; ++c)
+        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[c], wh[h], o[c], 0, 0, 0);
+    }
+  }
+};
+
+// Loading and converting tiles. A thread has 32 channels of one position's keys (D = 256: twice), and 4
+// positions of 8 channels of values (D = 256: 16 channels); at D = 64 half of the threads have keys and the
+// others 8 positions of 4 channels of values.
+template <int D, bool ONE_PAGE>
+struct TileReader {
+  static constexpr bool kSplitWaves = D == 64;
+  static constexpr int kKc = D / 16, kItems = D == 256 ? 2 : 1;
+  const AttnArgs& a;
+  TileBuffers<D>& lds;
+  const int32_t* table;                        // of the request
+  int head, kv_end, ek;                        // ek: exponent that the keys' scales are divided by
+  int page_mask;
+  int64_t pages;
+
+  // A thread's part of a tile, computed anew for each tile: kept, it would take registers that the products need.
+  struct Part {
+    int lane, wave, key_pos, key_item, v_block, v_group, v_half;
+    bool has_keys, has_values;
+    __device__ __forceinline__ Part() {
+      const int tid = here(threadIdx.x);
+      lane = tid & 63;
+      wave = tid >> 6;
+      has_keys = !kSplitWaves || wave < 2;
+      has_values = !kSplitWaves || wave >= 2;
+      key_pos = kSplitWaves ? (wave & 1) * 32 + (lane & 31) : wave * 16 + (lane & 15);
+      key_item = kSplitWaves ? lane >> 5 : lane >> 4;
+      v_block = kSplitWaves ? lane >> 3 : (lane >> 1) & 7;            // of 8 positions
+      v_group = kSplitWaves ? (wave & 1) * 8 + (lane & 7) : wave * 4 + (lane >> 5) * 2 + (lane & 1);
+      v_half = kSplitWaves ? 0 : (lane >> 4) & 1;
+    }
+  };
+
+  __device__ __forceinline__ TileReader(const AttnArgs& args, TileBuffers<D>& buffers, const int32_t* pages_of,
+                                        int kv_head, int end)
+      : a(args), lds(buffers), table(pages_of), head(kv_head), kv_end(end), ek(-200) {
+    page_mask = (1 << a.c.page_shift) - 1;
+    pages = a.c.slots >> a.c.page_shift;
+  }
+
+  struct Ids { int32_t lane, key, value; };
+  struct Raw {
+    u32x4 k[kItems], v[kItems];
+    uint16_t ks, lane_ks, lane_vs;           // of its keys' position, and of position `lane`
+    uint64_t valid;                          // positions of the tile that can be seen
+    bool key_ok;
+  };
+  __device__ __forceinline__ Ids load_ids(int base) const {
+    const Part me;
+    Ids ids;
+    const auto id_at = [&](int p) { return p < kv_end ? table[p >> a.c.page_shift] : -1; };
+    ids.lane = id_at(ONE_PAGE ? base : base + me.lane);
+    ids.key = ONE_PAGE ? ids.lane : id_at(base + me.key_pos);
+    ids.value = ONE_PAGE ? ids.lane : id_at(base + 8 * me.v_block);
+    return ids;
+  }
+  __device__ __forceinline__ Raw load_raw(int base, const Ids& ids) const {
+    const Part me;
+    Raw t;
+    // A row's place: scalar for the tile where it lies in one page, with a lane's offset.
+    const int32_t tile_id = __builtin_amdgcn_readfirstlane(ids.lane);
+    const int32_t tile_page = tile_id >= 0 && tile_id < pages ? tile_id : 0;
+    const int64_t tile_row = (((int64_t)tile_page * a.c.heads + head) << a.c.page_shift) + (base & page_mask);
+    const auto ok = [&](int32_t id) { return id >= 0 && id < pages; };
+    const auto place = [&](const auto* buffer, int row_size, int32_t id, int p, int offset) {
+      if constexpr (ONE_PAGE) return buffer + tile_row * row_size + (p * row_size + offset);
+      const int32_t page = ok(id) ? id : 0;
+      const int64_t row = (((int64_t)page * a.c.heads + head) << a.c.page_shift) + ((base + p) & page_mask);
+      return buffer + row * row_size + offset;
+    };
+    t.lane_ks = *place(a.c.k_scales, 1, ids.lane, me.lane, 0);
+    t.lane_vs = *place(a.c.v_scales, 1, ids.lane, me.lane, 0);
+    t.valid = __builtin_amdgcn_ballot_w64(ok(ids.lane) && base + me.lane < kv_end);
+    t.key_ok = ok(ids.key);
+    if (me.has_keys) {
+      t.ks = *place(a.c.k_scales, 1, ids.key, me.key_pos, 0);
+#pragma unroll
+      for (int i = 0; i < kItems; ++i)
+        t.k[i] = *reinterpret_cast<const u32x4*>(place(a.c.k_codes, D / 2, ids.key, me.key_pos, (me.key_item + 4 * i) * 16));
+    }
+    if (me.has_values) {
+      const uint8_t* from = place(a.c.v_codes, D / 2, ids.value, 8 * me.v_block, me.v_group * (D / 4) + me.v_half * (D / 8));
+#pragma unroll
+      for (int i = 0; i < kItems; ++i) t.v[i] = *reinterpret_cast<const u32x4*>(from + 16 * i);
+    }
+    return t;
+  }
+  // With care, returns the positions that are left for another time; lds.rest has the same, from one
+  // wavefront, for the number of times that all go round, which no change of the cache meanwhile may
+  // set apart.
+  template <class Careful>
+  __device__ __forceinline__ uint64_t convert(const Raw& t, int buf, Careful) {
+    constexpr bool kCareful = Careful::value;
+    const Part me;
+    // The exponent first; every wavefront sees all 64 scales, so all come to the same one. Positions
+    // that no row sees, and scales of 0, have no part in it.
+    const bool seen = (t.valid >> me.lane) & 1;
+    const bool counts = seen && (t.lane_ks & 0x7fff);
+    const int xk = (int)(t.lane_ks >> 7 & 0xff) - 127;
+    uint64_t rest = 0;
+    if (__builtin_amdgcn_ballot_w64(counts && (unsigned)(xk - ek + 13) > 25u)) {
+      int most = counts ? xk : -1000;
+      for (int d = 1; d < 64; d <<= 1) most = max(most, __shfl_xor(most, d));
+      rest = __builtin_amdgcn_ballot_w64(counts && xk < most - 25);
+      if constexpr (!kCareful)
+        if (rest) lds.set_again();
+      // Room for the largest to grow by 2 binades, where the smallest leaves it.
+      ek = __builtin_amdgcn_readfirstlane(most) - (__builtin_amdgcn_ballot_w64(counts && xk < most - 23) ? 12 : 10);
+    }
+    if constexpr (kCareful)
+      if (threadIdx.x == 0) lds.rest[buf] = rest;
+    if (me.wave == 0) lds.vscale[buf][me.lane] = seen ? bf16_value(t.lane_vs) : 0.0f;
+    if (me.has_keys) {
+      const half_t s = (half_t)(t.key_ok ? ldexpf(bf16_value(t.ks), -ek) : 0.0f);
+      const half8v s8 = {s, s, s, s, s, s, s, s};
+#pragma unroll
+      for (int i = 0; i < kItems; ++i)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const int chunk = 2 * (me.key_item + 4 * i) + (c >> 1), h = c & 1;
+          lds.k[buf][((me.key_pos >> 5) * kKc + chunk) * 64 + h * 32 + (me.key_pos & 31)] = values_of(t.k[i][c]) * s8;
+        }
+    }
+    if (me.has_values) {
+      const int chunk = me.v_block >> 1;
+      const auto put = [&](int channel, int h, bf16x2 x01, bf16x2 x23) {
+        bf16x2* to = reinterpret_cast<bf16x2*>(&lds.v[buf][value_slot((channel >> 5) * 4 + chunk, chunk, h, channel & 31)]) +
+                     2 * (me.v_block & 1);
+        *reinterpret_cast<bf16x4*>(to) = bf16x4{x01.x, x01.y, x23.x, x23.y};
+      };
+      constexpr uint32_t kLow = 0x0f0f0f0fu;
+      if constexpr (D == 64) {
+        // Word q: positions 2q and 2q + 1, 4 channels each.
+        uint32_t even[4], odd[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const uint32_t x = t.v[0][q] & kLow, y = (t.v[0][q] >> 4) & kLow;
+          even[q] = x | (x >> 12);
+          odd[q] = y | (y >> 12);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          put(4 * me.v_group, h, fp4_pair<0>(even[2 * h]), fp4_pair<0>(even[2 * h + 1]));
+          put(4 * me.v_group + 1, h, fp4_pair<0>(odd[2 * h]), fp4_pair<0>(odd[2 * h + 1]));
+          put(4 * me.v_group + 2, h, fp4_pair<1>(even[2 * h]), fp4_pair<1>(even[2 * h + 1]));
+          put(4 * me.v_group + 3, h, fp4_pair<1>(odd[2 * h]), fp4_pair<1>(odd[2 * h + 1]));
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+          // Position j's word of 8 channels.
+          uint32_t w[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            w[j] = D == 256 ? t.v[j >> 1][2 * (j & 1) + i] : t.v[0][j];
+          const uint32_t e01 = (w[0] & kLow) | ((w[1] << 4) & ~kLow), o01 = ((w[0] >> 4) & kLow) | (w[1] & ~kLow);
+          const uint32_t e23 = (w[2] & kLow) | ((w[3] << 4) & ~kLow), o23 = ((w[2] >> 4) & kLow) | (w[3] & ~kLow);
+          const int ch = me.v_group * (D / 16) + 8 * i;
+          put(ch, me.v_half, fp4_pair<0>(e01), fp4_pair<0>(e23));
+          put(ch + 1, me.v_half, fp4_pair<0>(o01), fp4_pair<0>(o23));
+          put(ch + 2, me.v_half, fp4_pair<1>(e01), fp4_pair<1>(e23));
+          put(ch + 3, me.v_half, fp4_pair<1>(o01), fp4_pair<1>(o23));
+          put(ch + 4, me.v_half, fp4_pair<2>(e01), fp4_pair<2>(e23));
+          put(ch + 5, me.v_half, fp4_pair<2>(o01), fp4_pair<2>(o23));
+          put(ch + 6, me.v_half, fp4_pair<3>(e01), fp4_pair<3>(e23));
+          put(ch + 7, me.v_half, fp4_pair<3>(o01), fp4_pair<3>(o23));
+        }
+      }
+    }
+    return kCareful ? rest : 0;
+  }
+
+  // The tiles of positions from .. stop (stop > from, a multiple of 64 apart): compute(base, positions that
+  // are valid, ek, buffer, careful) for each. The workgroup's threads come here together.
+  template <class Careful, class Compute>
+  __device__ __forceinline__ void go_over(int from, int stop, Compute&& compute, Careful careful) {
+    constexpr bool kCareful = Careful::value;
+    int base = from;
+    Raw raw = load_raw(base, load_ids(base));
+    Ids ids = load_ids(base + kTilePositions);
+    uint64_t valid = raw.valid & ~convert(raw, 0, careful);
+    int buf = 0, ek_of = ek;
+    __syncthreads();
+    while (base < stop) {
+      int next = base + kTilePositions;
+      if (next < stop) {
+        raw = load_raw(next, ids);
+        ids = load_ids(next + kTilePositions);
+      }
+      compute(base, valid, ek_of, buf, careful);
+      if constexpr (kCareful) {
+        const uint64_t held = lds.rest[buf];
+        const uint64_t rest = (uint64_t)__builtin_amdgcn_readfirstlane((int)(held >> 32)) << 32 |
+                              (uint32_t)__builtin_amdgcn_readfirstlane((int)held);
+        if (rest) {                     // the tile again, for these
+          next = base;
+          raw = load_raw(base, load_ids(base));
+          raw.valid = rest;
+          ids = load_ids(base + kTilePositions);
+        }
+      }
+      if (next < stop) {
+        valid = raw.valid & ~convert(raw, buf ^ 1, careful);
+        ek_of = ek;
+      }
+      base = next;
+      buf ^= 1;
+      __syncthreads();
+    }
+  }
+};
+
+// ------------------------------------------------------------------ trees
+// A node sees the cached positions (in a window, those that its own position reaches) and its ancestors'.
+// An item is up to 128 query rows (nodes x the query heads of one key/value head) of a request against all
+// of its positions. The items' units of positions are cut into equal shares, one a workgroup; a piece that
+// does not have all of its item's positions goes to the workspace for k_kv4_tree_join.
+//
+// A piece of 32 rows or fewer leaves three wavefronts without rows, one of 64 two: then wavefronts share the
+// rows and have a half of each tile's positions, and their sums are added up in LDS at the end.
+constexpr int kTreeMinShare = 2;              // units of a workgroup at least
+constexpr int kMaxNodes = 64;
+
+template <int D, bool QSPLIT, bool ONE_PAGE>
+__global__ __launch_bounds__(kTileThreads, D <= 128 ? 2 : 1)
+void k_kv4_tree(AttnArgs a, const uint64_t* masks) {
+  constexpr int kRows = kTileRows, kCb = D / 32;
+  __shared__ TileBuffers<D> lds;
+  __shared__ int32_t scan[4];
+  __shared__ int32_t found[2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int col = lane & 31, half = lane >> 5;
+  const auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+
+  // ---- this workgroup's part of all items' units (the host has seen that they fit 31 bits)
+  struct Items { int units, row_tiles, from; };          // of one item; of a request and head; first position
+  const auto items_of = [&](const Request& q) {
+    Items i;
+    i.from = q.from & ~(kTilePositions - 1);
+    i.row_tiles = (q.n * a.group + kRows - 1) / kRows;
+    i.units = q.end > i.from ? (unsigned)(q.end - i.from + a.unit - 1) / (unsigned)a.unit : 1;   // at least zeros to write
+    return i;
+  };
+  const auto units_of = [&](int r) {
+    const Items i = items_of(request_of(a, r));
+    return i.units * i.row_tiles * a.c.heads;
+  };
+  const int per = (a.requests + kTileThreads - 1) / kTileThreads;
+  const int r0 = tid * per < a.requests ? tid * per : a.requests;
+  const int r1 = r0 + per < a.requests ? r0 + per : a.requests;
+  int mine = 0;
+  for (int r = r0; r < r1; ++r) mine += units_of(r);
+  int upto = mine;
+  for (int d = 1; d < 64; d <<= 1) {
+    const int x = __shfl_up(upto, d);
+    if (lane >= d) upto += x;
+  }
+  if (lane == 63) scan[wave] = upto;
+  __syncthreads();
+  int total = 0;
+  for (int w = 0; w < kTileThreads / 64; ++w) {
+    if (w < wave) upto += scan[w];
+    total += scan[w];
+  }
+  total = uniform(total);
+  // Workgroups with work: the first `rest` of them have one unit more.
+  const int wanted = (total + kTreeMinShare - 1) / kTreeMinShare;
+  const int parts = wanted < a.parts ? wanted : a.parts;
+  const int w = blockIdx.x;
+  int32_t* desc = a.desc + 4 * (int64_t)w;
+  if (tid == 0) desc[0] = 0;
+  if (w >= parts) return;
+  const int share = (unsigned)total / (unsigned)parts, rest = total - share * parts;
+  int u = w * share + (w < rest ? w : rest);
+  const int u_end = u + share + (w < rest ? 1 : 0);
+  if (upto - mine <= u && u < upto) {
+    int at = upto - mine;
+    for (int r = r0; r < r1; ++r) {
+      const int n = units_of(r);
+      if (u < at + n) {
+        found[0] = r;
+        found[1] = u - at;
+        break;
+      }
+      at += n;
+    }
+  }
+  __syncthreads();
+  int r = uniform(found[0]), off = uniform(found[1]);
+
+  // ---- pieces: the units of one item that the workgroup has
+  while (u < u_end) {
+    Request req = request_of(a, r);
+    Items items = items_of(req);
+    while (off >= items.units * items.row_tiles * a.c.heads) {
+      off -= items.units * items.row_tiles * a.c.heads;
+      req = request_of(a, ++r);
+      items = items_of(req);
+    }
+    const int item = (unsigned)off / (unsigned)items.units, unit0 = off - item * items.units;
+    const int unit1 = u_end - u < items.units - unit0 ? unit0 + u_end - u : items.units;
+    const int head = (unsigned)item / (unsigned)items.row_tiles, row0 = (item - head * items.row_tiles) * kRows;
+    const int piece_u = u;
+    off += unit1 - unit0;
+    u += unit1 - unit0;
+
+    // ---- rows: sharers of each 32 of them, and the halves of a tile that a wavefront has
+    const int rows = req.n * a.group - row0 < kRows ? req.n * a.group - row0 : kRows;
+    const int row_waves = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+    const int share_of = wave / row_waves, wave_row = (wave & (row_waves - 1)) * 32;
+    const int pb0 = row_waves == 4 ? 0 : share_of, pb1 = row_waves == 4 ? 2 : share_of + 1;
+    const bool busy = share_of < 2 && wave_row < rows;
+    const int row = wave_row + col, token = (row0 + row) / a.group;
+    const bool has_row = row < rows;
+    const int64_t place = (int64_t)(req.t0 + token) * (a.c.heads * a.group) + head * a.group + (row0 + row) % a.group;
+    QueryRow<D, QSPLIT> mine_of;
+    mine_of.load(a, (int64_t)(req.t0 + token) * a.q_stride + (int64_t)(head * a.group + (row0 + row) % a.group) * D + half * 8,
+                 has_row && busy);
+    const uint64_t mask = has_row ? masks[req.t0 + token] : 0;
+    // The first position that the row's window holds; nodes lie at req.first and after.
+    const int depth = mask ? __popcll(mask) - 1 : 0;
+    const int64_t window_from = a.window ? (int64_t)req.first + depth - a.window + 1 : 0;
+
+    if (tid == 0) lds.again = 0;
+    __syncthreads();
+    TileReader<D, ONE_PAGE> reader(a, lds, a.table + (int64_t)r * a.width, head, req.end);
+    const int from = items.from + unit0 * a.unit;
+    const int unit_stop = items.from + unit1 * a.unit;
+    const int stop = unit_stop < req.end ? unit_stop : req.end;
+    const auto compute = [&](int base, uint64_t valid, int ek, int buf, auto careful) {
+      if (!busy || valid == 0) return;
+      // Whether every row sees all of the tile: cached positions, in reach of the deepest node's window.
+      const bool full = valid == ~0ull && base + kTilePositions <= req.first &&
+                        (!a.window || base > (int64_t)req.first + kMaxNodes - 1 - a.window);
+      uint64_t seen = valid;
+      if (!full) {
+        const int to_nodes = req.first - base;           // of the tile's positions, those before the nodes
+        const uint64_t cached = to_nodes >= 64 ? ~0ull : to_nodes > 0 ? (1ull << to_nodes) - 1 : 0;
+        const int64_t skip = window_from - base;
+        const uint64_t reach = skip <= 0 ? ~0ull : skip < 64 ? ~0ull << skip : 0;
+        const uint64_t nodes = to_nodes >= 64 || to_nodes <= -64 ? 0 : to_nodes >= 0 ? mask << to_nodes : mask >> -to_nodes;
+        seen &= (cached & reach) | nodes;
+      }
+#pragma unroll 1
+      for (int pb = pb0; pb < pb1; ++pb) {
+        const uint32_t bits = (uint32_t)(seen >> (32 * pb)) >> (4 * half);
+        mine_of.take(lds, buf, pb, ek, full, [&](int at) { return (bits >> at & 1u) != 0; }, careful);
+      }
+    };
+    const auto go_over = [&](auto careful) {
+      mine_of.clear();
+      if (from < stop) reader.go_over(from, stop, compute, careful);
+    };
+    go_over(std::false_type{});         // its last barrier is after the last time that `again` is set
+    if (uniform(lds.again)) go_over(std::true_type{});
+
+    // ---- a row's sums of two wavefronts together; the tiles' buffers are free after the last barrier
+    float sum = mine_of.sum + __shfl_xor(mine_of.sum, 32);
+    if (row_waves < 4) {
+      f32x4* shared_o = reinterpret_cast<f32x4*>(lds.k);
+      float* shared_rl = lds.vscale[0];               // 64 rows' references, then 64 rows' sums
+      static_assert(sizeof(lds.k) >= 64 * D * 4 && sizeof(lds.vscale) >= 64 * 2 * 4, "the sums of 64 rows fit");
+      if (busy && share_of == 1) {
+#pragma unroll
+        for (int c = 0; c < kCb; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            shared_o[((c * 4 + i) * 2 + half) * 64 + row] =
+                f32x4{mine_of.o[c][4 * i], mine_of.o[c][4 * i + 1], mine_of.o[c][4 * i + 2], mine_of.o[c][4 * i + 3]};
+        if (half == 0) {
+          shared_rl[row] = mine_of.ref;
+          shared_rl[64 + row] = sum;
+        }
+      }
+      __syncthreads();
+      if (busy && share_of == 0) {
+        const float other = shared_rl[row], top = fmaxf(mine_of.ref, other);
+        const float f = exp2_fast(mine_of.ref - top), g = exp2_fast(other - top);
+        sum = sum * f + shared_rl[64 + row] * g;
+        mine_of.ref = top;
+#pragma unroll
+        for (int c = 0; c < kCb; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const f32x4 v = shared_o[((c * 4 + i) * 2 + half) * 64 + row];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mine_of.o[c][4 * i + j] = mine_of.o[c][4 * i + j] * f + v[j] * g;
+          }
+      }
+      __syncthreads();
+    }
+
+    // ---- out: a lane has 4 consecutive channels of its row at a time
+    const bool whole = unit0 == 0 && unit1 == items.units;
+    const int64_t slot = 2 * (int64_t)w + (unit0 == 0 ? 1 : 0);
+    if (busy && share_of == 0 && has_row) {
+      const float inv = !whole ? 1.0f : sum != 0.0f ? 1.0f / sum : 0.0f;
+#pragma unroll
+      for (int c = 0; c < kCb; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const f32x4 v = {mine_of.o[c][4 * i] * inv, mine_of.o[c][4 * i + 1] * inv, mine_of.o[c][4 * i + 2] * inv,
+                           mine_of.o[c][4 * i + 3] * inv};
+          const int ch = 32 * c + 8 * i + 4 * half;
+          if (whole) store_four(a.out, a.out_dtype, place * D + ch, v);
+          else *reinterpret_cast<f32x4*>(a.part_o + (slot * kRows + row) * D + ch) = v;
+        }
+      if (half == 0) {
+        if (!whole) {
+          a.part_rl[(slot * kRows + row) * 2] = mine_of.ref;
+          a.part_rl[(slot * kRows + row) * 2 + 1] = sum;
+        } else if (a.lse) {
+          a.lse[place] = sum != 0.0f ? (mine_of.ref + __log2f(sum)) * kLn2 : -INFINITY;
+        }
+      }
+    }
+    if (!whole && unit0 == 0 && tid == 0) {
+      // The item begins here: parts 2 w + 1, then 2 (w + 1), ... of the workgroups up to the one that has
+      // the last unit.
+      const int last_unit = piece_u + items.units - 1, more_units = rest * (share + 1);
+      const int w1 = last_unit < more_units ? last_unit / (share + 1) : rest + (last_unit - more_units) / share;
+      desc[0] = w1 - w + 1;
+      desc[1] = r;
+      desc[2] = head;
+      desc[3] = row0;
+    }
+  }
+}
+
+// D / 4 threads have 4 channels each of a query row; kSlices such groups have every kSlices-th part of it.
+template <int D>
+__global__ __launch_bounds__(kTileThreads) void k_kv4_tree_join(AttnArgs a) {
+  constexpr int kRows = kTileRows, kSlices = 4, kPer = kTileThreads / (D / 4) / kSlices;
+  __shared__ f32x4 sums[kSlices][kPer][D / 4];
+  __shared__ float tops[kSlices][kPer], dens[kSlices][kPer];
+  const int64_t w = blockIdx.x;
+  const int32_t* desc = a.desc + 4 * w;
+  const int parts = desc[0];
+  if (parts < 2) return;
+  const Request req = request_of(a, desc[1]);
+  const int head = desc[2], row0 = desc[3];
+  const int rows = req.n * a.group - row0 < kRows ? req.n * a.group - row0 : kRows;
+  if ((int)blockIdx.y * kPer >= rows) return;
+  const int ch = threadIdx.x % (D / 4), sub = threadIdx.x / (D / 4) % kPer, slice = threadIdx.x / (D / 4) / kPer;
+  const int row = blockIdx.y * kPer + sub;
+  float top = kNone, den = 0.0f;
+  f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (row < rows) {
+    for (int i = slice; i < parts; i += kSlices) {
+      const int64_t slot = i == 0 ? 2 * w + 1 : 2 * (w + i);
+      top = fmaxf(top, a.part_rl[(slot * kRows + row) * 2]);
+    }
+#pragma unroll 4
+    for (int i = slice; i < parts; i += kSlices) {
+      const int64_t slot = i == 0 ? 2 * w + 1 : 2 * (w + i);
+      const float f = exp2_fast(a.part_rl[(slot * kRows + row) * 2] - top);
+      den += a.part_rl[(slot * kRows + row) * 2 + 1] * f;
+      v += *reinterpret_cast<const f32x4*>(a.part_o + (slot * kRows + row) * D + 4 * ch) * f;
+    }
+  }
+  sums[slice][sub][ch] = v;
+  if (ch == 0) {
+    tops[slice][sub] = top;
+    dens[slice][sub] = den;
+  }
+  __syncthreads();
+  if (slice || row >= rows) return;
+  float most = top;
+  for (int i = 1; i < kSlices; ++i) most = fmaxf(most, tops[i][sub]);
+  const float f = exp2_fast(top - most);
+  v *= f;
+  den *= f;
+  for (int i = 1; i < kSlices; ++i) {
+    const float g = exp2_fast(tops[i][sub] - most);
+    v += sums[i][sub][ch] * g;
+    den += dens[i][sub] * g;
+  }
+  const int64_t place = (int64_t)(req.t0 + (row0 + row) / a.group) * (a.c.heads * a.group) + head * a.group +
+                        (row0 + row) % a.group;
+  const float inv = den != 0.0f ? 1.0f / den : 0.0f;
+  store_four(a.out, a.out_dtype, place * D + 4 * ch, den != 0.0f ? v * inv : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+  if (a.lse && ch == 0) a.lse[place] = den != 0.0f ? (most + __log2f(den)) * kLn2 : -INFINITY;
+}
+
+// ------------------------------------------------------------------ host side
+// Workgroups: two a CU, one at 256 channels.
+template <int D>
+constexpr int kTreeParts = D <= 128 ? 512 : 256;
+
+template <int D>
+int32_t launch_tree(AttnArgs a, const uint64_t* masks, void* work, hipStream_t stream) {
+  constexpr int kParts = kTreeParts<D>, kPer = kTileThreads / (D / 4) / 4;
+  uint8_t* at = static_cast<uint8_t*>(work);
+  a.parts = kParts;
+  a.desc = reinterpret_cast<int32_t*>(at);
+  a.part_rl = reinterpret_cast<float*>(at + 16 * kParts);
+  a.part_o = a.part_rl + 2 * kParts * kTileRows * 2;
+  static_assert(16 * kParts + (int64_t)2 * kParts * kTileRows * (D + 2) * 4 <= LOGBQ_KV4_WORKSPACE_BYTES,
+                "the workspace holds every part");
+  a.unit = kTilePositions;
+  const bool split = a.q_dtype == LOGBQ_DTYPE_F32, one_page = a.c.page_shift >= 6;
+#define TREE(SPLIT, ONE_PAGE)                                                                        \
+  if (split == SPLIT && one_page == ONE_PAGE)                                                        \
+    hipLaunchKernelGGL((k_kv4_tree<D, SPLIT, ONE_PAGE>), dim3(kParts), dim3(kTileThreads), 0, stream, a, masks)
+  TREE(false, false); TREE(false, true); TREE(true, false); TREE(true, true);
+#undef TREE
+  if (launch_status() != LOGBQ_OK) return LOGBQ_ERR_HIP;
+  const int rows = a.max_new * a.group < kTileRows ? a.max_new * a.group : kTileRows;
+  hipLaunchKernelGGL(k_kv4_tree_join<D>, dim3(kParts, (rows + kPer - 1) / kPer), dim3(kTileThreads), 0, stream, a);
+  return launch_status();
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t logbq_kv4_tree_attention(const void* q_dev, int64_t q_stride, int32_t q_dtype, int64_t tokens,
+                                 int32_t q_heads, const logbq_kv4* cache, const int32_t* table_dev,
+                                 int64_t requests, int64_t width, const int32_t* seq_lens_dev,
+                                 const int32_t* q_starts_dev, const uint64_t* masks_dev, int64_t max_new,
+                                 float scale, int32_t window, void* out_dev, int32_t out_dtype,
+                                 float* lse_dev, void* work_dev, int64_t work_bytes, void* stream) {
+  AttnArgs a = {};
+  const int32_t bad = attention_args(q_dev, q_stride, q_dtype, tokens, q_heads, cache, table_dev, requests, width,
+                                     seq_lens_dev, q_starts_dev, max_new, scale, window, out_dev, out_dtype,
+                                     lse_dev, work_dev, work_bytes, &a);
+  if (bad != LOGBQ_OK) return bad;
+  if (max_new > kMaxNodes || (window > 0 && window < kMaxNodes)) return LOGBQ_ERR_UNSUPPORTED;
+  // Units of 64 positions of up to 128 query rows, and at least one of each, fit 31 bits.
+  const int64_t row_tiles = (max_new * a.group + kTileRows - 1) / kTileRows;
+  if ((double)requests * a.c.heads * row_tiles * ((double)width * cache->page / kTilePositions + 1) >= INT32_MAX)
+    return LOGBQ_ERR_UNSUPPORTED;
+  if (tokens == 0 || requests == 0 || max_new == 0) return LOGBQ_OK;
+  if (!masks_dev) return LOGBQ_ERR_INVALID_ARG;
+  if ((uintptr_t)masks_dev % 8) return LOGBQ_ERR_UNSUPPORTED;
+  return cache->dim == 64    ? launch_tree<64>(a, masks_dev, work_dev, (hipStream_t)stream)
+         : cache->dim == 128 ? launch_tree<128>(a, masks_dev, work_dev, (hipStream_t)stream)
+                             : launch_tree<256>(a, masks_dev, work_dev, (hipStream_t)stream);
+}
+
+}  // extern "C"

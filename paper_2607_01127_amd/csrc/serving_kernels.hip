@@ -3,6 +3,7 @@
 // probabilities (attention over the cache is in kv4_attention.hip).
 //
 //   k_batch_tables   prefix sums of the requests' lengths, then slots, positions and new pages.
+//   k_tree_tables    ancestor masks and positions of drafted trees from the nodes' parents.
 //   k_kv4_append     rows of keys and values -> 4-bit codes and bfloat16 scales in their slots.
 //   k_kv4_read       the values that the cache holds in given slots.
 //   k_token_logprobs log softmax of given tokens, entropy and top alternatives.
@@ -154,22 +155,53 @@ __global__ __launch_bounds__(kTabThreads) void k_batch_tables(TabArgs a) {
   }
 }
 
+// ------------------------------------------------------------------ trees of drafted tokens
+// A wavefront has a request, a lane a node. A node's mask and the end of its known path are joined with
+// those of that end, which doubles the path each time: six times for paths of 64 nodes. Parents come
+// before their children, so there is no circle. Bound by latency: three dependent loads and 18 shuffles.
+__global__ __launch_bounds__(kTabThreads) void k_tree_tables(const int32_t* parents, int64_t tokens,
+                                                             const int32_t* q_starts,
+                                                             const int32_t* seq_lens, int32_t requests,
+                                                             uint64_t* masks, int32_t* positions) {
+  const int lane = threadIdx.x & 63;
+  const int r = blockIdx.x * (kTabThreads / 64) + (threadIdx.x >> 6);
+  if (r >= requests) return;
+  int64_t t0 = q_starts[r], t1 = q_starts[r + 1];
+  t0 = t0 < 0 ? 0 : t0 > tokens ? tokens : t0;
+  t1 = t1 < t0 ? t0 : t1 > tokens ? tokens : t1;
+  const int64_t n = t1 - t0, length = seq_lens[r] > 0 ? seq_lens[r] : 0;
+  const int nodes = n < 64 ? (int)n : 64;
+  int32_t up = lane < nodes ? parents[t0 + lane] : -1;
+  if (up >= lane) up = -1;
+  uint64_t mask = 1ull << lane;
+#pragma unroll
+  for (int i = 0; i < 6; ++i) {
+    const int from = up < 0 ? lane : up;
+    mask |= (uint64_t)__shfl((uint32_t)(mask >> 32), from) << 32 | __shfl((uint32_t)mask, from);
+    const int32_t next = __shfl(up, from);
+    up = up < 0 ? -1 : next;
+  }
+  const int64_t position = length - n + __popcll(mask) - 1;
+  if (lane < nodes) {
+    masks[t0 + lane] = mask;
+    positions[t0 + lane] = (int32_t)(position > 0 ? position : 0);
+  }
+  // Nodes past the 64th see nothing.
+  for (int64_t i = 64 + lane; i < n; i += 64) {
+    masks[t0 + i] = 0;
+    positions[t0 + i] = 0;
+  }
+}
+
 // ------------------------------------------------------------------ the 4-bit cache
 // 16 lanes take a row: lane c has channels c D/16 .. (c + 1) D/16 - 1, which are one group of the
 // value layout. A workgroup takes 16 consecutive tokens of one head. Measured, 8191 tokens x 8 heads x
 // 128 channels: append from float16 (42 MB in and out) 16.5 us, bound by the 14 instructions a value
 // that comparing with seven thresholds takes; read into float16 (42 MB) 10.6 us, 4.0 TB/s. 48 tokens
 // take 3.8 and 3.4 us, the launches' latency.
-constexpr int kRowLanes = 16;
 constexpr int kRowThreads = 256;
 
-// N codes of 4 bits as N / 8 words (N = 4: the low half of one word).
-template <int N>
-__device__ __forceinline__ void store_codes(uint8_t* to, const uint32_t (&w)[(N + 7) / 8]) {
-  if (N == 4) *reinterpret_cast<uint16_t*>(to) = (uint16_t)w[0];
-  else if (N == 8) *reinterpret_cast<uint32_t*>(to) = w[0];
-  else *reinterpret_cast<u32x2*>(to) = u32x2{w[0], w[(N + 7) / 8 - 1]};
-}
+// N codes of 4 bits from N / 8 words (N = 4: the low half of one word).
 template <int N>
 __device__ __forceinline__ void load_codes(const uint8_t* from, uint32_t (&w)[(N + 7) / 8]) {
   if (N == 4) w[0] = *reinterpret_cast<const uint16_t*>(from);
@@ -179,50 +211,6 @@ __device__ __forceinline__ void load_codes(const uint8_t* from, uint32_t (&w)[(N
     w[0] = v.x;
     w[(N + 7) / 8 - 1] = v.y;
   }
-}
-
-// Largest value of the 16 lanes of a row.
-__device__ __forceinline__ uint32_t row_max(uint32_t v) {
-  // Rotations within 16 lanes by 8, 4, 2 and 1.
-  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x128, 0xf, 0xf, true));
-  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x124, 0xf, 0xf, true));
-  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x122, 0xf, 0xf, true));
-  return max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x121, 0xf, 0xf, true));
-}
-
-// Codes of one row: the scale is the smallest bfloat16 s with 6 s >= max |x|, found from the
-// truncated quotient with one exact comparison (6 s has at most 11 significant bits), and the
-// magnitudes compare |x| with t s (at most 11 bits too), so no rounding enters a code.
-template <int D, int DT, bool VALUES>
-__device__ __forceinline__ void append_row(const void* from, int64_t at, const Kv4& c, int64_t slot,
-                                           int head, int group) {
-  constexpr int N = D / 16;
-  float x[N];
-  load_row<DT, N>(from, at, x);
-  uint32_t top = 0;
-#pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const uint32_t u = __float_as_uint(x[j]) & 0x7fffffffu;
-    top = u < 0x7f800000u && u > top ? u : top;
-  }
-  const float size = __uint_as_float(row_max(top));
-  uint32_t s = __float_as_uint(size / 6.0f) & 0xffff0000u;
-  if (6.0f * __uint_as_float(s) < size) s += 0x10000u;
-  const float scale = __uint_as_float(s);
-  constexpr float kThr[7] = {0.25f, 0.75f, 1.25f, 1.75f, 2.5f, 3.5f, 5.0f};
-  uint32_t w[(N + 7) / 8] = {};
-#pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const float ax = __builtin_fabsf(x[j]);
-    uint32_t mag = 0;
-#pragma unroll
-    for (int t = 0; t < 7; ++t) mag += ax >= kThr[t] * scale ? 1u : 0u;
-    mag = s ? mag : 0u;
-    const uint32_t sign = x[j] < 0.0f && mag ? 8u : 0u;
-    w[j / 8] |= (mag | sign) << (4 * (j % 8));
-  }
-  store_codes<N>((VALUES ? c.v_codes : c.k_codes) + code_offset<D, VALUES>(c, slot, head, group), w);
-  if (group == 0) (VALUES ? c.v_scales : c.k_scales)[scale_index(c, slot, head)] = (uint16_t)(s >> 16);
 }
 
 template <int D, int DT>
@@ -235,8 +223,11 @@ __global__ __launch_bounds__(kRowThreads) void k_kv4_append(const void* k, int64
   const int64_t slot = t < tokens ? slots[t] : -1;
   if (slot < 0 || slot >= c.slots) return;        // whole rows of 16 lanes leave together
   const int64_t at = (int64_t)head * D + group * (D / 16);
-  append_row<D, DT, false>(k, t * k_stride + at, c, slot, head, group);
-  append_row<D, DT, true>(v, t * v_stride + at, c, slot, head, group);
+  float x[D / 16];
+  load_row<DT>(k, t * k_stride + at, x);
+  append_row<D, false>(x, c, slot, head, group);
+  load_row<DT>(v, t * v_stride + at, x);
+  append_row<D, true>(x, c, slot, head, group);
 }
 
 template <int D, bool VALUES>
@@ -689,18 +680,6 @@ dim3 row_grid(int64_t tokens, int32_t heads) {
   return dim3((unsigned)((tokens + kRowThreads / kRowLanes - 1) / (kRowThreads / kRowLanes)), (unsigned)heads);
 }
 
-// Whether a call would write what it reads: its workgroups have no order among them.
-struct Range { const void* at; int64_t bytes; };
-template <int N, int M>
-bool any_overlap(const Range (&in)[N], const Range (&out)[M]) {
-  for (const Range& i : in)
-    for (const Range& o : out)
-      if (i.bytes > 0 && o.bytes > 0 && (uintptr_t)i.at < (uintptr_t)o.at + o.bytes &&
-          (uintptr_t)o.at < (uintptr_t)i.at + i.bytes)
-        return true;
-  return false;
-}
-
 // A launch has fewer than 2^32 threads a dimension.
 constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - 1;
 constexpr int64_t kMaxTokens = ((int64_t)1 << 32) / kRowLanes - kRowThreads / kRowLanes;
@@ -735,6 +714,23 @@ int32_t logbq_batch_tables(const int32_t* cached_dev, const int32_t* new_dev, in
   grid = grid > by_request ? grid : by_request;
   grid = grid < 1 ? 1 : grid > 1024 ? 1024 : grid;
   hipLaunchKernelGGL(k_batch_tables, dim3((unsigned)grid), dim3(kTabThreads), 0, (hipStream_t)stream, a);
+  return launch_status();
+}
+
+int32_t logbq_tree_tables(const int32_t* parents_dev, int64_t tokens, const int32_t* q_starts_dev,
+                          const int32_t* seq_lens_dev, int64_t requests, uint64_t* masks_dev,
+                          int32_t* positions_dev, void* stream) {
+  if (tokens < 0 || requests < 0) return LOGBQ_ERR_INVALID_ARG;
+  if (tokens >= INT32_MAX || requests > kMaxThreads / 64 - 4) return LOGBQ_ERR_UNSUPPORTED;
+  if (tokens == 0 || requests == 0) return LOGBQ_OK;
+  if (!parents_dev || !q_starts_dev || !seq_lens_dev || !masks_dev || !positions_dev) return LOGBQ_ERR_INVALID_ARG;
+  const Range in[] = {{parents_dev, 4 * tokens}, {q_starts_dev, 4 * (requests + 1)}, {seq_lens_dev, 4 * requests}};
+  const Range out[] = {{masks_dev, 8 * tokens}, {positions_dev, 4 * tokens}};
+  const Range masks[] = {out[0]}, positions[] = {out[1]};
+  if (any_overlap(in, out) || any_overlap(masks, positions)) return LOGBQ_ERR_INVALID_ARG;
+  hipLaunchKernelGGL(k_tree_tables, dim3((unsigned)((requests + kTabThreads / 64 - 1) / (kTabThreads / 64))),
+                     dim3(kTabThreads), 0, (hipStream_t)stream, parents_dev, tokens, q_starts_dev,
+                     seq_lens_dev, (int32_t)requests, masks_dev, positions_dev);
   return launch_status();
 }
 

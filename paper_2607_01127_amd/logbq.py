@@ -1,8 +1,9 @@
 """Python binding of liblogbq (ctypes): argument marshalling only.
 
 Every step of the computation runs in the library: ``fit`` in its host code, ``encode``,
-``linear``, ``dequantize`` and a serving step's operators (``batch_tables``, ``kv4_append``,
-``kv4_read``, ``kv4_attention``, ``token_logprobs``) in its gfx950 kernels. PyTorch provides device memory and the
+``linear``, ``dequantize`` and a serving step's operators (``batch_tables``, ``tree_tables``,
+``linear_adapters``, ``qk_rotate``, ``kv4_append``, ``kv4_append_rotated``, ``kv4_read``, ``kv4_attention``,
+``kv4_tree_attention``, ``token_logprobs``) in its gfx950 kernels. PyTorch provides device memory and the
 current stream; nothing here computes on the data. If the library is not built, every call
 raises ``LogbqUnavailable``: there is no fallback path.
 """
@@ -71,6 +72,11 @@ class Kv4Struct(ctypes.Structure):
                 ("dim", c_int32), ("reserved", c_int32)]
 
 
+class RotationStruct(ctypes.Structure):
+    """Mirror of ``logbq_rotation`` (include/logbq.h)."""
+    _fields_ = [("inv_freq", c_void_p), ("pairs", c_int32), ("interleaved", c_int32), ("factor", c_double)]
+
+
 _lib = None
 
 SIGNATURES = {
@@ -114,6 +120,24 @@ SIGNATURES = {
                                       POINTER(Kv4Struct), c_void_p, c_int64, c_int64, c_void_p,
                                       c_void_p, c_int64, c_float, c_int32, c_void_p, c_int32,
                                       c_void_p, c_void_p, c_int64, c_void_p]),
+    "logbq_tree_tables": (c_int32, [c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_void_p, c_void_p,
+                                    c_void_p]),
+    "logbq_qk_rotate": (c_int32, [c_void_p, c_int64, c_int32, c_void_p, c_void_p, c_int64, c_int32, c_void_p,
+                                  c_int32, c_int64, c_int32, c_double, c_void_p, POINTER(RotationStruct),
+                                  c_void_p, c_void_p, c_int32, c_void_p]),
+    "logbq_kv4_append_rotated": (c_int32, [c_void_p, c_int64, c_int32, c_void_p, c_void_p, c_int64, c_void_p,
+                                           c_void_p, c_int64, c_int32, c_int64, c_double, c_void_p,
+                                           POINTER(RotationStruct), POINTER(Kv4Struct), c_void_p, c_void_p,
+                                           c_int32, c_void_p]),
+    "logbq_kv4_tree_attention": (c_int32, [c_void_p, c_int64, c_int32, c_int64, c_int32,
+                                           POINTER(Kv4Struct), c_void_p, c_int64, c_int64, c_void_p,
+                                           c_void_p, c_void_p, c_int64, c_float, c_int32, c_void_p, c_int32,
+                                           c_void_p, c_void_p, c_int64, c_void_p]),
+    "logbq_linear_adapters_workspace": (c_int64, [c_int64, c_int32, c_int32]),
+    "logbq_linear_adapters": (c_int32, [c_void_p, c_int64, c_int64, c_int32, POINTER(c_void_p), POINTER(c_void_p),
+                                        POINTER(c_int64), c_int32, c_int64, c_int32, c_void_p, c_void_p, c_void_p,
+                                        c_void_p, c_int64, c_int64, POINTER(c_void_p), POINTER(c_void_p), c_void_p,
+                                        c_int64, c_void_p]),
     "logbq_token_logprobs": (c_int32, [c_void_p, c_int32, c_int64, c_int64, c_int64, c_void_p,
                                        c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                                        c_int64, c_void_p]),
@@ -562,6 +586,121 @@ def batch_tables(cached, new, free_pages, table, page: int, tokens: int, out=Non
     return out
 
 
+def tree_tables(parents, q_starts, seq_lens, out=None, stream=None):
+    """logbq_tree_tables: ancestor masks and positions of drafted trees. `parents` (int32 [tokens]) has each
+    node's parent as an index among its request's tokens (negative: the last cached token); `q_starts` (int32
+    [requests + 1]) and `seq_lens` (int32 [requests]) are batch_tables' results. Returns a dict of masks (int64
+    [tokens], 64 bits each) and positions (int32 [tokens]); `out` may hold the tensors to write."""
+    import torch
+    i32 = torch.int32
+    tokens, n = parents.numel(), seq_lens.numel()
+    _device_array(parents, i32, (tokens,), "parents")
+    _device_array(q_starts, i32, (n + 1,), "q_starts")
+    _device_array(seq_lens, i32, (n,), "seq_lens")
+    if out is None:
+        with _made_on(stream):
+            out = dict(masks=torch.empty(tokens, device=parents.device, dtype=torch.int64),
+                       positions=torch.empty(tokens, device=parents.device, dtype=i32))
+    else:
+        _device_array(out["masks"], torch.int64, (tokens,), "masks")
+        _device_array(out["positions"], i32, (tokens,), "positions")
+    _check(lib().logbq_tree_tables(parents.data_ptr(), tokens, q_starts.data_ptr(), seq_lens.data_ptr(), n,
+                                   out["masks"].data_ptr(), out["positions"].data_ptr(), _stream(stream)),
+           "logbq_tree_tables")
+    return out
+
+
+class Rotation(NamedTuple):
+    """How queries and keys are turned by their positions (``logbq_rotation`` in include/logbq.h): the first
+    2 * len(inv_freq) channels of a head, as halves or as interleaved pairs."""
+    inv_freq: object              # float32 device tensor
+    interleaved: bool = False
+    factor: float = 1.0
+
+
+def _rotation_struct(rotation) -> RotationStruct:
+    import torch
+    inv_freq, interleaved, factor = rotation
+    _device_array(inv_freq, torch.float32, (inv_freq.numel(),), "inv_freq")
+    return RotationStruct(inv_freq.data_ptr() or None, inv_freq.numel(), 1 if interleaved else 0, factor)
+
+
+def _weight(x, dim, name):
+    if x is None:
+        return None
+    import torch
+    _device_array(x, torch.float32, (dim,), name)
+    return x.data_ptr()
+
+
+def _rotated_out(x, out, like, stream, name):
+    """The tensor that takes x's rotated rows: `out`, checked, or a new one of type `like`."""
+    import torch
+    if out is None:
+        with _made_on(stream):
+            return torch.empty(x.shape, dtype=like, device=x.device)
+    _device_array(out, out.dtype, x.shape, name)
+    return out
+
+
+def qk_rotate(q, k, positions, rotation, q_weight=None, k_weight=None, eps: float = 1e-6, q_out=None,
+              k_out=None, stream=None):
+    """logbq_qk_rotate: queries and keys [tokens][heads][dim] (float32, float16 or bfloat16; the tokens may be
+    strided), each head normed with `q_weight` / `k_weight` (float32 [dim]; None: no norm) and turned by
+    `positions` (int32 [tokens]) as a Rotation says. `k` may be None. Returns (q_out, k_out), contiguous, of the
+    inputs' type unless given; an output may be its own (contiguous) input."""
+    import torch
+    dim = q.shape[-1]
+    q_stride = _rows(q, 0, dim, "q")
+    tokens = q.shape[0]
+    _device_array(positions, torch.int32, (tokens,), "positions")
+    q_out = _rotated_out(q, q_out, q.dtype, stream, "q_out")
+    k_stride = k_heads = 0
+    if k is not None:
+        k_stride, k_heads = _rows(k, 0, dim, "k"), k.shape[1]
+        if k.dtype != q.dtype or k.shape[0] != tokens:
+            raise ValueError("q and k must have one type and number of tokens")
+        k_out = _rotated_out(k, k_out, q_out.dtype, stream, "k_out")
+        if k_out.dtype != q_out.dtype:
+            raise ValueError("q_out and k_out must have one type")
+    r = _rotation_struct(rotation)
+    _check(lib().logbq_qk_rotate(
+        q.data_ptr(), q_stride, q.shape[1], _weight(q_weight, dim, "q_weight"),
+        None if k is None else k.data_ptr(), k_stride, k_heads, _weight(k_weight, dim, "k_weight"),
+        _dtype_code(q.dtype), tokens, dim, eps, positions.data_ptr(), ctypes.byref(r), q_out.data_ptr(),
+        None if k is None else k_out.data_ptr(), _dtype_code(q_out.dtype), _stream(stream)), "logbq_qk_rotate")
+    return q_out, k_out
+
+
+def kv4_append_rotated(q, k, v, cache, slots, positions, rotation, q_weight=None, k_weight=None,
+                       eps: float = 1e-6, q_out=None, stream=None):
+    """logbq_kv4_append_rotated: keys normed and turned as in qk_rotate on their way into `slots` (int64 [tokens])
+    of a Kv4Cache, with the values, and the queries turned beside them. `q` may be None. Returns q_out
+    ([tokens][q_heads][dim], float16 unless given; None without queries)."""
+    import torch
+    c = _kv4_struct(cache)
+    k_stride, v_stride = _rows(k, c.heads, c.dim, "k"), _rows(v, c.heads, c.dim, "v")
+    tokens = k.shape[0]
+    if v.dtype != k.dtype or v.shape[0] != tokens:
+        raise ValueError("k and v must have one type and number of tokens")
+    _device_array(slots, torch.int64, (tokens,), "slots")
+    _device_array(positions, torch.int32, (tokens,), "positions")
+    q_stride = q_heads = q_at = 0
+    if q is not None:
+        q_stride, q_heads, q_at = _rows(q, 0, c.dim, "q"), q.shape[1], q.data_ptr()
+        if q.dtype != k.dtype or q.shape[0] != tokens:
+            raise ValueError("q and k must have one type and number of tokens")
+        q_out = _rotated_out(q, q_out, torch.float16, stream, "q_out")
+    r = _rotation_struct(rotation)
+    _check(lib().logbq_kv4_append_rotated(
+        q_at or None, q_stride, q_heads, _weight(q_weight, c.dim, "q_weight"), k.data_ptr(), k_stride,
+        _weight(k_weight, c.dim, "k_weight"), v.data_ptr(), v_stride, _dtype_code(k.dtype), tokens, eps,
+        positions.data_ptr(), ctypes.byref(r), ctypes.byref(c), slots.data_ptr(),
+        None if q is None else q_out.data_ptr(), 1 if q is None else _dtype_code(q_out.dtype), _stream(stream)),
+        "logbq_kv4_append_rotated")
+    return None if q is None else q_out
+
+
 def kv4_append(k, v, cache, slots, stream=None):
     """logbq_kv4_append: keys and values [tokens][heads][dim] (float32, float16 or bfloat16; the
     tokens may be strided) quantized into `slots` (int64 [tokens]; negative: left out; what a slot
@@ -593,15 +732,9 @@ def kv4_read(cache, slots, dtype=None, stream=None):
     return k, v
 
 
-def kv4_attention(q, cache, table, seq_lens, q_starts, max_new: int, scale=None, window: int = 0,
-                  out=None, lse=None, workspace=None, stream=None):
-    """logbq_kv4_attention: attention of q [tokens][q_heads][dim] (float32, float16 or bfloat16;
-    the tokens may be strided) over a Kv4Cache. `table` (int32 [requests][width]), `seq_lens`
-    (int32 [requests]) and `q_starts` (int32 [requests + 1]) are batch_tables' results; `max_new`
-    bounds a request's tokens. `scale` is dim ** -0.5 unless given; `window` 0 sees everything.
-    Returns `out` ([tokens][q_heads][dim], float16 unless given); `lse` (float32
-    [tokens][q_heads]), if given, receives the log sums of exponentials. `workspace`
-    (KV4_WORKSPACE_BYTES bytes serve any call) is allocated if not given."""
+def _attention_call(q, cache, table, seq_lens, q_starts, out, lse, workspace, stream):
+    """The arguments that the attention calls share, checked: (cache, those before max_new, those after the
+    window, out, the workspace, which the caller holds until the call is made)."""
     import torch
     c = _kv4_struct(cache)
     q_stride = _rows(q, 0, c.dim, "q")
@@ -625,13 +758,100 @@ def kv4_attention(q, cache, table, seq_lens, q_starts, max_new: int, scale=None,
             workspace = torch.empty(KV4_WORKSPACE_BYTES, dtype=torch.uint8, device=q.device)
     else:
         _device_workspace(workspace)
-    _check(lib().logbq_kv4_attention(
-        q.data_ptr(), q_stride, _dtype_code(q.dtype), tokens, q_heads, ctypes.byref(c),
-        table.data_ptr(), n, width, seq_lens.data_ptr(), q_starts.data_ptr(), max_new,
-        c.dim ** -0.5 if scale is None else scale, window, out.data_ptr(), _dtype_code(out.dtype),
-        None if lse is None else lse.data_ptr(), workspace.data_ptr(),
-        workspace.numel() * workspace.element_size(), _stream(stream)), "logbq_kv4_attention")
+    before = (q.data_ptr(), q_stride, _dtype_code(q.dtype), tokens, q_heads, ctypes.byref(c), table.data_ptr(), n,
+              width, seq_lens.data_ptr(), q_starts.data_ptr())
+    after = (out.data_ptr(), _dtype_code(out.dtype), None if lse is None else lse.data_ptr(), workspace.data_ptr(),
+             workspace.numel() * workspace.element_size())
+    return c, before, after, out, workspace
+
+
+def kv4_attention(q, cache, table, seq_lens, q_starts, max_new: int, scale=None, window: int = 0,
+                  out=None, lse=None, workspace=None, stream=None):
+    """logbq_kv4_attention: attention of q [tokens][q_heads][dim] (float32, float16 or bfloat16;
+    the tokens may be strided) over a Kv4Cache. `table` (int32 [requests][width]), `seq_lens`
+    (int32 [requests]) and `q_starts` (int32 [requests + 1]) are batch_tables' results; `max_new`
+    bounds a request's tokens. `scale` is dim ** -0.5 unless given; `window` 0 sees everything.
+    Returns `out` ([tokens][q_heads][dim], float16 unless given); `lse` (float32
+    [tokens][q_heads]), if given, receives the log sums of exponentials. `workspace`
+    (KV4_WORKSPACE_BYTES bytes serve any call) is allocated if not given."""
+    c, before, after, out, _held = _attention_call(q, cache, table, seq_lens, q_starts, out, lse, workspace, stream)
+    _check(lib().logbq_kv4_attention(*before, max_new, c.dim ** -0.5 if scale is None else scale, window, *after,
+                                     _stream(stream)), "logbq_kv4_attention")
     return out
+
+
+def kv4_tree_attention(q, cache, table, seq_lens, q_starts, masks, max_new: int, scale=None, window: int = 0,
+                       out=None, lse=None, workspace=None, stream=None):
+    """logbq_kv4_tree_attention: kv4_attention of a step whose new tokens are the nodes of drafted trees, each of
+    which sees its request's cached tokens and the nodes of its mask. `masks` (int64 [tokens]) is tree_tables'
+    result; `max_new` is at most 64; `window` is 0 or at least 64."""
+    import torch
+    _device_array(masks, torch.int64, (q.shape[0],), "masks")
+    c, before, after, out, _held = _attention_call(q, cache, table, seq_lens, q_starts, out, lse, workspace, stream)
+    _check(lib().logbq_kv4_tree_attention(*before, masks.data_ptr(), max_new,
+                                          c.dim ** -0.5 if scale is None else scale, window, *after,
+                                          _stream(stream)), "logbq_kv4_tree_attention")
+    return out
+
+
+def linear_adapters_workspace_bytes(tokens: int, count: int, rank: int) -> int:
+    """logbq_linear_adapters_workspace: bytes of workspace of a linear_adapters call with `tokens` tokens, `count`
+    projections and pools of `rank` ranks. Host only."""
+    return lib().logbq_linear_adapters_workspace(tokens, count, rank)
+
+
+def linear_adapters(x, ys, a_list, b_list, q_starts, adapter, max_new: int, scales=None, ranks=None, outs=None,
+                    workspace=None, stream=None):
+    """logbq_linear_adapters: low-rank adapters of many requests beside up to four projections that share x
+    (float16 [tokens][K]): outs[i][t] = ys[i][t] + scales[a] (x[t] A_i[a]^T) B_i[a]^T. `ys` are linear's or
+    linear_multi's results (float32 [tokens][N_i]), updated in place unless `outs` is given; `a_list[i]` is a pool
+    [adapters][rank][K] and `b_list[i]` [adapters][N_i][rank], float16 or bfloat16. `adapter` (int32 [requests])
+    has each request's adapter (negative: none), `q_starts` its first token, `max_new` bounds its tokens. `scales`
+    (float32 [adapters]) and `ranks` (int32 [adapters], how many of the pool's ranks an adapter has) may be None.
+    `workspace` (linear_adapters_workspace_bytes, one for each stream) is allocated if not given."""
+    import torch
+    if x.dtype != torch.float16 or x.dim() != 2 or not x.is_contiguous() or not x.is_cuda:
+        raise ValueError("x must be a contiguous 2-D float16 device tensor")
+    tokens, k = x.shape
+    count = len(ys)
+    if not 1 <= count <= 4 or len(a_list) != count or len(b_list) != count or \
+            (outs is not None and len(outs) != count):
+        raise ValueError("need 1..4 projections with a pool of A and one of B each")
+    outs = ys if outs is None else outs
+    if a_list[0].dim() != 3:
+        raise ValueError("a_list must hold [adapters][rank][K] tensors")
+    adapters, rank = a_list[0].shape[:2]
+    dtype = a_list[0].dtype
+    for y, a, b, out in zip(ys, a_list, b_list, outs):
+        if y.dim() != 2:
+            raise ValueError("ys must hold [tokens][N] tensors")
+        n = y.shape[1]
+        _device_array(y, torch.float32, (tokens, n), "ys")
+        _device_array(out, torch.float32, (tokens, n), "outs")
+        _device_array(a, dtype, (adapters, rank, k), "a_list")
+        _device_array(b, dtype, (adapters, n, rank), "b_list")
+    requests = adapter.numel()
+    _device_array(adapter, torch.int32, (requests,), "adapter")
+    _device_array(q_starts, torch.int32, (requests + 1,), "q_starts")
+    if scales is not None:
+        _device_array(scales, torch.float32, (adapters,), "scales")
+    if ranks is not None:
+        _device_array(ranks, torch.int32, (adapters,), "ranks")
+    if workspace is None:
+        with _made_on(stream):
+            workspace = torch.empty(linear_adapters_workspace_bytes(tokens, count, rank), dtype=torch.uint8,
+                                    device=x.device)
+    else:
+        _device_workspace(workspace)
+    pointers = c_void_p * count
+    _check(lib().logbq_linear_adapters(
+        x.data_ptr(), tokens, k, count, pointers(*[a.data_ptr() for a in a_list]),
+        pointers(*[b.data_ptr() for b in b_list]), (c_int64 * count)(*[y.shape[1] for y in ys]),
+        _dtype_code(dtype), adapters, rank, None if ranks is None else ranks.data_ptr(),
+        None if scales is None else scales.data_ptr(), q_starts.data_ptr(), adapter.data_ptr(), requests, max_new,
+        pointers(*[y.data_ptr() for y in ys]), pointers(*[o.data_ptr() for o in outs]), workspace.data_ptr(),
+        workspace.numel() * workspace.element_size(), _stream(stream)), "logbq_linear_adapters")
+    return outs
 
 
 def token_logprobs(logits, targets, top: int = 0, out=None, workspace=None, stream=None):
