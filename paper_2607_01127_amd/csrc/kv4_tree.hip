@@ -50,20 +50,28 @@ struct QueryRow {
 
   // Scaled by a power of two so that float16 holds them; the sign of the scale goes into the queries.
   __device__ __forceinline__ void load(const AttnArgs& a, int64_t at, bool present) {
+    // All loads first: one by one, each would wait for the one before.
+    constexpr int kWords = QSPLIT ? 2 : 1;
+    u32x4 raw[kKc][kWords];
+#pragma unroll
+    for (int c = 0; c < kKc; ++c)
+#pragma unroll
+      for (int h = 0; h < kWords; ++h)
+        raw[c][h] = present ? *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(a.q) +
+                                                              (at + 16 * c) * (2 * kWords) + 16 * h)
+                            : u32x4{0, 0, 0, 0};
     float x[kKc][8];
     float most = 0.0f;
 #pragma unroll
     for (int c = 0; c < kKc; ++c) {
-      if (present) {
-        if (a.q_dtype == LOGBQ_DTYPE_F32) load_row<LOGBQ_DTYPE_F32>(a.q, at + 16 * c, x[c]);
-        else if (a.q_dtype == LOGBQ_DTYPE_F16) load_row<LOGBQ_DTYPE_F16>(a.q, at + 16 * c, x[c]);
-        else load_row<LOGBQ_DTYPE_BF16>(a.q, at + 16 * c, x[c]);
-      } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[c][j] = 0.0f;
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t w = QSPLIT ? raw[c][j >> 2 & (kWords - 1)][j & 3] : raw[c][0][j >> 1];
+        if constexpr (QSPLIT) x[c][j] = __uint_as_float(w);
+        else if (a.q_dtype == LOGBQ_DTYPE_BF16) x[c][j] = __uint_as_float(j & 1 ? w & 0xffff0000u : w << 16);
+        else x[c][j] = (float)__builtin_bit_cast(half2v, w)[j & 1];
+        most = fmaxf(most, __builtin_fabsf(x[c][j]));
       }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) most = fmaxf(most, __builtin_fabsf(x[c][j]));
     }
     most = fmaxf(most, __shfl_xor(most, 32));
     const int e = most > 0.0f && most < INFINITY ? (int)(__float_as_uint(most) >> 23) - 127 : 0;
@@ -111,42 +119,40 @@ struct QueryRow {
       vs[i] = *reinterpret_cast<const f32x4*>(&lds.vscale[buf][32 * pb + 8 * i + 4 * half]);
     // By ldexp, as 2^ek alone may be below float32's normal numbers.
     const float f = ldexpf(qs, ek);
+    // The branches on `full` leave the outputs' registers alone: merged through them, the compiler copies all.
+    if (!full) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = seen_at(8 * (i >> 2) + (i & 3)) ? s[i] : -INFINITY;
+    }
+    float top = s[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+    // A row that sees none of the tile keeps its reference.
+    const float reach = !full && top == -INFINITY ? kNone : top * f;
+    if (__builtin_amdgcn_ballot_w64(reach - ref > 8.0f)) {
+      const float most = fmaxf(reach, __shfl_xor(reach, 32));
+      const float next = most - ref > 8.0f ? most : ref;
+      const float g = exp2_fast(ref - next);
+      if constexpr (!kCareful)
+        if (__builtin_amdgcn_ballot_w64(next != kNone && __builtin_fabsf(next) > kFar)) lds.set_again();
+      ref = next;
+      sum *= g;
+#pragma unroll
+      for (int c = 0; c < kCb; ++c) o[c] *= g;
+    }
     const auto weigh = [&](auto all_seen) {
       constexpr bool kAll = decltype(all_seen)::value;
-      bool seen[16];
-      if constexpr (!kAll) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          seen[i] = seen_at(8 * (i >> 2) + (i & 3));
-          s[i] = seen[i] ? s[i] : -INFINITY;
-        }
-      }
-      float top = s[0];
-#pragma unroll
-      for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
-      // A row that sees none of the tile keeps its reference.
-      const float reach = !kAll && top == -INFINITY ? kNone : top * f;
-      if (__builtin_amdgcn_ballot_w64(reach - ref > 8.0f)) {
-        const float most = fmaxf(reach, __shfl_xor(reach, 32));
-        const float next = most - ref > 8.0f ? most : ref;
-        const float g = exp2_fast(ref - next);
-        if constexpr (!kCareful)
-          if (__builtin_amdgcn_ballot_w64(next != kNone && __builtin_fabsf(next) > kFar)) lds.set_again();
-        ref = next;
-        sum *= g;
-#pragma unroll
-        for (int c = 0; c < kCb; ++c) o[c] *= g;
-      }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         float w[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const int i = 8 * h + j;
+          const bool seen = kAll || seen_at(8 * (i >> 2) + (i & 3));
           float e = exp2_fast(exponent<kCareful>(s[i], f, ref));
-          if constexpr (!kAll) e = seen[i] ? e : 0.0f;
+          if constexpr (!kAll) e = seen ? e : 0.0f;
           sum += e;
-          w[j] = kAll || seen[i] ? e * vs[i >> 2][i & 3] : 0.0f;
+          w[j] = seen ? e * vs[i >> 2][i & 3] : 0.0f;
         }
         split_weights(w, wh[h], wl[h]);
       }
@@ -171,7 +177,7 @@ struct QueryRow {
 // Loading and converting tiles. A thread has 32 channels of one position's keys (D = 256: twice), and 4
 // positions of 8 channels of values (D = 256: 16 channels); at D = 64 half of the threads have keys and the
 // others 8 positions of 4 channels of values.
-template <int D, bool ONE_PAGE>
+template <int D, bool ONE_PAGE, bool RECOMPUTED>
 struct TileReader {
   static constexpr bool kSplitWaves = D == 64;
   static constexpr int kKc = D / 16, kItems = D == 256 ? 2 : 1;
@@ -182,12 +188,13 @@ struct TileReader {
   int page_mask;
   int64_t pages;
 
-  // A thread's part of a tile, computed anew for each tile: kept, it would take registers that the products need.
+  // A thread's part of a tile. With split queries it is computed anew for each tile: kept, it would take registers
+  // that the products need.
   struct Part {
     int lane, wave, key_pos, key_item, v_block, v_group, v_half;
     bool has_keys, has_values;
     __device__ __forceinline__ Part() {
-      const int tid = here(threadIdx.x);
+      const int tid = RECOMPUTED ? here(threadIdx.x) : (int)threadIdx.x;
       lane = tid & 63;
       wave = tid >> 6;
       has_keys = !kSplitWaves || wave < 2;
@@ -339,55 +346,85 @@ struct TileReader {
     return kCareful ? rest : 0;
   }
 
-  // The tiles of positions from .. stop (stop > from, a multiple of 64 apart): compute(base, positions that
-  // are valid, ek, buffer, careful) for each. The workgroup's threads come here together.
-  template <class Careful, class Compute>
-  __device__ __forceinline__ void go_over(int from, int stop, Compute&& compute, Careful careful) {
-    constexpr bool kCareful = Careful::value;
-    int base = from;
-    Raw raw = load_raw(base, load_ids(base));
-    Ids ids = load_ids(base + kTilePositions);
-    uint64_t valid = raw.valid & ~convert(raw, 0, careful);
-    int buf = 0, ek_of = ek;
+  // The codes of the first two tiles from a position, and the third one's page ids: codes are asked for two tiles
+  // ahead of their use, a product's time being less than memory's.
+  struct Ahead {
+    Raw raw[2];
+    Ids ids;
+  };
+  __device__ __forceinline__ Ahead start(int from) const {
+    Ahead s;
+    const Ids first = load_ids(from), second = load_ids(from + kTilePositions);
+    s.ids = load_ids(from + 2 * kTilePositions);
+    s.raw[0] = load_raw(from, first);
+    s.raw[1] = load_raw(from + kTilePositions, second);       // page 0's, if there is none
+    return s;
+  }
+  // The tiles of positions from .. stop (stop > from) that `s` begins: compute(base, positions that are valid, ek,
+  // buffer, careful) for each. The workgroup's threads come here together. Two tiles a turn, as the buffers' and
+  // registers' roles change with each: moved from one to another, registers would have to wait for their loads.
+  template <class Compute>
+  __device__ __forceinline__ void go_over(int from, int stop, Ahead& s, Compute&& compute) {
+    const std::false_type careful;
+    uint64_t valid = s.raw[0].valid & ~convert(s.raw[0], 0, careful);
+    int ek_of = ek, base = from;
     __syncthreads();
-    while (base < stop) {
-      int next = base + kTilePositions;
-      if (next < stop) {
-        raw = load_raw(next, ids);
-        ids = load_ids(next + kTilePositions);
+    const auto tile = [&](auto which) {
+      constexpr int buf = decltype(which)::value;
+      const int next = base + kTilePositions;
+      if (next + kTilePositions < stop) {
+        s.raw[buf] = load_raw(next + kTilePositions, s.ids);
+        s.ids = load_ids(next + 2 * kTilePositions);
       }
       compute(base, valid, ek_of, buf, careful);
-      if constexpr (kCareful) {
-        const uint64_t held = lds.rest[buf];
-        const uint64_t rest = (uint64_t)__builtin_amdgcn_readfirstlane((int)(held >> 32)) << 32 |
-                              (uint32_t)__builtin_amdgcn_readfirstlane((int)held);
-        if (rest) {                     // the tile again, for these
-          next = base;
-          raw = load_raw(base, load_ids(base));
-          raw.valid = rest;
-          ids = load_ids(base + kTilePositions);
-        }
-      }
       if (next < stop) {
-        valid = raw.valid & ~convert(raw, buf ^ 1, careful);
+        valid = s.raw[buf ^ 1].valid & ~convert(s.raw[buf ^ 1], buf ^ 1, careful);
         ek_of = ek;
       }
       base = next;
-      buf ^= 1;
       __syncthreads();
+    };
+    for (;;) {
+      tile(std::integral_constant<int, 0>{});
+      if (base >= stop) break;
+      tile(std::integral_constant<int, 1>{});
+      if (base >= stop) break;
     }
+  }
+  // The same with care: what `convert` leaves of a tile is taken again, and again, before the next one.
+  template <class Compute>
+  __device__ __forceinline__ void go_over_carefully(int from, int stop, Compute&& compute) {
+    const std::true_type careful;
+    uint64_t left = ~0ull;
+    int buf = 0;
+    for (int base = from; base < stop;) {
+      Raw raw = load_raw(base, load_ids(base));
+      raw.valid &= left;
+      const uint64_t valid = raw.valid & ~convert(raw, buf, careful);
+      __syncthreads();
+      compute(base, valid, ek, buf, careful);
+      const uint64_t held = lds.rest[buf];
+      left = (uint64_t)__builtin_amdgcn_readfirstlane((int)(held >> 32)) << 32 |
+             (uint32_t)__builtin_amdgcn_readfirstlane((int)held);
+      if (!left) {
+        left = ~0ull;
+        base += kTilePositions;
+      }
+      buf ^= 1;
+    }
+    __syncthreads();
   }
 };
 
 // ------------------------------------------------------------------ trees
 // A node sees the cached positions (in a window, those that its own position reaches) and its ancestors'.
 // An item is up to 128 query rows (nodes x the query heads of one key/value head) of a request against all
-// of its positions. The items' units of positions are cut into equal shares, one a workgroup; a piece that
-// does not have all of its item's positions goes to the workspace for k_kv4_tree_join.
+// of its positions. An item of many positions is cut into equal pieces, a workgroup each, so that no piece
+// has more than its share of the batch's; their sums go to the workspace for k_kv4_tree_join.
 //
 // A piece of 32 rows or fewer leaves three wavefronts without rows, one of 64 two: then wavefronts share the
 // rows and have a half of each tile's positions, and their sums are added up in LDS at the end.
-constexpr int kTreeMinShare = 2;              // units of a workgroup at least
+constexpr int kTreeMinShare = 4;              // cost of a piece at least: two tiles of few rows
 constexpr int kMaxNodes = 64;
 
 template <int D, bool QSPLIT, bool ONE_PAGE>
@@ -395,287 +432,327 @@ __global__ __launch_bounds__(kTileThreads, D <= 128 ? 2 : 1)
 void k_kv4_tree(AttnArgs a, const uint64_t* masks) {
   constexpr int kRows = kTileRows, kCb = D / 32;
   __shared__ TileBuffers<D> lds;
-  __shared__ int32_t scan[4];
-  __shared__ int32_t found[2];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int col = lane & 31, half = lane >> 5;
+  __shared__ int32_t counts[2][4], scan[3][4];
+  __shared__ int32_t found[4];
+  __shared__ uint64_t row_mask[kRows];          // what the rows' nodes see
   const auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
 
-  // ---- this workgroup's part of all items' units (the host has seen that they fit 31 bits)
-  struct Items { int units, row_tiles, from; };          // of one item; of a request and head; first position
+  // ---- which piece (the host has seen that the costs of all items fit 31 bits)
+  struct Items { int tiles, row_tiles, from, cost; };    // of one item; of a request and head; first position
   const auto items_of = [&](const Request& q) {
     Items i;
     i.from = q.from & ~(kTilePositions - 1);
     i.row_tiles = (q.n * a.group + kRows - 1) / kRows;
-    i.units = q.end > i.from ? (unsigned)(q.end - i.from + a.unit - 1) / (unsigned)a.unit : 1;   // at least zeros to write
+    i.tiles = q.end > i.from ? (q.end - i.from + kTilePositions - 1) / kTilePositions : 0;
+    // A tile of more than 64 rows takes half as long again (128 channels: 3.3 us against 2.2).
+    i.cost = i.tiles * (q.n * a.group > kRows / 2 ? 3 : 2);
     return i;
-  };
-  const auto units_of = [&](int r) {
-    const Items i = items_of(request_of(a, r));
-    return i.units * i.row_tiles * a.c.heads;
   };
   const int per = (a.requests + kTileThreads - 1) / kTileThreads;
   const int r0 = tid * per < a.requests ? tid * per : a.requests;
   const int r1 = r0 + per < a.requests ? r0 + per : a.requests;
-  int mine = 0;
-  for (int r = r0; r < r1; ++r) mine += units_of(r);
-  int upto = mine;
+  int cost = 0, items = 0;
+  for (int r = r0; r < r1; ++r) {
+    const Items i = items_of(request_of(a, r));
+    cost += i.cost * i.row_tiles * a.c.heads;
+    items += i.row_tiles * a.c.heads;
+  }
   for (int d = 1; d < 64; d <<= 1) {
-    const int x = __shfl_up(upto, d);
-    if (lane >= d) upto += x;
+    cost += __shfl_xor(cost, d);
+    items += __shfl_xor(items, d);
   }
-  if (lane == 63) scan[wave] = upto;
+  if (lane == 0) {
+    counts[0][wave] = cost;
+    counts[1][wave] = items;
+  }
   __syncthreads();
-  int total = 0;
+  cost = items = 0;
   for (int w = 0; w < kTileThreads / 64; ++w) {
-    if (w < wave) upto += scan[w];
-    total += scan[w];
+    cost += counts[0][w];
+    items += counts[1][w];
   }
-  total = uniform(total);
-  // Workgroups with work: the first `rest` of them have one unit more.
-  const int wanted = (total + kTreeMinShare - 1) / kTreeMinShare;
-  const int parts = wanted < a.parts ? wanted : a.parts;
+  // The share with which about a.parts workgroups have pieces, those that their items' ends leave short among them.
+  int room = a.parts - items / 2;
+  room = room < a.parts / 2 ? a.parts / 2 : room;
+  int share = (unsigned)(cost + room - 1) / (unsigned)room;
+  share = uniform(share < kTreeMinShare ? kTreeMinShare : share);
+  const auto pieces_of = [&](int n) { return n > share ? (unsigned)(n + share - 1) / (unsigned)share : 1; };    // of an item
+
+  // Pieces before each thread's requests, those of them that are parts of an item, and the items that have parts.
+  int mine[3] = {0, 0, 0}, upto[3];
+  for (int r = r0; r < r1; ++r) {
+    const Items i = items_of(request_of(a, r));
+    const int n = i.row_tiles * a.c.heads, pieces = pieces_of(i.cost);
+    mine[0] += n * pieces;
+    mine[1] += pieces > 1 ? n * pieces : 0;
+    mine[2] += pieces > 1 ? n : 0;
+  }
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    upto[k] = mine[k];
+    for (int d = 1; d < 64; d <<= 1) {
+      const int x = __shfl_up(upto[k], d);
+      if (lane >= d) upto[k] += x;
+    }
+    if (lane == 63) scan[k][wave] = upto[k];
+  }
+  if (tid == 0) found[0] = -1;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 3; ++k)
+    for (int w = 0; w < wave; ++w) upto[k] += scan[k][w];
   const int w = blockIdx.x;
-  int32_t* desc = a.desc + 4 * (int64_t)w;
-  if (tid == 0) desc[0] = 0;
-  if (w >= parts) return;
-  const int share = (unsigned)total / (unsigned)parts, rest = total - share * parts;
-  int u = w * share + (w < rest ? w : rest);
-  const int u_end = u + share + (w < rest ? 1 : 0);
-  if (upto - mine <= u && u < upto) {
-    int at = upto - mine;
+  if (w == 0 && tid == kTileThreads - 1) *a.desc = upto[2];
+  if (upto[0] - mine[0] <= w && w < upto[0]) {
+    int at[3] = {upto[0] - mine[0], upto[1] - mine[1], upto[2] - mine[2]};
     for (int r = r0; r < r1; ++r) {
-      const int n = units_of(r);
-      if (u < at + n) {
+      const Items i = items_of(request_of(a, r));
+      const int n = i.row_tiles * a.c.heads, pieces = pieces_of(i.cost);
+      if (w < at[0] + n * pieces) {
         found[0] = r;
-        found[1] = u - at;
+        found[1] = w - at[0];
+        found[2] = at[1];
+        found[3] = at[2];
         break;
       }
-      at += n;
+      at[0] += n * pieces;
+      at[1] += pieces > 1 ? n * pieces : 0;
+      at[2] += pieces > 1 ? n : 0;
     }
   }
   __syncthreads();
-  int r = uniform(found[0]), off = uniform(found[1]);
+  const int r = uniform(found[0]);
+  if (r < 0) return;
+  const Request req = request_of(a, r);
+  const Items of = items_of(req);
+  const int pieces = uniform(pieces_of(of.cost)), index = uniform(found[1]);
+  const int item = (unsigned)index / (unsigned)pieces, piece = index - item * pieces;
+  const int head = (unsigned)item / (unsigned)of.row_tiles, row0 = (item - head * of.row_tiles) * kRows;
+  const int64_t slot = uniform(found[2]) + index;         // of its sums, if the item has parts
+  const bool whole = pieces == 1;
+  const int from = of.from + (int)((int64_t)of.tiles * piece / pieces) * kTilePositions;
+  const int piece_stop = of.from + (int)((int64_t)of.tiles * (piece + 1) / pieces) * kTilePositions;
+  const int stop = piece_stop < req.end ? piece_stop : req.end;
+  if (!whole && piece == 0 && tid == 0) {
+    int32_t* desc = a.desc + 8 + 8 * (uniform(found[3]) + item);
+    desc[0] = pieces;
+    desc[1] = (int)slot;
+    desc[2] = r;
+    desc[3] = head;
+    desc[4] = row0;
+  }
+  typedef TileReader<D, ONE_PAGE, QSPLIT> Reader;
+  Reader reader(a, lds, a.table + (int64_t)r * a.width, head, req.end);
+  typename Reader::Ahead ahead;
+  if (from < stop) ahead = reader.start(from);            // else there may be no cache
 
-  // ---- pieces: the units of one item that the workgroup has
-  while (u < u_end) {
-    Request req = request_of(a, r);
-    Items items = items_of(req);
-    while (off >= items.units * items.row_tiles * a.c.heads) {
-      off -= items.units * items.row_tiles * a.c.heads;
-      req = request_of(a, ++r);
-      items = items_of(req);
+  // ---- rows: sharers of each 32 of them, and the halves of a tile that a wavefront has
+  const int rows = req.n * a.group - row0 < kRows ? req.n * a.group - row0 : kRows;
+  const int row_waves = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+  // The wavefronts that have rows are others in every other 256 workgroups, which share the compute units.
+  const int turned = (wave + (blockIdx.x >> 8 & 1) * 2) & 3;
+  const int share_of = turned / row_waves, wave_row = (turned & (row_waves - 1)) * 32;
+  const int pb0 = row_waves == 4 ? 0 : share_of, pb1 = row_waves == 4 ? 2 : share_of + 1;
+  const bool busy = share_of < 2 && wave_row < rows;
+  // What follows from a lane's row is computed where it is used: kept, it would take registers from the products.
+  struct Row { int row, half; int64_t token, head; };    // of the piece; lane / 32; in the call
+  const auto row_of = [&] {
+    const int l = here(lane), at = wave_row + (l & 31);
+    const int row = at < rows ? row0 + at : row0;
+    return Row{at, l >> 5, req.t0 + row / a.group, head * a.group + row % a.group};
+  };
+  QueryRow<D, QSPLIT> mine_of;
+  {
+    const Row me = row_of();
+    mine_of.load(a, me.token * a.q_stride + me.head * D + me.half * 8, busy && me.row < rows);
+    if (tid < kRows) row_mask[tid] = tid < rows ? masks[req.t0 + (row0 + tid) / a.group] : 0;
+  }
+  if (tid == 0) lds.again = 0;
+  __syncthreads();
+  const auto compute = [&](int base, uint64_t valid, int ek, int buf, auto careful) {
+    if (!busy || valid == 0) return;
+    // Whether every row sees all of the tile: cached positions, in reach of the deepest node's window.
+    const bool full = valid == ~0ull && base + kTilePositions <= req.first &&
+                      (!a.window || base > (int64_t)req.first + kMaxNodes - 1 - a.window);
+    uint64_t seen = valid;
+    if (!full) {
+      const int to_nodes = req.first - base;           // of the tile's positions, those before the nodes
+      const uint64_t mask = row_mask[row_of().row];
+      // The first position that the row's window holds; nodes lie at req.first and after.
+      const int depth = mask ? __popcll(mask) - 1 : 0;
+      const int64_t window_from = a.window ? (int64_t)req.first + depth - a.window + 1 : 0;
+      const uint64_t cached = to_nodes >= 64 ? ~0ull : to_nodes > 0 ? (1ull << to_nodes) - 1 : 0;
+      const int64_t skip = window_from - base;
+      const uint64_t reach = skip <= 0 ? ~0ull : skip < 64 ? ~0ull << skip : 0;
+      const uint64_t nodes = to_nodes >= 64 || to_nodes <= -64 ? 0 : to_nodes >= 0 ? mask << to_nodes : mask >> -to_nodes;
+      seen &= (cached & reach) | nodes;
     }
-    const int item = (unsigned)off / (unsigned)items.units, unit0 = off - item * items.units;
-    const int unit1 = u_end - u < items.units - unit0 ? unit0 + u_end - u : items.units;
-    const int head = (unsigned)item / (unsigned)items.row_tiles, row0 = (item - head * items.row_tiles) * kRows;
-    const int piece_u = u;
-    off += unit1 - unit0;
-    u += unit1 - unit0;
-
-    // ---- rows: sharers of each 32 of them, and the halves of a tile that a wavefront has
-    const int rows = req.n * a.group - row0 < kRows ? req.n * a.group - row0 : kRows;
-    const int row_waves = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
-    const int share_of = wave / row_waves, wave_row = (wave & (row_waves - 1)) * 32;
-    const int pb0 = row_waves == 4 ? 0 : share_of, pb1 = row_waves == 4 ? 2 : share_of + 1;
-    const bool busy = share_of < 2 && wave_row < rows;
-    const int row = wave_row + col, token = (row0 + row) / a.group;
-    const bool has_row = row < rows;
-    const int64_t place = (int64_t)(req.t0 + token) * (a.c.heads * a.group) + head * a.group + (row0 + row) % a.group;
-    QueryRow<D, QSPLIT> mine_of;
-    mine_of.load(a, (int64_t)(req.t0 + token) * a.q_stride + (int64_t)(head * a.group + (row0 + row) % a.group) * D + half * 8,
-                 has_row && busy);
-    const uint64_t mask = has_row ? masks[req.t0 + token] : 0;
-    // The first position that the row's window holds; nodes lie at req.first and after.
-    const int depth = mask ? __popcll(mask) - 1 : 0;
-    const int64_t window_from = a.window ? (int64_t)req.first + depth - a.window + 1 : 0;
-
-    if (tid == 0) lds.again = 0;
-    __syncthreads();
-    TileReader<D, ONE_PAGE> reader(a, lds, a.table + (int64_t)r * a.width, head, req.end);
-    const int from = items.from + unit0 * a.unit;
-    const int unit_stop = items.from + unit1 * a.unit;
-    const int stop = unit_stop < req.end ? unit_stop : req.end;
-    const auto compute = [&](int base, uint64_t valid, int ek, int buf, auto careful) {
-      if (!busy || valid == 0) return;
-      // Whether every row sees all of the tile: cached positions, in reach of the deepest node's window.
-      const bool full = valid == ~0ull && base + kTilePositions <= req.first &&
-                        (!a.window || base > (int64_t)req.first + kMaxNodes - 1 - a.window);
-      uint64_t seen = valid;
-      if (!full) {
-        const int to_nodes = req.first - base;           // of the tile's positions, those before the nodes
-        const uint64_t cached = to_nodes >= 64 ? ~0ull : to_nodes > 0 ? (1ull << to_nodes) - 1 : 0;
-        const int64_t skip = window_from - base;
-        const uint64_t reach = skip <= 0 ? ~0ull : skip < 64 ? ~0ull << skip : 0;
-        const uint64_t nodes = to_nodes >= 64 || to_nodes <= -64 ? 0 : to_nodes >= 0 ? mask << to_nodes : mask >> -to_nodes;
-        seen &= (cached & reach) | nodes;
-      }
-#pragma unroll 1
-      for (int pb = pb0; pb < pb1; ++pb) {
-        const uint32_t bits = (uint32_t)(seen >> (32 * pb)) >> (4 * half);
-        mine_of.take(lds, buf, pb, ek, full, [&](int at) { return (bits >> at & 1u) != 0; }, careful);
-      }
-    };
-    const auto go_over = [&](auto careful) {
+#pragma unroll
+    for (int pb = 0; pb < 2; ++pb) {
+      if (pb < pb0 || pb >= pb1) continue;
+      const uint32_t bits = (uint32_t)(seen >> (32 * pb)) >> (4 * (here(lane) >> 5));
+      mine_of.take(lds, buf, pb, ek, full, [&](int at) { return (bits >> at & 1u) != 0; }, careful);
+    }
+  };
+  mine_of.clear();
+  if (from < stop) {
+    reader.go_over(from, stop, ahead, compute);       // its last barrier is after the last time that `again` is set
+    if (uniform(lds.again)) {
       mine_of.clear();
-      if (from < stop) reader.go_over(from, stop, compute, careful);
-    };
-    go_over(std::false_type{});         // its last barrier is after the last time that `again` is set
-    if (uniform(lds.again)) go_over(std::true_type{});
-
-    // ---- a row's sums of two wavefronts together; the tiles' buffers are free after the last barrier
-    float sum = mine_of.sum + __shfl_xor(mine_of.sum, 32);
-    if (row_waves < 4) {
-      f32x4* shared_o = reinterpret_cast<f32x4*>(lds.k);
-      float* shared_rl = lds.vscale[0];               // 64 rows' references, then 64 rows' sums
-      static_assert(sizeof(lds.k) >= 64 * D * 4 && sizeof(lds.vscale) >= 64 * 2 * 4, "the sums of 64 rows fit");
-      if (busy && share_of == 1) {
-#pragma unroll
-        for (int c = 0; c < kCb; ++c)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            shared_o[((c * 4 + i) * 2 + half) * 64 + row] =
-                f32x4{mine_of.o[c][4 * i], mine_of.o[c][4 * i + 1], mine_of.o[c][4 * i + 2], mine_of.o[c][4 * i + 3]};
-        if (half == 0) {
-          shared_rl[row] = mine_of.ref;
-          shared_rl[64 + row] = sum;
-        }
-      }
-      __syncthreads();
-      if (busy && share_of == 0) {
-        const float other = shared_rl[row], top = fmaxf(mine_of.ref, other);
-        const float f = exp2_fast(mine_of.ref - top), g = exp2_fast(other - top);
-        sum = sum * f + shared_rl[64 + row] * g;
-        mine_of.ref = top;
-#pragma unroll
-        for (int c = 0; c < kCb; ++c)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const f32x4 v = shared_o[((c * 4 + i) * 2 + half) * 64 + row];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) mine_of.o[c][4 * i + j] = mine_of.o[c][4 * i + j] * f + v[j] * g;
-          }
-      }
-      __syncthreads();
+      reader.go_over_carefully(from, stop, compute);
     }
+  }
 
-    // ---- out: a lane has 4 consecutive channels of its row at a time
-    const bool whole = unit0 == 0 && unit1 == items.units;
-    const int64_t slot = 2 * (int64_t)w + (unit0 == 0 ? 1 : 0);
-    if (busy && share_of == 0 && has_row) {
-      const float inv = !whole ? 1.0f : sum != 0.0f ? 1.0f / sum : 0.0f;
+  // ---- a row's sums of two wavefronts together; the tiles' buffers are free after the last barrier
+  const Row me = row_of();
+  float sum = mine_of.sum + __shfl_xor(mine_of.sum, 32);
+  if (row_waves < 4) {
+    f32x4* shared_o = reinterpret_cast<f32x4*>(lds.k);
+    float* shared_rl = lds.vscale[0];               // 64 rows' references, then 64 rows' sums
+    static_assert(sizeof(lds.k) >= 64 * D * 4 && sizeof(lds.vscale) >= 64 * 2 * 4, "the sums of 64 rows fit");
+    if (busy && share_of == 1) {
+#pragma unroll
+      for (int c = 0; c < kCb; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          shared_o[((c * 4 + i) * 2 + me.half) * 64 + me.row] =
+              f32x4{mine_of.o[c][4 * i], mine_of.o[c][4 * i + 1], mine_of.o[c][4 * i + 2], mine_of.o[c][4 * i + 3]};
+      if (me.half == 0) {
+        shared_rl[me.row] = mine_of.ref;
+        shared_rl[64 + me.row] = sum;
+      }
+    }
+    __syncthreads();
+    if (busy && share_of == 0) {
+      const float other = shared_rl[me.row], top = fmaxf(mine_of.ref, other);
+      const float f = exp2_fast(mine_of.ref - top), g = exp2_fast(other - top);
+      sum = sum * f + shared_rl[64 + me.row] * g;
+      mine_of.ref = top;
 #pragma unroll
       for (int c = 0; c < kCb; ++c)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const f32x4 v = {mine_of.o[c][4 * i] * inv, mine_of.o[c][4 * i + 1] * inv, mine_of.o[c][4 * i + 2] * inv,
-                           mine_of.o[c][4 * i + 3] * inv};
-          const int ch = 32 * c + 8 * i + 4 * half;
-          if (whole) store_four(a.out, a.out_dtype, place * D + ch, v);
-          else *reinterpret_cast<f32x4*>(a.part_o + (slot * kRows + row) * D + ch) = v;
+          const f32x4 v = shared_o[((c * 4 + i) * 2 + me.half) * 64 + me.row];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) mine_of.o[c][4 * i + j] = mine_of.o[c][4 * i + j] * f + v[j] * g;
         }
-      if (half == 0) {
-        if (!whole) {
-          a.part_rl[(slot * kRows + row) * 2] = mine_of.ref;
-          a.part_rl[(slot * kRows + row) * 2 + 1] = sum;
-        } else if (a.lse) {
-          a.lse[place] = sum != 0.0f ? (mine_of.ref + __log2f(sum)) * kLn2 : -INFINITY;
-        }
-      }
     }
-    if (!whole && unit0 == 0 && tid == 0) {
-      // The item begins here: parts 2 w + 1, then 2 (w + 1), ... of the workgroups up to the one that has
-      // the last unit.
-      const int last_unit = piece_u + items.units - 1, more_units = rest * (share + 1);
-      const int w1 = last_unit < more_units ? last_unit / (share + 1) : rest + (last_unit - more_units) / share;
-      desc[0] = w1 - w + 1;
-      desc[1] = r;
-      desc[2] = head;
-      desc[3] = row0;
+    __syncthreads();
+  }
+
+  // ---- out: a lane has 4 consecutive channels of its row at a time
+  const int64_t place = me.token * (a.c.heads * a.group) + me.head;
+  if (busy && share_of == 0 && me.row < rows) {
+    const float inv = !whole ? 1.0f : sum != 0.0f ? 1.0f / sum : 0.0f;
+#pragma unroll
+    for (int c = 0; c < kCb; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x4 v = {mine_of.o[c][4 * i] * inv, mine_of.o[c][4 * i + 1] * inv, mine_of.o[c][4 * i + 2] * inv,
+                         mine_of.o[c][4 * i + 3] * inv};
+        const int ch = 32 * c + 8 * i + 4 * me.half;
+        if (whole) store_four(a.out, a.out_dtype, place * D + ch, v);
+        else *reinterpret_cast<f32x4*>(a.part_o + (slot * kRows + me.row) * D + ch) = v;
+      }
+    if (me.half == 0) {
+      if (!whole) {
+        a.part_rl[(slot * kRows + me.row) * 2] = mine_of.ref;
+        a.part_rl[(slot * kRows + me.row) * 2 + 1] = sum;
+      } else if (a.lse) {
+        a.lse[place] = sum != 0.0f ? (mine_of.ref + __log2f(sum)) * kLn2 : -INFINITY;
+      }
     }
   }
 }
 
-// D / 4 threads have 4 channels each of a query row; kSlices such groups have every kSlices-th part of it.
+// A workgroup has kPer rows of an item at a time: D / 4 threads have 4 channels each of a row, and kSlices such
+// groups every kSlices-th of its parts.
 template <int D>
 __global__ __launch_bounds__(kTileThreads) void k_kv4_tree_join(AttnArgs a) {
   constexpr int kRows = kTileRows, kSlices = 4, kPer = kTileThreads / (D / 4) / kSlices;
   __shared__ f32x4 sums[kSlices][kPer][D / 4];
   __shared__ float tops[kSlices][kPer], dens[kSlices][kPer];
-  const int64_t w = blockIdx.x;
-  const int32_t* desc = a.desc + 4 * w;
-  const int parts = desc[0];
-  if (parts < 2) return;
-  const Request req = request_of(a, desc[1]);
-  const int head = desc[2], row0 = desc[3];
-  const int rows = req.n * a.group - row0 < kRows ? req.n * a.group - row0 : kRows;
-  if ((int)blockIdx.y * kPer >= rows) return;
+  const int items = a.desc[0];
+  const int most = a.max_new * a.group < kRows ? a.max_new * a.group : kRows, steps = (most + kPer - 1) / kPer;
   const int ch = threadIdx.x % (D / 4), sub = threadIdx.x / (D / 4) % kPer, slice = threadIdx.x / (D / 4) / kPer;
-  const int row = blockIdx.y * kPer + sub;
-  float top = kNone, den = 0.0f;
-  f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-  if (row < rows) {
-    for (int i = slice; i < parts; i += kSlices) {
-      const int64_t slot = i == 0 ? 2 * w + 1 : 2 * (w + i);
-      top = fmaxf(top, a.part_rl[(slot * kRows + row) * 2]);
-    }
+  for (int64_t task = blockIdx.x; task < (int64_t)items * steps; task += gridDim.x) {
+    const int32_t* desc = a.desc + 8 + 8 * (task / steps);
+    const int parts = desc[0], row0 = desc[4], row = (int)(task % steps) * kPer + sub;
+    const int64_t first = desc[1];
+    const Request req = request_of(a, desc[2]);
+    const int rows = req.n * a.group - row0 < kRows ? req.n * a.group - row0 : kRows;
+    if (row - sub >= rows) continue;             // the workgroup's threads together
+    float top = kNone, den = 0.0f;
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (row < rows) {
+      for (int i = slice; i < parts; i += kSlices) top = fmaxf(top, a.part_rl[((first + i) * kRows + row) * 2]);
 #pragma unroll 4
-    for (int i = slice; i < parts; i += kSlices) {
-      const int64_t slot = i == 0 ? 2 * w + 1 : 2 * (w + i);
-      const float f = exp2_fast(a.part_rl[(slot * kRows + row) * 2] - top);
-      den += a.part_rl[(slot * kRows + row) * 2 + 1] * f;
-      v += *reinterpret_cast<const f32x4*>(a.part_o + (slot * kRows + row) * D + 4 * ch) * f;
+      for (int i = slice; i < parts; i += kSlices) {
+        const int64_t at = (first + i) * kRows + row;
+        const float f = exp2_fast(a.part_rl[at * 2] - top);
+        den += a.part_rl[at * 2 + 1] * f;
+        v += *reinterpret_cast<const f32x4*>(a.part_o + at * D + 4 * ch) * f;
+      }
     }
+    sums[slice][sub][ch] = v;
+    if (ch == 0) {
+      tops[slice][sub] = top;
+      dens[slice][sub] = den;
+    }
+    __syncthreads();
+    if (slice == 0 && row < rows) {
+      float highest = top;
+      for (int i = 1; i < kSlices; ++i) highest = fmaxf(highest, tops[i][sub]);
+      const float f = exp2_fast(top - highest);
+      v *= f;
+      den *= f;
+      for (int i = 1; i < kSlices; ++i) {
+        const float g = exp2_fast(tops[i][sub] - highest);
+        v += sums[i][sub][ch] * g;
+        den += dens[i][sub] * g;
+      }
+      const int64_t place = (int64_t)(req.t0 + (row0 + row) / a.group) * (a.c.heads * a.group) + desc[3] * a.group +
+                            (row0 + row) % a.group;
+      const float inv = den != 0.0f ? 1.0f / den : 0.0f;
+      store_four(a.out, a.out_dtype, place * D + 4 * ch, den != 0.0f ? v * inv : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+      if (a.lse && ch == 0) a.lse[place] = den != 0.0f ? (highest + __log2f(den)) * kLn2 : -INFINITY;
+    }
+    __syncthreads();
   }
-  sums[slice][sub][ch] = v;
-  if (ch == 0) {
-    tops[slice][sub] = top;
-    dens[slice][sub] = den;
-  }
-  __syncthreads();
-  if (slice || row >= rows) return;
-  float most = top;
-  for (int i = 1; i < kSlices; ++i) most = fmaxf(most, tops[i][sub]);
-  const float f = exp2_fast(top - most);
-  v *= f;
-  den *= f;
-  for (int i = 1; i < kSlices; ++i) {
-    const float g = exp2_fast(tops[i][sub] - most);
-    v += sums[i][sub][ch] * g;
-    den += dens[i][sub] * g;
-  }
-  const int64_t place = (int64_t)(req.t0 + (row0 + row) / a.group) * (a.c.heads * a.group) + head * a.group +
-                        (row0 + row) % a.group;
-  const float inv = den != 0.0f ? 1.0f / den : 0.0f;
-  store_four(a.out, a.out_dtype, place * D + 4 * ch, den != 0.0f ? v * inv : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
-  if (a.lse && ch == 0) a.lse[place] = den != 0.0f ? (most + __log2f(den)) * kLn2 : -INFINITY;
 }
 
 // ------------------------------------------------------------------ host side
 // Workgroups: two a CU, one at 256 channels.
 template <int D>
 constexpr int kTreeParts = D <= 128 ? 512 : 256;
+constexpr int kTreeJoinGrid = 2048;
 
 template <int D>
 int32_t launch_tree(AttnArgs a, const uint64_t* masks, void* work, hipStream_t stream) {
-  constexpr int kParts = kTreeParts<D>, kPer = kTileThreads / (D / 4) / 4;
+  // The batch has kParts shares at most. An item with parts has more than one, so there are fewer than kParts of them,
+  // with fewer than 2 kParts pieces.
+  constexpr int kParts = kTreeParts<D>, kSlots = 2 * kParts;
   uint8_t* at = static_cast<uint8_t*>(work);
   a.parts = kParts;
   a.desc = reinterpret_cast<int32_t*>(at);
-  a.part_rl = reinterpret_cast<float*>(at + 16 * kParts);
-  a.part_o = a.part_rl + 2 * kParts * kTileRows * 2;
-  static_assert(16 * kParts + (int64_t)2 * kParts * kTileRows * (D + 2) * 4 <= LOGBQ_KV4_WORKSPACE_BYTES,
+  a.part_rl = reinterpret_cast<float*>(at + 32 * (kParts + 1));
+  a.part_o = a.part_rl + kSlots * kTileRows * 2;
+  static_assert(32 * (kParts + 1) + (int64_t)kSlots * kTileRows * (D + 2) * 4 <= LOGBQ_KV4_WORKSPACE_BYTES,
                 "the workspace holds every part");
-  a.unit = kTilePositions;
+  // As many pieces as there can be: a share each, and one an item.
+  const int64_t row_tiles = ((int64_t)a.max_new * a.group + kTileRows - 1) / kTileRows;
+  const int64_t grid = kParts + a.requests * row_tiles * a.c.heads;
+  if (grid > (((int64_t)1 << 32) - 1) / kTileThreads) return LOGBQ_ERR_UNSUPPORTED;
   const bool split = a.q_dtype == LOGBQ_DTYPE_F32, one_page = a.c.page_shift >= 6;
 #define TREE(SPLIT, ONE_PAGE)                                                                        \
   if (split == SPLIT && one_page == ONE_PAGE)                                                        \
-    hipLaunchKernelGGL((k_kv4_tree<D, SPLIT, ONE_PAGE>), dim3(kParts), dim3(kTileThreads), 0, stream, a, masks)
+    hipLaunchKernelGGL((k_kv4_tree<D, SPLIT, ONE_PAGE>), dim3((unsigned)grid), dim3(kTileThreads), 0, stream, \
+                       a, masks)
   TREE(false, false); TREE(false, true); TREE(true, false); TREE(true, true);
 #undef TREE
   if (launch_status() != LOGBQ_OK) return LOGBQ_ERR_HIP;
-  const int rows = a.max_new * a.group < kTileRows ? a.max_new * a.group : kTileRows;
-  hipLaunchKernelGGL(k_kv4_tree_join<D>, dim3(kParts, (rows + kPer - 1) / kPer), dim3(kTileThreads), 0, stream, a);
+  hipLaunchKernelGGL(k_kv4_tree_join<D>, dim3(kTreeJoinGrid), dim3(kTileThreads), 0, stream, a);
   return launch_status();
 }
 
@@ -695,9 +772,9 @@ int32_t logbq_kv4_tree_attention(const void* q_dev, int64_t q_stride, int32_t q_
                                      lse_dev, work_dev, work_bytes, &a);
   if (bad != LOGBQ_OK) return bad;
   if (max_new > kMaxNodes || (window > 0 && window < kMaxNodes)) return LOGBQ_ERR_UNSUPPORTED;
-  // Units of 64 positions of up to 128 query rows, and at least one of each, fit 31 bits.
+  // Tiles of 64 positions of up to 128 query rows, and at least one of each, fit 29 bits, as their costs do 31.
   const int64_t row_tiles = (max_new * a.group + kTileRows - 1) / kTileRows;
-  if ((double)requests * a.c.heads * row_tiles * ((double)width * cache->page / kTilePositions + 1) >= INT32_MAX)
+  if ((double)requests * a.c.heads * row_tiles * ((double)width * cache->page / kTilePositions + 1) >= (1 << 29))
     return LOGBQ_ERR_UNSUPPORTED;
   if (tokens == 0 || requests == 0 || max_new == 0) return LOGBQ_OK;
   if (!masks_dev) return LOGBQ_ERR_INVALID_ARG;

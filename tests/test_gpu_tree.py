@@ -219,6 +219,16 @@ def test_lengths_that_do_not_fit():
     attend(q, cache, table, lens, new, masks, 16)
 
 
+def test_a_cache_without_pages_and_a_table_without_columns():
+    q = torch.randn(5, 4, 64, device=DEV).half()
+    bits, starts, lens = dev(np.full(5, 31, dtype=np.int64)), ints([0, 3, 5]), ints([10, 2])
+    for pages, width in ((0, 0), (0, 2), (2, 0)):
+        out, lse = torch.full_like(q, 7.0), torch.zeros(5, 4, device=DEV)
+        L.kv4_tree_attention(q, L.kv4_cache(pages, 2, 64, 16), torch.zeros((2, width), dtype=torch.int32, device=DEV), lens,
+                             starts, bits, 3, out=out, lse=lse)
+        assert not out.any() and torch.isneginf(lse).all()
+
+
 def test_max_new_leaves_tokens_out():
     lens, new = [100, 30], [20, 6]
     q, cache, table, masks = step(7, lens, new, 1, 4, 128, 16, "f16")
