@@ -1,13 +1,16 @@
 // gfx950 kernels of low-rank adapters beside the quantized linears, and their entry points of the C ABI:
 // y[t] + scale (x[t] A^T) B^T with the adapter of the request that token t belongs to.
 //
-//   k_adapter_shrink   h = x A^T, K split over wavefronts and workgroups.
-//   k_adapter_expand   out = y + scale h B^T.
+//   k_adapter_shrink_few, k_adapter_expand_few   requests of up to four tokens: h = x A^T by rows of A, and
+//                      out = y + scale h B^T by rows of B, which stream past a few activations in registers.
+//   k_adapter_shrink, k_adapter_expand           more tokens: the same with MFMAs, K split over wavefronts and
+//                      workgroups.
 
 #include <hip/hip_runtime.h>
 
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "kv4_detail.h"
 #include "logbq.h"
@@ -16,10 +19,13 @@ namespace {
 
 constexpr int kAdThreads = 256;
 constexpr int kAdWaves = kAdThreads / 64;
-constexpr int kAdTile = 32;                    // tokens of a tile, and ranks of a rank tile
+constexpr int kAdTile = 32;                    // tokens of a tile
+constexpr int kRankTile = 16;
+constexpr int kFewTokens = 4;                  // tokens of requests that go without tiles
 constexpr int kAdCount = 4;                    // projections of a call
 constexpr int kAdRank = LOGBQ_ADAPTERS_MAX_RANK;
 constexpr int kAdColumns = 256;                // out features of a workgroup of the second kernel
+constexpr int kFewColumns = 512;               // the same for requests of a few tokens
 constexpr int kAdSplits = 16;
 constexpr int64_t kAdSplitTokens = 32768;      // tokens times splits, where K is split
 
@@ -36,6 +42,7 @@ struct AdapterArgs {
   const int32_t* ranks;
   const float* scales;
   float* h;                                    // [splits][tokens][count][rank]
+  int32_t* tiles;                              // [tiles][4]: what the second kernel has to know of a tile
   int64_t k;
   int32_t tokens, requests, adapters, rank, count, max_new, splits;
 };
@@ -54,11 +61,11 @@ __device__ __forceinline__ Span tokens_of(const AdapterArgs& a, int r) {
   return {t0, t1 - t0 < a.max_new ? t1 - t0 : a.max_new};
 }
 
-// The tile of an index. Requests of up to 32 tokens are a tile each; longer ones are counted out by the
-// workgroup, which all of its threads call this for.
+// The tile of an index. Where no request has more than a few tokens they are a tile each; else the workgroup counts
+// tiles out, which all of its threads call this for.
 __device__ __forceinline__ TokenTile tile_of(const AdapterArgs& a, int64_t index) {
   int r = (int)index, first = 0;
-  if (a.max_new > kAdTile) {
+  if (a.max_new > kFewTokens) {
     __shared__ int64_t scan[kAdWaves];
     __shared__ int32_t found[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -118,200 +125,441 @@ __device__ __forceinline__ float16v product(u32x4 a, u32x4 b, float16v c) {
 // What rounding x to bfloat16 leaves, 0 where it leaves nothing (an infinity less itself would be NaN).
 __device__ __forceinline__ float rest_of(float x, __bf16 h) { return (float)h == x ? 0.0f : x - (float)h; }
 
-// h^T = A x^T with 32x32x16 MFMAs: a wavefront has its share of K for one tile of tokens and up to G tiles
-// of 32 ranks (of any of the projections), so that activations are read once for them. float16 activations
-// are the sum of two bfloat16 numbers exactly, which is how they meet bfloat16 weights.
+// ------------------------------------------------------------------ a few tokens
+// Both products stream the adapter's weights once: bound by HBM where many adapters are in use, by latency
+// otherwise. A wavefront's loads are 1 KiB of consecutive weights of a row of A (8 a lane), or of rows of B.
+constexpr int kFewRows = 4;                    // ranks of a workgroup of the first kernel
+
+// Float32 values of 8 weights or activations.
+template <bool BF16>
+__device__ __forceinline__ void eight_values(const u32x4& v, float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (BF16) {
+      x[2 * i] = __uint_as_float(v[i] << 16);
+      x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+    } else {
+      const half2v h = __builtin_bit_cast(half2v, (uint32_t)v[i]);
+      x[2 * i] = (float)h.x;
+      x[2 * i + 1] = (float)h.y;
+    }
+  }
+}
+
+// Sum over groups of L lanes (1 .. 64, a power of two), the same in all of them.
+template <int L>
+__device__ __forceinline__ float lanes_sum(float x) {
+  const auto turned = [](float v, auto by) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), decltype(by)::value, 0xf, 0xf, true));
+  };
+  if constexpr (L >= 2) x += turned(x, std::integral_constant<int, 0xb1>{});       // quads 1 0 3 2
+  if constexpr (L >= 4) x += turned(x, std::integral_constant<int, 0x4e>{});       // quads 2 3 0 1
+  if constexpr (L >= 8) x += turned(x, std::integral_constant<int, 0x141>{});      // halves of 16, mirrored
+  if constexpr (L >= 16) x += turned(x, std::integral_constant<int, 0x140>{});     // 16, mirrored
+  if constexpr (L >= 32) x += __shfl_xor(x, 16);
+  if constexpr (L >= 64) x += __shfl_xor(x, 32);
+  return x;
+}
+
+// Four ranks of a projection a workgroup; its wavefronts have every fourth 512 of K, so that all loads of K = 4096
+// are on their way at once.
+template <bool BF16, int T>
+__global__ __launch_bounds__(kAdThreads) void k_adapter_shrink_few(AdapterArgs a) {
+  __shared__ float sums[kAdWaves][T][kFewRows];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const TokenTile tile = tile_of(a, blockIdx.x);
+  const int per_projection = a.rank / kFewRows;
+  const int projection = (int)blockIdx.y / per_projection, row0 = ((int)blockIdx.y - projection * per_projection) * kFewRows;
+  if (tile.n <= 0 || row0 >= tile.rank) return;
+  const uint16_t* from = a.a[projection] + ((int64_t)tile.adapter * a.rank + row0) * a.k;
+  float acc[T][kFewRows];
+#pragma unroll
+  for (int t = 0; t < T; ++t)
+#pragma unroll
+    for (int i = 0; i < kFewRows; ++i) acc[t][i] = 0.0f;
+#pragma unroll 2
+  for (int64_t k = wave * 512 + lane * 8; k < a.k; k += kAdWaves * 512) {
+    u32x4 w[kFewRows], x[T];
+#pragma unroll
+    for (int i = 0; i < kFewRows; ++i)                   // the pool has the rows past the adapter's rank
+      w[i] = *reinterpret_cast<const u32x4*>(from + i * a.k + k);
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+      x[t] = *reinterpret_cast<const u32x4*>(a.x + (int64_t)(tile.t0 + (t < tile.n ? t : 0)) * a.k + k);
+    float xf[T][8];
+#pragma unroll
+    for (int t = 0; t < T; ++t) eight_values<false>(x[t], xf[t]);
+#pragma unroll
+    for (int i = 0; i < kFewRows; ++i) {
+      float wf[8];
+      eight_values<BF16>(w[i], wf);
+#pragma unroll
+      for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[t][i] = __builtin_fmaf(xf[t][j], wf[j], acc[t][i]);
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < T; ++t)
+#pragma unroll
+    for (int i = 0; i < kFewRows; ++i) {
+      const float v = lanes_sum<64>(acc[t][i]);
+      if (lane == 0) sums[wave][t][i] = v;
+    }
+  __syncthreads();
+  if (tid < T * kFewRows) {
+    const int t = tid / kFewRows, i = tid % kFewRows;
+    float v = sums[0][t][i];
+    for (int w = 1; w < kAdWaves; ++w) v += sums[w][t][i];
+    if (t < tile.n)
+      a.h[(((int64_t)tile.t0 + t) * a.count + projection) * a.rank + row0 + i] = v;
+  }
+}
+
+// L lanes have a row of B, 8 ranks each; 64 rows a wavefront at a time, of which lane i in the end has the sums of
+// row i, so that the outputs are consecutive.
+template <bool BF16, int T, int L>
+__device__ __forceinline__ void expand_few(const AdapterArgs& a, const TokenTile& tile, int projection, int n0) {
+  const int lane = threadIdx.x & 63, sub = lane & (L - 1), group = lane / L;
+  const int width = a.n[projection], r = 8 * sub;
+  const bool has = r < tile.rank;
+  const float scale = a.scales ? a.scales[tile.adapter] : 1.0f;
+  float h[T][8];
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) h[t][j] = 0.0f;
+    if (t < tile.n && has) {
+      load_row<LOGBQ_DTYPE_F32>(a.h, (((int64_t)tile.t0 + t) * a.count + projection) * a.rank + r, h[t]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) h[t][j] = r + j < tile.rank ? h[t][j] * scale : 0.0f;
+    }
+  }
+  const uint16_t* from = a.b[projection] + (int64_t)tile.adapter * width * a.rank + r;
+  const int stop = n0 + kFewColumns / kAdWaves < width ? n0 + kFewColumns / kAdWaves : width;
+  for (int n = n0; n < stop; n += 64) {
+    u32x4 w[L];
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      const int row = n + group * L + i;
+      w[i] = has && row < stop ? *reinterpret_cast<const u32x4*>(from + (int64_t)row * a.rank) : u32x4{0, 0, 0, 0};
+    }
+    float y[T], sum[T];
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      y[t] = t < tile.n && n + lane < stop ? a.y[projection][(int64_t)(tile.t0 + t) * width + n + lane] : 0.0f;
+      sum[t] = 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      float wf[8];
+      eight_values<BF16>(w[i], wf);
+      // What lies past the adapter's rank is not its own.
+#pragma unroll
+      for (int j = 0; j < 8; ++j) wf[j] = r + j < tile.rank ? wf[j] : 0.0f;
+#pragma unroll
+      for (int t = 0; t < T; ++t) {
+        float v = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v = __builtin_fmaf(h[t][j], wf[j], v);
+        v = lanes_sum<L>(v);
+        sum[t] = sub == i ? v : sum[t];
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+      if (t < tile.n && n + lane < stop) a.out[projection][(int64_t)(tile.t0 + t) * width + n + lane] = y[t] + sum[t];
+  }
+}
+
+template <bool BF16, int T>
+__global__ __launch_bounds__(kAdThreads) void k_adapter_expand_few(AdapterArgs a) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const TokenTile tile = tile_of(a, blockIdx.x);
+  if (tile.n <= 0) return;
+  int projection = 0;
+  while (projection + 1 < a.count && (int)blockIdx.y >= a.block0[projection + 1]) ++projection;
+  const int n0 = ((int)blockIdx.y - a.block0[projection]) * kFewColumns + wave * (kFewColumns / kAdWaves);
+  const int width = a.n[projection];
+  if (n0 >= width) return;
+  if (tile.rank > 64) return expand_few<BF16, T, 16>(a, tile, projection, n0);
+  if (tile.rank > 32) return expand_few<BF16, T, 8>(a, tile, projection, n0);
+  if (tile.rank > 16) return expand_few<BF16, T, 4>(a, tile, projection, n0);
+  if (tile.rank > 8) return expand_few<BF16, T, 2>(a, tile, projection, n0);
+  if (tile.rank > 0) return expand_few<BF16, T, 1>(a, tile, projection, n0);
+  if (a.y[projection] == a.out[projection]) return;
+  for (int t = 0; t < tile.n; ++t)
+    for (int n = n0 + lane; n < n0 + kFewColumns / kAdWaves && n < width; n += 64)
+      a.out[projection][(int64_t)(tile.t0 + t) * width + n] = a.y[projection][(int64_t)(tile.t0 + t) * width + n];
+}
+
+// ------------------------------------------------------------------ more tokens
+// h^T = A x^T with 16x16x32 MFMAs, whose operands are 64 consecutive bytes of 16 rows: a wavefront has its share of K
+// for a tile of tokens and up to G tiles of 16 ranks (of any of the projections), so that activations are read once
+// for them. float16 activations are the sum of two bfloat16 numbers exactly, which is how they meet bfloat16 weights.
+// Bound by the loads' rows, which are apart.
+template <bool BF16>
+__device__ __forceinline__ f32x4 small_product(u32x4 a, u32x4 b, f32x4 c) {
+  if constexpr (BF16)
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8v, a), __builtin_bit_cast(half8v, b), c, 0, 0, 0);
+}
+
 template <bool BF16, int G>
 __global__ __launch_bounds__(kAdThreads) void k_adapter_shrink(AdapterArgs a) {
-  __shared__ float sums[kAdWaves][kAdTile][kAdTile + 4];
+  constexpr int kAhead = 2;                      // steps of 32 whose loads are on their way together: 128 bytes of a row
+  __shared__ float sums[kAdWaves][kAdTile][kRankTile + 4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int col = lane & 31, half = lane >> 5;
+  const int col = lane & 15, quarter = lane >> 4;
   const TokenTile tile = tile_of(a, blockIdx.x);
+  if (blockIdx.y == 0 && blockIdx.z == 0 && tid == 0)
+    *reinterpret_cast<int4*>(a.tiles + 4 * (int64_t)blockIdx.x) = int4{tile.t0, tile.n, tile.adapter, tile.rank};
   if (tile.n <= 0 || tile.rank <= 0) return;
-  const int per_projection = (a.rank + kAdTile - 1) / kAdTile;
+  const int per_projection = (a.rank + kRankTile - 1) / kRankTile;
   const int id0 = blockIdx.z * G, ids = a.count * per_projection;
-  const int64_t steps = a.k / 16, chunks = (int64_t)a.splits * kAdWaves, chunk = blockIdx.y * kAdWaves + wave;
-  const int step0 = (int)(steps * chunk / chunks), step1 = (int)(steps * (chunk + 1) / chunks);
+  const int64_t blocks = (a.k + 32 * kAhead - 1) / (32 * kAhead), chunks = (int64_t)a.splits * kAdWaves;
+  const int64_t chunk = blockIdx.y * kAdWaves + wave;
+  const int step0 = (int)(blocks * chunk / chunks) * kAhead, all = (int)(a.k / 32);
+  const int end = (int)(blocks * (chunk + 1) / chunks) * kAhead, step1 = end < all ? end : all;
 
-  const bool has_token = col < tile.n;
-  const uint16_t* x = a.x + (int64_t)(tile.t0 + (has_token ? col : 0)) * a.k + 8 * half;
+  const uint16_t* x[2];
+  bool has_token[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    has_token[h] = 16 * h + col < tile.n;
+    x[h] = a.x + (int64_t)(tile.t0 + (has_token[h] ? 16 * h + col : 0)) * a.k + 8 * quarter;
+  }
+  const bool both = tile.n > 16;
   const uint16_t* rows[G];
   bool has_row[G], any[G];
 #pragma unroll
   for (int g = 0; g < G; ++g) {
     const int projection = id0 + g < ids ? (id0 + g) / per_projection : 0;
-    const int row = (id0 + g) % per_projection * kAdTile + col;
+    const int row = (id0 + g) % per_projection * kRankTile + col;
     any[g] = id0 + g < ids && row - col < tile.rank;
     has_row[g] = any[g] && row < tile.rank;
-    rows[g] = a.a[projection] + ((int64_t)tile.adapter * a.rank + (has_row[g] ? row : 0)) * a.k + 8 * half;
+    rows[g] = a.a[projection] + ((int64_t)tile.adapter * a.rank + (has_row[g] ? row : 0)) * a.k + 8 * quarter;
   }
-  float16v acc[G];
+  f32x4 acc[G][2];
 #pragma unroll
-  for (int g = 0; g < G; ++g)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) acc[g][i] = 0.0f;
+  for (int g = 0; g < G; ++g) acc[g][0] = acc[g][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   const u32x4 zero = {0, 0, 0, 0};
-#pragma unroll 4
-  for (int s = step0; s < step1; ++s) {
-    const u32x4 xv = has_token ? *reinterpret_cast<const u32x4*>(x + (int64_t)16 * s) : zero;
-    u32x4 lo = zero, hi = xv;
-    if constexpr (BF16) {
-      const half8v v = __builtin_bit_cast(half8v, xv);
-      bf16x8 h, l;
+  for (int s = step0; s < step1; s += kAhead) {
+    u32x4 xv[kAhead][2], av[kAhead][G];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        h[j] = (__bf16)(float)v[j];
-        l[j] = (__bf16)rest_of((float)v[j], h[j]);
+    for (int u = 0; u < kAhead; ++u) {
+      const bool in = s + u < step1;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        xv[u][h] = has_token[h] && in ? *reinterpret_cast<const u32x4*>(x[h] + (int64_t)32 * (s + u)) : zero;
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+        av[u][g] = has_row[g] && in ? *reinterpret_cast<const u32x4*>(rows[g] + (int64_t)32 * (s + u)) : zero;
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (h && !both) continue;
+        u32x4 lo = zero, hi = xv[u][h];
+        if constexpr (BF16) {
+          const half8v v = __builtin_bit_cast(half8v, xv[u][h]);
+          bf16x8 high, low;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            high[j] = (__bf16)(float)v[j];
+            low[j] = (__bf16)rest_of((float)v[j], high[j]);
+          }
+          hi = __builtin_bit_cast(u32x4, high);
+          lo = __builtin_bit_cast(u32x4, low);
+        }
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          acc[g][h] = small_product<BF16>(av[u][g], hi, acc[g][h]);
+          if constexpr (BF16) acc[g][h] = small_product<BF16>(av[u][g], lo, acc[g][h]);
+        }
       }
-      hi = __builtin_bit_cast(u32x4, h);
-      lo = __builtin_bit_cast(u32x4, l);
-    }
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
-      if (!any[g]) continue;
-      const u32x4 av = has_row[g] ? *reinterpret_cast<const u32x4*>(rows[g] + (int64_t)16 * s) : zero;
-      acc[g] = product<BF16>(av, hi, acc[g]);
-      if constexpr (BF16) acc[g] = product<BF16>(av, lo, acc[g]);
-    }
   }
 #pragma unroll
   for (int g = 0; g < G; ++g) {
     if (!any[g]) continue;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      *reinterpret_cast<f32x4*>(&sums[wave][col][8 * i + 4 * half]) =
-          f32x4{acc[g][4 * i], acc[g][4 * i + 1], acc[g][4 * i + 2], acc[g][4 * i + 3]};
+    for (int h = 0; h < 2; ++h) *reinterpret_cast<f32x4*>(&sums[wave][16 * h + col][4 * quarter]) = acc[g][h];
     __syncthreads();
-    const int token = tid >> 3, at = (tid & 7) * 4;
-    const int projection = (id0 + g) / per_projection, row = (id0 + g) % per_projection * kAdTile + at;
-    f32x4 v = *reinterpret_cast<const f32x4*>(&sums[0][token][at]);
-    for (int w = 1; w < kAdWaves; ++w) v += *reinterpret_cast<const f32x4*>(&sums[w][token][at]);
-    if (token < tile.n && row < a.rank)
+    const int token = tid >> 2, at = (tid & 3) * 4;
+    const int projection = (id0 + g) / per_projection, row = (id0 + g) % per_projection * kRankTile + at;
+    if (token < tile.n && row < a.rank) {
+      f32x4 v = *reinterpret_cast<const f32x4*>(&sums[0][token][at]);
+      for (int w = 1; w < kAdWaves; ++w) v += *reinterpret_cast<const f32x4*>(&sums[w][token][at]);
       *reinterpret_cast<f32x4*>(a.h + ((((int64_t)blockIdx.y * a.tokens + tile.t0 + token) * a.count + projection) *
                                        a.rank + row)) = v;
+    }
     __syncthreads();
   }
 }
 
-// out = y + scale h B^T: a wavefront has 64 out features of a tile of tokens. h, summed over the splits,
-// goes into the products as two float16 numbers about its token's largest (22 bits) or as three bfloat16
-// ones (24 bits), so that nothing is lost beside float32 sums.
-template <bool BF16>
+// out = y + scale h B^T for a tile of tokens and 256 out features: 64 a wavefront, by 32x32x16 MFMAs, whose
+// results go through LDS so that y is read and written a row's 1 KiB at a time (straight from the MFMAs' layout, 128
+// bytes of 32 rows each, the same took 92 us, where this takes 60). Bound by reading and writing y. h, summed over the splits,
+// goes into the products as two float16 numbers about its token's largest (22 bits) or as three bfloat16 ones (24
+// bits), so that nothing is lost beside float32 sums. STEPS: products of 16 ranks that the pool has room for.
+template <bool BF16, int STEPS>
 __global__ __launch_bounds__(kAdThreads) void k_adapter_expand(AdapterArgs a) {
-  constexpr int kSteps = kAdRank / 16, kTerms = BF16 ? 3 : 2;
-  __shared__ float factor[kAdWaves][kAdTile];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  constexpr int kTerms = BF16 ? 3 : 2, kRows = kAdTile / kAdWaves;
+  __shared__ float factors[kAdWaves][kAdTile];
+  __shared__ float sums[kAdTile][kAdColumns + 4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
-  const TokenTile tile = tile_of(a, blockIdx.x);
+  const int4 known = *reinterpret_cast<const int4*>(a.tiles + 4 * (int64_t)blockIdx.x);
+  const auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  const TokenTile tile = {uniform(known.x), uniform(known.y), uniform(known.z), uniform(known.w)};
   if (tile.n <= 0) return;
   int projection = 0;
   while (projection + 1 < a.count && (int)blockIdx.y >= a.block0[projection + 1]) ++projection;
-  const int n0 = ((int)blockIdx.y - a.block0[projection]) * kAdColumns + wave * (kAdColumns / kAdWaves);
+  const int n0 = ((int)blockIdx.y - a.block0[projection]) * kAdColumns;
   const int width = a.n[projection];
-  const float* y = a.y[projection];
-  float* out = a.out[projection];
-  if (n0 >= width) return;                       // no barrier below: a wavefront's LDS is its own
+  const int stop = n0 + kAdColumns < width ? n0 + kAdColumns : width;
+  const float* y = a.y[projection] + (int64_t)tile.t0 * width;
+  float* out = a.out[projection] + (int64_t)tile.t0 * width;
   if (tile.rank <= 0) {
     if (y == out) return;
-    for (int t = 0; t < tile.n; ++t)
-      if (n0 + lane < width) out[(int64_t)(tile.t0 + t) * width + n0 + lane] = y[(int64_t)(tile.t0 + t) * width + n0 + lane];
+    for (int t = wave; t < tile.n; t += kAdWaves)
+      for (int n = n0 + lane; n < stop; n += 64) out[(int64_t)t * width + n] = y[(int64_t)t * width + n];
     return;
   }
 
-  float base[2][16];
+  // A wavefront reads and writes rows kRows wave .. of a pass: four consecutive columns a lane, or, where rows are not
+  // aligned for that, columns 64 apart.
+  const bool vectors = width % 4 == 0 && ((uintptr_t)y | (uintptr_t)out) % 16 == 0;
+  // What lies past the tile is read from its last row and column; loads without branches leave their registers alone.
+  f32x4 base[kRows];
+  const auto row_at = [&](int i) {
+    const int t = kRows * wave + i;
+    return y + (int64_t)(t < tile.n ? t : tile.n - 1) * width;
+  };
+  if (vectors) {
+    const int at = n0 + 4 * lane < stop ? n0 + 4 * lane : stop - 4;
 #pragma unroll
-  for (int nb = 0; nb < 2; ++nb)
+    for (int i = 0; i < kRows; ++i) base[i] = *reinterpret_cast<const f32x4*>(row_at(i) + at);
+  } else {
+    int at[4];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int t = 8 * (i >> 2) + 4 * half + (i & 3), n = n0 + 32 * nb + col;
-      base[nb][i] = t < tile.n && n < width ? y[(int64_t)(tile.t0 + t) * width + n] : 0.0f;
-    }
-  // The lane's part of its token's h, summed in the order of the splits.
-  float h[kSteps][8];
-  float most = 0.0f;
-  const float scale = a.scales ? a.scales[tile.adapter] : 1.0f;
+    for (int j = 0; j < 4; ++j) at[j] = n0 + 64 * j + lane < stop ? n0 + 64 * j + lane : stop - 1;
 #pragma unroll
-  for (int s = 0; s < kSteps; ++s) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) h[s][j] = 0.0f;
-    const int r = 16 * s + 8 * half;
-    if (r >= tile.rank || col >= tile.n) continue;
-    const float* from = a.h + (((int64_t)tile.t0 + col) * a.count + projection) * a.rank + r;
-    for (int i = 0; i < a.splits; ++i) {
-      float v[8];
-      load_row<LOGBQ_DTYPE_F32>(from, 0, v);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) h[s][j] += v[j];
-      from += (int64_t)a.tokens * a.count * a.rank;
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      h[s][j] *= scale;
-      most = fmaxf(most, __builtin_fabsf(h[s][j]));
+    for (int i = 0; i < kRows; ++i) {
+      const float* from = row_at(i);
+      base[i] = f32x4{from[at[0]], from[at[1]], from[at[2]], from[at[3]]};
     }
   }
-  most = fmaxf(most, __shfl_xor(most, 32));
-  const int e = most > 0.0f && most < INFINITY ? (int)(__float_as_uint(most) >> 23) - 127 : 0;
-  if (half == 0) factor[wave][col] = ldexpf(1.0f, e);
+  const uint16_t* b = a.b[projection] + (int64_t)tile.adapter * width * a.rank + 8 * half;
+  u32x4 weights[2][STEPS];
+#pragma unroll
+  for (int nb = 0; nb < 2; ++nb) {
+    const int at = n0 + 64 * wave + 32 * nb + col;
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s)
+      weights[nb][s] = at < stop && 16 * s + 8 * half < tile.rank
+                           ? *reinterpret_cast<const u32x4*>(b + (int64_t)at * a.rank + 16 * s) : u32x4{0, 0, 0, 0};
+  }
 
-  float16v acc[2];
+  // The lane's part of its token's h, summed in the order of the splits, as terms.
+  u32x4 term[STEPS][kTerms];
+  {
+    float h[STEPS][8];
+    float most = 0.0f;
+    const float scale = a.scales ? a.scales[tile.adapter] : 1.0f;
 #pragma unroll
-  for (int nb = 0; nb < 2; ++nb)
+    for (int s = 0; s < STEPS; ++s) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) acc[nb][i] = 0.0f;
+      for (int j = 0; j < 8; ++j) h[s][j] = 0.0f;
+      const int r = 16 * s + 8 * half;
+      if (r < tile.rank && col < tile.n) {
+        const float* from = a.h + (((int64_t)tile.t0 + col) * a.count + projection) * a.rank + r;
+#pragma unroll 1
+        for (int i = 0; i < a.splits; ++i) {
+          float v[8];
+          load_row<LOGBQ_DTYPE_F32>(from, 0, v);
 #pragma unroll
-  for (int s = 0; s < kSteps; ++s) {
-    if (16 * s >= tile.rank) break;
-    u32x4 term[kTerms];
-    float left[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) left[j] = ldexpf(h[s][j], -e);
-#pragma unroll
-    for (int i = 0; i < kTerms; ++i) {
-      if constexpr (BF16) {
-        bf16x8 v;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          v[j] = (__bf16)left[j];
-          left[j] = rest_of(left[j], v[j]);
+          for (int j = 0; j < 8; ++j) h[s][j] += v[j];
+          from += (int64_t)a.tokens * a.count * a.rank;
         }
-        term[i] = __builtin_bit_cast(u32x4, v);
-      } else {
-        half8v v;
+      }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          v[j] = (half_t)left[j];
-          left[j] -= (float)v[j];
-        }
-        term[i] = __builtin_bit_cast(u32x4, v);
+      for (int j = 0; j < 8; ++j) {
+        h[s][j] *= scale;
+        most = fmaxf(most, __builtin_fabsf(h[s][j]));
       }
     }
-    const int r = 16 * s + 8 * half;
+    int e = 0;
+    if constexpr (!BF16) {
+      most = fmaxf(most, __shfl_xor(most, 32));
+      e = most > 0.0f && most < INFINITY ? (int)(__float_as_uint(most) >> 23) - 127 : 0;
+      if (half == 0) factors[wave][col] = ldexpf(1.0f, e);     // read by the same wavefront, after a barrier
+    }
 #pragma unroll
-    for (int nb = 0; nb < 2; ++nb) {
-      const int n = n0 + 32 * nb + col;
-      u32x4 bv = {0, 0, 0, 0};
-      if (n < width && r < tile.rank) {
-        bv = *reinterpret_cast<const u32x4*>(a.b[projection] + ((int64_t)tile.adapter * width + n) * a.rank + r);
-        // What lies past the adapter's rank is not its own.
+    for (int s = 0; s < STEPS; ++s) {
+      float left[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          bv[j] = r + 2 * j + 1 < tile.rank ? bv[j] : r + 2 * j < tile.rank ? bv[j] & 0xffffu : 0u;
+      for (int j = 0; j < 8; ++j) left[j] = BF16 ? h[s][j] : ldexpf(h[s][j], -e);
+#pragma unroll
+      for (int i = 0; i < kTerms; ++i) {
+        if constexpr (BF16) {
+          bf16x8 v;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            v[j] = (__bf16)left[j];
+            left[j] = rest_of(left[j], v[j]);
+          }
+          term[s][i] = __builtin_bit_cast(u32x4, v);
+        } else {
+          half8v v;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            v[j] = (half_t)left[j];
+            left[j] -= (float)v[j];
+          }
+          term[s][i] = __builtin_bit_cast(u32x4, v);
         }
       }
-#pragma unroll
-      for (int i = kTerms - 1; i >= 0; --i) acc[nb] = product<BF16>(term[i], bv, acc[nb]);
     }
   }
-  __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-  __builtin_amdgcn_wave_barrier();
+
 #pragma unroll
-  for (int nb = 0; nb < 2; ++nb)
+  for (int nb = 0; nb < 2; ++nb) {
+    float16v acc;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int t = 8 * (i >> 2) + 4 * half + (i & 3), n = n0 + 32 * nb + col;
-      if (t < tile.n && n < width) out[(int64_t)(tile.t0 + t) * width + n] = base[nb][i] + acc[nb][i] * factor[wave][t];
+    for (int i = 0; i < 16; ++i) acc[i] = 0.0f;
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      if (16 * s >= tile.rank) break;
+      u32x4 bv = weights[nb][s];
+      // What lies past the adapter's rank is not its own.
+      const int r = 16 * s + 8 * half;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) bv[j] = r + 2 * j + 1 < tile.rank ? bv[j] : r + 2 * j < tile.rank ? bv[j] & 0xffffu : 0u;
+#pragma unroll
+      for (int i = kTerms - 1; i >= 0; --i) acc = product<BF16>(term[s][i], bv, acc);
     }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sums[8 * (i >> 2) + 4 * half + (i & 3)][64 * wave + 32 * nb + col] = acc[i];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) {
+    const int t = kRows * wave + i;
+    if (t >= tile.n) continue;
+    const float f = BF16 ? 1.0f : factors[wave][t];
+    float* to = out + (int64_t)t * width + n0;
+    if (vectors) {
+      const f32x4 v = *reinterpret_cast<const f32x4*>(&sums[t][4 * lane]);
+      if (n0 + 4 * lane < stop) __builtin_nontemporal_store(base[i] + v * f, reinterpret_cast<f32x4*>(to + 4 * lane));
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (n0 + 64 * j + lane < stop) to[64 * j + lane] = base[i][j] + sums[t][64 * j + lane] * f;
+    }
+  }
 }
 
 // ------------------------------------------------------------------ host side
@@ -329,7 +577,8 @@ int64_t logbq_linear_adapters_workspace(int64_t tokens, int32_t count, int32_t r
   if (tokens < 0 || count < 1 || rank < 1 || !adapter_sizes_fit(tokens, count, rank)) return 0;
   int64_t rows = tokens * kAdSplits < kAdSplitTokens ? tokens * kAdSplits : kAdSplitTokens;
   rows = rows > tokens ? rows : tokens;
-  return rows * count * rank * 4;
+  // A request's last tile is not full, so there may be a tile a token and as many as all of them fill.
+  return rows * count * rank * 4 + 16 * (tokens + tokens / kAdTile + 1);
 }
 
 int32_t logbq_linear_adapters(const uint16_t* x_dev, int64_t tokens, int64_t k, int32_t count,
@@ -349,17 +598,18 @@ int32_t logbq_linear_adapters(const uint16_t* x_dev, int64_t tokens, int64_t k, 
       adapters >= INT32_MAX)
     return LOGBQ_ERR_UNSUPPORTED;
   AdapterArgs a = {};
+  const int columns = max_new <= kFewTokens ? kFewColumns : kAdColumns;
   int64_t blocks = 0;
   for (int i = 0; i < count; ++i) {
-    if (n[i] >= INT32_MAX) return LOGBQ_ERR_UNSUPPORTED;
+    if (n[i] >= 1 << 24) return LOGBQ_ERR_UNSUPPORTED;
     a.n[i] = (int32_t)n[i];
     a.block0[i] = (int32_t)blocks;
-    blocks += (n[i] + kAdColumns - 1) / kAdColumns;
+    blocks += (n[i] + columns - 1) / columns;
     if (blocks > 65535) return LOGBQ_ERR_UNSUPPORTED;
   }
   a.block0[count] = (int32_t)blocks;
   // Tiles: a request each, or as many as the requests can have.
-  const int64_t tiles = max_new <= kAdTile ? requests : tokens / kAdTile + (requests < tokens ? requests : tokens);
+  const int64_t tiles = max_new <= kFewTokens ? requests : tokens / kAdTile + (requests < tokens ? requests : tokens);
   if (tiles > kAdMaxBlocks) return LOGBQ_ERR_UNSUPPORTED;
   // No adapter's weights pass 2^62 bytes.
   for (int i = 0; i < count; ++i)
@@ -398,7 +648,8 @@ int32_t logbq_linear_adapters(const uint16_t* x_dev, int64_t tokens, int64_t k, 
   a.adapter = adapter_dev;
   a.ranks = ranks_dev;
   a.scales = scales_dev;
-  a.h = static_cast<float*>(work_dev);
+  a.tiles = static_cast<int32_t*>(work_dev);
+  a.h = static_cast<float*>(work_dev) + 4 * (tokens + tokens / kAdTile + 1);
   a.k = k;
   a.tokens = (int32_t)tokens;
   a.requests = (int32_t)requests;
@@ -406,28 +657,43 @@ int32_t logbq_linear_adapters(const uint16_t* x_dev, int64_t tokens, int64_t k, 
   a.rank = rank;
   a.count = count;
   a.max_new = max_new < INT32_MAX ? (int32_t)max_new : INT32_MAX;
-  // Few tiles: a rank tile a workgroup, and K split until the chip is full. Many: activations are read
-  // once for up to four rank tiles.
-  const int rank_tiles = count * ((rank + kAdTile - 1) / kAdTile);
-  const int group = tiles * rank_tiles <= 1024 || rank_tiles == 1 ? 1 : rank_tiles == 2 ? 2 : 4;
+  const bool bf16 = dtype == LOGBQ_DTYPE_BF16;
+  if (max_new <= kFewTokens) {
+    const dim3 shrink((unsigned)requests, (unsigned)(count * (rank / kFewRows))), expand((unsigned)requests, (unsigned)blocks);
+#define FEW(BF16, T)                                                                                          \
+  if (bf16 == BF16 && (max_new > 1) == (T > 1)) {                                                             \
+    hipLaunchKernelGGL((k_adapter_shrink_few<BF16, T>), shrink, dim3(kAdThreads), 0, (hipStream_t)stream, a); \
+    if (launch_status() != LOGBQ_OK) return LOGBQ_ERR_HIP;                                                    \
+    hipLaunchKernelGGL((k_adapter_expand_few<BF16, T>), expand, dim3(kAdThreads), 0, (hipStream_t)stream, a); \
+  }
+    FEW(false, 1) FEW(true, 1) FEW(false, kFewTokens) FEW(true, kFewTokens)
+#undef FEW
+    return launch_status();
+  }
+  // Activations are read once for up to eight rank tiles; K is split until two workgroups a CU have work.
+  const int rank_tiles = count * ((rank + kRankTile - 1) / kRankTile);
+  const int group = rank_tiles <= 2 ? 2 : rank_tiles <= 4 ? 4 : 8;
   const int groups = (rank_tiles + group - 1) / group;
-  int64_t splits = 1024 / (tiles * groups);
+  int64_t splits = 512 / (tiles * groups);
   splits = splits > kAdSplits ? kAdSplits : splits;
   splits = splits > k / 512 ? k / 512 : splits;
   splits = splits > kAdSplitTokens / tokens ? kAdSplitTokens / tokens : splits;
   a.splits = splits < 1 ? 1 : (int32_t)splits;
   const dim3 shrink((unsigned)tiles, (unsigned)a.splits, (unsigned)groups), expand((unsigned)tiles, (unsigned)blocks);
 #define SHRINK(BF16, G)                                                                        \
-  if ((dtype == LOGBQ_DTYPE_BF16) == BF16 && group == G)                                       \
+  if (bf16 == BF16 && group == G)                                                              \
     hipLaunchKernelGGL((k_adapter_shrink<BF16, G>), shrink, dim3(kAdThreads), 0, (hipStream_t)stream, a)
-  SHRINK(false, 1); SHRINK(false, 2); SHRINK(false, 4);
-  SHRINK(true, 1); SHRINK(true, 2); SHRINK(true, 4);
+  SHRINK(false, 2); SHRINK(false, 4); SHRINK(false, 8);
+  SHRINK(true, 2); SHRINK(true, 4); SHRINK(true, 8);
 #undef SHRINK
   if (launch_status() != LOGBQ_OK) return LOGBQ_ERR_HIP;
-  if (dtype == LOGBQ_DTYPE_BF16)
-    hipLaunchKernelGGL(k_adapter_expand<true>, expand, dim3(kAdThreads), 0, (hipStream_t)stream, a);
-  else
-    hipLaunchKernelGGL(k_adapter_expand<false>, expand, dim3(kAdThreads), 0, (hipStream_t)stream, a);
+  const int steps = rank <= 32 ? 2 : rank <= 64 ? 4 : 8;
+#define EXPAND(BF16, STEPS)                                                                    \
+  if (bf16 == BF16 && steps == STEPS)                                                          \
+    hipLaunchKernelGGL((k_adapter_expand<BF16, STEPS>), expand, dim3(kAdThreads), 0, (hipStream_t)stream, a)
+  EXPAND(false, 2); EXPAND(false, 4); EXPAND(false, 8);
+  EXPAND(true, 2); EXPAND(true, 4); EXPAND(true, 8);
+#undef EXPAND
   return launch_status();
 }
 

@@ -794,6 +794,10 @@ def kv4_tree_attention(q, cache, table, seq_lens, q_starts, masks, max_new: int,
     return out
 
 
+# ctypes arrays of up to four pointers and sizes; making the types takes longer than filling them.
+_ARRAYS = [(c_void_p * n, c_int64 * n) for n in range(5)]
+
+
 def linear_adapters_workspace_bytes(tokens: int, count: int, rank: int) -> int:
     """logbq_linear_adapters_workspace: bytes of workspace of a linear_adapters call with `tokens` tokens, `count`
     projections and pools of `rank` ranks. Host only."""
@@ -820,16 +824,22 @@ def linear_adapters(x, ys, a_list, b_list, q_starts, adapter, max_new: int, scal
     outs = ys if outs is None else outs
     if a_list[0].dim() != 3:
         raise ValueError("a_list must hold [adapters][rank][K] tensors")
-    adapters, rank = a_list[0].shape[:2]
-    dtype = a_list[0].dtype
+    shape, dtype, f32 = a_list[0].shape, a_list[0].dtype, torch.float32
+    adapters, rank, _ = shape
+    widths = []
     for y, a, b, out in zip(ys, a_list, b_list, outs):
         if y.dim() != 2:
             raise ValueError("ys must hold [tokens][N] tensors")
         n = y.shape[1]
-        _device_array(y, torch.float32, (tokens, n), "ys")
-        _device_array(out, torch.float32, (tokens, n), "outs")
-        _device_array(a, dtype, (adapters, rank, k), "a_list")
-        _device_array(b, dtype, (adapters, n, rank), "b_list")
+        widths.append(n)
+        if not (y.shape[0] == tokens and out.shape == y.shape and a.shape == shape and shape[2] == k and
+                b.shape == (adapters, n, rank) and y.dtype == out.dtype == f32 and a.dtype == b.dtype == dtype and
+                y.is_cuda and out.is_cuda and a.is_cuda and b.is_cuda and y.is_contiguous() and
+                out.is_contiguous() and a.is_contiguous() and b.is_contiguous()):
+            _device_array(y, f32, (tokens, n), "ys")
+            _device_array(out, f32, (tokens, n), "outs")
+            _device_array(a, dtype, (adapters, rank, k), "a_list")
+            _device_array(b, dtype, (adapters, n, rank), "b_list")
     requests = adapter.numel()
     _device_array(adapter, torch.int32, (requests,), "adapter")
     _device_array(q_starts, torch.int32, (requests + 1,), "q_starts")
@@ -843,10 +853,10 @@ def linear_adapters(x, ys, a_list, b_list, q_starts, adapter, max_new: int, scal
                                     device=x.device)
     else:
         _device_workspace(workspace)
-    pointers = c_void_p * count
+    pointers, sizes = _ARRAYS[count]
     _check(lib().logbq_linear_adapters(
         x.data_ptr(), tokens, k, count, pointers(*[a.data_ptr() for a in a_list]),
-        pointers(*[b.data_ptr() for b in b_list]), (c_int64 * count)(*[y.shape[1] for y in ys]),
+        pointers(*[b.data_ptr() for b in b_list]), sizes(*widths),
         _dtype_code(dtype), adapters, rank, None if ranks is None else ranks.data_ptr(),
         None if scales is None else scales.data_ptr(), q_starts.data_ptr(), adapter.data_ptr(), requests, max_new,
         pointers(*[y.data_ptr() for y in ys]), pointers(*[o.data_ptr() for o in outs]), workspace.data_ptr(),

@@ -106,7 +106,7 @@ def adapters_call(**change):
     (dict(dtype=0), NO), (dict(dtype=3), NO), (dict(adapters=-1), BAD), (dict(rank=0), BAD), (dict(rank=12), NO),
     (dict(rank=136), NO), (dict(k=48), NO), (dict(requests=-1), BAD), (dict(max_new=-1), BAD), (dict(x=None), BAD),
     (dict(starts=None), BAD), (dict(adapter=None), BAD), (dict(work=None), BAD), (dict(work_bytes=-1), BAD),
-    (dict(work_bytes=5 * 16 * 2 * 16 * 4 - 1), NO), (dict(x=Q + 8), NO), (dict(work=KO + 8), NO),
+    (dict(work_bytes=5 * 16 * 2 * 16 * 4 + 6 * 16 - 1), NO), (dict(x=Q + 8), NO), (dict(work=KO + 8), NO),
     (dict(a=[A, None]), BAD), (dict(b=[None, K]), BAD), (dict(a=[A, A + 2]), NO), (dict(b=[K + 8, K]), NO),
     (dict(y=[V, V + 2]), NO), (dict(out=[QO, QO + 2]), NO), (dict(y=[None, V]), BAD), (dict(out=[QO, None]), BAD),
     (dict(out=[QO, QO + 4]), BAD), (dict(out=[Q, QO]), BAD), (dict(out=[V + 4, QO]), BAD), (dict(out=[QO, V]), BAD),
@@ -119,9 +119,9 @@ def test_adapters_refusals(change, status):
 
 def test_adapters_workspace():
     size = L.linear_adapters_workspace_bytes
-    assert size(0, 1, 8) == 0 and size(1, 1, 8) == 16 * 8 * 4 and size(5, 2, 16) == 5 * 16 * 2 * 16 * 4
-    assert size(100000, 4, 128) == 100000 * 4 * 128 * 4            # no split: one part a token
-    assert size(4000, 1, 8) == 32768 * 8 * 4                       # split in eight at most
+    assert size(0, 1, 8) == 16 and size(1, 1, 8) == 16 * 8 * 4 + 32 and size(5, 2, 16) == 5 * 16 * 2 * 16 * 4 + 6 * 16
+    assert size(100000, 4, 128) == 100000 * 4 * 128 * 4 + 16 * 103126      # no split: one part a token
+    assert size(4000, 1, 8) == 32768 * 8 * 4 + 16 * 4126                   # split in eight at most
     assert size(-1, 1, 8) == size(5, 0, 8) == size(5, 5, 8) == size(5, 1, 12) == size(5, 1, 136) == 0
 
 
