@@ -19,8 +19,12 @@ namespace {
 //
 // Arithmetic is in 64 bits from the inputs to one rounding to float32: then a key's codes, which flip
 // where a value crosses a threshold, do not depend on the order of a sum or on an angle's last bit, and
-// any two implementations agree on them. CDNA4 does float64 products at the rate of unpacked float32
-// ones, so this costs registers, not time.
+// any two implementations agree on them. It costs registers, not time: float64 products issue at the rate of
+// float32 ones, and vector instructions take 40 % of the slots.
+//
+// Bound by memory, small calls by latency. Measured: 8191 tokens of 32 query and 8 key/value heads of 128 channels, float32
+// in, float16 queries and codes out (277 MB), 53 us, 5.2 TB/s; 6001 tokens of 32 and 8 heads of 64, bfloat16 (61 MB),
+// 14.5 us; 48 tokens 4.1 us.
 constexpr int kRotThreads = 256;
 constexpr int kRotWaves = kRotThreads / 64;
 
@@ -91,10 +95,71 @@ __device__ __forceinline__ double row_sum(double x) {
   return x + turned(x, std::integral_constant<int, 0x121>{});
 }
 
-template <int D, int DT, bool APPEND>
+// N consecutive elements as they are, in the widest loads, and their float32 values.
+template <int DT, int N>
+struct Row {
+  static constexpr int kWords = N * (DT == LOGBQ_DTYPE_F32 ? 4 : 2) / 4;
+  uint32_t w[kWords];
+  __device__ __forceinline__ void load(const void* from, int64_t at) {
+    const uint8_t* p = static_cast<const uint8_t*>(from) + at * (DT == LOGBQ_DTYPE_F32 ? 4 : 2);
+    if constexpr (kWords == 2) {
+      const u32x2 v = *reinterpret_cast<const u32x2*>(p);
+      w[0] = v.x; w[1] = v.y;
+    } else {
+#pragma unroll
+      for (int i = 0; i < kWords; i += 4) {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(p + 4 * i);
+        w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
+      }
+    }
+  }
+  __device__ __forceinline__ void values(float (&x)[N]) const {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      if constexpr (DT == LOGBQ_DTYPE_F32) x[j] = __uint_as_float(w[j]);
+      else if constexpr (DT == LOGBQ_DTYPE_BF16) x[j] = __uint_as_float(j & 1 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
+      else x[j] = (float)__builtin_bit_cast(half2v, w[j / 2])[j & 1];
+    }
+  }
+};
+
+// x rounded to nearest into N consecutive elements; STREAMED: without a place in cache.
+template <bool STREAMED, int N>
+__device__ __forceinline__ void store_row(void* to, int32_t dtype, int64_t at, const float (&x)[N]) {
+  const auto put = [&](auto v, void* place) {
+    auto* p = static_cast<decltype(v)*>(place);
+    if constexpr (STREAMED) __builtin_nontemporal_store(v, p);
+    else *p = v;
+  };
+  if (dtype == LOGBQ_DTYPE_F32) {
+#pragma unroll
+    for (int j = 0; j < N; j += 4) put(f32x4{x[j], x[j + 1], x[j + 2], x[j + 3]}, static_cast<float*>(to) + at + j);
+    return;
+  }
+  constexpr int kWide = N < 8 ? N : 8;           // elements of a store
+  typedef half_t halves __attribute__((ext_vector_type(kWide)));
+  typedef __bf16 bfloats __attribute__((ext_vector_type(kWide)));
+#pragma unroll
+  for (int j = 0; j < N; j += kWide) {
+    if (dtype == LOGBQ_DTYPE_F16) {
+      halves v;
+#pragma unroll
+      for (int i = 0; i < kWide; ++i) v[i] = (half_t)x[j + i];
+      put(v, static_cast<half_t*>(to) + at + j);
+    } else {
+      bfloats v;
+#pragma unroll
+      for (int i = 0; i < kWide; ++i) v[i] = (__bf16)x[j + i];
+      put(v, static_cast<__bf16*>(to) + at + j);
+    }
+  }
+}
+
+template <int D, int DT, bool APPEND, bool STREAMED>
 __global__ __launch_bounds__(kRotThreads) void k_rotate(RotateArgs a) {
   constexpr int N = D / 16;                      // channels of a lane
   constexpr int kPairs = D / 2;
+  constexpr int kAhead = 2;                      // rows of a lane whose loads are on their way together
   __shared__ double2 turns[kRotWaves][kPairs];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = lane & 15;
   const int64_t t = (int64_t)blockIdx.x * kRotWaves + wave;
@@ -115,6 +180,7 @@ __global__ __launch_bounds__(kRotThreads) void k_rotate(RotateArgs a) {
   const int half_lanes = a.pairs / N;
   const bool in_pairs = group < 2 * half_lanes, second = group >= half_lanes;
   const int other = a.interleaved || !in_pairs ? lane : second ? lane - half_lanes : lane + half_lanes;
+  const bool all_turn = half_lanes == 8 && !a.interleaved;     // the other lane is 8 away, round the 16
   double cs[N], sn[N];
 #pragma unroll
   for (int j = 0; j < N; ++j) {
@@ -127,51 +193,69 @@ __global__ __launch_bounds__(kRotThreads) void k_rotate(RotateArgs a) {
   }
 
   const int64_t slot = APPEND && a.slots ? a.slots[t] : -1;
-  for (int h = first + (lane >> 4); h < last; h += 4) {
+  // Rows are loaded four (one a 16 lanes) times kAhead at once; those past the last head repeat it and are not used.
+  const int mine = lane >> 4;
+  const auto load = [&](int h, Row<DT, N>& row) {
+    h = h < last ? h : last - 1;
     const bool is_q = h < a.q_heads, is_v = h >= a.q_heads + a.k_heads;
     const int head = is_q ? h : is_v ? h - a.q_heads - a.k_heads : h - a.q_heads;
-    const void* from = is_q ? a.q : is_v ? a.v : a.k;
-    const int64_t at = t * (is_q ? a.q_stride : is_v ? a.v_stride : a.k_stride) + (int64_t)head * D + group * N;
-    float x[N];
-    load_row<DT>(from, at, x);
-    if (!is_v) {
-      const float* weight = is_q ? a.q_weight : a.k_weight;
-      double y[N];
+    row.load(is_q ? a.q : is_v ? a.v : a.k,
+             t * (is_q ? a.q_stride : is_v ? a.v_stride : a.k_stride) + (int64_t)head * D + group * N);
+  };
+  for (int h0 = first; h0 < last; h0 += 4 * kAhead) {
+    Row<DT, N> rows[kAhead];
 #pragma unroll
-      for (int j = 0; j < N; ++j) y[j] = x[j];
-      if (weight) {
-        double sum = 0.0;
+    for (int u = 0; u < kAhead; ++u) load(h0 + 4 * u + mine, rows[u]);
 #pragma unroll
-        for (int j = 0; j < N; ++j) sum = __builtin_fma(y[j], y[j], sum);
-        const double f = rsqrt(row_sum(sum) * (1.0 / D) + a.eps);
-        float w[N];
-        load_row<LOGBQ_DTYPE_F32>(weight, group * N, w);
+    for (int u = 0; u < kAhead; ++u) {
+      const int h = h0 + 4 * u + mine;
+      if (h >= last) continue;                   // a row's 16 lanes together, as below
+      const bool is_q = h < a.q_heads, is_v = h >= a.q_heads + a.k_heads;
+      const int head = is_q ? h : is_v ? h - a.q_heads - a.k_heads : h - a.q_heads;
+      float x[N];
+      rows[u].values(x);
+      if (!is_v) {
+        const float* weight = is_q ? a.q_weight : a.k_weight;
+        double y[N], z[N];                       // the row's elements, and their pairs' other ones
 #pragma unroll
-        for (int j = 0; j < N; ++j) y[j] *= f * w[j];
+        for (int j = 0; j < N; ++j) {
+          y[j] = x[j];
+          if (a.interleaved) z[j] = x[j ^ 1];
+          else if (all_turn) z[j] = __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(x[j]), 0x128, 0xf, 0xf, true));
+          else z[j] = __shfl(x[j], other);
+        }
+        if (weight) {
+          double sum = 0.0;
+#pragma unroll
+          for (int j = 0; j < N; ++j) sum = __builtin_fma(y[j], y[j], sum);
+          const double f = rsqrt(row_sum(sum) * (1.0 / D) + a.eps);
+          float w[N], v[N];
+          load_row<LOGBQ_DTYPE_F32>(weight, group * N, w);
+          if (!a.interleaved) load_row<LOGBQ_DTYPE_F32>(weight, (other & 15) * N, v);
+#pragma unroll
+          for (int j = 0; j < N; ++j) {
+            y[j] *= f * w[j];
+            z[j] *= f * (a.interleaved ? w[j ^ 1] : v[j]);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[j] = (float)(in_pairs ? __builtin_fma(y[j], cs[j], z[j] * sn[j]) : y[j]);
       }
-#pragma unroll
-      for (int j = 0; j < N; j += 2) {
-        const double u = a.interleaved ? y[j + 1] : __shfl(y[j], other);
-        const double v = a.interleaved ? y[j] : __shfl(y[j + 1], other);
-        const double p = __builtin_fma(y[j], cs[j], u * sn[j]), q = __builtin_fma(y[j + 1], cs[j + 1], v * sn[j + 1]);
-        x[j] = (float)(in_pairs ? p : y[j]);
-        x[j + 1] = (float)(in_pairs ? q : y[j + 1]);
+      if (APPEND && !is_q) {
+        if (slot < 0 || slot >= a.c.slots) continue;
+        if (is_v) append_row<D, true>(x, a.c, slot, head, group);
+        else append_row<D, false>(x, a.c, slot, head, group);
+        continue;
       }
+      store_row<STREAMED>(is_q ? a.q_out : a.k_out, a.out_dtype, (t * (is_q ? a.q_heads : a.k_heads) + head) * D + group * N, x);
     }
-    if (APPEND && !is_q) {
-      if (slot < 0 || slot >= a.c.slots) continue;         // the row's 16 lanes together
-      if (is_v) append_row<D, true>(x, a.c, slot, head, group);
-      else append_row<D, false>(x, a.c, slot, head, group);
-      continue;
-    }
-    void* to = is_q ? a.q_out : a.k_out;
-    const int64_t out = (t * (is_q ? a.q_heads : a.k_heads) + head) * D + group * N;
-#pragma unroll
-    for (int j = 0; j < N; j += 4) store_four(to, a.out_dtype, out + j, f32x4{x[j], x[j + 1], x[j + 2], x[j + 3]});
   }
 }
 
 // ------------------------------------------------------------------ host side
+// Outputs larger than this are not kept in cache, where they would take the place of what is read (8191 tokens, 67 MB of
+// queries: 62 us against 74); a decode step's are, for the attention that follows.
+constexpr int64_t kStreamedBytes = 16 << 20;
 constexpr int64_t kMaxTokens = ((int64_t)1 << 32) / kRotThreads * kRotWaves - kRotWaves;
 
 // Bytes from a tensor's first element to its last.
@@ -218,13 +302,16 @@ int32_t launch_rotate(RotateArgs a, int32_t dim, int32_t dtype, hipStream_t stre
   int64_t parts = 512 / blocks;
   parts = parts < 1 ? 1 : parts > (heads + 3) / 4 ? (heads + 3) / 4 : parts;
   a.span = (int32_t)(((heads + parts - 1) / parts + 3) / 4 * 4);
+  const bool streamed = a.tokens * (a.q_heads + (APPEND ? 0 : a.k_heads)) * dim * dtype_bytes(a.out_dtype) > kStreamedBytes;
   const dim3 grid((unsigned)blocks, (unsigned)((heads + a.span - 1) / a.span));
-#define ROTATE(D, DT)                                                                          \
-  if (dim == D && dtype == DT)                                                                 \
-    hipLaunchKernelGGL((k_rotate<D, DT, APPEND>), grid, dim3(kRotThreads), 0, stream, a)
-  ROTATE(64, LOGBQ_DTYPE_F32); ROTATE(64, LOGBQ_DTYPE_F16); ROTATE(64, LOGBQ_DTYPE_BF16);
-  ROTATE(128, LOGBQ_DTYPE_F32); ROTATE(128, LOGBQ_DTYPE_F16); ROTATE(128, LOGBQ_DTYPE_BF16);
-  ROTATE(256, LOGBQ_DTYPE_F32); ROTATE(256, LOGBQ_DTYPE_F16); ROTATE(256, LOGBQ_DTYPE_BF16);
+#define ROTATE(D, DT)                                                                               \
+  if (dim == D && dtype == DT) {                                                                     \
+    if (streamed) hipLaunchKernelGGL((k_rotate<D, DT, APPEND, true>), grid, dim3(kRotThreads), 0, stream, a); \
+    else hipLaunchKernelGGL((k_rotate<D, DT, APPEND, false>), grid, dim3(kRotThreads), 0, stream, a); \
+  }
+  ROTATE(64, LOGBQ_DTYPE_F32) ROTATE(64, LOGBQ_DTYPE_F16) ROTATE(64, LOGBQ_DTYPE_BF16)
+  ROTATE(128, LOGBQ_DTYPE_F32) ROTATE(128, LOGBQ_DTYPE_F16) ROTATE(128, LOGBQ_DTYPE_BF16)
+  ROTATE(256, LOGBQ_DTYPE_F32) ROTATE(256, LOGBQ_DTYPE_F16) ROTATE(256, LOGBQ_DTYPE_BF16)
 #undef ROTATE
   return launch_status();
 }
