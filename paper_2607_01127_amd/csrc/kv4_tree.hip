@@ -424,8 +424,18 @@ struct TileReader {
 //
 // A piece of 32 rows or fewer leaves three wavefronts without rows, one of 64 two: then wavefronts share the
 // rows and have a half of each tile's positions, and their sums are added up in LDS at the end.
-constexpr int kTreeMinShare = 4;              // cost of a piece at least: two tiles of few rows
+constexpr int kTreeMinShare = 6;              // cost of a piece at least: two tiles of few rows
 constexpr int kMaxNodes = 64;
+
+// Sums over a wavefront's lanes up to each one, by shifts within 16 and broadcasts of the rows' last lanes.
+__device__ __forceinline__ int lanes_upto(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+  return x + __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+}
 
 template <int D, bool QSPLIT, bool ONE_PAGE>
 __global__ __launch_bounds__(kTileThreads, D <= 128 ? 2 : 1)
@@ -445,24 +455,24 @@ void k_kv4_tree(AttnArgs a, const uint64_t* masks) {
     i.from = q.from & ~(kTilePositions - 1);
     i.row_tiles = (q.n * a.group + kRows - 1) / kRows;
     i.tiles = q.end > i.from ? (q.end - i.from + kTilePositions - 1) / kTilePositions : 0;
-    // A tile of more than 64 rows takes half as long again (128 channels: 3.3 us against 2.2).
-    i.cost = i.tiles * (q.n * a.group > kRows / 2 ? 3 : 2);
+    // A tile of more than 64 rows takes 5/3 as long (128 channels: 3.0 to 3.5 us against 1.8 to 2.1).
+    i.cost = i.tiles * (q.n * a.group > kRows / 2 ? 5 : 3);
     return i;
   };
   const int per = (a.requests + kTileThreads - 1) / kTileThreads;
   const int r0 = tid * per < a.requests ? tid * per : a.requests;
   const int r1 = r0 + per < a.requests ? r0 + per : a.requests;
+  const Items own = r0 < r1 ? items_of(request_of(a, r0)) : Items{0, 0, 0, 0};    // of the thread's first request
+  const auto again_of = [&](int r) { return r == r0 ? own : items_of(request_of(a, r)); };
   int cost = 0, items = 0;
   for (int r = r0; r < r1; ++r) {
-    const Items i = items_of(request_of(a, r));
+    const Items i = again_of(r);
     cost += i.cost * i.row_tiles * a.c.heads;
     items += i.row_tiles * a.c.heads;
   }
-  for (int d = 1; d < 64; d <<= 1) {
-    cost += __shfl_xor(cost, d);
-    items += __shfl_xor(items, d);
-  }
-  if (lane == 0) {
+  cost = lanes_upto(cost);
+  items = lanes_upto(items);
+  if (lane == 63) {
     counts[0][wave] = cost;
     counts[1][wave] = items;
   }
@@ -482,7 +492,7 @@ void k_kv4_tree(AttnArgs a, const uint64_t* masks) {
   // Pieces before each thread's requests, those of them that are parts of an item, and the items that have parts.
   int mine[3] = {0, 0, 0}, upto[3];
   for (int r = r0; r < r1; ++r) {
-    const Items i = items_of(request_of(a, r));
+    const Items i = again_of(r);
     const int n = i.row_tiles * a.c.heads, pieces = pieces_of(i.cost);
     mine[0] += n * pieces;
     mine[1] += pieces > 1 ? n * pieces : 0;
@@ -490,11 +500,7 @@ void k_kv4_tree(AttnArgs a, const uint64_t* masks) {
   }
 #pragma unroll
   for (int k = 0; k < 3; ++k) {
-    upto[k] = mine[k];
-    for (int d = 1; d < 64; d <<= 1) {
-      const int x = __shfl_up(upto[k], d);
-      if (lane >= d) upto[k] += x;
-    }
+    upto[k] = lanes_upto(mine[k]);
     if (lane == 63) scan[k][wave] = upto[k];
   }
   if (tid == 0) found[0] = -1;
@@ -503,11 +509,14 @@ void k_kv4_tree(AttnArgs a, const uint64_t* masks) {
   for (int k = 0; k < 3; ++k)
     for (int w = 0; w < wave; ++w) upto[k] += scan[k][w];
   const int w = blockIdx.x;
-  if (w == 0 && tid == kTileThreads - 1) *a.desc = upto[2];
+  if (w == 0 && tid == kTileThreads - 1) {
+    a.desc[0] = upto[2];
+    a.desc[1] = upto[1];
+  }
   if (upto[0] - mine[0] <= w && w < upto[0]) {
     int at[3] = {upto[0] - mine[0], upto[1] - mine[1], upto[2] - mine[2]};
     for (int r = r0; r < r1; ++r) {
-      const Items i = items_of(request_of(a, r));
+      const Items i = again_of(r);
       const int n = i.row_tiles * a.c.heads, pieces = pieces_of(i.cost);
       if (w < at[0] + n * pieces) {
         found[0] = r;
@@ -666,19 +675,27 @@ void k_kv4_tree(AttnArgs a, const uint64_t* masks) {
   }
 }
 
-// A workgroup has kPer rows of an item at a time: D / 4 threads have 4 channels each of a row, and kSlices such
-// groups every kSlices-th of its parts.
+// D / 4 threads have 4 channels each of a row. A workgroup has kGroups such groups: rows of an item, or, where the grid
+// has room for it, slices of their parts (24 drafts of 1 to 24 nodes, 3 parts an item: 6 us with whole rows, 10 with four
+// slices).
+constexpr int kTreeJoinGrid = 2048;
+
 template <int D>
 __global__ __launch_bounds__(kTileThreads) void k_kv4_tree_join(AttnArgs a) {
-  constexpr int kRows = kTileRows, kSlices = 4, kPer = kTileThreads / (D / 4) / kSlices;
-  __shared__ f32x4 sums[kSlices][kPer][D / 4];
-  __shared__ float tops[kSlices][kPer], dens[kSlices][kPer];
+  constexpr int kRows = kTileRows, kGroups = kTileThreads / (D / 4);
+  __shared__ f32x4 sums[kGroups][D / 4];
+  __shared__ float tops[kGroups], dens[kGroups];
   const int items = a.desc[0];
-  const int most = a.max_new * a.group < kRows ? a.max_new * a.group : kRows, steps = (most + kPer - 1) / kPer;
-  const int ch = threadIdx.x % (D / 4), sub = threadIdx.x / (D / 4) % kPer, slice = threadIdx.x / (D / 4) / kPer;
+  if (items == 0) return;
+  const int most = a.max_new * a.group < kRows ? a.max_new * a.group : kRows;
+  int slices = 1;
+  while (slices < kGroups && slices * (int64_t)items < a.desc[1] && (int64_t)items * most * slices * 2 <= kTreeJoinGrid * kGroups)
+    slices *= 2;
+  const int rows_at_once = kGroups / slices, steps = (most + rows_at_once - 1) / rows_at_once;
+  const int ch = threadIdx.x % (D / 4), group = threadIdx.x / (D / 4), slice = group & (slices - 1), sub = group / slices;
   for (int64_t task = blockIdx.x; task < (int64_t)items * steps; task += gridDim.x) {
     const int32_t* desc = a.desc + 8 + 8 * (task / steps);
-    const int parts = desc[0], row0 = desc[4], row = (int)(task % steps) * kPer + sub;
+    const int parts = desc[0], row0 = desc[4], row = (int)(task % steps) * rows_at_once + sub;
     const int64_t first = desc[1];
     const Request req = request_of(a, desc[2]);
     const int rows = req.n * a.group - row0 < kRows ? req.n * a.group - row0 : kRows;
@@ -686,39 +703,45 @@ __global__ __launch_bounds__(kTileThreads) void k_kv4_tree_join(AttnArgs a) {
     float top = kNone, den = 0.0f;
     f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
     if (row < rows) {
-      for (int i = slice; i < parts; i += kSlices) top = fmaxf(top, a.part_rl[((first + i) * kRows + row) * 2]);
 #pragma unroll 4
-      for (int i = slice; i < parts; i += kSlices) {
+      for (int i = slice; i < parts; i += slices) top = fmaxf(top, a.part_rl[((first + i) * kRows + row) * 2]);
+#pragma unroll 4
+      for (int i = slice; i < parts; i += slices) {
         const int64_t at = (first + i) * kRows + row;
         const float f = exp2_fast(a.part_rl[at * 2] - top);
         den += a.part_rl[at * 2 + 1] * f;
         v += *reinterpret_cast<const f32x4*>(a.part_o + at * D + 4 * ch) * f;
       }
     }
-    sums[slice][sub][ch] = v;
-    if (ch == 0) {
-      tops[slice][sub] = top;
-      dens[slice][sub] = den;
-    }
-    __syncthreads();
-    if (slice == 0 && row < rows) {
-      float highest = top;
-      for (int i = 1; i < kSlices; ++i) highest = fmaxf(highest, tops[i][sub]);
-      const float f = exp2_fast(top - highest);
-      v *= f;
-      den *= f;
-      for (int i = 1; i < kSlices; ++i) {
-        const float g = exp2_fast(tops[i][sub] - highest);
-        v += sums[i][sub][ch] * g;
-        den += dens[i][sub] * g;
+    if (slices > 1) {
+      sums[group][ch] = v;
+      if (ch == 0) {
+        tops[group] = top;
+        dens[group] = den;
       }
+      __syncthreads();
+      if (slice == 0) {
+        float highest = top;
+        for (int i = 1; i < slices; ++i) highest = fmaxf(highest, tops[group + i]);
+        const float f = exp2_fast(top - highest);
+        v *= f;
+        den *= f;
+        for (int i = 1; i < slices; ++i) {
+          const float g = exp2_fast(tops[group + i] - highest);
+          v += sums[group + i][ch] * g;
+          den += dens[group + i] * g;
+        }
+        top = highest;
+      }
+      __syncthreads();
+    }
+    if (slice == 0 && row < rows) {
       const int64_t place = (int64_t)(req.t0 + (row0 + row) / a.group) * (a.c.heads * a.group) + desc[3] * a.group +
                             (row0 + row) % a.group;
       const float inv = den != 0.0f ? 1.0f / den : 0.0f;
       store_four(a.out, a.out_dtype, place * D + 4 * ch, den != 0.0f ? v * inv : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
-      if (a.lse && ch == 0) a.lse[place] = den != 0.0f ? (highest + __log2f(den)) * kLn2 : -INFINITY;
+      if (a.lse && ch == 0) a.lse[place] = den != 0.0f ? (top + __log2f(den)) * kLn2 : -INFINITY;
     }
-    __syncthreads();
   }
 }
 
@@ -726,7 +749,6 @@ __global__ __launch_bounds__(kTileThreads) void k_kv4_tree_join(AttnArgs a) {
 // Workgroups: two a CU, one at 256 channels.
 template <int D>
 constexpr int kTreeParts = D <= 128 ? 512 : 256;
-constexpr int kTreeJoinGrid = 2048;
 
 template <int D>
 int32_t launch_tree(AttnArgs a, const uint64_t* masks, void* work, hipStream_t stream) {
