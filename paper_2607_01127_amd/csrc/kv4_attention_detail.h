@@ -28,7 +28,10 @@ struct AttnArgs {
   int32_t width, tokens, requests, group, window, max_new, q_dtype, out_dtype, parts;
   int32_t unit;           // positions that the workgroups' shares are counted in
   float scale;
+  const uint64_t* masks;  // of trees: the nodes that a token sees
 };
+
+constexpr int kMaxNodes = 64;           // of a tree
 
 // log2 of a sum that has no terms yet; finite, so that differences stay numbers.
 constexpr float kNone = -1.7e38f;

@@ -1,7 +1,8 @@
 // gfx950 kernels of attention of drafted trees over the 4-bit paged cache, and their entry point of the C
 // ABI.
 //
-//   k_kv4_tree       up to 128 query rows of a request and key/value head a workgroup, converted keys and
+//   k_kv4_decode     requests of up to 16 query rows a key/value head, 32 at 64 channels (kv4_decode.h).
+//   k_kv4_tree       more: up to 128 query rows of a request and key/value head a workgroup, converted keys and
 //                    values in LDS, the positions of the whole batch dealt out evenly.
 //   k_kv4_tree_join  sums the parts of what more than one workgroup had.
 
@@ -12,6 +13,7 @@
 #include <type_traits>
 
 #include "kv4_attention_detail.h"
+#include "kv4_decode.h"
 #include "kv4_detail.h"
 #include "logbq.h"
 
@@ -425,7 +427,6 @@ struct TileReader {
 // A piece of 32 rows or fewer leaves three wavefronts without rows, one of 64 two: then wavefronts share the
 // rows and have a half of each tile's positions, and their sums are added up in LDS at the end.
 constexpr int kTreeMinShare = 6;              // cost of a piece at least: two tiles of few rows
-constexpr int kMaxNodes = 64;
 
 // Sums over a wavefront's lanes up to each one, by shifts within 16 and broadcasts of the rows' last lanes.
 __device__ __forceinline__ int lanes_upto(int x) {
@@ -439,7 +440,7 @@ __device__ __forceinline__ int lanes_upto(int x) {
 
 template <int D, bool QSPLIT, bool ONE_PAGE>
 __global__ __launch_bounds__(kTileThreads, D <= 128 ? 2 : 1)
-void k_kv4_tree(AttnArgs a, const uint64_t* masks) {
+void k_kv4_tree(AttnArgs a) {
   constexpr int kRows = kTileRows, kCb = D / 32;
   __shared__ TileBuffers<D> lds;
   __shared__ int32_t counts[2][4], scan[3][4];
@@ -575,7 +576,7 @@ void k_kv4_tree(AttnArgs a, const uint64_t* masks) {
   {
     const Row me = row_of();
     mine_of.load(a, me.token * a.q_stride + me.head * D + me.half * 8, busy && me.row < rows);
-    if (tid < kRows) row_mask[tid] = tid < rows ? masks[req.t0 + (row0 + tid) / a.group] : 0;
+    if (tid < kRows) row_mask[tid] = tid < rows ? a.masks[req.t0 + (row0 + tid) / a.group] : 0;
   }
   if (tid == 0) lds.again = 0;
   __syncthreads();
@@ -751,7 +752,11 @@ template <int D>
 constexpr int kTreeParts = D <= 128 ? 512 : 256;
 
 template <int D>
-int32_t launch_tree(AttnArgs a, const uint64_t* masks, void* work, hipStream_t stream) {
+int32_t launch_tree(AttnArgs a, void* work, hipStream_t stream) {
+  const int64_t rows = (int64_t)a.max_new * a.group;
+  // One of 100000 positions: 16 rows of 128 channels 39 us against 63, 32 rows of 64 channels 42 against 48.
+  if (rows <= 16) return launch_few_rows<D, true>(a, rows, work, stream);
+  if (D == 64 && rows <= 32) return launch_decode<D, D == 64 ? 2 : 1, 1, true>(a, work, stream);
   // The batch has kParts shares at most. An item with parts has more than one, so there are fewer than kParts of them,
   // with fewer than 2 kParts pieces.
   constexpr int kParts = kTreeParts<D>, kSlots = 2 * kParts;
@@ -763,14 +768,13 @@ int32_t launch_tree(AttnArgs a, const uint64_t* masks, void* work, hipStream_t s
   static_assert(32 * (kParts + 1) + (int64_t)kSlots * kTileRows * (D + 2) * 4 <= LOGBQ_KV4_WORKSPACE_BYTES,
                 "the workspace holds every part");
   // As many pieces as there can be: a share each, and one an item.
-  const int64_t row_tiles = ((int64_t)a.max_new * a.group + kTileRows - 1) / kTileRows;
+  const int64_t row_tiles = (rows + kTileRows - 1) / kTileRows;
   const int64_t grid = kParts + a.requests * row_tiles * a.c.heads;
   if (grid > (((int64_t)1 << 32) - 1) / kTileThreads) return LOGBQ_ERR_UNSUPPORTED;
   const bool split = a.q_dtype == LOGBQ_DTYPE_F32, one_page = a.c.page_shift >= 6;
 #define TREE(SPLIT, ONE_PAGE)                                                                        \
   if (split == SPLIT && one_page == ONE_PAGE)                                                        \
-    hipLaunchKernelGGL((k_kv4_tree<D, SPLIT, ONE_PAGE>), dim3((unsigned)grid), dim3(kTileThreads), 0, stream, \
-                       a, masks)
+    hipLaunchKernelGGL((k_kv4_tree<D, SPLIT, ONE_PAGE>), dim3((unsigned)grid), dim3(kTileThreads), 0, stream, a)
   TREE(false, false); TREE(false, true); TREE(true, false); TREE(true, true);
 #undef TREE
   if (launch_status() != LOGBQ_OK) return LOGBQ_ERR_HIP;
@@ -801,9 +805,10 @@ int32_t logbq_kv4_tree_attention(const void* q_dev, int64_t q_stride, int32_t q_
   if (tokens == 0 || requests == 0 || max_new == 0) return LOGBQ_OK;
   if (!masks_dev) return LOGBQ_ERR_INVALID_ARG;
   if ((uintptr_t)masks_dev % 8) return LOGBQ_ERR_UNSUPPORTED;
-  return cache->dim == 64    ? launch_tree<64>(a, masks_dev, work_dev, (hipStream_t)stream)
-         : cache->dim == 128 ? launch_tree<128>(a, masks_dev, work_dev, (hipStream_t)stream)
-                             : launch_tree<256>(a, masks_dev, work_dev, (hipStream_t)stream);
+  a.masks = masks_dev;
+  return cache->dim == 64    ? launch_tree<64>(a, work_dev, (hipStream_t)stream)
+         : cache->dim == 128 ? launch_tree<128>(a, work_dev, (hipStream_t)stream)
+                             : launch_tree<256>(a, work_dev, (hipStream_t)stream);
 }
 
 }  // extern "C"
