@@ -1,7 +1,7 @@
 // gfx950 kernels of attention of drafted trees over the 4-bit paged cache, and their entry point of the C
 // ABI.
 //
-//   k_kv4_decode     requests of up to 16 query rows a key/value head, 32 at 64 channels (kv4_decode.h).
+//   k_kv4_decode     requests of up to 16 query rows a key/value head (kv4_decode.h).
 //   k_kv4_tree       more: up to 128 query rows of a request and key/value head a workgroup, converted keys and
 //                    values in LDS, the positions of the whole batch dealt out evenly.
 //   k_kv4_tree_join  sums the parts of what more than one workgroup had.
@@ -754,9 +754,9 @@ constexpr int kTreeParts = D <= 128 ? 512 : 256;
 template <int D>
 int32_t launch_tree(AttnArgs a, void* work, hipStream_t stream) {
   const int64_t rows = (int64_t)a.max_new * a.group;
-  // One of 100000 positions: 16 rows of 128 channels 39 us against 63, 32 rows of 64 channels 42 against 48.
+  // 16 rows over 100000 positions of 128 channels: 39 us against 63. (At 64 channels the decode kernel's form of 32 rows
+  // takes 43 us against 48 there, but 16.4 against 14.1 for 28 rows over 700 positions.)
   if (rows <= 16) return launch_few_rows<D, true>(a, rows, work, stream);
-  if (D == 64 && rows <= 32) return launch_decode<D, D == 64 ? 2 : 1, 1, true>(a, work, stream);
   // The batch has kParts shares at most. An item with parts has more than one, so there are fewer than kParts of them,
   // with fewer than 2 kParts pieces.
   constexpr int kParts = kTreeParts<D>, kSlots = 2 * kParts;
