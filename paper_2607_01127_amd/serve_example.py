@@ -1,5 +1,5 @@
-"""A small decoder served with this library: 4-bit linears, a paged 4-bit key/value cache, attention
-over it and the log probabilities of what it answers.
+"""A small decoder served with this library: 4-bit linears with low-rank adapters beside them, a paged 4-bit
+key/value cache, attention over it, drafted trees, and the log probabilities of what it answers.
 
     python -m paper_2607_01127_amd.serve_example
 
@@ -8,10 +8,11 @@ random weights, each projection quantized with its own codebook; the embedding a
 stay in 16 bits, as in the paper (Sec. 4). A step is what a serving program runs for any mixture of
 prompts and single tokens:
 
-    batch_tables -> for each layer: linear_multi (q, k, v), kv4_append, kv4_attention, linear (o),
-    linear_multi (gate, up), linear (down) -> output head, token_logprobs
+    batch_tables -> for each layer: linear_multi (q, k, v), linear_adapters, kv4_append_rotated,
+    kv4_attention, linear (o), linear_multi (gate, up), linear (down) -> output head, token_logprobs
 
-Nothing in a step waits for the GPU; the lengths that the host needs are its own.
+A step of drafted trees (speculative decode) takes its positions from tree_tables and kv4_tree_attention for
+the attention. Nothing in a step waits for the GPU; the lengths that the host needs are its own.
 """
 from __future__ import annotations
 
@@ -57,6 +58,7 @@ class Decoder:
         self.embedding = torch.randn((s.vocab, s.hidden), generator=g, device=device).half()
         self.head = (torch.randn((s.vocab, s.hidden), generator=g, device=device) * s.hidden ** -0.5).half()
         self.rotation = 10000.0 ** (-torch.arange(0, s.dim, 2, device=device).float() / s.dim)
+        self.turn = L.Rotation(self.rotation)
         self.free = torch.randperm(pages, generator=g, device=device).int()      # ids of pages
         self.used = 0                      # the first of them, which its batches have taken
         self.kv_work = torch.empty(L.KV4_WORKSPACE_BYTES, dtype=torch.uint8, device=device)
@@ -71,37 +73,68 @@ class Decoder:
         c, s = angle.cos(), angle.sin()
         return torch.cat([a * c - b * s, b * c + a * s], -1)
 
-    def step(self, tokens, tables, max_new: int):
+    def step(self, tokens, tables, max_new: int, adapters=None, adapter=None):
         """float32 logits [tokens][vocab] of the step's tokens, whose keys and values go into the
-        caches; `tables` is batch_tables' result with the block table as "table"."""
+        caches; `tables` is batch_tables' result with the block table as "table", and with tree_tables'
+        masks and positions where the tokens are the nodes of drafts. `adapters` (Adapters) go to the
+        requests by `adapter` (int32 [requests])."""
         s, t = self.shape, tokens.numel()
         x = self.embedding[tokens].float()
-        for lin, cache in self.layers:
-            q, k, v = L.linear_multi(self._norm(x), *zip(*(lin[n] for n in ("q", "k", "v"))))
-            q = self._rotate(q.view(t, s.heads, s.dim), tables["positions"])
-            k = self._rotate(k.view(t, s.kv_heads, s.dim), tables["positions"])
-            L.kv4_append(k, v.view(t, s.kv_heads, s.dim), cache, tables["slots"])
-            a = L.kv4_attention(q, cache, tables["table"], tables["seq_lens"], tables["q_starts"],
-                                max_new, workspace=self.kv_work)
+        lengths = (tables["table"], tables["seq_lens"], tables["q_starts"])
+        for i, (lin, cache) in enumerate(self.layers):
+            h = self._norm(x)
+            qkv = L.linear_multi(h, *zip(*(lin[n] for n in ("q", "k", "v"))))
+            if adapters is not None:
+                L.linear_adapters(h, qkv, *adapters.layers[i], tables["q_starts"], adapter, max_new,
+                                  scales=adapters.scales, ranks=adapters.ranks)
+            q, k, v = (y.view(t, -1, s.dim) for y in qkv)
+            q = L.kv4_append_rotated(q, k, v, cache, tables["slots"], tables["positions"], self.turn,
+                                     q_out=q if q.is_contiguous() else None)
+            if "masks" in tables:
+                a = L.kv4_tree_attention(q, cache, *lengths, tables["masks"], max_new, workspace=self.kv_work)
+            else:
+                a = L.kv4_attention(q, cache, *lengths, max_new, workspace=self.kv_work)
             x = x + L.linear(a.view(t, -1), *lin["o"])
             gate, up = L.linear_multi(self._norm(x), *zip(*(lin[n] for n in ("gate", "up"))))
             x = x + L.linear((torch.nn.functional.silu(gate) * up).half(), *lin["down"])
         return (self._norm(x) @ self.head.T).float()
 
 
+class Adapters:
+    """Random low-rank adapters beside a decoder's query, key and value projections. They share a pool of
+    `rank` ranks; `ranks` says how many each has."""
+
+    def __init__(self, decoder: Decoder, ranks, scale: float = 1.0, seed: int = 0, dtype=torch.bfloat16):
+        s, device = decoder.shape, decoder.device
+        g = torch.Generator(device=device).manual_seed(seed)
+        rank, n = -(-max(ranks) // 8) * 8, len(ranks)
+        self.ranks = torch.tensor(ranks, dtype=torch.int32).to(device)
+        self.scales = torch.full((n,), scale, device=device)
+        draw = lambda *shape: torch.randn(shape, generator=g, device=device)  # noqa: E731
+        self.layers = []
+        for _ in range(s.layers):
+            widths = [s.heads * s.dim, s.kv_heads * s.dim, s.kv_heads * s.dim]
+            self.layers.append(([(draw(n, rank, s.hidden) * s.hidden ** -0.5).to(dtype) for _ in widths],
+                                [(draw(n, w, rank) * rank ** -0.5).to(dtype) for w in widths]))
+
+
 class Batch:
     """Requests that are served together. The host keeps their lengths. Pages are taken from the decoder
-    for good, so that batches of one decoder may live side by side."""
+    for good, so that batches of one decoder may live side by side. `adapter` names each request's adapter
+    of `adapters` (negative: none)."""
 
-    def __init__(self, decoder: Decoder, requests: int, most: int):
+    def __init__(self, decoder: Decoder, requests: int, most: int, adapters: Adapters = None, adapter=None):
         self.decoder = decoder
         self.lengths = [0] * requests
         width = -(-most // decoder.page)
         self.table = torch.full((requests, width), -1, dtype=torch.int32, device=decoder.device)
+        self.adapters = adapters
+        self.adapter = None if adapters is None else torch.tensor(adapter, dtype=torch.int32).to(decoder.device)
 
-    def step(self, new_tokens):
+    def step(self, new_tokens, parents=None):
         """One step: a list of token lists (one a request, empty for none) -> logits of all of them
-        in order."""
+        in order. With `parents` (a list of lists, indexes among the request's tokens, negative for
+        none) the tokens are the nodes of drafted trees, at most 64 a request."""
         d, page = self.decoder, self.decoder.page
         new = [len(x) for x in new_tokens]
         ints = torch.tensor([self.lengths, new], dtype=torch.int32).to(d.device)
@@ -111,9 +144,68 @@ class Batch:
         if max(total) > self.table.shape[1] * page or d.used + pages > d.free.numel():
             raise ValueError("the cache or the block table is too small for this step")
         tables = L.batch_tables(ints[0], ints[1], d.free[d.used:], self.table, page, len(tokens))
-        logits = d.step(tokens, dict(tables, table=self.table), max(new))
+        if parents is not None:
+            up = torch.tensor(sum(parents, []), dtype=torch.int32).to(d.device)
+            tables.update(L.tree_tables(up, tables["q_starts"], tables["seq_lens"]))
+        self.slots, self.nodes = tables["slots"], new
+        logits = d.step(tokens, dict(tables, table=self.table), max(new), self.adapters, self.adapter)
         self.lengths, d.used = total, d.used + pages
         return logits
+
+    def keep(self, paths):
+        """After a step of trees: of each request's nodes, those of `paths` (lists of indexes, rising) stay,
+        as its next cached tokens in order; the pages that only others had go back. What the cache holds
+        reads back exactly and is appended as the same codes, so keys and values move without loss."""
+        d, page = self.decoder, self.decoder.page
+        at, source, to, left, lengths = 0, [], [], [], []
+        for r, (total, path) in enumerate(zip(self.lengths, paths)):
+            nodes = self.nodes[r]
+            source += [at + i for j, i in enumerate(path) if i != j]
+            to += [at + j for j, i in enumerate(path) if i != j]
+            at += nodes
+            lengths.append(total - nodes + len(path))
+            left += [(r, c) for c in range(-(-lengths[-1] // page), -(-total // page))]
+        if source:
+            source, to = (self.slots[torch.tensor(i).to(d.device)] for i in (source, to))
+            for _, cache in d.layers:
+                L.kv4_append(*L.kv4_read(cache, source, torch.float32), cache, to)
+        if left:
+            rows, columns = (torch.tensor(i).to(d.device) for i in zip(*left))
+            d.free[d.used - len(left):d.used] = self.table[rows, columns]
+            self.table[rows, columns] = -1
+            d.used -= len(left)
+        self.lengths = lengths
+
+    def speculate(self, prompts, steps: int, draft):
+        """Greedy continuation with drafts: draft(text) gives (tokens, parents) of a tree whose root,
+        node 0, is the text's last token; of the drafted tokens below it the longest path that greedy
+        decoding would have taken stays. Returns the chosen tokens (`steps` of each request, a list of
+        lists) and the number of steps that it took."""
+        if steps < 1 or not all(prompts):
+            raise ValueError("speculate needs a step and a token of each prompt")
+        logits = self.step(prompts)
+        ends = torch.tensor([len(p) for p in prompts]).cumsum(0) - 1
+        chosen, taken = [[t] for t in logits[ends.to(self.decoder.device)].argmax(1).tolist()], 1
+        while min(len(c) for c in chosen) < steps:
+            trees = [draft(p + c) if len(c) < steps else ([c[-1]], [-1]) for p, c in zip(prompts, chosen)]
+            best = self.step([t for t, _ in trees], [p for _, p in trees]).argmax(1).tolist()
+            taken += 1
+            paths, at = [], 0
+            for c, (tokens, parents) in zip(chosen, trees):
+                path, answer = [0], best[at]
+                while True:
+                    below = [i for i in range(path[-1] + 1, len(tokens))
+                             if parents[i] == path[-1] and tokens[i] == answer]
+                    if not below:
+                        break
+                    c.append(answer)
+                    path.append(below[0])
+                    answer = best[at + below[0]]
+                c.append(answer)
+                paths.append(path)
+                at += len(tokens)
+            self.keep(paths)
+        return [c[:steps] for c in chosen], taken
 
     def generate(self, prompts, steps: int, top: int = 5):
         """Greedy continuation: the chosen tokens [requests][steps] (a list of lists), their log
@@ -146,6 +238,21 @@ class Batch:
         return L.token_logprobs(logits[keep], targets, workspace=self.decoder.lp_work)["logprob"]
 
 
+def repeated(text, branches: int = 3, length: int = 4):
+    """A draft from the text itself: what followed the last token before, the latest places first."""
+    tokens, parents = [text[-1]], [-1]
+    places = [i for i in range(len(text) - 2, -1, -1) if text[i] == text[-1]][:branches]
+    for place in places:
+        at = 0
+        for token in text[place + 1:place + 1 + length]:
+            same = [i for i in range(1, len(tokens)) if parents[i] == at and tokens[i] == token]
+            if not same:
+                tokens.append(token)
+                parents.append(at)
+            at = same[0] if same else len(tokens) - 1
+    return tokens, parents
+
+
 def main():
     decoder = Decoder(Shape(), pages=64)
     prompts = [list(range(5, 105)), [7, 8, 9], list(range(300, 377))]
@@ -154,6 +261,11 @@ def main():
         print(f"request {r}: {tokens}")
         print(f"  log probabilities {[round(x, 2) for x in logprobs[r].tolist()]}")
     score = Batch(decoder, len(prompts), 512).score(prompts)
+    drafted, taken = Batch(decoder, len(prompts), 512).speculate(prompts, 16, repeated)
+    same = sum(a == b for a, b in zip(sum(drafted, []), sum(chosen, [])))
+    print(f"with drafts: {same} of {16 * len(prompts)} tokens alike in {taken} steps")
+    adapted = Batch(decoder, len(prompts), 512, Adapters(decoder, (8, 5), seed=1), (0, -1, 1))
+    print(f"with adapters: {adapted.generate(prompts, steps=4)[0]}")
     print(f"perplexity of the prompts: {math.exp(-score.mean().item()):.1f}; alternatives at the end "
           f"{last['top_index'].tolist()}")
 
