@@ -25,7 +25,7 @@ constexpr int kFewTokens = 4;                  // tokens of requests that go wit
 constexpr int kAdCount = 4;                    // projections of a call
 constexpr int kAdRank = LOGBQ_ADAPTERS_MAX_RANK;
 constexpr int kAdColumns = 256;                // out features of a workgroup of the second kernel
-constexpr int kFewColumns = 512;               // the same for requests of a few tokens
+constexpr int kTileRows = 32768;               // tiles along y of the second kernel's grid
 constexpr int kAdSplits = 16;
 constexpr int64_t kAdSplitTokens = 32768;      // tokens times splits, where K is split
 
@@ -42,7 +42,8 @@ struct AdapterArgs {
   const int32_t* ranks;
   const float* scales;
   float* h;                                    // [splits][tokens][count][rank]
-  int32_t* tiles;                              // [tiles][4]: what the second kernel has to know of a tile
+  int32_t* tiles;                              // [tile_count][4]: what the second kernel has to know of a tile
+  int64_t tile_count;
   int64_t k;
   int32_t tokens, requests, adapters, rank, count, max_new, splits;
 };
@@ -127,7 +128,9 @@ __device__ __forceinline__ float rest_of(float x, __bf16 h) { return (float)h ==
 
 // ------------------------------------------------------------------ a few tokens
 // Both products stream the adapter's weights once: bound by HBM where many adapters are in use, by latency
-// otherwise. A wavefront's loads are 1 KiB of consecutive weights of a row of A (8 a lane), or of rows of B.
+// otherwise. A wavefront's loads are 1 KiB of consecutive weights of a row of A (8 a lane), or of rows of B. 64 tokens
+// of 40 adapters with ranks up to 64, K = 4096 and two times 14336 out features, weights from HBM: 11 us and 33 us,
+// where B's rows of 128 bytes come whole whatever the rank.
 constexpr int kFewRows = 4;                    // ranks of a workgroup of the first kernel
 
 // Float32 values of 8 weights or activations.
@@ -216,17 +219,31 @@ __global__ __launch_bounds__(kAdThreads) void k_adapter_shrink_few(AdapterArgs a
   }
 }
 
-// L lanes have a row of B, 8 ranks each; 64 rows a wavefront at a time, of which lane i in the end has the sums of
-// row i, so that the outputs are consecutive.
+// L lanes have a row of B, 8 ranks each; a wavefront has 64 rows, of which lane i in the end has the sum of row i, so
+// that the outputs are consecutive. Loads of 128 or 256 rows with as many registers took as long or longer.
 template <bool BF16, int T, int L>
 __device__ __forceinline__ void expand_few(const AdapterArgs& a, const TokenTile& tile, int projection, int n0) {
   const int lane = threadIdx.x & 63, sub = lane & (L - 1), group = lane / L;
   const int width = a.n[projection], r = 8 * sub;
   const bool has = r < tile.rank;
+  const uint16_t* from = a.b[projection] + (int64_t)tile.adapter * width * a.rank + (has ? r : 0);
+  const int n = n0 + lane;
+  // All loads first: the weights wait for nothing but the tile. What lies past the end is read from the last row.
+  u32x4 w[L];
+  float y[T];
+#pragma unroll
+  for (int i = 0; i < L; ++i) {
+    const int row = n0 + group * L + i;
+    w[i] = *reinterpret_cast<const u32x4*>(from + (int64_t)(row < width ? row : width - 1) * a.rank);
+  }
+#pragma unroll
+  for (int t = 0; t < T; ++t)
+    y[t] = a.y[projection][(int64_t)(tile.t0 + (t < tile.n ? t : 0)) * width + (n < width ? n : width - 1)];
   const float scale = a.scales ? a.scales[tile.adapter] : 1.0f;
-  float h[T][8];
+  float h[T][8], sum[T];
 #pragma unroll
   for (int t = 0; t < T; ++t) {
+    sum[t] = 0.0f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) h[t][j] = 0.0f;
     if (t < tile.n && has) {
@@ -235,41 +252,25 @@ __device__ __forceinline__ void expand_few(const AdapterArgs& a, const TokenTile
       for (int j = 0; j < 8; ++j) h[t][j] = r + j < tile.rank ? h[t][j] * scale : 0.0f;
     }
   }
-  const uint16_t* from = a.b[projection] + (int64_t)tile.adapter * width * a.rank + r;
-  const int stop = n0 + kFewColumns / kAdWaves < width ? n0 + kFewColumns / kAdWaves : width;
-  for (int n = n0; n < stop; n += 64) {
-    u32x4 w[L];
 #pragma unroll
-    for (int i = 0; i < L; ++i) {
-      const int row = n + group * L + i;
-      w[i] = has && row < stop ? *reinterpret_cast<const u32x4*>(from + (int64_t)row * a.rank) : u32x4{0, 0, 0, 0};
-    }
-    float y[T], sum[T];
+  for (int i = 0; i < L; ++i) {
+    float wf[8];
+    eight_values<BF16>(w[i], wf);
+    // What lies past the adapter's rank is not its own.
+#pragma unroll
+    for (int j = 0; j < 8; ++j) wf[j] = r + j < tile.rank ? wf[j] : 0.0f;
 #pragma unroll
     for (int t = 0; t < T; ++t) {
-      y[t] = t < tile.n && n + lane < stop ? a.y[projection][(int64_t)(tile.t0 + t) * width + n + lane] : 0.0f;
-      sum[t] = 0.0f;
+      float v = 0.0f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v = __builtin_fmaf(h[t][j], wf[j], v);
+      v = lanes_sum<L>(v);
+      sum[t] = sub == i ? v : sum[t];
     }
-#pragma unroll
-    for (int i = 0; i < L; ++i) {
-      float wf[8];
-      eight_values<BF16>(w[i], wf);
-      // What lies past the adapter's rank is not its own.
-#pragma unroll
-      for (int j = 0; j < 8; ++j) wf[j] = r + j < tile.rank ? wf[j] : 0.0f;
-#pragma unroll
-      for (int t = 0; t < T; ++t) {
-        float v = 0.0f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v = __builtin_fmaf(h[t][j], wf[j], v);
-        v = lanes_sum<L>(v);
-        sum[t] = sub == i ? v : sum[t];
-      }
-    }
-#pragma unroll
-    for (int t = 0; t < T; ++t)
-      if (t < tile.n && n + lane < stop) a.out[projection][(int64_t)(tile.t0 + t) * width + n + lane] = y[t] + sum[t];
   }
+#pragma unroll
+  for (int t = 0; t < T; ++t)
+    if (t < tile.n && n < width) a.out[projection][(int64_t)(tile.t0 + t) * width + n] = y[t] + sum[t];
 }
 
 template <bool BF16, int T>
@@ -279,7 +280,7 @@ __global__ __launch_bounds__(kAdThreads) void k_adapter_expand_few(AdapterArgs a
   if (tile.n <= 0) return;
   int projection = 0;
   while (projection + 1 < a.count && (int)blockIdx.y >= a.block0[projection + 1]) ++projection;
-  const int n0 = ((int)blockIdx.y - a.block0[projection]) * kFewColumns + wave * (kFewColumns / kAdWaves);
+  const int n0 = ((int)blockIdx.y - a.block0[projection]) * kAdColumns + wave * 64;
   const int width = a.n[projection];
   if (n0 >= width) return;
   if (tile.rank > 64) return expand_few<BF16, T, 16>(a, tile, projection, n0);
@@ -288,16 +289,18 @@ __global__ __launch_bounds__(kAdThreads) void k_adapter_expand_few(AdapterArgs a
   if (tile.rank > 8) return expand_few<BF16, T, 2>(a, tile, projection, n0);
   if (tile.rank > 0) return expand_few<BF16, T, 1>(a, tile, projection, n0);
   if (a.y[projection] == a.out[projection]) return;
-  for (int t = 0; t < tile.n; ++t)
-    for (int n = n0 + lane; n < n0 + kFewColumns / kAdWaves && n < width; n += 64)
-      a.out[projection][(int64_t)(tile.t0 + t) * width + n] = a.y[projection][(int64_t)(tile.t0 + t) * width + n];
+  for (int t = 0; t < tile.n; ++t) {
+    const int64_t at = (int64_t)(tile.t0 + t) * width + n0 + lane;
+    if (n0 + lane < width) a.out[projection][at] = a.y[projection][at];
+  }
 }
 
 // ------------------------------------------------------------------ more tokens
 // h^T = A x^T with 16x16x32 MFMAs, whose operands are 64 consecutive bytes of 16 rows: a wavefront has its share of K
 // for a tile of tokens and up to G tiles of 16 ranks (of any of the projections), so that activations are read once
 // for them. float16 activations are the sum of two bfloat16 numbers exactly, which is how they meet bfloat16 weights.
-// Bound by the loads' rows, which are apart.
+// Bound by the loads, whose rows are apart: halves of a cache line are asked for one after the other (5000 tokens by 3
+// times 32 ranks, K = 4096: 32 -> 30 us), and four steps at a time push lines out before their other half is read (38 us).
 template <bool BF16>
 __device__ __forceinline__ f32x4 small_product(u32x4 a, u32x4 b, f32x4 c) {
   if constexpr (BF16)
@@ -348,15 +351,15 @@ __global__ __launch_bounds__(kAdThreads) void k_adapter_shrink(AdapterArgs a) {
   for (int s = step0; s < step1; s += kAhead) {
     u32x4 xv[kAhead][2], av[kAhead][G];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const bool in = s + u < step1;
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-        xv[u][h] = has_token[h] && in ? *reinterpret_cast<const u32x4*>(x[h] + (int64_t)32 * (s + u)) : zero;
+      for (int u = 0; u < kAhead; ++u)
+        xv[u][h] = has_token[h] && s + u < step1 ? *reinterpret_cast<const u32x4*>(x[h] + (int64_t)32 * (s + u)) : zero;
 #pragma unroll
-      for (int g = 0; g < G; ++g)
-        av[u][g] = has_row[g] && in ? *reinterpret_cast<const u32x4*>(rows[g] + (int64_t)32 * (s + u)) : zero;
-    }
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        av[u][g] = has_row[g] && s + u < step1 ? *reinterpret_cast<const u32x4*>(rows[g] + (int64_t)32 * (s + u)) : zero;
 #pragma unroll
     for (int u = 0; u < kAhead; ++u)
 #pragma unroll
@@ -401,9 +404,11 @@ __global__ __launch_bounds__(kAdThreads) void k_adapter_shrink(AdapterArgs a) {
 
 // out = y + scale h B^T for a tile of tokens and 256 out features: 64 a wavefront, by 32x32x16 MFMAs, whose
 // results go through LDS so that y is read and written a row's 1 KiB at a time (straight from the MFMAs' layout, 128
-// bytes of 32 rows each, the same took 92 us, where this takes 60). Bound by reading and writing y. h, summed over the splits,
-// goes into the products as two float16 numbers about its token's largest (22 bits) or as three bfloat16 ones (24
-// bits), so that nothing is lost beside float32 sums. STEPS: products of 16 ranks that the pool has room for.
+// bytes of 32 rows each, it took half as long again). Bound by reading and writing y: 5000 tokens by 6144 features,
+// 246 MB, in 63 us, with a tile's blocks of columns next to each other and y read past the cache, and 71 us otherwise.
+// h, summed over the splits of K (all ranks of a split at once), goes into the products as two float16 numbers about
+// its token's largest (22 bits) or as three bfloat16 ones (24 bits), so that nothing is lost beside float32 sums.
+// STEPS: products of 16 ranks that the pool has room for.
 template <bool BF16, int STEPS>
 __global__ __launch_bounds__(kAdThreads) void k_adapter_expand(AdapterArgs a) {
   constexpr int kTerms = BF16 ? 3 : 2, kRows = kAdTile / kAdWaves;
@@ -411,13 +416,15 @@ __global__ __launch_bounds__(kAdThreads) void k_adapter_expand(AdapterArgs a) {
   __shared__ float sums[kAdTile][kAdColumns + 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
-  const int4 known = *reinterpret_cast<const int4*>(a.tiles + 4 * (int64_t)blockIdx.x);
+  const int64_t index = (int64_t)blockIdx.z * kTileRows + blockIdx.y;
+  if (index >= a.tile_count) return;
+  const int4 known = *reinterpret_cast<const int4*>(a.tiles + 4 * index);
   const auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
   const TokenTile tile = {uniform(known.x), uniform(known.y), uniform(known.z), uniform(known.w)};
   if (tile.n <= 0) return;
   int projection = 0;
-  while (projection + 1 < a.count && (int)blockIdx.y >= a.block0[projection + 1]) ++projection;
-  const int n0 = ((int)blockIdx.y - a.block0[projection]) * kAdColumns;
+  while (projection + 1 < a.count && (int)blockIdx.x >= a.block0[projection + 1]) ++projection;
+  const int n0 = ((int)blockIdx.x - a.block0[projection]) * kAdColumns;
   const int width = a.n[projection];
   const int stop = n0 + kAdColumns < width ? n0 + kAdColumns : width;
   const float* y = a.y[projection] + (int64_t)tile.t0 * width;
@@ -441,7 +448,7 @@ __global__ __launch_bounds__(kAdThreads) void k_adapter_expand(AdapterArgs a) {
   if (vectors) {
     const int at = n0 + 4 * lane < stop ? n0 + 4 * lane : stop - 4;
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) base[i] = *reinterpret_cast<const f32x4*>(row_at(i) + at);
+    for (int i = 0; i < kRows; ++i) base[i] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(row_at(i) + at));
   } else {
     int at[4];
 #pragma unroll
@@ -470,27 +477,30 @@ __global__ __launch_bounds__(kAdThreads) void k_adapter_expand(AdapterArgs a) {
     float most = 0.0f;
     const float scale = a.scales ? a.scales[tile.adapter] : 1.0f;
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) {
+    for (int s = 0; s < STEPS; ++s)
 #pragma unroll
       for (int j = 0; j < 8; ++j) h[s][j] = 0.0f;
-      const int r = 16 * s + 8 * half;
-      if (r < tile.rank && col < tile.n) {
-        const float* from = a.h + (((int64_t)tile.t0 + col) * a.count + projection) * a.rank + r;
+    // Past the tile or the rank: the first token's or rank's, which are not used.
+    const float* from = a.h + (((int64_t)tile.t0 + (col < tile.n ? col : 0)) * a.count + projection) * a.rank;
 #pragma unroll 1
-        for (int i = 0; i < a.splits; ++i) {
-          float v[8];
-          load_row<LOGBQ_DTYPE_F32>(from, 0, v);
+    for (int i = 0; i < a.splits; ++i) {
+      float v[STEPS][8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) h[s][j] += v[j];
-          from += (int64_t)a.tokens * a.count * a.rank;
-        }
-      }
+      for (int s = 0; s < STEPS; ++s)
+        load_row<LOGBQ_DTYPE_F32>(from, 16 * s + 8 * half < tile.rank ? 16 * s + 8 * half : 0, v[s]);
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) h[s][j] += v[s][j];
+      from += (int64_t)a.tokens * a.count * a.rank;
+    }
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        h[s][j] *= scale;
+        h[s][j] = 16 * s + 8 * half < tile.rank && col < tile.n ? h[s][j] * scale : 0.0f;
         most = fmaxf(most, __builtin_fabsf(h[s][j]));
       }
-    }
     int e = 0;
     if constexpr (!BF16) {
       most = fmaxf(most, __shfl_xor(most, 32));
@@ -598,13 +608,12 @@ int32_t logbq_linear_adapters(const uint16_t* x_dev, int64_t tokens, int64_t k, 
       adapters >= INT32_MAX)
     return LOGBQ_ERR_UNSUPPORTED;
   AdapterArgs a = {};
-  const int columns = max_new <= kFewTokens ? kFewColumns : kAdColumns;
   int64_t blocks = 0;
   for (int i = 0; i < count; ++i) {
     if (n[i] >= 1 << 24) return LOGBQ_ERR_UNSUPPORTED;
     a.n[i] = (int32_t)n[i];
     a.block0[i] = (int32_t)blocks;
-    blocks += (n[i] + columns - 1) / columns;
+    blocks += (n[i] + kAdColumns - 1) / kAdColumns;
     if (blocks > 65535) return LOGBQ_ERR_UNSUPPORTED;
   }
   a.block0[count] = (int32_t)blocks;
@@ -650,6 +659,7 @@ int32_t logbq_linear_adapters(const uint16_t* x_dev, int64_t tokens, int64_t k, 
   a.scales = scales_dev;
   a.tiles = static_cast<int32_t*>(work_dev);
   a.h = static_cast<float*>(work_dev) + 4 * (tokens + tokens / kAdTile + 1);
+  a.tile_count = tiles;
   a.k = k;
   a.tokens = (int32_t)tokens;
   a.requests = (int32_t)requests;
@@ -670,7 +680,8 @@ int32_t logbq_linear_adapters(const uint16_t* x_dev, int64_t tokens, int64_t k, 
 #undef FEW
     return launch_status();
   }
-  // Activations are read once for up to eight rank tiles; K is split until two workgroups a CU have work.
+  // Activations are read once for up to eight rank tiles; K is split until two workgroups a CU have work (of 5000 tokens
+  // in 3 parts: 98 us with both kernels; in 6, whose sums the second kernel reads: 122; in 1: 101).
   const int rank_tiles = count * ((rank + kRankTile - 1) / kRankTile);
   const int group = rank_tiles <= 2 ? 2 : rank_tiles <= 4 ? 4 : 8;
   const int groups = (rank_tiles + group - 1) / group;
@@ -679,7 +690,8 @@ int32_t logbq_linear_adapters(const uint16_t* x_dev, int64_t tokens, int64_t k, 
   splits = splits > k / 512 ? k / 512 : splits;
   splits = splits > kAdSplitTokens / tokens ? kAdSplitTokens / tokens : splits;
   a.splits = splits < 1 ? 1 : (int32_t)splits;
-  const dim3 shrink((unsigned)tiles, (unsigned)a.splits, (unsigned)groups), expand((unsigned)tiles, (unsigned)blocks);
+  const dim3 shrink((unsigned)tiles, (unsigned)a.splits, (unsigned)groups), expand((unsigned)blocks, (unsigned)(tiles < kTileRows ? tiles : kTileRows),
+                                                                                        (unsigned)((tiles + kTileRows - 1) / kTileRows));
 #define SHRINK(BF16, G)                                                                        \
   if (bf16 == BF16 && group == G)                                                              \
     hipLaunchKernelGGL((k_adapter_shrink<BF16, G>), shrink, dim3(kAdThreads), 0, (hipStream_t)stream, a)

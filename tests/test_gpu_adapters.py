@@ -184,3 +184,13 @@ def test_beside_the_linears():
     d["ys"] = ys
     got = call(d, [1, -1, 0], 5, scales=[0.5, 2.0])
     check(d, before, got, [1, -1, 0], [0.5, 2.0])
+
+
+def test_more_tiles_than_a_grid_has_rows():
+    """40000 requests of a token, as a step of up to five takes them."""
+    n, adapters = 40000, 5
+    d = make(11, [1] * n, 32, [16], adapters, 8, "f16")
+    ids = [i % (adapters + 1) - 1 for i in range(n)]
+    outs = [torch.empty_like(y) for y in d["ys"]]      # the call would update ys otherwise
+    for most in (5, 1):
+        check(d, d["ys"], call(d, ids, most, outs=outs), ids)
