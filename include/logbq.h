@@ -652,7 +652,7 @@ int64_t logbq_linear_adapters_workspace(int64_t tokens, int32_t count, int32_t r
  *   count    : projections, 1 .. 4.
  *   a_dev, b_dev : host arrays of device pointers, 16-byte aligned: A_i [adapters][rank][k], B_i
  *              [adapters][n_i][rank].
- *   n        : host array, out features of the projections (any number; 0 leaves one out).
+ *   n        : host array, out features of the projections (0 leaves one out; fewer than 2^24 - 1024 in all).
  *   dtype    : logbq_dtype of A and B, float16 or bfloat16.
  *   adapters : adapters in the pool.
  *   rank     : ranks that the pool has room for, a multiple of 8, at most LOGBQ_ADAPTERS_MAX_RANK.

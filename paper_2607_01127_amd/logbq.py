@@ -638,7 +638,7 @@ def _rotated_out(x, out, like, stream, name):
     import torch
     if out is None:
         with _made_on(stream):
-            return torch.empty(x.shape, dtype=like, device=x.device)
+            return torch.empty_like(x, dtype=like, memory_format=torch.contiguous_format)
     _device_array(out, out.dtype, x.shape, name)
     return out
 
@@ -724,7 +724,7 @@ def kv4_read(cache, slots, dtype=None, stream=None):
     _device_array(slots, torch.int64, (slots.numel(),), "slots")
     shape = (slots.numel(), c.heads, c.dim)
     with _made_on(stream):
-        k = torch.empty(shape, dtype=dtype or torch.float16, device=slots.device)
+        k = slots.new_empty(shape, dtype=dtype or torch.float16)
         v = torch.empty_like(k)
     _check(lib().logbq_kv4_read(ctypes.byref(c), slots.data_ptr(), shape[0], k.data_ptr(),
                                 v.data_ptr(), _dtype_code(k.dtype), _stream(stream)),
@@ -748,14 +748,14 @@ def _attention_call(q, cache, table, seq_lens, q_starts, out, lse, workspace, st
     _device_array(q_starts, i32, (n + 1,), "q_starts")
     if out is None:
         with _made_on(stream):
-            out = torch.empty((tokens, q_heads, c.dim), dtype=torch.float16, device=q.device)
+            out = torch.empty_like(q, dtype=torch.float16, memory_format=torch.contiguous_format)
     else:
         _device_array(out, out.dtype, (tokens, q_heads, c.dim), "out")
     if lse is not None:
         _device_array(lse, torch.float32, (tokens, q_heads), "lse")
     if workspace is None:
         with _made_on(stream):
-            workspace = torch.empty(KV4_WORKSPACE_BYTES, dtype=torch.uint8, device=q.device)
+            workspace = q.new_empty(KV4_WORKSPACE_BYTES, dtype=torch.uint8)
     else:
         _device_workspace(workspace)
     before = (q.data_ptr(), q_stride, _dtype_code(q.dtype), tokens, q_heads, ctypes.byref(c), table.data_ptr(), n,
@@ -849,8 +849,7 @@ def linear_adapters(x, ys, a_list, b_list, q_starts, adapter, max_new: int, scal
         _device_array(ranks, torch.int32, (adapters,), "ranks")
     if workspace is None:
         with _made_on(stream):
-            workspace = torch.empty(linear_adapters_workspace_bytes(tokens, count, rank), dtype=torch.uint8,
-                                    device=x.device)
+            workspace = x.new_empty(linear_adapters_workspace_bytes(tokens, count, rank), dtype=torch.uint8)
     else:
         _device_workspace(workspace)
     pointers, sizes = _ARRAYS[count]
