@@ -619,12 +619,13 @@ int32_t logbq_kv4_attention(const void* q_dev, int64_t q_stride, int32_t q_dtype
 /*
  * logbq_kv4_tree_attention -- logbq_kv4_attention for a step whose new tokens are the nodes of drafted trees.
  *   masks_dev : device, [tokens] uint64 (logbq_tree_tables): bit j is set where the token sees the j-th new token of
- *               its request. Bits past the request's tokens count for nothing. Any masks do, a tree's or not.
+ *               its request. Bits past the request's tokens (max_new of them at most) count for nothing. Any masks
+ *               do, a tree's or not.
  *   max_new   : upper bound of a request's tokens (host), at most 64.
  *   window    : 0, or 64 at least: a token of depth d = (bits of its mask) - 1 sees the cached positions past
  *               cached + d - window, and all the new tokens of its mask.
  *   The others, what is written and what a row without anything to see gets: as logbq_kv4_attention, but
- *               requests * heads * ceil(max_new * (q_heads / heads) / 128) * (width * page / 64 + 1) < 2^29.
+ *               requests * heads * ceil(max_new * (q_heads / heads) / 128) * (width * page / 64 + 1) < 2^28.
  * A new token of a request sees all of its cached tokens (seq_len less its new tokens) that the window holds, and new
  * tokens by its mask. The new tokens' keys and values lie in the cache behind the cached ones, in order, as
  * logbq_batch_tables gives their slots. A chain (parents i - 1) gets what logbq_kv4_attention computes.

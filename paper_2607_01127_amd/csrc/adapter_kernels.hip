@@ -611,12 +611,9 @@ int32_t logbq_linear_adapters(const uint16_t* x_dev, int64_t tokens, int64_t k, 
   int64_t blocks = 0;
   for (int i = 0; i < count; ++i) {
     if (n[i] >= 1 << 24) return LOGBQ_ERR_UNSUPPORTED;
-    a.n[i] = (int32_t)n[i];
-    a.block0[i] = (int32_t)blocks;
     blocks += (n[i] + kAdColumns - 1) / kAdColumns;
     if (blocks > 65535) return LOGBQ_ERR_UNSUPPORTED;
   }
-  a.block0[count] = (int32_t)blocks;
   // Tiles: a request each, or as many as the requests can have.
   const int64_t tiles = max_new <= kFewTokens ? requests : tokens / kAdTile + (requests < tokens ? requests : tokens);
   if (tiles > kAdMaxBlocks) return LOGBQ_ERR_UNSUPPORTED;
@@ -628,27 +625,32 @@ int32_t logbq_linear_adapters(const uint16_t* x_dev, int64_t tokens, int64_t k, 
   if (!x_dev || !q_starts_dev || !adapter_dev || !work_dev) return LOGBQ_ERR_INVALID_ARG;
   if (!aligned16(x_dev) || !aligned16(work_dev) || work_bytes < logbq_linear_adapters_workspace(tokens, count, rank))
     return LOGBQ_ERR_UNSUPPORTED;
+  // The projections that have features; the kernels know no others.
   for (int i = 0; i < count; ++i) {
-    a.a[i] = static_cast<const uint16_t*>(a_dev[i]);
-    a.b[i] = static_cast<const uint16_t*>(b_dev[i]);
-    a.y[i] = y_dev[i];
-    a.out[i] = out_dev[i];
     if (n[i] == 0) continue;
-    if (!a.y[i] || !a.out[i] || (adapters > 0 && (!a.a[i] || !a.b[i]))) return LOGBQ_ERR_INVALID_ARG;
-    if (!aligned16(a.a[i]) || !aligned16(a.b[i]) || (uintptr_t)a.y[i] % 4 || (uintptr_t)a.out[i] % 4)
+    if (!y_dev[i] || !out_dev[i] || (adapters > 0 && (!a_dev[i] || !b_dev[i]))) return LOGBQ_ERR_INVALID_ARG;
+    if (!aligned16(a_dev[i]) || !aligned16(b_dev[i]) || (uintptr_t)y_dev[i] % 4 || (uintptr_t)out_dev[i] % 4)
       return LOGBQ_ERR_UNSUPPORTED;
+    const int j = a.count++;
+    a.a[j] = static_cast<const uint16_t*>(a_dev[i]);
+    a.b[j] = static_cast<const uint16_t*>(b_dev[i]);
+    a.y[j] = y_dev[i];
+    a.out[j] = out_dev[i];
+    a.n[j] = (int32_t)n[i];
+    a.block0[j + 1] = a.block0[j] + (int32_t)((n[i] + kAdColumns - 1) / kAdColumns);
   }
+  count = a.count;
   for (int i = 0; i < count; ++i) {
     // An output is its own input, or apart from whatever the call reads and from the other outputs.
-    const Range out[] = {{a.out[i], 4 * tokens * n[i]}};
+    const Range out[] = {{a.out[i], 4 * tokens * a.n[i]}};
     const Range in[] = {{x_dev, 2 * tokens * k}, {q_starts_dev, 4 * (requests + 1)}, {adapter_dev, 4 * requests},
                         {ranks_dev, ranks_dev ? 4 * adapters : 0}, {scales_dev, scales_dev ? 4 * adapters : 0}};
     const Range work[] = {{work_dev, work_bytes}};
     if (any_overlap(in, out) || any_overlap(work, out)) return LOGBQ_ERR_INVALID_ARG;
     for (int j = 0; j < count; ++j) {
-      const Range other[] = {{j == i && a.y[j] == a.out[j] ? nullptr : a.y[j], j == i && a.y[j] == a.out[j] ? 0 : 4 * tokens * n[j]},
-                             {a.a[j], 2 * adapters * rank * k}, {a.b[j], 2 * adapters * rank * n[j]},
-                             {a.out[j], j == i ? 0 : 4 * tokens * n[j]}};
+      const bool in_place = j == i && a.y[j] == a.out[j];
+      const Range other[] = {{a.y[j], in_place ? 0 : 4 * tokens * a.n[j]}, {a.a[j], 2 * adapters * rank * k},
+                             {a.b[j], 2 * adapters * rank * a.n[j]}, {a.out[j], j == i ? 0 : 4 * tokens * a.n[j]}};
       if (any_overlap(other, out)) return LOGBQ_ERR_INVALID_ARG;
     }
   }
@@ -665,7 +667,6 @@ int32_t logbq_linear_adapters(const uint16_t* x_dev, int64_t tokens, int64_t k, 
   a.requests = (int32_t)requests;
   a.adapters = (int32_t)adapters;
   a.rank = rank;
-  a.count = count;
   a.max_new = max_new < INT32_MAX ? (int32_t)max_new : INT32_MAX;
   const bool bf16 = dtype == LOGBQ_DTYPE_BF16;
   if (max_new <= kFewTokens) {

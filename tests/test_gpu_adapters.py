@@ -5,6 +5,8 @@ bfloat16): off by at most (K + 16) 2^-23 sum |x_k a_rk|. The second product take
 its token's largest (2^-22 of itself, 2^-24 of the largest) or three bfloat16 ones (2^-23), times the scale
 (2^-24), in a float32 sum of up to 3 R terms: (3 R + 8) 2^-23 of sum |s h_r b_r|; the sum with y rounds twice.
 """
+import ctypes
+
 import numpy as np
 import pytest
 
@@ -184,6 +186,28 @@ def test_beside_the_linears():
     d["ys"] = ys
     got = call(d, [1, -1, 0], 5, scales=[0.5, 2.0])
     check(d, before, got, [1, -1, 0], [0.5, 2.0])
+
+
+@pytest.mark.parametrize("most", [1, 40])
+def test_projections_without_features_need_no_buffers(most):
+    """Each of four projections left out in turn, with null pointers, and all of them."""
+    new, k, n = [most, 1, most], 96, [40, 300, 0, 7]
+    d = make(7, new, k, n, 2, 16, "f16")
+    ids = [1, -1, 0]
+    want = [torch.empty_like(y) for y in d["ys"]]
+    check(d, d["ys"], call(d, ids, most, outs=want), ids)
+    tokens, where = sum(new), ints(ids)
+    work = torch.empty(L.linear_adapters_workspace_bytes(tokens, 4, 16), dtype=torch.uint8, device=DEV)
+    pointers, sizes = ctypes.c_void_p * 4, ctypes.c_int64 * 4
+    for left in [set(), {0}, {1}, {3}, {0, 1}, {0, 1, 2, 3}]:
+        outs = [torch.full_like(y, 3.0) for y in d["ys"]]
+        at = lambda ts: pointers(*[None if i in left | {2} else t.data_ptr() for i, t in enumerate(ts)])  # noqa: E731
+        assert L.lib().logbq_linear_adapters(
+            d["x"].data_ptr(), tokens, k, 4, at(d["a"]), at(d["b"]),
+            sizes(*[0 if i in left else m for i, m in enumerate(n)]), 1, 2, 16, None, None, d["starts"].data_ptr(),
+            where.data_ptr(), 3, most, at(d["ys"]), at(outs), work.data_ptr(), work.numel(), L._stream(None)) == L.OK
+        for i in range(4):
+            assert torch.equal(outs[i], want[i]) if i not in left else bool((outs[i] == 3.0).all())
 
 
 def test_more_tiles_than_a_grid_has_rows():
