@@ -86,6 +86,11 @@ __device__ __forceinline__ Request request_of(const AttnArgs& a, int r) {
   return q;
 }
 
+// What a token sees of its request's new tokens; a mask's bits past them count for nothing.
+__device__ __forceinline__ uint64_t nodes_seen(const AttnArgs& a, const Request& q, int64_t token) {
+  return a.masks[token] & (q.n < kMaxNodes ? (1ull << q.n) - 1 : ~0ull);
+}
+
 // Float16 values of a word of 8 codes.
 __device__ __forceinline__ half8v values_of(uint32_t w) {
   const half2v a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 0);

@@ -576,7 +576,7 @@ void k_kv4_tree(AttnArgs a) {
   {
     const Row me = row_of();
     mine_of.load(a, me.token * a.q_stride + me.head * D + me.half * 8, busy && me.row < rows);
-    if (tid < kRows) row_mask[tid] = tid < rows ? a.masks[req.t0 + (row0 + tid) / a.group] : 0;
+    if (tid < kRows) row_mask[tid] = tid < rows ? nodes_seen(a, req, req.t0 + (row0 + tid) / a.group) : 0;
   }
   if (tid == 0) lds.again = 0;
   __syncthreads();
@@ -798,9 +798,9 @@ int32_t logbq_kv4_tree_attention(const void* q_dev, int64_t q_stride, int32_t q_
                                      lse_dev, work_dev, work_bytes, &a);
   if (bad != LOGBQ_OK) return bad;
   if (max_new > kMaxNodes || (window > 0 && window < kMaxNodes)) return LOGBQ_ERR_UNSUPPORTED;
-  // Tiles of 64 positions of up to 128 query rows, and at least one of each, fit 29 bits, as their costs do 31.
+  // Tiles of 64 positions of up to 128 query rows, and at least one of each: their costs, of 5 at most, fit 31 bits.
   const int64_t row_tiles = (max_new * a.group + kTileRows - 1) / kTileRows;
-  if ((double)requests * a.c.heads * row_tiles * ((double)width * cache->page / kTilePositions + 1) >= (1 << 29))
+  if ((double)requests * a.c.heads * row_tiles * ((double)width * cache->page / kTilePositions + 1) >= (1 << 28))
     return LOGBQ_ERR_UNSUPPORTED;
   if (tokens == 0 || requests == 0 || max_new == 0) return LOGBQ_OK;
   if (!masks_dev) return LOGBQ_ERR_INVALID_ARG;

@@ -80,7 +80,7 @@ def exact(q, k, v, table, lens, starts, masks, page, scale, window, max_new):
         a, b = int(starts[r]), int(starts[r + 1])
         cached = int(lens[r]) - (b - a)
         for t in range(a, min(b, a + max_new)):
-            bits = int(masks[t])
+            bits = int(masks[t]) & ((1 << min(b - a, max_new)) - 1)
             depth = max(0, bin(bits).count("1") - 1)
             j = np.arange(max(0, cached + depth - window + 1 if window else 0), max(0, cached))
             nodes = [cached + i for i in range(min(b - a, max_new)) if bits >> i & 1 and cached + i >= 0]
@@ -177,6 +177,19 @@ def test_windows(window, dim, page, group):
     lens, new = [400, 70, 64, 129], [20, 33, 64, 1]
     q, cache, table, masks = step(window, lens, new, 1, group, dim, page, "f16")
     attend(q, cache, table, lens, new, masks, page, "f32", window=window)
+
+
+@pytest.mark.parametrize("group", [1, 2, 4])
+def test_bits_past_the_tokens_make_no_depth(group):
+    """A window goes by the bits of the request's own tokens, max_new of them at most."""
+    lens, new = [300, 200, 128], [7, 20, 64]
+    q, cache, table, masks = step(17, lens, new, 1, group, 64, 16, "f16")
+    starts = np.concatenate([[0], np.cumsum(new)]).tolist()
+    for a, b in zip(starts[:-1], starts[1:]):
+        for t in range(a, b):
+            masks[t] |= (2**64 - 1) >> (b - a) << (b - a)
+    attend(q, cache, table, lens, new, masks, 16, "f32", window=70)
+    attend(q, cache, table, lens, new, [2**64 - 1] * sum(new), 16, "f32", window=70, max_new=8)
 
 
 def test_a_chain_is_what_causal_attention_computes():
