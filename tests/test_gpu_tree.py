@@ -327,3 +327,13 @@ def test_long_and_short_requests_share_the_chip():
     lens, new = [6000] + [70] * 30, [40] + [2] * 30
     q, cache, table, masks = step(12, lens, new, 2, 4, 64, 64, "f16")
     attend(q, cache, table, lens, new, masks, 64)
+
+
+@pytest.mark.parametrize("dim,most", [(64, 24), (128, 3)])
+def test_more_requests_than_a_workgroup_has_threads(dim, most):
+    rng = np.random.default_rng(dim)
+    new = [int(n) for n in rng.integers(0, most + 1, 700)]
+    new[13] = most
+    lens = [n + int(c) for n, c in zip(new, rng.integers(0, 90, 700))]
+    q, cache, table, masks = step(dim, lens, new, 1, 2, dim, 32, "f16")
+    attend(q, cache, table, lens, new, masks, 32)
