@@ -660,7 +660,8 @@ int64_t logbq_linear_adapters_workspace(int64_t tokens, int32_t count, int32_t r
  *   ranks_dev : device, [adapters] int32: rows of A and columns of B that an adapter has (0 .. rank; what
  *              lies past them is not used, whatever it holds). NULL: all of them have `rank`.
  *   scales_dev : device, [adapters] float32. NULL: 1.
- *   q_starts_dev : device, [requests + 1] int32, first token of each request.
+ *   q_starts_dev : device, [requests + 1] int32, first token of each request, ascending (else what is written to the
+ *              outputs is not specified).
  *   adapter_dev : device, [requests] int32: the request's adapter; one outside the pool: none.
  *   max_new  : upper bound of a request's tokens (host). Tokens of a request past it are left out.
  *   y_dev, out_dev : host arrays of device pointers, [tokens][n_i] float32. out_i may be y_i (in place), and

@@ -20,6 +20,7 @@ namespace {
 constexpr int kAdThreads = 256;
 constexpr int kAdWaves = kAdThreads / 64;
 constexpr int kAdTile = 32;                    // tokens of a tile
+constexpr int kWideTile = 64;                  // of the first kernel's, where requests have more than 32
 constexpr int kRankTile = 16;
 constexpr int kFewTokens = 4;                  // tokens of requests that go without tiles
 constexpr int kAdCount = 4;                    // projections of a call
@@ -42,8 +43,9 @@ struct AdapterArgs {
   const int32_t* ranks;
   const float* scales;
   float* h;                                    // [splits][tokens][count][rank]
-  int32_t* tiles;                              // [tile_count][4]: what the second kernel has to know of a tile
-  int64_t tile_count;
+  int32_t* tiles;                              // the number of tiles, and from [1][4] on what the second kernel has to
+                                               // know of each
+  int64_t tile_count;                          // most that there can be
   int64_t k;
   int32_t tokens, requests, adapters, rank, count, max_new, splits;
 };
@@ -62,57 +64,75 @@ __device__ __forceinline__ Span tokens_of(const AdapterArgs& a, int r) {
   return {t0, t1 - t0 < a.max_new ? t1 - t0 : a.max_new};
 }
 
-// The tile of an index. Where no request has more than a few tokens they are a tile each; else the workgroup counts
-// tiles out, which all of its threads call this for.
-__device__ __forceinline__ TokenTile tile_of(const AdapterArgs& a, int64_t index) {
-  int r = (int)index, first = 0;
-  if (a.max_new > kFewTokens) {
-    __shared__ int64_t scan[kAdWaves];
-    __shared__ int32_t found[2];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int per = (a.requests + kAdThreads - 1) / kAdThreads;
-    const int r0 = tid * per < a.requests ? tid * per : a.requests;
-    const int r1 = r0 + per < a.requests ? r0 + per : a.requests;
-    const auto tiles = [&](int i) { return (tokens_of(a, i).n + kAdTile - 1) / kAdTile; };
-    int64_t mine = 0;
-    for (int i = r0; i < r1; ++i) mine += tiles(i);
-    int64_t upto = mine;
-    for (int d = 1; d < 64; d <<= 1) {
-      const int64_t v = __shfl_up(upto, d);
-      if (lane >= d) upto += v;
-    }
-    if (lane == 63) scan[wave] = upto;
-    if (tid == 0) found[0] = -1;
-    __syncthreads();
-    for (int w = 0; w < wave; ++w) upto += scan[w];
-    if (upto - mine <= index && index < upto) {
-      int64_t at = upto - mine;
-      for (int i = r0; i < r1; ++i) {
-        const int m = tiles(i);
-        if (index < at + m) {
-          found[0] = i;
-          found[1] = (int)(index - at);
-          break;
-        }
-        at += m;
-      }
-    }
-    __syncthreads();
-    r = found[0];
-    first = found[1] * kAdTile;
-  }
-  r = __builtin_amdgcn_readfirstlane(r);
-  if (r < 0) return {0, 0, -1, 0};
-  first = __builtin_amdgcn_readfirstlane(first);
+// The first up to TOKENS tokens of a request from `first`.
+template <int TOKENS>
+__device__ __forceinline__ TokenTile tile_at(const AdapterArgs& a, int r, int first) {
   const Span s = tokens_of(a, r);
   TokenTile t;
   t.t0 = s.t0 + first;
-  t.n = s.n - first < kAdTile ? s.n - first : kAdTile;
+  t.n = s.n - first < TOKENS ? s.n - first : TOKENS;
   const int32_t id = a.adapter[r];
   t.adapter = id >= 0 && id < a.adapters ? id : -1;
   t.rank = t.adapter < 0 ? 0 : a.ranks ? a.ranks[t.adapter] : a.rank;
   t.rank = t.rank < 0 ? 0 : t.rank > a.rank ? a.rank : t.rank;
   return t;
+}
+
+// Where a workgroup's tile of TOKENS tokens is, counted out by all of its threads.
+struct Place {
+  int r, first;               // request (-1: none) and first of its tokens
+  int64_t below, all;         // tiles of kAdTile tokens: those before it, and of the whole call (0: starts that do not
+                              // ascend, with which there are more tiles than the call has room for)
+};
+template <int TOKENS>
+__device__ __forceinline__ Place place_of(const AdapterArgs& a, int64_t index) {
+  __shared__ int64_t scan[2][kAdWaves];
+  __shared__ int32_t found[2];
+  __shared__ int64_t found_below;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int per = (a.requests + kAdThreads - 1) / kAdThreads;
+  const int r0 = tid * per < a.requests ? tid * per : a.requests;
+  const int r1 = r0 + per < a.requests ? r0 + per : a.requests;
+  int64_t mine[2] = {0, 0}, upto[2], all[2] = {0, 0};      // tiles of TOKENS tokens, and of kAdTile
+  for (int i = r0; i < r1; ++i) {
+    const int n = tokens_of(a, i).n;
+    mine[0] += (n + TOKENS - 1) / TOKENS;
+    mine[1] += (n + kAdTile - 1) / kAdTile;
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    upto[k] = mine[k];
+    for (int d = 1; d < 64; d <<= 1) {
+      const int64_t v = __shfl_up(upto[k], d);
+      if (lane >= d) upto[k] += v;
+    }
+    if (lane == 63) scan[k][wave] = upto[k];
+  }
+  if (tid == 0) found[0] = -1;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    for (int w = 0; w < kAdWaves; ++w) {
+      upto[k] += w < wave ? scan[k][w] : 0;
+      all[k] += scan[k][w];
+    }
+  if (all[0] > gridDim.x || all[1] > a.tile_count) return {-1, 0, 0, 0};
+  if (upto[0] - mine[0] <= index && index < upto[0]) {
+    int64_t at = upto[0] - mine[0], below = upto[1] - mine[1];
+    for (int i = r0; i < r1; ++i) {
+      const int n = tokens_of(a, i).n, m = (n + TOKENS - 1) / TOKENS;
+      if (index < at + m) {
+        found[0] = i;
+        found[1] = (int)(index - at) * TOKENS;
+        found_below = below + (index - at) * (TOKENS / kAdTile);
+        break;
+      }
+      at += m;
+      below += (n + kAdTile - 1) / kAdTile;
+    }
+  }
+  __syncthreads();
+  return {__builtin_amdgcn_readfirstlane(found[0]), __builtin_amdgcn_readfirstlane(found[1]), found_below, all[1]};
 }
 
 template <bool BF16>
@@ -170,7 +190,7 @@ template <bool BF16, int T>
 __global__ __launch_bounds__(kAdThreads) void k_adapter_shrink_few(AdapterArgs a) {
   __shared__ float sums[kAdWaves][T][kFewRows];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const TokenTile tile = tile_of(a, blockIdx.x);
+  const TokenTile tile = tile_at<T>(a, blockIdx.x, 0);
   const int per_projection = a.rank / kFewRows;
   const int projection = (int)blockIdx.y / per_projection, row0 = ((int)blockIdx.y - projection * per_projection) * kFewRows;
   if (tile.n <= 0 || row0 >= tile.rank) return;
@@ -276,7 +296,7 @@ __device__ __forceinline__ void expand_few(const AdapterArgs& a, const TokenTile
 template <bool BF16, int T>
 __global__ __launch_bounds__(kAdThreads) void k_adapter_expand_few(AdapterArgs a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const TokenTile tile = tile_of(a, blockIdx.x);
+  const TokenTile tile = tile_at<T>(a, blockIdx.x, 0);
   if (tile.n <= 0) return;
   int projection = 0;
   while (projection + 1 < a.count && (int)blockIdx.y >= a.block0[projection + 1]) ++projection;
@@ -299,8 +319,9 @@ __global__ __launch_bounds__(kAdThreads) void k_adapter_expand_few(AdapterArgs a
 // h^T = A x^T with 16x16x32 MFMAs, whose operands are 64 consecutive bytes of 16 rows: a wavefront has its share of K
 // for a tile of tokens and up to G tiles of 16 ranks (of any of the projections), so that activations are read once
 // for them. float16 activations are the sum of two bfloat16 numbers exactly, which is how they meet bfloat16 weights.
-// Bound by the loads, whose rows are apart: halves of a cache line are asked for one after the other (5000 tokens by 3
-// times 32 ranks, K = 4096: 32 -> 30 us), and four steps at a time push lines out before their other half is read (38 us).
+// Bound by the loads: a CU has few lines on their way at once, so what counts is how many it asks for. 5000 tokens by 3
+// times 32 ranks, K = 4096: 28 us with 64 tokens a tile, 30 with 32 (twice the weights' loads), 32 with both halves of a
+// line apart in the program; four steps at a time push lines out before their other half is read (38 us).
 template <bool BF16>
 __device__ __forceinline__ f32x4 small_product(u32x4 a, u32x4 b, f32x4 c) {
   if constexpr (BF16)
@@ -309,16 +330,23 @@ __device__ __forceinline__ f32x4 small_product(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8v, a), __builtin_bit_cast(half8v, b), c, 0, 0, 0);
 }
 
-template <bool BF16, int G>
+template <bool BF16, int G, int TOKENS>
 __global__ __launch_bounds__(kAdThreads) void k_adapter_shrink(AdapterArgs a) {
+  constexpr int kHalves = TOKENS / 16;
   constexpr int kAhead = 2;                      // steps of 32 whose loads are on their way together: 128 bytes of a row
-  __shared__ float sums[kAdWaves][kAdTile][kRankTile + 4];
+  __shared__ float sums[kAdWaves][TOKENS][kRankTile + 4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int col = lane & 15, quarter = lane >> 4;
-  const TokenTile tile = tile_of(a, blockIdx.x);
-  if (blockIdx.y == 0 && blockIdx.z == 0 && tid == 0)
-    *reinterpret_cast<int4*>(a.tiles + 4 * (int64_t)blockIdx.x) = int4{tile.t0, tile.n, tile.adapter, tile.rank};
-  if (tile.n <= 0 || tile.rank <= 0) return;
+  const Place place = place_of<TOKENS>(a, blockIdx.x);
+  const bool tells = blockIdx.y == 0 && blockIdx.z == 0;      // the second kernel of its tiles
+  if (tells && blockIdx.x == 0 && tid == 0) a.tiles[0] = (int32_t)place.all;
+  if (place.r < 0) return;
+  const TokenTile tile = tile_at<TOKENS>(a, place.r, place.first);
+  if (tells && tid < TOKENS / kAdTile && tid * kAdTile < tile.n)
+    *reinterpret_cast<int4*>(a.tiles + 4 * (1 + place.below + tid)) =
+        int4{tile.t0 + tid * kAdTile, tile.n - tid * kAdTile < kAdTile ? tile.n - tid * kAdTile : kAdTile, tile.adapter,
+             tile.rank};
+  if (tile.rank <= 0) return;
   const int per_projection = (a.rank + kRankTile - 1) / kRankTile;
   const int id0 = blockIdx.z * G, ids = a.count * per_projection;
   const int64_t blocks = (a.k + 32 * kAhead - 1) / (32 * kAhead), chunks = (int64_t)a.splits * kAdWaves;
@@ -326,14 +354,13 @@ __global__ __launch_bounds__(kAdThreads) void k_adapter_shrink(AdapterArgs a) {
   const int step0 = (int)(blocks * chunk / chunks) * kAhead, all = (int)(a.k / 32);
   const int end = (int)(blocks * (chunk + 1) / chunks) * kAhead, step1 = end < all ? end : all;
 
-  const uint16_t* x[2];
-  bool has_token[2];
+  const uint16_t* x[kHalves];
+  bool has_token[kHalves];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
+  for (int h = 0; h < kHalves; ++h) {
     has_token[h] = 16 * h + col < tile.n;
     x[h] = a.x + (int64_t)(tile.t0 + (has_token[h] ? 16 * h + col : 0)) * a.k + 8 * quarter;
   }
-  const bool both = tile.n > 16;
   const uint16_t* rows[G];
   bool has_row[G], any[G];
 #pragma unroll
@@ -344,14 +371,16 @@ __global__ __launch_bounds__(kAdThreads) void k_adapter_shrink(AdapterArgs a) {
     has_row[g] = any[g] && row < tile.rank;
     rows[g] = a.a[projection] + ((int64_t)tile.adapter * a.rank + (has_row[g] ? row : 0)) * a.k + 8 * quarter;
   }
-  f32x4 acc[G][2];
+  f32x4 acc[G][kHalves];
 #pragma unroll
-  for (int g = 0; g < G; ++g) acc[g][0] = acc[g][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h) acc[g][h] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   const u32x4 zero = {0, 0, 0, 0};
   for (int s = step0; s < step1; s += kAhead) {
-    u32x4 xv[kAhead][2], av[kAhead][G];
+    u32x4 xv[kAhead][kHalves], av[kAhead][G];
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < kHalves; ++h)
 #pragma unroll
       for (int u = 0; u < kAhead; ++u)
         xv[u][h] = has_token[h] && s + u < step1 ? *reinterpret_cast<const u32x4*>(x[h] + (int64_t)32 * (s + u)) : zero;
@@ -363,8 +392,8 @@ __global__ __launch_bounds__(kAdThreads) void k_adapter_shrink(AdapterArgs a) {
 #pragma unroll
     for (int u = 0; u < kAhead; ++u)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        if (h && !both) continue;
+      for (int h = 0; h < kHalves; ++h) {
+        if (h && 16 * h >= tile.n) continue;
         u32x4 lo = zero, hi = xv[u][h];
         if constexpr (BF16) {
           const half8v v = __builtin_bit_cast(half8v, xv[u][h]);
@@ -388,7 +417,7 @@ __global__ __launch_bounds__(kAdThreads) void k_adapter_shrink(AdapterArgs a) {
   for (int g = 0; g < G; ++g) {
     if (!any[g]) continue;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) *reinterpret_cast<f32x4*>(&sums[wave][16 * h + col][4 * quarter]) = acc[g][h];
+    for (int h = 0; h < kHalves; ++h) *reinterpret_cast<f32x4*>(&sums[wave][16 * h + col][4 * quarter]) = acc[g][h];
     __syncthreads();
     const int token = tid >> 2, at = (tid & 3) * 4;
     const int projection = (id0 + g) / per_projection, row = (id0 + g) % per_projection * kRankTile + at;
@@ -405,20 +434,22 @@ __global__ __launch_bounds__(kAdThreads) void k_adapter_shrink(AdapterArgs a) {
 // out = y + scale h B^T for a tile of tokens and 256 out features: 64 a wavefront, by 32x32x16 MFMAs, whose
 // results go through LDS so that y is read and written a row's 1 KiB at a time (straight from the MFMAs' layout, 128
 // bytes of 32 rows each, it took half as long again). Bound by reading and writing y: 5000 tokens by 6144 features,
-// 246 MB, in 63 us, with a tile's blocks of columns next to each other and y read past the cache, and 71 us otherwise.
-// h, summed over the splits of K (all ranks of a split at once), goes into the products as two float16 numbers about
+// 246 MB, in 58 us. It took 71 with a tile's blocks of columns far apart in the grid and y kept in cache, and 63 with h
+// loaded by every wavefront for itself. h, summed over the splits of K, goes into the products as two float16 numbers about
 // its token's largest (22 bits) or as three bfloat16 ones (24 bits), so that nothing is lost beside float32 sums.
 // STEPS: products of 16 ranks that the pool has room for.
 template <bool BF16, int STEPS>
 __global__ __launch_bounds__(kAdThreads) void k_adapter_expand(AdapterArgs a) {
   constexpr int kTerms = BF16 ? 3 : 2, kRows = kAdTile / kAdWaves;
-  __shared__ float factors[kAdWaves][kAdTile];
-  __shared__ float sums[kAdTile][kAdColumns + 4];
+  constexpr int kPieces = 2 * STEPS, kTermRow = kPieces * kTerms + 1;    // of 8 ranks; a token's terms
+  __shared__ float factors[kAdTile];
+  __shared__ float sums[kAdTile][kAdColumns + 4];                        // at first all tokens' terms
+  static_assert(sizeof(u32x4) * kAdTile * kTermRow <= sizeof(sums), "the terms fit");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
   const int64_t index = (int64_t)blockIdx.z * kTileRows + blockIdx.y;
-  if (index >= a.tile_count) return;
-  const int4 known = *reinterpret_cast<const int4*>(a.tiles + 4 * index);
+  if (index >= a.tiles[0]) return;
+  const int4 known = *reinterpret_cast<const int4*>(a.tiles + 4 * (1 + index));
   const auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
   const TokenTile tile = {uniform(known.x), uniform(known.y), uniform(known.z), uniform(known.w)};
   if (tile.n <= 0) return;
@@ -470,70 +501,81 @@ __global__ __launch_bounds__(kAdThreads) void k_adapter_expand(AdapterArgs a) {
                            ? *reinterpret_cast<const u32x4*>(b + (int64_t)at * a.rank + 16 * s) : u32x4{0, 0, 0, 0};
   }
 
-  // The lane's part of its token's h, summed in the order of the splits, as terms.
-  u32x4 term[STEPS][kTerms];
+  // h, summed in the order of the splits, as terms: 8 threads have a token, a piece of 8 ranks or two each. The wavefronts
+  // all need all of it.
+  u32x4* terms = reinterpret_cast<u32x4*>(&sums[0][0]);
   {
-    float h[STEPS][8];
-    float most = 0.0f;
+    constexpr int kOwn = (kPieces + 7) / 8;
+    const int token = threadIdx.x >> 3, piece = threadIdx.x & 7;
     const float scale = a.scales ? a.scales[tile.adapter] : 1.0f;
-#pragma unroll
-    for (int s = 0; s < STEPS; ++s)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) h[s][j] = 0.0f;
     // Past the tile or the rank: the first token's or rank's, which are not used.
-    const float* from = a.h + (((int64_t)tile.t0 + (col < tile.n ? col : 0)) * a.count + projection) * a.rank;
+    const float* from = a.h + (((int64_t)tile.t0 + (token < tile.n ? token : 0)) * a.count + projection) * a.rank;
+    float h[kOwn][8], most = 0.0f;
+#pragma unroll
+    for (int o = 0; o < kOwn; ++o)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) h[o][j] = 0.0f;
 #pragma unroll 1
     for (int i = 0; i < a.splits; ++i) {
-      float v[STEPS][8];
 #pragma unroll
-      for (int s = 0; s < STEPS; ++s)
-        load_row<LOGBQ_DTYPE_F32>(from, 16 * s + 8 * half < tile.rank ? 16 * s + 8 * half : 0, v[s]);
+      for (int o = 0; o < kOwn; ++o) {
+        const int at = 8 * (piece + 8 * o);
+        float v[8];
+        load_row<LOGBQ_DTYPE_F32>(from, at < tile.rank ? at : 0, v);
 #pragma unroll
-      for (int s = 0; s < STEPS; ++s)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) h[s][j] += v[s][j];
+        for (int j = 0; j < 8; ++j) h[o][j] += v[j];
+      }
       from += (int64_t)a.tokens * a.count * a.rank;
     }
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s)
+    for (int o = 0; o < kOwn; ++o)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        h[s][j] = 16 * s + 8 * half < tile.rank && col < tile.n ? h[s][j] * scale : 0.0f;
-        most = fmaxf(most, __builtin_fabsf(h[s][j]));
+        h[o][j] = 8 * (piece + 8 * o) < tile.rank && token < tile.n ? h[o][j] * scale : 0.0f;
+        most = fmaxf(most, __builtin_fabsf(h[o][j]));
       }
     int e = 0;
     if constexpr (!BF16) {
-      most = fmaxf(most, __shfl_xor(most, 32));
+      for (int d = 1; d < 8; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
       e = most > 0.0f && most < INFINITY ? (int)(__float_as_uint(most) >> 23) - 127 : 0;
-      if (half == 0) factors[wave][col] = ldexpf(1.0f, e);     // read by the same wavefront, after a barrier
+      if (piece == 0) factors[token] = ldexpf(1.0f, e);
     }
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) {
+    for (int o = 0; o < kOwn; ++o) {
       float left[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) left[j] = BF16 ? h[s][j] : ldexpf(h[s][j], -e);
+      for (int j = 0; j < 8; ++j) left[j] = BF16 ? h[o][j] : ldexpf(h[o][j], -e);
 #pragma unroll
       for (int i = 0; i < kTerms; ++i) {
+        u32x4 v;
         if constexpr (BF16) {
-          bf16x8 v;
+          bf16x8 b8;
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            v[j] = (__bf16)left[j];
-            left[j] = rest_of(left[j], v[j]);
+            b8[j] = (__bf16)left[j];
+            left[j] = rest_of(left[j], b8[j]);
           }
-          term[s][i] = __builtin_bit_cast(u32x4, v);
+          v = __builtin_bit_cast(u32x4, b8);
         } else {
-          half8v v;
+          half8v h8;
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            v[j] = (half_t)left[j];
-            left[j] -= (float)v[j];
+            h8[j] = (half_t)left[j];
+            left[j] -= (float)h8[j];
           }
-          term[s][i] = __builtin_bit_cast(u32x4, v);
+          v = __builtin_bit_cast(u32x4, h8);
         }
+        if (piece + 8 * o < kPieces) terms[token * kTermRow + (piece + 8 * o) * kTerms + i] = v;
       }
     }
   }
+  __syncthreads();
+  u32x4 term[STEPS][kTerms];
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+    for (int i = 0; i < kTerms; ++i) term[s][i] = terms[col * kTermRow + (2 * s + half) * kTerms + i];
+  __syncthreads();
 
 #pragma unroll
   for (int nb = 0; nb < 2; ++nb) {
@@ -559,7 +601,7 @@ __global__ __launch_bounds__(kAdThreads) void k_adapter_expand(AdapterArgs a) {
   for (int i = 0; i < kRows; ++i) {
     const int t = kRows * wave + i;
     if (t >= tile.n) continue;
-    const float f = BF16 ? 1.0f : factors[wave][t];
+    const float f = BF16 ? 1.0f : factors[t];
     float* to = out + (int64_t)t * width + n0;
     if (vectors) {
       const f32x4 v = *reinterpret_cast<const f32x4*>(&sums[t][4 * lane]);
@@ -587,7 +629,8 @@ int64_t logbq_linear_adapters_workspace(int64_t tokens, int32_t count, int32_t r
   if (tokens < 0 || count < 1 || rank < 1 || !adapter_sizes_fit(tokens, count, rank)) return 0;
   int64_t rows = tokens * kAdSplits < kAdSplitTokens ? tokens * kAdSplits : kAdSplitTokens;
   rows = rows > tokens ? rows : tokens;
-  // A request's last tile is not full, so there may be a tile a token and as many as all of them fill.
+  // A request's last tile is not full, so there may be a tile a token and as many as all of them fill; before them
+  // their number.
   return rows * count * rank * 4 + 16 * (tokens + tokens / kAdTile + 1);
 }
 
@@ -604,7 +647,7 @@ int32_t logbq_linear_adapters(const uint16_t* x_dev, int64_t tokens, int64_t k, 
   for (int i = 0; i < count; ++i)
     if (n[i] < 0) return LOGBQ_ERR_INVALID_ARG;
   if (dtype != LOGBQ_DTYPE_F16 && dtype != LOGBQ_DTYPE_BF16) return LOGBQ_ERR_UNSUPPORTED;
-  if (!adapter_sizes_fit(tokens, count, rank) || k % 32 || k > INT32_MAX || requests >= INT32_MAX ||
+  if (!adapter_sizes_fit(tokens, count, rank) || k % 32 || k > INT32_MAX || requests > INT32_MAX - kAdThreads ||
       adapters >= INT32_MAX)
     return LOGBQ_ERR_UNSUPPORTED;
   AdapterArgs a = {};
@@ -681,23 +724,29 @@ int32_t logbq_linear_adapters(const uint16_t* x_dev, int64_t tokens, int64_t k, 
 #undef FEW
     return launch_status();
   }
-  // Activations are read once for up to eight rank tiles; K is split until two workgroups a CU have work (of 5000 tokens
-  // in 3 parts: 98 us with both kernels; in 6, whose sums the second kernel reads: 122; in 1: 101).
+  // Activations are read once for up to eight rank tiles, and weights for 64 tokens where they are as many as the
+  // activations. K is split until a workgroup of 64 tokens a CU has work, which has all registers, or two of 32 tokens.
+  // 5000 tokens by 3 times 32 ranks in 2, 3 and 4 parts: 33, 28 and 40 us; 9000 tokens by 16 ranks: 38 us (both kernels)
+  // with 64 tokens, 35 with 32.
   const int rank_tiles = count * ((rank + kRankTile - 1) / kRankTile);
   const int group = rank_tiles <= 2 ? 2 : rank_tiles <= 4 ? 4 : 8;
   const int groups = (rank_tiles + group - 1) / group;
-  int64_t splits = 512 / (tiles * groups);
+  const bool wide = max_new > kAdTile && group > 2;
+  const int64_t first_tiles = wide ? tokens / kWideTile + (requests < tokens ? requests : tokens) : tiles;
+  int64_t splits = (wide ? 256 : 512) / (first_tiles * groups);
   splits = splits > kAdSplits ? kAdSplits : splits;
   splits = splits > k / 512 ? k / 512 : splits;
   splits = splits > kAdSplitTokens / tokens ? kAdSplitTokens / tokens : splits;
   a.splits = splits < 1 ? 1 : (int32_t)splits;
-  const dim3 shrink((unsigned)tiles, (unsigned)a.splits, (unsigned)groups), expand((unsigned)blocks, (unsigned)(tiles < kTileRows ? tiles : kTileRows),
-                                                                                        (unsigned)((tiles + kTileRows - 1) / kTileRows));
-#define SHRINK(BF16, G)                                                                        \
-  if (bf16 == BF16 && group == G)                                                              \
-    hipLaunchKernelGGL((k_adapter_shrink<BF16, G>), shrink, dim3(kAdThreads), 0, (hipStream_t)stream, a)
-  SHRINK(false, 2); SHRINK(false, 4); SHRINK(false, 8);
-  SHRINK(true, 2); SHRINK(true, 4); SHRINK(true, 8);
+  const dim3 shrink((unsigned)first_tiles, (unsigned)a.splits, (unsigned)groups);
+  const dim3 expand((unsigned)blocks, (unsigned)(tiles < kTileRows ? tiles : kTileRows),
+                    (unsigned)((tiles + kTileRows - 1) / kTileRows));
+#define SHRINK(BF16, G, TOKENS)                                                                        \
+  if (bf16 == BF16 && group == G && wide == (TOKENS == kWideTile))                                     \
+    hipLaunchKernelGGL((k_adapter_shrink<BF16, G, TOKENS>), shrink, dim3(kAdThreads), 0, (hipStream_t)stream, a)
+  SHRINK(false, 2, kAdTile); SHRINK(false, 4, kAdTile); SHRINK(false, 8, kAdTile);
+  SHRINK(true, 2, kAdTile); SHRINK(true, 4, kAdTile); SHRINK(true, 8, kAdTile);
+  SHRINK(false, 4, kWideTile); SHRINK(false, 8, kWideTile); SHRINK(true, 4, kWideTile); SHRINK(true, 8, kWideTile);
 #undef SHRINK
   if (launch_status() != LOGBQ_OK) return LOGBQ_ERR_HIP;
   const int steps = rank <= 32 ? 2 : rank <= 64 ? 4 : 8;

@@ -218,3 +218,15 @@ def test_more_tiles_than_a_grid_has_rows():
     outs = [torch.empty_like(y) for y in d["ys"]]      # the call would update ys otherwise
     for most in (5, 1):
         check(d, d["ys"], call(d, ids, most, outs=outs), ids)
+
+
+@pytest.mark.parametrize("most,rank", [(100, 128), (100, 16), (20, 64), (3, 8)])
+def test_starts_that_do_not_ascend_stay_within_the_buffers(most, rank):
+    tokens, requests, k, n = 100, 50, 64, 300
+    d = make(most, [tokens], k, [n, n], 2, rank, "f16")
+    d["starts"] = ints([0, tokens] * (requests // 2) + [-7])
+    need = L.linear_adapters_workspace_bytes(tokens, 2, rank)
+    held = torch.full((need + 4096,), 0x5a, dtype=torch.uint8, device=DEV)
+    outs = [torch.full((tokens + 8, n), 7.0, device=DEV) for _ in range(2)]
+    call(d, [0, 1] * (requests // 2), most, outs=[o[:tokens] for o in outs], workspace=held[:need])
+    assert bool((held[need:] == 0x5a).all()) and all(bool((o[tokens:] == 7.0).all()) for o in outs)
