@@ -509,9 +509,9 @@ def _kv4_struct(cache) -> Kv4Struct:
         raise ValueError("k_codes must be [pages][heads][page][dim/2]")
     shape = kc.shape
     pages, heads, page, half = shape
-    values, scales = (pages, heads, page // 8, 16, 8, half // 16), shape[:3]
+    values, scales = (pages, heads, page // 8, 16, 8, half // 16), (pages, heads, page)
     u8, bf16 = torch.uint8, torch.bfloat16
-    if not (vc.shape == values and ks.shape == vs.shape == scales and kc.is_cuda and vc.is_cuda
+    if not (vc.shape == values and ks.shape == scales and vs.shape == scales and kc.is_cuda and vc.is_cuda
             and ks.is_cuda and vs.is_cuda and kc.dtype == vc.dtype == u8 and ks.dtype == vs.dtype == bf16
             and kc.is_contiguous() and vc.is_contiguous() and ks.is_contiguous()
             and vs.is_contiguous()):
@@ -539,13 +539,14 @@ def _made_on(stream):
 def _rows(x, heads, dim, name):
     """Elements between the tokens of x [tokens][heads][dim], whose heads and channels are
     contiguous."""
-    if x.dim() != 3 or not x.is_cuda or x.shape[2] != dim or (heads and x.shape[1] != heads):
+    shape = x.shape
+    if len(shape) != 3 or not x.is_cuda or shape[2] != dim or (heads and shape[1] != heads):
         raise ValueError(f"{name} must be a [tokens][{heads or 'heads'}][{dim}] device tensor")
     stride = x.stride()
-    if stride[2] != 1 or (stride[1] != dim and x.shape[1] != 1):
+    if stride[2] != 1 or (stride[1] != dim and shape[1] != 1):
         raise ValueError(f"the heads and channels of {name} must be contiguous")
     # One token has no distance to the next; its stride may be anything.
-    return stride[0] if x.shape[0] > 1 else x.shape[1] * dim
+    return stride[0] if shape[0] > 1 else shape[1] * dim
 
 
 def batch_tables(cached, new, free_pages, table, page: int, tokens: int, out=None, stream=None):
@@ -618,29 +619,29 @@ class Rotation(NamedTuple):
     factor: float = 1.0
 
 
-def _rotation_struct(rotation) -> RotationStruct:
-    import torch
+def _rotation_struct(rotation, f32) -> RotationStruct:
     inv_freq, interleaved, factor = rotation
-    _device_array(inv_freq, torch.float32, (inv_freq.numel(),), "inv_freq")
-    return RotationStruct(inv_freq.data_ptr() or None, inv_freq.numel(), 1 if interleaved else 0, factor)
+    pairs = inv_freq.numel()
+    _device_array(inv_freq, f32, (pairs,), "inv_freq")
+    return RotationStruct(inv_freq.data_ptr() or None, pairs, 1 if interleaved else 0, factor)
 
 
-def _weight(x, dim, name):
+def _weight(x, f32, dim, name):
     if x is None:
         return None
-    import torch
-    _device_array(x, torch.float32, (dim,), name)
+    _device_array(x, f32, (dim,), name)
     return x.data_ptr()
 
 
 def _rotated_out(x, out, like, stream, name):
-    """The tensor that takes x's rotated rows: `out`, checked, or a new one of type `like`."""
-    import torch
+    """The tensor that takes x's rotated rows: `out`, checked, or a new one of type `like`; its type."""
     if out is None:
+        import torch
         with _made_on(stream):
-            return torch.empty_like(x, dtype=like, memory_format=torch.contiguous_format)
-    _device_array(out, out.dtype, x.shape, name)
-    return out
+            return torch.empty_like(x, dtype=like, memory_format=torch.contiguous_format), like
+    dtype = out.dtype
+    _device_array(out, dtype, x.shape, name)
+    return out, dtype
 
 
 def qk_rotate(q, k, positions, rotation, q_weight=None, k_weight=None, eps: float = 1e-6, q_out=None,
@@ -650,25 +651,28 @@ def qk_rotate(q, k, positions, rotation, q_weight=None, k_weight=None, eps: floa
     `positions` (int32 [tokens]) as a Rotation says. `k` may be None. Returns (q_out, k_out), contiguous, of the
     inputs' type unless given; an output may be its own (contiguous) input."""
     import torch
-    dim = q.shape[-1]
+    shape, dtype, f32 = q.shape, q.dtype, torch.float32
+    dim = shape[-1] if len(shape) == 3 else 0
     q_stride = _rows(q, 0, dim, "q")
-    tokens = q.shape[0]
+    tokens = shape[0]
     _device_array(positions, torch.int32, (tokens,), "positions")
-    q_out = _rotated_out(q, q_out, q.dtype, stream, "q_out")
-    k_stride = k_heads = 0
+    q_out, out_dtype = _rotated_out(q, q_out, dtype, stream, "q_out")
+    k_stride = k_heads = k_at = k_out_at = 0
     if k is not None:
-        k_stride, k_heads = _rows(k, 0, dim, "k"), k.shape[1]
-        if k.dtype != q.dtype or k.shape[0] != tokens:
+        k_stride = _rows(k, 0, dim, "k")
+        k_tokens, k_heads, _ = k.shape
+        if k.dtype != dtype or k_tokens != tokens:
             raise ValueError("q and k must have one type and number of tokens")
-        k_out = _rotated_out(k, k_out, q_out.dtype, stream, "k_out")
-        if k_out.dtype != q_out.dtype:
+        k_out, k_out_dtype = _rotated_out(k, k_out, out_dtype, stream, "k_out")
+        if k_out_dtype != out_dtype:
             raise ValueError("q_out and k_out must have one type")
-    r = _rotation_struct(rotation)
+        k_at, k_out_at = k.data_ptr(), k_out.data_ptr()
+    r = _rotation_struct(rotation, f32)
     _check(lib().logbq_qk_rotate(
-        q.data_ptr(), q_stride, q.shape[1], _weight(q_weight, dim, "q_weight"),
-        None if k is None else k.data_ptr(), k_stride, k_heads, _weight(k_weight, dim, "k_weight"),
-        _dtype_code(q.dtype), tokens, dim, eps, positions.data_ptr(), ctypes.byref(r), q_out.data_ptr(),
-        None if k is None else k_out.data_ptr(), _dtype_code(q_out.dtype), _stream(stream)), "logbq_qk_rotate")
+        q.data_ptr(), q_stride, shape[1], _weight(q_weight, f32, dim, "q_weight"), k_at or None, k_stride, k_heads,
+        _weight(k_weight, f32, dim, "k_weight"), _dtype_code(dtype), tokens, dim, eps, positions.data_ptr(),
+        ctypes.byref(r), q_out.data_ptr(), k_out_at or None, _dtype_code(out_dtype), _stream(stream)),
+        "logbq_qk_rotate")
     return q_out, k_out
 
 
@@ -679,25 +683,27 @@ def kv4_append_rotated(q, k, v, cache, slots, positions, rotation, q_weight=None
     ([tokens][q_heads][dim], float16 unless given; None without queries)."""
     import torch
     c = _kv4_struct(cache)
-    k_stride, v_stride = _rows(k, c.heads, c.dim, "k"), _rows(v, c.heads, c.dim, "v")
+    dim, f32, dtype, out_dtype = c.dim, torch.float32, k.dtype, torch.float16
+    k_stride, v_stride = _rows(k, c.heads, dim, "k"), _rows(v, c.heads, dim, "v")
     tokens = k.shape[0]
-    if v.dtype != k.dtype or v.shape[0] != tokens:
+    if v.dtype != dtype or v.shape[0] != tokens:
         raise ValueError("k and v must have one type and number of tokens")
     _device_array(slots, torch.int64, (tokens,), "slots")
     _device_array(positions, torch.int32, (tokens,), "positions")
-    q_stride = q_heads = q_at = 0
+    q_stride = q_heads = q_at = q_out_at = 0
     if q is not None:
-        q_stride, q_heads, q_at = _rows(q, 0, c.dim, "q"), q.shape[1], q.data_ptr()
-        if q.dtype != k.dtype or q.shape[0] != tokens:
+        q_stride = _rows(q, 0, dim, "q")
+        q_tokens, q_heads, _ = q.shape
+        if q.dtype != dtype or q_tokens != tokens:
             raise ValueError("q and k must have one type and number of tokens")
-        q_out = _rotated_out(q, q_out, torch.float16, stream, "q_out")
-    r = _rotation_struct(rotation)
+        q_out, out_dtype = _rotated_out(q, q_out, out_dtype, stream, "q_out")
+        q_at, q_out_at = q.data_ptr(), q_out.data_ptr()
+    r = _rotation_struct(rotation, f32)
     _check(lib().logbq_kv4_append_rotated(
-        q_at or None, q_stride, q_heads, _weight(q_weight, c.dim, "q_weight"), k.data_ptr(), k_stride,
-        _weight(k_weight, c.dim, "k_weight"), v.data_ptr(), v_stride, _dtype_code(k.dtype), tokens, eps,
-        positions.data_ptr(), ctypes.byref(r), ctypes.byref(c), slots.data_ptr(),
-        None if q is None else q_out.data_ptr(), 1 if q is None else _dtype_code(q_out.dtype), _stream(stream)),
-        "logbq_kv4_append_rotated")
+        q_at or None, q_stride, q_heads, _weight(q_weight, f32, dim, "q_weight"), k.data_ptr(), k_stride,
+        _weight(k_weight, f32, dim, "k_weight"), v.data_ptr(), v_stride, _dtype_code(dtype), tokens, eps,
+        positions.data_ptr(), ctypes.byref(r), ctypes.byref(c), slots.data_ptr(), q_out_at or None,
+        _dtype_code(out_dtype), _stream(stream)), "logbq_kv4_append_rotated")
     return None if q is None else q_out
 
 
