@@ -427,6 +427,11 @@ struct TileReader {
 // A piece of 32 rows or fewer leaves three wavefronts without rows, one of 64 two: then wavefronts share the
 // rows and have a half of each tile's positions, and their sums are added up in LDS at the end.
 constexpr int kTreeMinShare = 6;              // cost of a piece at least: two tiles of few rows
+// At 128 channels workgroups that share a CU slow each other down: up to this cost a piece, one a CU does better (8
+// requests of 32 rows and 1000 positions 23.0 -> 19.5 us, 4 of 120 rows 28.1 -> 23.7; beyond it 7 of 36 rows and 1100 to
+// 3500 positions take 25.9, and would 28.8, and 4 of 32 rows and 6000 positions 28.7 and 30.3). At 64 channels it gains
+// nothing.
+constexpr int kTreeAlone = 23;
 
 // Sums over a wavefront's lanes up to each one, by shifts within 16 and broadcasts of the rows' last lanes.
 __device__ __forceinline__ int lanes_upto(int x) {
@@ -483,10 +488,17 @@ void k_kv4_tree(AttnArgs a) {
     cost += counts[0][w];
     items += counts[1][w];
   }
-  // The share with which about a.parts workgroups have pieces, those that their items' ends leave short among them.
-  int room = a.parts - items / 2;
-  room = room < a.parts / 2 ? a.parts / 2 : room;
-  int share = (unsigned)(cost + room - 1) / (unsigned)room;
+  // The share with which about so many workgroups have pieces, those that their items' ends leave short among them.
+  const auto share_of_parts = [&](int parts) {
+    int room = parts - items / 2;
+    room = room < parts / 2 ? parts / 2 : room;
+    return (int)((unsigned)(cost + room - 1) / (unsigned)room);
+  };
+  int share = share_of_parts(a.parts);
+  if (D == 128) {
+    const int alone = share_of_parts(a.parts / 2);
+    share = alone <= kTreeAlone ? alone : share;
+  }
   share = uniform(share < kTreeMinShare ? kTreeMinShare : share);
   const auto pieces_of = [&](int n) { return n > share ? (unsigned)(n + share - 1) / (unsigned)share : 1; };    // of an item
 
