@@ -27,6 +27,7 @@ constexpr int kAdCount = 4;                    // projections of a call
 constexpr int kAdRank = LOGBQ_ADAPTERS_MAX_RANK;
 constexpr int kAdColumns = 256;                // out features of a workgroup of the second kernel
 constexpr int kTileRows = 32768;               // tiles along y of the second kernel's grid
+constexpr double kStreamedPool = 128 << 20;    // bytes of B
 constexpr int kAdSplits = 16;
 constexpr int64_t kAdSplitTokens = 32768;      // tokens times splits, where K is split
 
@@ -149,7 +150,7 @@ __device__ __forceinline__ float rest_of(float x, __bf16 h) { return (float)h ==
 // ------------------------------------------------------------------ a few tokens
 // Both products stream the adapter's weights once: bound by HBM where many adapters are in use, by latency
 // otherwise. A wavefront's loads are 1 KiB of consecutive weights of a row of A (8 a lane), or of rows of B. 64 tokens
-// of 40 adapters with ranks up to 64, K = 4096 and two times 14336 out features, weights from HBM: 11 us and 33 us,
+// of 40 adapters with ranks up to 64, K = 4096 and two times 14336 out features, weights from HBM: 10 us and 27 us,
 // where B's rows of 128 bytes come whole whatever the rank.
 constexpr int kFewRows = 4;                    // ranks of a workgroup of the first kernel
 
@@ -241,7 +242,7 @@ __global__ __launch_bounds__(kAdThreads) void k_adapter_shrink_few(AdapterArgs a
 
 // L lanes have a row of B, 8 ranks each; a wavefront has 64 rows, of which lane i in the end has the sum of row i, so
 // that the outputs are consecutive. Loads of 128 or 256 rows with as many registers took as long or longer.
-template <bool BF16, int T, int L>
+template <bool BF16, int T, int L, bool STREAMED>
 __device__ __forceinline__ void expand_few(const AdapterArgs& a, const TokenTile& tile, int projection, int n0) {
   const int lane = threadIdx.x & 63, sub = lane & (L - 1), group = lane / L;
   const int width = a.n[projection], r = 8 * sub;
@@ -254,7 +255,9 @@ __device__ __forceinline__ void expand_few(const AdapterArgs& a, const TokenTile
 #pragma unroll
   for (int i = 0; i < L; ++i) {
     const int row = n0 + group * L + i;
-    w[i] = *reinterpret_cast<const u32x4*>(from + (int64_t)(row < width ? row : width - 1) * a.rank);
+    const u32x4* at = reinterpret_cast<const u32x4*>(from + (int64_t)(row < width ? row : width - 1) * a.rank);
+    if constexpr (STREAMED) w[i] = __builtin_nontemporal_load(at);
+    else w[i] = *at;
   }
 #pragma unroll
   for (int t = 0; t < T; ++t)
@@ -293,7 +296,7 @@ __device__ __forceinline__ void expand_few(const AdapterArgs& a, const TokenTile
     if (t < tile.n && n < width) a.out[projection][(int64_t)(tile.t0 + t) * width + n] = y[t] + sum[t];
 }
 
-template <bool BF16, int T>
+template <bool BF16, int T, bool STREAMED>
 __global__ __launch_bounds__(kAdThreads) void k_adapter_expand_few(AdapterArgs a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const TokenTile tile = tile_at<T>(a, blockIdx.x, 0);
@@ -303,11 +306,11 @@ __global__ __launch_bounds__(kAdThreads) void k_adapter_expand_few(AdapterArgs a
   const int n0 = ((int)blockIdx.y - a.block0[projection]) * kAdColumns + wave * 64;
   const int width = a.n[projection];
   if (n0 >= width) return;
-  if (tile.rank > 64) return expand_few<BF16, T, 16>(a, tile, projection, n0);
-  if (tile.rank > 32) return expand_few<BF16, T, 8>(a, tile, projection, n0);
-  if (tile.rank > 16) return expand_few<BF16, T, 4>(a, tile, projection, n0);
-  if (tile.rank > 8) return expand_few<BF16, T, 2>(a, tile, projection, n0);
-  if (tile.rank > 0) return expand_few<BF16, T, 1>(a, tile, projection, n0);
+  if (tile.rank > 64) return expand_few<BF16, T, 16, STREAMED>(a, tile, projection, n0);
+  if (tile.rank > 32) return expand_few<BF16, T, 8, STREAMED>(a, tile, projection, n0);
+  if (tile.rank > 16) return expand_few<BF16, T, 4, STREAMED>(a, tile, projection, n0);
+  if (tile.rank > 8) return expand_few<BF16, T, 2, STREAMED>(a, tile, projection, n0);
+  if (tile.rank > 0) return expand_few<BF16, T, 1, STREAMED>(a, tile, projection, n0);
   if (a.y[projection] == a.out[projection]) return;
   for (int t = 0; t < tile.n; ++t) {
     const int64_t at = (int64_t)(tile.t0 + t) * width + n0 + lane;
@@ -713,12 +716,21 @@ int32_t logbq_linear_adapters(const uint16_t* x_dev, int64_t tokens, int64_t k, 
   a.max_new = max_new < INT32_MAX ? (int32_t)max_new : INT32_MAX;
   const bool bf16 = dtype == LOGBQ_DTYPE_BF16;
   if (max_new <= kFewTokens) {
-    const dim3 shrink((unsigned)requests, (unsigned)(count * (rank / kFewRows))), expand((unsigned)requests, (unsigned)blocks);
-#define FEW(BF16, T)                                                                                          \
-  if (bf16 == BF16 && (max_new > 1) == (T > 1)) {                                                             \
-    hipLaunchKernelGGL((k_adapter_shrink_few<BF16, T>), shrink, dim3(kAdThreads), 0, (hipStream_t)stream, a); \
-    if (launch_status() != LOGBQ_OK) return LOGBQ_ERR_HIP;                                                    \
-    hipLaunchKernelGGL((k_adapter_expand_few<BF16, T>), expand, dim3(kAdThreads), 0, (hipStream_t)stream, a); \
+    const dim3 shrink((unsigned)requests, (unsigned)(count * (rank / kFewRows)));
+    const dim3 expand((unsigned)requests, (unsigned)a.block0[count]);
+    // Rows of B go past the cache where the pool does not stay in it and few requests share an adapter: 64 requests of 40
+    // adapters (147 MB) 43 -> 38 us. Where all share one, they would take 31 instead of 24.
+    double pool = 0.0;
+    for (int i = 0; i < count; ++i) pool += 2.0 * adapters * rank * a.n[i];
+    const bool streamed = pool >= kStreamedPool && requests <= 2 * adapters;
+#define FEW(BF16, T)                                                                                           \
+  if (bf16 == BF16 && (max_new > 1) == (T > 1)) {                                                              \
+    hipLaunchKernelGGL((k_adapter_shrink_few<BF16, T>), shrink, dim3(kAdThreads), 0, (hipStream_t)stream, a);  \
+    if (launch_status() != LOGBQ_OK) return LOGBQ_ERR_HIP;                                                     \
+    if (streamed)                                                                                              \
+      hipLaunchKernelGGL((k_adapter_expand_few<BF16, T, true>), expand, dim3(kAdThreads), 0, (hipStream_t)stream, a);  \
+    else                                                                                                       \
+      hipLaunchKernelGGL((k_adapter_expand_few<BF16, T, false>), expand, dim3(kAdThreads), 0, (hipStream_t)stream, a); \
   }
     FEW(false, 1) FEW(true, 1) FEW(false, kFewTokens) FEW(true, kFewTokens)
 #undef FEW

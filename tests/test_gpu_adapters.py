@@ -230,3 +230,17 @@ def test_starts_that_do_not_ascend_stay_within_the_buffers(most, rank):
     outs = [torch.full((tokens + 8, n), 7.0, device=DEV) for _ in range(2)]
     call(d, [0, 1] * (requests // 2), most, outs=[o[:tokens] for o in outs], workspace=held[:need])
     assert bool((held[need:] == 0x5a).all()) and all(bool((o[tokens:] == 7.0).all()) for o in outs)
+
+
+@pytest.mark.parametrize("new", [1, 3])
+def test_a_pool_that_goes_past_the_cache(new):
+    """More weights than 128 MiB, two and four requests an adapter."""
+    for requests in (36, 72):
+        d = make(new, [new] * requests, 64, [33000], 18, 128, "bf16")
+        ids = [r % 19 - 1 for r in range(requests)]
+        outs = [torch.empty_like(y) for y in d["ys"]]
+        rows = slice(0, 8 * new)
+        call(d, ids, new, outs=outs)
+        part = {k: ([v[0][rows]] if k == "ys" else v[rows] if k == "x" else v) for k, v in d.items()}
+        part["starts"] = d["starts"][:9]
+        check(part, part["ys"], [outs[0][rows]], ids[:8])
