@@ -2,7 +2,8 @@
 // y[t] + scale (x[t] A^T) B^T with the adapter of the request that token t belongs to.
 //
 //   k_adapter_shrink_few, k_adapter_expand_few   requests of up to four tokens: h = x A^T by rows of A, and
-//                      out = y + scale h B^T by rows of B, which stream past a few activations in registers.
+//                      out = y + scale h B^T by rows of B, which stream past a few activations in registers; small
+//                      calls by the second alone.
 //   k_adapter_shrink, k_adapter_expand           more tokens: the same with MFMAs, K split over wavefronts and
 //                      workgroups.
 
@@ -27,6 +28,7 @@ constexpr int kAdCount = 4;                    // projections of a call
 constexpr int kAdRank = LOGBQ_ADAPTERS_MAX_RANK;
 constexpr int kAdColumns = 256;                // out features of a workgroup of the second kernel
 constexpr int kTileRows = 32768;               // tiles along y of the second kernel's grid
+constexpr int64_t kAloneBlocks = 256, kAloneRank = 65536;
 constexpr double kStreamedPool = 128 << 20;    // bytes of B
 constexpr int kAdSplits = 16;
 constexpr int64_t kAdSplitTokens = 32768;      // tokens times splits, where K is split
@@ -242,7 +244,51 @@ __global__ __launch_bounds__(kAdThreads) void k_adapter_shrink_few(AdapterArgs a
 
 // L lanes have a row of B, 8 ranks each; a wavefront has 64 rows, of which lane i in the end has the sum of row i, so
 // that the outputs are consecutive. Loads of 128 or 256 rows with as many registers took as long or longer.
-template <bool BF16, int T, int L, bool STREAMED>
+// FUSED: h is the workgroup's own, four ranks a wavefront at a time, while rows of B are on their way.
+template <bool BF16, int T>
+__device__ __forceinline__ void shrink_alone(const AdapterArgs& a, const TokenTile& tile, int projection,
+                                             float (&h)[T][kAdRank]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int row0 = wave * kFewRows; row0 < tile.rank; row0 += kAdWaves * kFewRows) {
+    const uint16_t* from = a.a[projection] + ((int64_t)tile.adapter * a.rank + row0) * a.k;
+    float acc[T][kFewRows];
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+#pragma unroll
+      for (int i = 0; i < kFewRows; ++i) acc[t][i] = 0.0f;
+#pragma unroll 4
+    for (int64_t k = lane * 8; k < a.k; k += 512) {
+      u32x4 w[kFewRows], x[T];
+#pragma unroll
+      for (int i = 0; i < kFewRows; ++i) w[i] = *reinterpret_cast<const u32x4*>(from + i * a.k + k);
+#pragma unroll
+      for (int t = 0; t < T; ++t)
+        x[t] = *reinterpret_cast<const u32x4*>(a.x + (int64_t)(tile.t0 + (t < tile.n ? t : 0)) * a.k + k);
+      float xf[T][8];
+#pragma unroll
+      for (int t = 0; t < T; ++t) eight_values<false>(x[t], xf[t]);
+#pragma unroll
+      for (int i = 0; i < kFewRows; ++i) {
+        float wf[8];
+        eight_values<BF16>(w[i], wf);
+#pragma unroll
+        for (int t = 0; t < T; ++t)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) acc[t][i] = __builtin_fmaf(xf[t][j], wf[j], acc[t][i]);
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+#pragma unroll
+      for (int i = 0; i < kFewRows; ++i) {
+        const float v = lanes_sum<64>(acc[t][i]);
+        if (lane == 0) h[t][row0 + i] = v;
+      }
+  }
+  __syncthreads();
+}
+
+template <bool BF16, int T, int L, bool STREAMED, bool FUSED>
 __device__ __forceinline__ void expand_few(const AdapterArgs& a, const TokenTile& tile, int projection, int n0) {
   const int lane = threadIdx.x & 63, sub = lane & (L - 1), group = lane / L;
   const int width = a.n[projection], r = 8 * sub;
@@ -263,6 +309,8 @@ __device__ __forceinline__ void expand_few(const AdapterArgs& a, const TokenTile
   for (int t = 0; t < T; ++t)
     y[t] = a.y[projection][(int64_t)(tile.t0 + (t < tile.n ? t : 0)) * width + (n < width ? n : width - 1)];
   const float scale = a.scales ? a.scales[tile.adapter] : 1.0f;
+  __shared__ float own[FUSED ? T : 1][kAdRank];
+  if constexpr (FUSED) shrink_alone<BF16>(a, tile, projection, own);
   float h[T][8], sum[T];
 #pragma unroll
   for (int t = 0; t < T; ++t) {
@@ -270,7 +318,12 @@ __device__ __forceinline__ void expand_few(const AdapterArgs& a, const TokenTile
 #pragma unroll
     for (int j = 0; j < 8; ++j) h[t][j] = 0.0f;
     if (t < tile.n && has) {
-      load_row<LOGBQ_DTYPE_F32>(a.h, (((int64_t)tile.t0 + t) * a.count + projection) * a.rank + r, h[t]);
+      if constexpr (FUSED) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) h[t][j] = own[t][r + j];
+      } else {
+        load_row<LOGBQ_DTYPE_F32>(a.h, (((int64_t)tile.t0 + t) * a.count + projection) * a.rank + r, h[t]);
+      }
 #pragma unroll
       for (int j = 0; j < 8; ++j) h[t][j] = r + j < tile.rank ? h[t][j] * scale : 0.0f;
     }
@@ -296,7 +349,7 @@ __device__ __forceinline__ void expand_few(const AdapterArgs& a, const TokenTile
     if (t < tile.n && n < width) a.out[projection][(int64_t)(tile.t0 + t) * width + n] = y[t] + sum[t];
 }
 
-template <bool BF16, int T, bool STREAMED>
+template <bool BF16, int T, bool STREAMED, bool FUSED>
 __global__ __launch_bounds__(kAdThreads) void k_adapter_expand_few(AdapterArgs a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const TokenTile tile = tile_at<T>(a, blockIdx.x, 0);
@@ -305,12 +358,12 @@ __global__ __launch_bounds__(kAdThreads) void k_adapter_expand_few(AdapterArgs a
   while (projection + 1 < a.count && (int)blockIdx.y >= a.block0[projection + 1]) ++projection;
   const int n0 = ((int)blockIdx.y - a.block0[projection]) * kAdColumns + wave * 64;
   const int width = a.n[projection];
-  if (n0 >= width) return;
-  if (tile.rank > 64) return expand_few<BF16, T, 16, STREAMED>(a, tile, projection, n0);
-  if (tile.rank > 32) return expand_few<BF16, T, 8, STREAMED>(a, tile, projection, n0);
-  if (tile.rank > 16) return expand_few<BF16, T, 4, STREAMED>(a, tile, projection, n0);
-  if (tile.rank > 8) return expand_few<BF16, T, 2, STREAMED>(a, tile, projection, n0);
-  if (tile.rank > 0) return expand_few<BF16, T, 1, STREAMED>(a, tile, projection, n0);
+  if (!FUSED && n0 >= width) return;             // a fused one has its part of h to sum, and then nothing to store
+  if (tile.rank > 64) return expand_few<BF16, T, 16, STREAMED, FUSED>(a, tile, projection, n0);
+  if (tile.rank > 32) return expand_few<BF16, T, 8, STREAMED, FUSED>(a, tile, projection, n0);
+  if (tile.rank > 16) return expand_few<BF16, T, 4, STREAMED, FUSED>(a, tile, projection, n0);
+  if (tile.rank > 8) return expand_few<BF16, T, 2, STREAMED, FUSED>(a, tile, projection, n0);
+  if (tile.rank > 0) return expand_few<BF16, T, 1, STREAMED, FUSED>(a, tile, projection, n0);
   if (a.y[projection] == a.out[projection]) return;
   for (int t = 0; t < tile.n; ++t) {
     const int64_t at = (int64_t)(tile.t0 + t) * width + n0 + lane;
@@ -723,16 +776,25 @@ int32_t logbq_linear_adapters(const uint16_t* x_dev, int64_t tokens, int64_t k, 
     double pool = 0.0;
     for (int i = 0; i < count; ++i) pool += 2.0 * adapters * rank * a.n[i];
     const bool streamed = pool >= kStreamedPool && requests <= 2 * adapters;
+    // A small call is one launch: each workgroup sums its projection's h for itself, while a CU has no more than one and
+    // A is small. One request, 16 ranks of K = 4096, 6144 features: 5.4 -> 4.1 us in a graph, 16.3 -> 13.2 called one by
+    // one; 32 ranks, or 2 requests of 4 tokens and 16, would take 6.4 for 5.7 us, 8.8 for 8.1 in a graph.
+    const bool fused = requests * a.block0[count] <= kAloneBlocks &&
+                       (int64_t)rank * k * (max_new > 1 ? 2 : 1) <= kAloneRank && !streamed;
+#define EXPAND(BF16, T, STREAMED, FUSED)                                                                       \
+  if (streamed == STREAMED && fused == FUSED)                                                                  \
+    hipLaunchKernelGGL((k_adapter_expand_few<BF16, T, STREAMED, FUSED>), expand, dim3(kAdThreads), 0, (hipStream_t)stream, a)
 #define FEW(BF16, T)                                                                                           \
   if (bf16 == BF16 && (max_new > 1) == (T > 1)) {                                                              \
-    hipLaunchKernelGGL((k_adapter_shrink_few<BF16, T>), shrink, dim3(kAdThreads), 0, (hipStream_t)stream, a);  \
+    if (!fused)                                                                                                \
+      hipLaunchKernelGGL((k_adapter_shrink_few<BF16, T>), shrink, dim3(kAdThreads), 0, (hipStream_t)stream, a);  \
     if (launch_status() != LOGBQ_OK) return LOGBQ_ERR_HIP;                                                     \
-    if (streamed)                                                                                              \
-      hipLaunchKernelGGL((k_adapter_expand_few<BF16, T, true>), expand, dim3(kAdThreads), 0, (hipStream_t)stream, a);  \
-    else                                                                                                       \
-      hipLaunchKernelGGL((k_adapter_expand_few<BF16, T, false>), expand, dim3(kAdThreads), 0, (hipStream_t)stream, a); \
+    EXPAND(BF16, T, true, false);                                                                              \
+    EXPAND(BF16, T, false, false);                                                                             \
+    EXPAND(BF16, T, false, true);                                                                              \
   }
     FEW(false, 1) FEW(true, 1) FEW(false, kFewTokens) FEW(true, kFewTokens)
+#undef EXPAND
 #undef FEW
     return launch_status();
   }

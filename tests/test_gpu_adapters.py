@@ -244,3 +244,28 @@ def test_a_pool_that_goes_past_the_cache(new):
         part = {k: ([v[0][rows]] if k == "ys" else v[rows] if k == "x" else v) for k, v in d.items()}
         part["starts"] = d["starts"][:9]
         check(part, part["ys"], [outs[0][rows]], ids[:8])
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("new,k,n,rank", [
+    (1, 4096, [4096, 1024, 1024], 16), (1, 512, [257, 1, 300, 64], 128), (1, 32, [1], 8), (4, 2048, [700, 33], 16),
+    (3, 96, [255], 128), (1, 4128, [640], 8)])
+def test_small_calls(new, k, n, rank, dtype):
+    """Calls of one launch, in place and out of it, and beside others that take two."""
+    d = make(k + rank, [new, 0, 1, new, 1], k, n, 3, rank, dtype)
+    ids, ranks, scales = [2, 1, 0, -1, 1], [rank, max(1, rank - 3), 0], [0.5, -1.5, 2.0]
+    for a, b in zip(d["a"], d["b"]):
+        for i, r in enumerate(ranks):
+            a[i, r:] = float("nan")
+            b[i, :, r:] = float("nan")
+    outs = [torch.empty_like(y) for y in d["ys"]]
+    check(d, d["ys"], call(d, ids, new, scales, ranks, outs=outs), ids, scales, ranks)
+    before = [y.clone() for y in d["ys"]]
+    call(d, ids, new, scales, ranks)
+    assert all(torch.equal(a, b) for a, b in zip(d["ys"], outs))
+    many = {key: [torch.cat([y] * 90) for y in before] if key == "ys" else v for key, v in d.items()}
+    many["x"] = torch.cat([d["x"]] * 90)
+    starts, total = host(d["starts"]), d["x"].shape[0]
+    many["starts"] = ints(np.concatenate([starts[:-1] + i * total for i in range(90)] + [[90 * total]]))
+    big = [torch.empty_like(y) for y in many["ys"]]
+    check(many, many["ys"], call(many, ids * 90, new, scales, ranks, outs=big), ids * 90, scales, ranks)
