@@ -622,8 +622,8 @@ int32_t logbq_kv4_attention(const void* q_dev, int64_t q_stride, int32_t q_dtype
  *               its request. Bits past the request's tokens (max_new of them at most) count for nothing. Any masks
  *               do, a tree's or not.
  *   max_new   : upper bound of a request's tokens (host), at most 64.
- *   window    : 0, or 64 at least: a token of depth d = (bits of its mask) - 1 sees the cached positions past
- *               cached + d - window, and all the new tokens of its mask.
+ *   window    : 0, or 64 at least: a token of depth d = (bits of its mask) - 1 (-1 for a mask without any) sees the
+ *               cached positions past cached + d - window, and all the new tokens of its mask.
  *   The others, what is written and what a row without anything to see gets: as logbq_kv4_attention, but
  *               requests * heads * ceil(max_new * (q_heads / heads) / 128) * (width * page / 64 + 1) < 2^28.
  * A new token of a request sees all of its cached tokens (seq_len less its new tokens) that the window holds, and new

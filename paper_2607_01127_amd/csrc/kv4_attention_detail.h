@@ -27,6 +27,7 @@ struct AttnArgs {
   int64_t q_stride;
   int32_t width, tokens, requests, group, window, max_new, q_dtype, out_dtype, parts;
   int32_t unit;           // positions that the workgroups' shares are counted in
+  int32_t reach;          // of a window: positions before a request's first token that some token of it may see
   float scale;
   const uint64_t* masks;  // of trees: the nodes that a token sees
 };
@@ -81,7 +82,7 @@ __device__ __forceinline__ Request request_of(const AttnArgs& a, int r) {
   q.n = t1 - t0 < a.max_new ? t1 - t0 : a.max_new;
   q.first = len - (t1 - t0);
   q.end = q.first + q.n < span ? q.first + q.n : (int32_t)span;
-  int64_t from = a.window ? (int64_t)q.first - a.window + 1 : 0;
+  int64_t from = a.window ? (int64_t)q.first - a.reach : 0;
   q.from = from > 0 ? (int32_t)from & ~31 : 0;
   return q;
 }
@@ -167,6 +168,7 @@ inline int32_t attention_args(const void* q_dev, int64_t q_stride, int32_t q_dty
   to->requests = (int32_t)requests;
   to->group = q_heads / c.heads;
   to->window = window;
+  to->reach = window - 1;
   to->max_new = max_new < INT32_MAX ? (int32_t)max_new : INT32_MAX;
   to->q_dtype = q_dtype;
   to->out_dtype = out_dtype;

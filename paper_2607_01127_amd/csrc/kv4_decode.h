@@ -354,7 +354,7 @@ void k_kv4_decode(AttnArgs a) {
       last[nt] = row < rows ? req.first + token : INT32_MAX;
       if constexpr (TREE) {
         mask[nt] = row < rows ? nodes_seen(a, req, req.t0 + token) : 0;
-        const int depth = mask[nt] ? __popcll(mask[nt]) - 1 : 0;
+        const int depth = __popcll(mask[nt]) - 1;            // -1 without a bit
         const int64_t from = (int64_t)req.first + depth - a.window + 1;
         last[nt] = a.window && row < rows && from > 0 ? (int32_t)from : 0;
       }

@@ -602,7 +602,7 @@ void k_kv4_tree(AttnArgs a) {
       const int to_nodes = req.first - base;           // of the tile's positions, those before the nodes
       const uint64_t mask = row_mask[row_of().row];
       // The first position that the row's window holds; nodes lie at req.first and after.
-      const int depth = mask ? __popcll(mask) - 1 : 0;
+      const int depth = __popcll(mask) - 1;            // -1 without a bit
       const int64_t window_from = a.window ? (int64_t)req.first + depth - a.window + 1 : 0;
       const uint64_t cached = to_nodes >= 64 ? ~0ull : to_nodes > 0 ? (1ull << to_nodes) - 1 : 0;
       const int64_t skip = window_from - base;
@@ -818,6 +818,7 @@ int32_t logbq_kv4_tree_attention(const void* q_dev, int64_t q_stride, int32_t q_
   if (!masks_dev) return LOGBQ_ERR_INVALID_ARG;
   if ((uintptr_t)masks_dev % 8) return LOGBQ_ERR_UNSUPPORTED;
   a.masks = masks_dev;
+  a.reach = window;           // of a token without a bit, whose depth is -1
   return cache->dim == 64    ? launch_tree<64>(a, work_dev, (hipStream_t)stream)
          : cache->dim == 128 ? launch_tree<128>(a, work_dev, (hipStream_t)stream)
                              : launch_tree<256>(a, work_dev, (hipStream_t)stream);
