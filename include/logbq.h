@@ -671,7 +671,8 @@ int64_t logbq_linear_adapters_workspace(int64_t tokens, int32_t count, int32_t r
  * Rows of requests without an adapter are copied (in place: left alone); rows that belong to no request are left as
  * they were. Sums are float32; x A^T goes into the second product as two float16 numbers about its largest (22
  * bits) or as three bfloat16 ones.
- * Results do not change from call to call. Enqueues one or two kernels.
+ * An infinity in x or y reaches the outputs as in the formula; weights are finite (an infinite one may give NaN in
+ * its place). Results do not change from call to call. Enqueues one or two kernels.
  * Errors: INVALID_ARG (null pointer, negative size, count, overlap), UNSUPPORTED (dtype, k % 32, rank, alignment,
  * sizes, a workspace that is too small), HIP.
  */

@@ -146,8 +146,9 @@ __device__ __forceinline__ float16v product(u32x4 a, u32x4 b, float16v c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8v, a), __builtin_bit_cast(half8v, b), c, 0, 0, 0);
 }
 
-// What rounding x to bfloat16 leaves, 0 where it leaves nothing (an infinity less itself would be NaN).
-__device__ __forceinline__ float rest_of(float x, __bf16 h) { return (float)h == x ? 0.0f : x - (float)h; }
+// What rounding x to 16 bits leaves, 0 where it leaves nothing (an infinity less itself would be NaN).
+template <class Half>
+__device__ __forceinline__ float rest_of(float x, Half h) { return (float)h == x ? 0.0f : x - (float)h; }
 
 // ------------------------------------------------------------------ a few tokens
 // Both products stream the adapter's weights once: bound by HBM where many adapters are in use, by latency
@@ -587,13 +588,15 @@ __global__ __launch_bounds__(kAdThreads) void k_adapter_expand(AdapterArgs a) {
     for (int o = 0; o < kOwn; ++o)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        h[o][j] = 8 * (piece + 8 * o) < tile.rank && token < tile.n ? h[o][j] * scale : 0.0f;
-        most = fmaxf(most, __builtin_fabsf(h[o][j]));
+        // Past the adapter's rank stands what an infinite activation and a 0 gave; infinities do not choose the factor.
+        h[o][j] = 8 * (piece + 8 * o) + j < tile.rank && token < tile.n ? h[o][j] * scale : 0.0f;
+        const float size = __builtin_fabsf(h[o][j]);
+        most = fmaxf(most, size < INFINITY ? size : 0.0f);
       }
     int e = 0;
     if constexpr (!BF16) {
       for (int d = 1; d < 8; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
-      e = most > 0.0f && most < INFINITY ? (int)(__float_as_uint(most) >> 23) - 127 : 0;
+      e = most > 0.0f ? (int)(__float_as_uint(most) >> 23) - 127 : 0;
       if (piece == 0) factors[token] = ldexpf(1.0f, e);
     }
 #pragma unroll
@@ -617,7 +620,7 @@ __global__ __launch_bounds__(kAdThreads) void k_adapter_expand(AdapterArgs a) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             h8[j] = (half_t)left[j];
-            left[j] -= (float)h8[j];
+            left[j] = rest_of(left[j], h8[j]);
           }
           v = __builtin_bit_cast(u32x4, h8);
         }
