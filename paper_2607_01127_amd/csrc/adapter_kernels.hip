@@ -774,14 +774,20 @@ int32_t logbq_linear_adapters(const uint16_t* x_dev, int64_t tokens, int64_t k, 
   if (max_new <= kFewTokens) {
     const dim3 shrink((unsigned)requests, (unsigned)(count * (rank / kFewRows)));
     const dim3 expand((unsigned)requests, (unsigned)a.block0[count]);
-    // Rows of B go past the cache where the pool does not stay in it and few requests share an adapter: 64 requests of 40
-    // adapters (147 MB) 43 -> 38 us. Where all share one, they would take 31 instead of 24.
+    // Rows of B go past the cache where the pool does not stay in it and few requests share an adapter. 64 requests with
+    // adapters of their own or two of one, weights from memory: pools of 117, 147, 235 and 470 MB 38.3 -> 34.8, 42.9 -> 39.9,
+    // 63 -> 57 and 62 -> 56 us (59 MB, 32 requests: 22.3 -> 20.1). A pool that is the only one and stays in the cache would
+    // lose: 117 and 147 MB 33 -> 41 and 38 -> 43, while 235 MB take 65 -> 59; and so would 64 requests of 20 adapters, 34.6
+    // -> 39.8. The host knows neither which adapters a call names nor what else the program reads, so the line is where a
+    // pool takes half of the cache.
     double pool = 0.0;
     for (int i = 0; i < count; ++i) pool += 2.0 * adapters * rank * a.n[i];
     const bool streamed = pool >= kStreamedPool && requests <= 2 * adapters;
     // A small call is one launch: each workgroup sums its projection's h for itself, while a CU has no more than one and
     // A is small. One request, 16 ranks of K = 4096, 6144 features: 5.4 -> 4.1 us in a graph, 16.3 -> 13.2 called one by
     // one; 32 ranks, or 2 requests of 4 tokens and 16, would take 6.4 for 5.7 us, 8.8 for 8.1 in a graph.
+    // Not with a large pool, whose weights come from memory: there the one launch takes 7.1 us in a graph and two take 5.5
+    // (one by one 12.4 and 14.8); for 128 ranks of K = 512 and 28672 features 11.8 and 7.5.
     const bool fused = requests * a.block0[count] <= kAloneBlocks &&
                        (int64_t)rank * k * (max_new > 1 ? 2 : 1) <= kAloneRank && !streamed;
 #define EXPAND(BF16, T, STREAMED, FUSED)                                                                       \
