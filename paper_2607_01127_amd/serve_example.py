@@ -176,36 +176,52 @@ class Batch:
             d.used -= len(left)
         self.lengths = lengths
 
+    def _within_room(self, trees):
+        """Of each tree the first nodes, which are a tree too: those that the block table has room for, and where
+        the decoder has too few free pages for all of them, those that need none (the roots aside)."""
+        d, page = self.decoder, self.decoder.page
+        most = self.table.shape[1] * page
+        left = [max(1, most - n) for n in self.lengths]
+        trees = [(t[:m], p[:m]) for m, (t, p) in zip(left, trees)]
+        pages = sum(-(-(n + len(t)) // page) - -(-n // page) for n, (t, _) in zip(self.lengths, trees))
+        if d.used + pages > d.free.numel():
+            own = [max(1, -n % page) for n in self.lengths]
+            trees = [(t[:m], p[:m]) for m, (t, p) in zip(own, trees)]
+        return trees
+
     def speculate(self, prompts, steps: int, draft):
         """Greedy continuation with drafts: draft(text) gives (tokens, parents) of a tree whose root,
         node 0, is the text's last token; of the drafted tokens below it the longest path that greedy
-        decoding would have taken stays. Returns the chosen tokens (`steps` of each request, a list of
-        lists) and the number of steps that it took."""
+        decoding would have taken stays. Drafts are cut to the room that there is, so whatever generate
+        has room for works, and a request that has its tokens takes no further part. Returns the chosen
+        tokens (`steps` of each request, a list of lists) and the number of steps that it took."""
         if steps < 1 or not all(prompts):
             raise ValueError("speculate needs a step and a token of each prompt")
         logits = self.step(prompts)
         ends = torch.tensor([len(p) for p in prompts]).cumsum(0) - 1
         chosen, taken = [[t] for t in logits[ends.to(self.decoder.device)].argmax(1).tolist()], 1
         while min(len(c) for c in chosen) < steps:
-            trees = [draft(p + c) if len(c) < steps else ([c[-1]], [-1]) for p, c in zip(prompts, chosen)]
+            trees = [draft(p + c) if len(c) < steps else ([], []) for p, c in zip(prompts, chosen)]
+            if any(len(c) < steps and not t for c, (t, _) in zip(chosen, trees)):
+                raise ValueError("a draft has its root at least")
+            trees = self._within_room(trees)
             best = self.step([t for t, _ in trees], [p for _, p in trees]).argmax(1).tolist()
             taken += 1
             paths, at = [], 0
             for c, (tokens, parents) in zip(chosen, trees):
-                path, answer = [0], best[at]
-                while True:
+                path = [0] if tokens else []
+                while path:
+                    answer = best[at + path[-1]]
+                    c.append(answer)
                     below = [i for i in range(path[-1] + 1, len(tokens))
                              if parents[i] == path[-1] and tokens[i] == answer]
-                    if not below:
+                    if not below or len(c) == steps:
                         break
-                    c.append(answer)
                     path.append(below[0])
-                    answer = best[at + below[0]]
-                c.append(answer)
                 paths.append(path)
                 at += len(tokens)
             self.keep(paths)
-        return [c[:steps] for c in chosen], taken
+        return chosen, taken
 
     def generate(self, prompts, steps: int, top: int = 5):
         """Greedy continuation: the chosen tokens [requests][steps] (a list of lists), their log
