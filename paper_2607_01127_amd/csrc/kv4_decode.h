@@ -678,7 +678,9 @@ int32_t launch_decode(AttnArgs a, void* work, hipStream_t stream) {
 // Requests of up to 16 query rows.
 // Tiles of four blocks have twice the codes in flight of tiles of two, but take longer to start: for shares of
 // 20 units or more, and for long requests (D = 128: 128 requests of 3000 to 9000 163 us against 172, one of
-// 131071 37.2 against 38.5, 32 of 300 to 4100 33.6 against 31.5).
+// 131071 37.2 against 38.5, 32 of 300 to 4100 33.6 against 31.5). Trees' forms of it spill 2 to 4 vector registers at 128
+// channels and 1 to 5 at 256: one node by 4 heads over 131071 positions of 128 channels takes 45 us, and would 43 with
+// two blocks, over 100000 of 256 channels 79 and 74; of 64 channels 27 and 30; 128 requests of 3000 to 9000 170 and 175.
 template <int D, bool TREE = false>
 int32_t launch_few_rows(const AttnArgs& a, int64_t rows, void* work, hipStream_t stream) {
   const int64_t span = (int64_t)a.width << a.c.page_shift;

@@ -22,9 +22,10 @@ namespace {
 // any two implementations agree on them. It costs registers, not time: float64 products issue at the rate of
 // float32 ones, and vector instructions take 40 % of the slots.
 //
-// Bound by memory, small calls by latency. Measured: 8191 tokens of 32 query and 8 key/value heads of 128 channels, float32
-// in, float16 queries and codes out (277 MB), 53 us, 5.2 TB/s; 6001 tokens of 32 and 8 heads of 64, bfloat16 (61 MB),
-// 14.5 us; 48 tokens 4.1 us.
+// Bound by memory, small calls by latency. Measured, inputs from memory: 8191 tokens of 32 query and 8 key/value heads of
+// 128 channels, float32 in, float16 queries and codes out (277 MB), 65 us, 4.3 TB/s (56 us with inputs in the cache); 6001
+// tokens of 32 and 8 heads of 64, bfloat16 (61 MB), 15.8 us, 3.9 TB/s; 48 tokens 4.7 us in a graph. With 16-bit inputs and a
+// norm, or 256 channels, the 64-bit arithmetic bounds it: 6001 tokens of 256 channels (246 MB) take 110 us.
 constexpr int kRotThreads = 256;
 constexpr int kRotWaves = kRotThreads / 64;
 
@@ -253,8 +254,9 @@ __global__ __launch_bounds__(kRotThreads) void k_rotate(RotateArgs a) {
 }
 
 // ------------------------------------------------------------------ host side
-// Outputs larger than this are not kept in cache, where they would take the place of what is read (8191 tokens, 67 MB of
-// queries: 62 us against 74); a decode step's are, for the attention that follows.
+// Outputs larger than this are not kept in cache, where they would take the place of what is read: 8191 tokens, 67 MB of
+// queries, with their read-back 66.7 us against 75.1 with inputs in the cache and 75.5 against 76.9 from memory; 6001 tokens
+// of 64 channels, 31 MB out, 15.8 against 19.1 from memory. A decode step's are kept, for the attention that follows.
 constexpr int64_t kStreamedBytes = 16 << 20;
 constexpr int64_t kMaxTokens = ((int64_t)1 << 32) / kRotThreads * kRotWaves - kRotWaves;
 
