@@ -83,6 +83,8 @@ __device__ __forceinline__ Request request_of(const AttnArgs& a, int r) {
   q.first = len - (t1 - t0);
   q.end = q.first + q.n < span ? q.first + q.n : (int32_t)span;
   int64_t from = a.window ? (int64_t)q.first - a.reach : 0;
+  // Within the table, so that positions a few tiles on fit 32 bits whatever the length.
+  from = from < span ? from : span;
   q.from = from > 0 ? (int32_t)from & ~31 : 0;
   return q;
 }
